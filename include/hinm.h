@@ -358,6 +358,100 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
                        const void* X, int64_t ldx, void* Y, int64_t ldy,
                        void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- around the compressed layers: 4-bit layers and a block's norms ------------------------------
+ * What a transformer's feed-forward block needs beside HiNM layers, on the same matrices (channels x
+ * tokens, row-major): layers kept in microscaled 4-bit form, and the norms on both sides of the block.
+ * In this part leading dimensions are any value >= the row length and 16-bit matrices need the alignment of
+ * their elements only; rows that begin at multiples of 16 bytes (aligned base, leading dimension a multiple
+ * of 8) are read and written in 16-byte pieces, others element by element.  Nothing beyond the row length
+ * is read or written.
+ *
+ * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
+ * version 1.0): 32 consecutive values of a row share a power of two, and every value is one of
+ * 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives times it.
+ *   codes   uint8 [rows][64 ceil(length / 128)]  value k of a row in byte k / 2, low nibble for even
+ *           k; a nibble is the sign (bit 3) and the place in the list above.  Beyond `length`: zero.
+ *   scales  uint8 [rows][16 ceil(length / 512)]  one byte e for 32 values: their power of two is
+ *           2^(e - 127), 255 = not a number.  Block j = k / 32 of a row sits at byte
+ *           16 (j / 16) + 4 (j % 4) + (j % 16) / 4: in sixteen blocks' bytes the four of every
+ *           fourth block are neighbours, so one 4-byte load serves a lane of the scaled matrix
+ *           instruction for 512 values.  Blocks that begin at or beyond `length`: 127.
+ * Both 16-byte aligned.  hinm_mx4_sizes gives their sizes in bytes; either output pointer may be NULL. */
+enum { HINM_MX4_ROWS = 0, HINM_MX4_COLUMNS = 1 };
+hinm_status hinm_mx4_sizes(int32_t rows, int32_t length, size_t* code_bytes, size_t* scale_bytes);
+
+/* src (16-bit [rows][cols], leading dimension ld) to 4-bit form.  along = HINM_MX4_ROWS: blocks run
+ * along the rows (weights [M][K]), the form has `rows` rows of length `cols`.  along =
+ * HINM_MX4_COLUMNS: blocks run down the columns (activations [K][N]), the form has `cols` rows of
+ * length `rows`, one for each column.  Block scale: the power of two of the block's largest
+ * magnitude, divided by 4, at least 2^-127; a value over its scale is rounded to the nearest of the
+ * list, ties to the even place, and beyond 6 becomes 6.  A block that holds an infinity or a NaN
+ * becomes not-a-number as a whole (scale 255, codes 0). */
+hinm_status hinm_mx4_quantize(int32_t rows, int32_t cols, int32_t dtype, const void* src, int64_t ld,
+                              int32_t along, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* The values that a 4-bit form stands for: dst 16-bit [rows][length], leading dimension ld, rounded to
+ * nearest-even where dtype does not hold them (a form made from dtype is held exactly). */
+hinm_status hinm_mx4_unpack(int32_t rows, int32_t length, int32_t dtype, const uint8_t* codes,
+                            const uint8_t* scales, void* dst, int64_t ld, void* stream);
+
+/* Y = A B^T on the values of two 4-bit forms: A has M rows, B has N rows, both of length K.  Products and sums in
+ * fp32 on the matrix cores; Y [M][N] (leading dimension ldy) in dtype, rounded to nearest-even, or float32
+ * with HINM_OUT_F32; HINM_EPI_RELU as for hinm_spmm.  A layer is A = weights along their rows, B = activations
+ * along their columns; its input gradient is A = weights along their columns, B = output gradient along its
+ * columns; its weight gradient is A = output gradient along its rows, B = activations along their rows. */
+hinm_status hinm_mx4_product(int32_t M, int32_t N, int32_t K, int32_t dtype, const uint8_t* a_codes,
+                             const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales,
+                             void* Y, int64_t ldy, uint32_t flags, void* stream);
+
+/* A 4-bit layer on 16-bit activations: Y [M][N] = W X with W in 4-bit form (M rows of length K) and X [K][N]
+ * quantised along its columns on the way; the result is that of hinm_mx4_quantize and hinm_mx4_product, bit for
+ * bit.  workspace: hinm_mx4_linear_workspace bytes of device memory, 256-byte aligned. */
+hinm_status hinm_mx4_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const uint8_t* codes,
+                            const uint8_t* scales, const void* X, int64_t ldx, void* Y, int64_t ldy,
+                            uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norms on both sides of a block with its gates and residual, K channels x N tokens:
+ *   rstd_y[n] = (mean_k y[k][n]^2 + eps)^-1/2        h[k][n] = residual_scale x[k][n]
+ *             + gate[k] token_gate[n] w_post[k] rstd_y[n] y[k][n]
+ *   rstd_h[n] = (mean_k h[k][n]^2 + eps)^-1/2        u[k][n] = w_pre[k] rstd_h[n] h[k][n]
+ * x: the residual stream, y: the block's output, h: the new residual stream, u: the next block's input;
+ * 16-bit.  w_post, gate, w_pre float32 [K], token_gate float32 [N]; rstd_y, rstd_h float32 [N] outputs.
+ * NULL means: y no block yet (h = residual_scale x; w_post, gate and token_gate must be NULL too);
+ * w_post no norm after the block (rstd_y is left alone); gate / token_gate one; w_pre no norm before the next
+ * block (u and rstd_h are left alone and may be NULL); rstd_y / rstd_h not wanted; h not wanted (then w_pre and u
+ * are needed).  u is computed from h before its rounding.  x and h have leading dimension ld_stream, y
+ * and u ld_block.  h may be x and u may be y; apart from that outputs must not overlap inputs.  Sums
+ * in fp32 in a fixed order.  workspace: hinm_block_norm_workspace bytes, 256-byte aligned. */
+hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_block_norm(int32_t K, int32_t N, int32_t dtype, float residual_scale, float eps,
+                            const void* x, const void* y, const float* w_post, const float* gate,
+                            const float* token_gate, const float* w_pre, void* h, int64_t ld_stream,
+                            void* u, int64_t ld_block, float* rstd_y, float* rstd_h,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of hinm_block_norm from h, y, rstd_y and rstd_h (as it took and left them) and the gradients
+ * dh (of h from the stream beyond; NULL = zero) and du (of u), 16-bit, at least one of them:
+ *   d[k][n]  = dh + rstd_h w_pre du - h rstd_h^3 / K sum_k(w_pre du h)
+ *   dx       = residual_scale d
+ *   dy       = token_gate (gate w_post rstd_y d - y rstd_y^3 / K sum_k(gate w_post d y))
+ *              (without w_post: token_gate gate d)
+ *   dw_pre   = sum_n du h rstd_h                     dw_post = gate sum_n token_gate rstd_y d y
+ *   dgate    = w_post sum_n token_gate rstd_y d y    dtoken_gate = sum_k gate w_post rstd_y d y
+ * (absent factors are one).  w_pre, rstd_h, h and du go together (all or none); w_post needs rstd_y.  y NULL:
+ * no block, only dx and dw_pre.  Outputs may be NULL where they are not wanted; dw_post, dgate, dtoken_gate and
+ * dw_pre (float32, overwritten) only where their input is given.  dx may be dh and dy may be du; h, dh and dx
+ * have leading dimension ld_stream, y, du and dy ld_block.  Sums in fp32 in a fixed order.
+ * workspace: hinm_block_norm_grad_workspace bytes, 256-byte aligned. */
+hinm_status hinm_block_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float residual_scale, const void* h,
+                                 const void* y, const float* w_post, const float* gate, const float* token_gate,
+                                 const float* w_pre, const float* rstd_y, const float* rstd_h, const void* dh,
+                                 const void* du, void* dx, int64_t ld_stream, void* dy, int64_t ld_block,
+                                 float* dw_post, float* dgate, float* dtoken_gate, float* dw_pre,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
 const char* hinm_status_str(hinm_status s);
 
 /* Library version, 1000*major + minor. */

@@ -7,6 +7,7 @@ from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
 
 F16, BF16 = 0, 1
+MX4_ROWS, MX4_COLUMNS = 0, 1
 EPI_RELU, OUT_F32 = 1, 2
 KERNEL_REFERENCE, KERNEL_SMFMAC, KERNEL_GEMV = 0x100, 0x200, 0x400
 
@@ -42,7 +43,9 @@ def exported_symbols() -> Tuple[str, ...]:
             "hinm_icp_sizes", "hinm_icp_search", "hinm_ocp_sizes", "hinm_ocp_search",
             "hinm_ocp_cluster_sizes", "hinm_ocp_cluster", "hinm_unpack", "hinm_spmm", "hinm_spmm_vectors", "hinm_prepare_sizes", "hinm_prepare",
             "hinm_spmm_prepared_workspace", "hinm_spmm_prepared", "hinm_spmm_prepared_plan", "hinm_chain_sizes",
-            "hinm_chain", "hinm_status_str", "hinm_version") + calib_symbols()
+            "hinm_chain", "hinm_mx4_sizes", "hinm_mx4_quantize", "hinm_mx4_unpack", "hinm_mx4_product",
+            "hinm_mx4_linear_workspace", "hinm_mx4_linear", "hinm_block_norm_workspace", "hinm_block_norm",
+            "hinm_block_norm_grad_workspace", "hinm_block_norm_grad", "hinm_status_str", "hinm_version") + calib_symbols()
 
 
 def calib_symbols() -> Tuple[str, ...]:
@@ -111,6 +114,22 @@ def load_library():
                  "hinm_ocp_cluster_sizes", "hinm_ocp_cluster", "hinm_unpack", "hinm_spmm", "hinm_spmm_vectors", "hinm_chain_sizes", "hinm_chain",
                  "hinm_prepare_sizes", "hinm_prepare", "hinm_spmm_prepared_workspace", "hinm_spmm_prepared"):
         getattr(lib, name).restype = C.c_int
+    i32, i64, vp, sz, f32 = C.c_int32, C.c_int64, C.c_void_p, C.c_size_t, C.c_float
+    lib.hinm_mx4_sizes.argtypes = [i32, i32, szp, szp]
+    lib.hinm_mx4_quantize.argtypes = [i32, i32, i32, vp, i64, i32, vp, vp, vp]
+    lib.hinm_mx4_unpack.argtypes = [i32, i32, i32, vp, vp, vp, i64, vp]
+    lib.hinm_mx4_product.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i64, C.c_uint32, vp]
+    lib.hinm_mx4_linear_workspace.argtypes = [i32, i32, i32, szp]
+    lib.hinm_mx4_linear.argtypes = [i32, i32, i32, i32, vp, vp, vp, i64, vp, i64, C.c_uint32, vp, sz, vp]
+    lib.hinm_block_norm_workspace.argtypes = [i32, i32, szp]
+    lib.hinm_block_norm.argtypes = [i32, i32, i32, f32, f32, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.hinm_block_norm_grad_workspace.argtypes = [i32, i32, szp]
+    lib.hinm_block_norm_grad.argtypes = [i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
+                                         vp, vp, sz, vp]
+    for name in ("hinm_mx4_sizes", "hinm_mx4_quantize", "hinm_mx4_unpack", "hinm_mx4_product", "hinm_mx4_linear_workspace",
+                 "hinm_mx4_linear", "hinm_block_norm_workspace", "hinm_block_norm", "hinm_block_norm_grad_workspace",
+                 "hinm_block_norm_grad"):
+        getattr(lib, name).restype = C.c_int
     lib.hinm_calib_copy.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p]
     lib.hinm_calib_fill.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p]
     lib.hinm_calib_read.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p, C.c_void_p]
@@ -135,7 +154,9 @@ def load_library():
         raise RuntimeError("the call module of this package is missing: build it with "
                            "`python -m paper_2407_20496_amd.build`") from e
     _calls.bind(*[C.cast(getattr(lib, f), C.c_void_p).value for f in
-                  ("hinm_pack", "hinm_prepare", "hinm_spmm", "hinm_spmm_vectors", "hinm_spmm_prepared", "hinm_chain")],
+                  ("hinm_pack", "hinm_prepare", "hinm_spmm", "hinm_spmm_vectors", "hinm_spmm_prepared", "hinm_chain",
+                   "hinm_mx4_quantize", "hinm_mx4_unpack", "hinm_mx4_product", "hinm_mx4_linear", "hinm_block_norm",
+                   "hinm_block_norm_grad")],
                 _dtype_code, _stream)
     _native = _calls
     _lib = lib
@@ -374,6 +395,88 @@ def hinm_spmm_prepared_plan(M, K, V, Kv, dtype, N, ldx, ldy, flags=0) -> Tuple[s
     _check(lib.hinm_spmm_prepared_plan(C.byref(_shape(M, K, V, Kv, dtype)), int(N), int(ldx), int(ldy), int(flags),
                                        buf, len(buf), C.byref(n)), "hinm_spmm_prepared_plan")
     return buf.value.decode(), int(n.value)
+
+
+# ---- around the compressed layers: 4-bit layers and a block's norms -------------------------------
+
+def hinm_mx4_sizes(rows, length) -> Tuple[int, int]:
+    """(code_bytes, scale_bytes) of `rows` rows of `length` values in 4-bit form."""
+    out = [C.c_size_t(0) for _ in range(2)]
+    _check(load_library().hinm_mx4_sizes(int(rows), int(length), *[C.byref(o) for o in out]), "hinm_mx4_sizes")
+    return tuple(int(o.value) for o in out)
+
+
+def hinm_mx4_quantize(rows, cols, dtype, src, ld, along, codes, scales, stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.mx4_quantize(rows, cols, dtype, src, ld, along, codes, scales, stream)
+    if status:
+        raise HinmError(status, "hinm_mx4_quantize")
+
+
+def hinm_mx4_unpack(rows, length, dtype, codes, scales, dst, ld, stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.mx4_unpack(rows, length, dtype, codes, scales, dst, ld, stream)
+    if status:
+        raise HinmError(status, "hinm_mx4_unpack")
+
+
+def hinm_mx4_product(M, N, K, dtype, a_codes, a_scales, b_codes, b_scales, Y, ldy, flags=0, stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.mx4_product(M, N, K, dtype, a_codes, a_scales, b_codes, b_scales, Y, ldy, flags, stream)
+    if status:
+        raise HinmError(status, "hinm_mx4_product")
+
+
+def hinm_mx4_linear_workspace(M, K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_mx4_linear_workspace(int(M), int(K), int(N), C.byref(out)), "hinm_mx4_linear_workspace")
+    return int(out.value)
+
+
+def hinm_mx4_linear(M, K, N, dtype, codes, scales, X, ldx, Y, ldy, flags=0, workspace=None, workspace_bytes=0,
+                    stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.mx4_linear(M, K, N, dtype, codes, scales, X, ldx, Y, ldy, flags, workspace, workspace_bytes, stream)
+    if status:
+        raise HinmError(status, "hinm_mx4_linear")
+
+
+def hinm_block_norm_workspace(K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_block_norm_workspace(int(K), int(N), C.byref(out)), "hinm_block_norm_workspace")
+    return int(out.value)
+
+
+def hinm_block_norm(K, N, dtype, residual_scale, eps, x, y, w_post, gate, token_gate, w_pre, h, ld_stream, u, ld_block,
+                    rstd_y=None, rstd_h=None, workspace=None, workspace_bytes=0, stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.block_norm(K, N, dtype, residual_scale, eps, x, y, w_post, gate, token_gate, w_pre, h, ld_stream, u,
+                                ld_block, rstd_y, rstd_h, workspace, workspace_bytes, stream)
+    if status:
+        raise HinmError(status, "hinm_block_norm")
+
+
+def hinm_block_norm_grad_workspace(K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_block_norm_grad_workspace(int(K), int(N), C.byref(out)), "hinm_block_norm_grad_workspace")
+    return int(out.value)
+
+
+def hinm_block_norm_grad(K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh, du, dx,
+                         ld_stream, dy, ld_block, dw_post=None, dgate=None, dtoken_gate=None, dw_pre=None, workspace=None,
+                         workspace_bytes=0, stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.block_norm_grad(K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh,
+                                     du, dx, ld_stream, dy, ld_block, dw_post, dgate, dtoken_gate, dw_pre, workspace,
+                                     workspace_bytes, stream)
+    if status:
+        raise HinmError(status, "hinm_block_norm_grad")
 
 
 # ---- measurement aids (include/hinm_calib.h) -------------------------------------------------------

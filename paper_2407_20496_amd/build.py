@@ -25,7 +25,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["hinm_api.hip", "pack_kernels.hip", "assignment.hip", "icp_search.hip", "ocp_search.hip", "prepare.hip", "spmm_reference.hip", "spmm_skinny.hip", "spmm_tile.hip", "spmm_mid.hip", "spmm_vectors.hip",
            "spmm_tile_prepared.hip", "spmm_rings.hip", "spmm_skinny_prepared.hip", "spmm_rows16_prepared.hip", "spmm_panel_prepared.hip",
-           "calib_kernels.hip"]
+           "calib_kernels.hip", "mx4_quantize.hip", "mx4_product.hip", "block_norm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

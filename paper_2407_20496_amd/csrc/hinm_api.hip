@@ -2,6 +2,7 @@
 // Every check here runs before anything is launched, so the error paths need no GPU.
 #include "hinm_internal.h"
 
+#include "mx4_form.h"
 #include "prepared_layout.h"
 #include "hinm_calib.h"
 
@@ -62,6 +63,44 @@ hinm_status run_spmm(const SpmmArgs& a, uint32_t flags, hipStream_t stream) {
 }
 
 size_t elem_bytes_out(uint32_t flags) { return (flags & HINM_OUT_F32) ? 4 : 2; }
+
+// ---- 4-bit form and norms around a block ---------------------------------------------------------------
+bool known_dtype(int32_t d) { return d == HINM_F16 || d == HINM_BF16; }
+hinm_status launched(hipError_t e) { return e == hipSuccess ? HINM_OK : HINM_ERR_DEVICE; }
+
+// rows of `length` values in 4-bit form
+hinm_status check_form(const uint8_t* codes, const uint8_t* scales) {
+  if (!codes || !scales) return HINM_ERR_NULL;
+  return aligned(codes, 16) && aligned(scales, 16) ? HINM_OK : HINM_ERR_SHAPE;
+}
+
+hinm_status check_product(int32_t M, int32_t N, int32_t K, int32_t dtype, const void* Y, int64_t ldy, uint32_t flags) {
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  if (M <= 0 || N <= 0 || K <= 0) return HINM_ERR_SHAPE;
+  if (!Y) return HINM_ERR_NULL;
+  if (ldy < N || !aligned(Y, (flags & HINM_OUT_F32) ? 4 : 2)) return HINM_ERR_SHAPE;
+  if (flags & ~(uint32_t)(HINM_EPI_RELU | HINM_OUT_F32)) return HINM_ERR_UNSUPPORTED;
+  // workgroups of one launch: at least one for 16 x 128 outputs
+  if ((((int64_t)M + 15) / 16) * (((int64_t)N + 127) / 128) >= (int64_t{1} << 22)) return HINM_ERR_UNSUPPORTED;
+  return HINM_OK;
+}
+
+struct LinearPlan {
+  size_t codes, scales;  // bytes of the activations' 4-bit form, each rounded to 256
+};
+LinearPlan linear_plan(int32_t K, int32_t N) {
+  const size_t c = (size_t)N * mx4_code_pitch(K), s = (size_t)N * mx4_scale_pitch(K);
+  return {(c + 255) & ~size_t{255}, (s + 255) & ~size_t{255}};
+}
+
+// a workgroup's strip is 64 tokens and a launch holds at most 64 of them a strip
+constexpr int32_t kMostTokens = 1 << 22;
+
+hinm_status check_norm(int32_t K, int32_t N, int32_t dtype) {
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  if (K <= 0 || N <= 0) return HINM_ERR_SHAPE;
+  return N > kMostTokens ? HINM_ERR_UNSUPPORTED : HINM_OK;
+}
 
 // ---- hinm_pack_static: the score workspace of the pack kernels in a file-scope device array -------------
 // One binary64 score per tile and column, at most kStaticScoreCount of them (4 MiB).  Every GPU the library runs
@@ -635,6 +674,136 @@ hinm_status hinm_calib_mid_plan(const hinm_shape* shape, int32_t N, int32_t form
     if (spmm_mid_vectors_preferred(a) && !spmm_ring_vectors_preferred(a)) e = launch_spmm_mid_vectors(a, nullptr);
   }
   return e == hipSuccess ? HINM_OK : HINM_ERR_DEVICE;
+}
+
+hinm_status hinm_mx4_sizes(int32_t rows, int32_t length, size_t* code_bytes, size_t* scale_bytes) {
+  if (rows <= 0 || length <= 0) return HINM_ERR_SHAPE;
+  if (code_bytes) *code_bytes = (size_t)rows * mx4_code_pitch(length);
+  if (scale_bytes) *scale_bytes = (size_t)rows * mx4_scale_pitch(length);
+  return HINM_OK;
+}
+
+hinm_status hinm_mx4_quantize(int32_t rows, int32_t cols, int32_t dtype, const void* src, int64_t ld, int32_t along,
+                              uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  if (rows <= 0 || cols <= 0) return HINM_ERR_SHAPE;
+  if (!src) return HINM_ERR_NULL;
+  const hinm_status st = check_form(codes, scales);
+  if (st != HINM_OK) return st;
+  if (ld < cols || !aligned(src, 2)) return HINM_ERR_SHAPE;
+  if (along != HINM_MX4_ROWS && along != HINM_MX4_COLUMNS) return HINM_ERR_UNSUPPORTED;
+  return launched(launch_mx4_quantize(rows, cols, dtype, src, ld, along == HINM_MX4_COLUMNS, codes, scales,
+                                      static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_mx4_unpack(int32_t rows, int32_t length, int32_t dtype, const uint8_t* codes, const uint8_t* scales, void* dst,
+                            int64_t ld, void* stream) {
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  if (rows <= 0 || length <= 0) return HINM_ERR_SHAPE;
+  if (!dst) return HINM_ERR_NULL;
+  const hinm_status st = check_form(codes, scales);
+  if (st != HINM_OK) return st;
+  if (ld < length || !aligned(dst, 2)) return HINM_ERR_SHAPE;
+  return launched(launch_mx4_unpack(rows, length, dtype, codes, scales, dst, ld, static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_mx4_product(int32_t M, int32_t N, int32_t K, int32_t dtype, const uint8_t* a_codes, const uint8_t* a_scales,
+                             const uint8_t* b_codes, const uint8_t* b_scales, void* Y, int64_t ldy, uint32_t flags,
+                             void* stream) {
+  hinm_status st = check_product(M, N, K, dtype, Y, ldy, flags);
+  if (st != HINM_OK) return st;
+  if ((st = check_form(a_codes, a_scales)) != HINM_OK || (st = check_form(b_codes, b_scales)) != HINM_OK) return st;
+  const Mx4ProductArgs a{M, N, K, dtype, a_codes, a_scales, b_codes, b_scales, Y, ldy, (flags & HINM_EPI_RELU) != 0,
+                         (flags & HINM_OUT_F32) != 0};
+  return launched(launch_mx4_product(a, static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_mx4_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  if (M <= 0 || K <= 0 || N <= 0) return HINM_ERR_SHAPE;
+  const LinearPlan p = linear_plan(K, N);
+  *workspace_bytes = p.codes + p.scales;
+  return HINM_OK;
+}
+
+hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const uint8_t* codes, const uint8_t* scales,
+                            const void* X, int64_t ldx, void* Y, int64_t ldy, uint32_t flags, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  hinm_status st = check_product(M, N, K, dtype, Y, ldy, flags);
+  if (st != HINM_OK) return st;
+  if (!X) return HINM_ERR_NULL;
+  if ((st = check_form(codes, scales)) != HINM_OK) return st;
+  if (ldx < N || !aligned(X, 2)) return HINM_ERR_SHAPE;
+  const LinearPlan p = linear_plan(K, N);
+  if (!workspace || workspace_bytes < p.codes + p.scales || !aligned(workspace, 256)) return HINM_ERR_WORKSPACE;
+  uint8_t* x_codes = static_cast<uint8_t*>(workspace);
+  uint8_t* x_scales = x_codes + p.codes;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_mx4_quantize(K, N, dtype, X, ldx, true, x_codes, x_scales, s);
+  if (e != hipSuccess) return HINM_ERR_DEVICE;
+  const Mx4ProductArgs a{M, N, K, dtype, codes, scales, x_codes, x_scales, Y, ldy, (flags & HINM_EPI_RELU) != 0,
+                         (flags & HINM_OUT_F32) != 0};
+  return launched(launch_mx4_product(a, s));
+}
+
+hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  const hinm_status st = check_norm(K, N, HINM_F16);
+  if (st != HINM_OK) return st;
+  *workspace_bytes = block_norm_workspace_bytes(K, N);
+  return HINM_OK;
+}
+
+hinm_status hinm_block_norm(int32_t K, int32_t N, int32_t dtype, float residual_scale, float eps, const void* x, const void* y,
+                            const float* w_post, const float* gate, const float* token_gate, const float* w_pre, void* h,
+                            int64_t ld_stream, void* u, int64_t ld_block, float* rstd_y, float* rstd_h, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  const hinm_status st = check_norm(K, N, dtype);
+  if (st != HINM_OK) return st;
+  if (!x || (w_pre && !u) || (!w_pre && !h)) return HINM_ERR_NULL;
+  if (!y && (w_post || gate || token_gate)) return HINM_ERR_NULL;
+  if (ld_stream < N || ((y || w_pre) && ld_block < N)) return HINM_ERR_SHAPE;
+  if (!aligned(x, 2) || !aligned(y, 2) || !aligned(h, 2) || !aligned(u, 2)) return HINM_ERR_SHAPE;
+  for (const float* p : {w_post, gate, token_gate, w_pre, const_cast<const float*>(rstd_y), const_cast<const float*>(rstd_h)})
+    if (!aligned(p, 4)) return HINM_ERR_SHAPE;
+  const size_t need = block_norm_workspace_bytes(K, N);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
+  const BlockNormArgs a{K, N, dtype, residual_scale, eps, x, y, w_post, gate, token_gate, w_pre, h, ld_stream,
+                        w_pre ? u : nullptr, ld_block, w_post ? rstd_y : nullptr, w_pre ? rstd_h : nullptr,
+                        static_cast<float*>(workspace)};
+  return launched(launch_block_norm(a, static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_block_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  const hinm_status st = check_norm(K, N, HINM_F16);
+  if (st != HINM_OK) return st;
+  *workspace_bytes = block_norm_grad_workspace_bytes(K, N);
+  return HINM_OK;
+}
+
+hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float residual_scale, const void* h, const void* y,
+                                 const float* w_post, const float* gate, const float* token_gate, const float* w_pre,
+                                 const float* rstd_y, const float* rstd_h, const void* dh, const void* du, void* dx,
+                                 int64_t ld_stream, void* dy, int64_t ld_block, float* dw_post, float* dgate,
+                                 float* dtoken_gate, float* dw_pre, void* workspace, size_t workspace_bytes, void* stream) {
+  const hinm_status st = check_norm(K, N, dtype);
+  if (st != HINM_OK) return st;
+  if (w_pre ? (!h || !du || !rstd_h) : (du || !dh)) return HINM_ERR_NULL;
+  if ((w_post && !rstd_y) || (!y && (w_post || gate || token_gate || dy))) return HINM_ERR_NULL;
+  if ((dw_post && !w_post) || (dgate && !gate) || (dtoken_gate && !token_gate) || (dw_pre && !w_pre)) return HINM_ERR_NULL;
+  if (((h && w_pre) || dh || dx) && ld_stream < N) return HINM_ERR_SHAPE;
+  if ((y || du || dy) && ld_block < N) return HINM_ERR_SHAPE;
+  for (const void* p : {h, y, dh, du, const_cast<const void*>(dx), const_cast<const void*>(dy)})
+    if (!aligned(p, 2)) return HINM_ERR_SHAPE;
+  for (const float* p : {w_post, gate, token_gate, w_pre, rstd_y, rstd_h, const_cast<const float*>(dw_post),
+                         const_cast<const float*>(dgate), const_cast<const float*>(dtoken_gate), const_cast<const float*>(dw_pre)})
+    if (!aligned(p, 4)) return HINM_ERR_SHAPE;
+  const size_t need = block_norm_grad_workspace_bytes(K, N);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
+  const BlockNormGradArgs a{K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh, du, dx,
+                            ld_stream, dy, ld_block, dw_post, dgate, dtoken_gate, dw_pre, static_cast<float*>(workspace)};
+  return launched(launch_block_norm_grad(a, static_cast<hipStream_t>(stream)));
 }
 
 const char* hinm_status_str(hinm_status s) {

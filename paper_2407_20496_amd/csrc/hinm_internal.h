@@ -287,4 +287,53 @@ bool spmm_mid_vectors_preferred(const VectorsArgs& a);
 double spmm_mid_vectors_us(const VectorsArgs& a);  // estimate, from 65 columns on
 hipError_t launch_spmm_mid_vectors(const VectorsArgs& a, hipStream_t stream);
 
+// ---- microscaled 4-bit form (mx4_quantize.hip, mx4_product.hip) -----------------------------------------------
+hipError_t launch_mx4_quantize(int rows, int cols, int dtype, const void* src, int64_t ld, bool columns, uint8_t* codes,
+                               uint8_t* scales, hipStream_t stream);
+hipError_t launch_mx4_unpack(int rows, int length, int dtype, const uint8_t* codes, const uint8_t* scales, void* dst, int64_t ld,
+                             hipStream_t stream);
+struct Mx4ProductArgs {
+  int M, N, K, dtype;
+  const uint8_t* a_codes;
+  const uint8_t* a_scales;
+  const uint8_t* b_codes;
+  const uint8_t* b_scales;
+  void* Y;
+  int64_t ldy;
+  bool relu;
+  bool out_f32;
+};
+hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream);
+
+// ---- norms around a block (block_norm.hip) -------------------------------------------------------------------
+struct BlockNormArgs {
+  int K, N, dtype;
+  float residual_scale, eps;
+  const void *x, *y;
+  const float *w_post, *gate, *token_gate, *w_pre;
+  void* h;
+  int64_t ld_stream;
+  void* u;
+  int64_t ld_block;
+  float *rstd_y, *rstd_h;
+  float* workspace;
+};
+size_t block_norm_workspace_bytes(int K, int N);
+hipError_t launch_block_norm(const BlockNormArgs& a, hipStream_t stream);
+struct BlockNormGradArgs {
+  int K, N, dtype;
+  float residual_scale;
+  const void *h, *y;
+  const float *w_post, *gate, *token_gate, *w_pre, *rstd_y, *rstd_h;
+  const void *dh, *du;
+  void* dx;
+  int64_t ld_stream;
+  void* dy;
+  int64_t ld_block;
+  float *dw_post, *dgate, *dtoken_gate, *dw_pre;
+  float* workspace;
+};
+size_t block_norm_grad_workspace_bytes(int K, int N);
+hipError_t launch_block_norm_grad(const BlockNormGradArgs& a, hipStream_t stream);
+
 }  // namespace hinm

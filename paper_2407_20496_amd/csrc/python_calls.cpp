@@ -20,6 +20,12 @@ decltype(&hinm_spmm) f_spmm;
 decltype(&hinm_spmm_vectors) f_spmm_vectors;
 decltype(&hinm_spmm_prepared) f_spmm_prepared;
 decltype(&hinm_chain) f_chain;
+decltype(&hinm_mx4_quantize) f_mx4_quantize;
+decltype(&hinm_mx4_unpack) f_mx4_unpack;
+decltype(&hinm_mx4_product) f_mx4_product;
+decltype(&hinm_mx4_linear) f_mx4_linear;
+decltype(&hinm_block_norm) f_block_norm;
+decltype(&hinm_block_norm_grad) f_block_norm_grad;
 
 PyObject* g_dtype_code;      // any accepted dtype -> HINM_F16 / HINM_BF16
 PyObject* g_current_stream;  // () -> raw pointer of the current stream or None; used until a source is set
@@ -59,6 +65,27 @@ bool to_ptr(PyObject* o, void** out) {
   *out = PyLong_AsVoidPtr(o);
   Py_XDECREF(n);
   return !(*out == nullptr && PyErr_Occurred());
+}
+
+bool to_float(PyObject* o, float* out) {
+  const double v = PyFloat_AsDouble(o);
+  *out = (float)v;
+  return !(v == -1.0 && PyErr_Occurred());
+}
+
+// n pointers / n sizes in a row
+bool to_ptrs(PyObject* const* a, int n, void** out) {
+  for (int i = 0; i < n; ++i)
+    if (!to_ptr(a[i], &out[i])) return false;
+  return true;
+}
+bool to_sizes(PyObject* const* a, int n, int32_t* out) {
+  for (int i = 0; i < n; ++i) {
+    int64_t v;
+    if (!to_i64(a[i], &v)) return false;
+    out[i] = (int32_t)v;
+  }
+  return true;
 }
 
 bool to_stream(PyObject* o, void** out) {
@@ -264,22 +291,121 @@ PyObject* chain(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (rows, cols, dtype, src, ld, along, codes, scales, stream)
+PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[2], dtype, along;
+  void *src, *form[2], *stream;
+  int64_t ld;
+  if (!takes(n, 9) || !to_sizes(a, 2, d) || !to_dtype(a[2], &dtype) || !to_ptr(a[3], &src) || !to_i64(a[4], &ld) ||
+      !to_sizes(a + 5, 1, &along) || !to_ptrs(a + 6, 2, form) || !to_stream(a[8], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_mx4_quantize(d[0], d[1], dtype, src, ld, along, static_cast<uint8_t*>(form[0]), static_cast<uint8_t*>(form[1]),
+                          stream);
+  });
+}
+
+// (rows, length, dtype, codes, scales, dst, ld, stream)
+PyObject* mx4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[2], dtype;
+  void *p[3], *stream;
+  int64_t ld;
+  if (!takes(n, 8) || !to_sizes(a, 2, d) || !to_dtype(a[2], &dtype) || !to_ptrs(a + 3, 3, p) || !to_i64(a[6], &ld) ||
+      !to_stream(a[7], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_mx4_unpack(d[0], d[1], dtype, static_cast<uint8_t*>(p[0]), static_cast<uint8_t*>(p[1]), p[2], ld, stream);
+  });
+}
+
+// (M, N, K, dtype, a_codes, a_scales, b_codes, b_scales, Y, ldy, flags, stream)
+PyObject* mx4_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[3], dtype;
+  void *p[5], *stream;
+  int64_t ldy, flags;
+  if (!takes(n, 12) || !to_sizes(a, 3, d) || !to_dtype(a[3], &dtype) || !to_ptrs(a + 4, 5, p) || !to_i64(a[9], &ldy) ||
+      !to_i64(a[10], &flags) || !to_stream(a[11], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_mx4_product(d[0], d[1], d[2], dtype, static_cast<uint8_t*>(p[0]), static_cast<uint8_t*>(p[1]),
+                         static_cast<uint8_t*>(p[2]), static_cast<uint8_t*>(p[3]), p[4], ldy, (uint32_t)flags, stream);
+  });
+}
+
+// (M, K, N, dtype, codes, scales, X, ldx, Y, ldy, flags, workspace, workspace_bytes, stream)
+PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[3], dtype;
+  void *form[2], *x, *y, *ws, *stream;
+  int64_t ldx, ldy, flags, bytes;
+  if (!takes(n, 14) || !to_sizes(a, 3, d) || !to_dtype(a[3], &dtype) || !to_ptrs(a + 4, 2, form) || !to_ptr(a[6], &x) ||
+      !to_i64(a[7], &ldx) || !to_ptr(a[8], &y) || !to_i64(a[9], &ldy) || !to_i64(a[10], &flags) || !to_ptr(a[11], &ws) ||
+      !to_i64(a[12], &bytes) || !to_stream(a[13], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_mx4_linear(d[0], d[1], d[2], dtype, static_cast<uint8_t*>(form[0]), static_cast<uint8_t*>(form[1]), x, ldx, y, ldy,
+                        (uint32_t)flags, ws, (size_t)bytes, stream);
+  });
+}
+
+// (K, N, dtype, residual_scale, eps, x, y, w_post, gate, token_gate, w_pre, h, ld_stream, u, ld_block, rstd_y, rstd_h, workspace,
+//  workspace_bytes, stream)
+PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[2], dtype;
+  float scale, eps;
+  void *in[6], *h, *u, *out[2], *ws, *stream;
+  int64_t ld_stream, ld_block, bytes;
+  if (!takes(n, 20) || !to_sizes(a, 2, d) || !to_dtype(a[2], &dtype) || !to_float(a[3], &scale) || !to_float(a[4], &eps) ||
+      !to_ptrs(a + 5, 6, in) || !to_ptr(a[11], &h) || !to_i64(a[12], &ld_stream) || !to_ptr(a[13], &u) ||
+      !to_i64(a[14], &ld_block) || !to_ptrs(a + 15, 2, out) || !to_ptr(a[17], &ws) || !to_i64(a[18], &bytes) ||
+      !to_stream(a[19], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_block_norm(d[0], d[1], dtype, scale, eps, in[0], in[1], static_cast<float*>(in[2]), static_cast<float*>(in[3]),
+                        static_cast<float*>(in[4]), static_cast<float*>(in[5]), h, ld_stream, u, ld_block,
+                        static_cast<float*>(out[0]), static_cast<float*>(out[1]), ws, (size_t)bytes, stream);
+  });
+}
+
+// (K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh, du, dx, ld_stream, dy, ld_block, dw_post,
+//  dgate, dtoken_gate, dw_pre, workspace, workspace_bytes, stream)
+PyObject* block_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[2], dtype;
+  float scale;
+  void *in[10], *dx, *dy, *out[4], *ws, *stream;
+  int64_t ld_stream, ld_block, bytes;
+  if (!takes(n, 25) || !to_sizes(a, 2, d) || !to_dtype(a[2], &dtype) || !to_float(a[3], &scale) || !to_ptrs(a + 4, 10, in) ||
+      !to_ptr(a[14], &dx) || !to_i64(a[15], &ld_stream) || !to_ptr(a[16], &dy) || !to_i64(a[17], &ld_block) ||
+      !to_ptrs(a + 18, 4, out) || !to_ptr(a[22], &ws) || !to_i64(a[23], &bytes) || !to_stream(a[24], &stream))
+    return nullptr;
+  return status_of([&] {
+    auto f = [&](int i) { return static_cast<float*>(in[i]); };
+    auto g = [&](int i) { return static_cast<float*>(out[i]); };
+    return f_block_norm_grad(d[0], d[1], dtype, scale, in[0], in[1], f(2), f(3), f(4), f(5), f(6), f(7), in[8], in[9], dx,
+                             ld_stream, dy, ld_block, g(0), g(1), g(2), g(3), ws, (size_t)bytes, stream);
+  });
+}
+
 // (addresses in the order below, dtype_code, current_stream)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* f[6];
-  if (!takes(n, 8)) return nullptr;
-  for (int i = 0; i < 6; ++i)
-    if (!to_ptr(a[i], &f[i])) return nullptr;
+  constexpr int kEntries = 12;
+  void* f[kEntries];
+  if (!takes(n, kEntries + 2) || !to_ptrs(a, kEntries, f)) return nullptr;
   f_pack = reinterpret_cast<decltype(f_pack)>(f[0]);
   f_prepare = reinterpret_cast<decltype(f_prepare)>(f[1]);
   f_spmm = reinterpret_cast<decltype(f_spmm)>(f[2]);
   f_spmm_vectors = reinterpret_cast<decltype(f_spmm_vectors)>(f[3]);
   f_spmm_prepared = reinterpret_cast<decltype(f_spmm_prepared)>(f[4]);
   f_chain = reinterpret_cast<decltype(f_chain)>(f[5]);
-  Py_INCREF(a[6]);
-  Py_XSETREF(g_dtype_code, a[6]);
-  Py_INCREF(a[7]);
-  Py_XSETREF(g_current_stream, a[7]);
+  f_mx4_quantize = reinterpret_cast<decltype(f_mx4_quantize)>(f[6]);
+  f_mx4_unpack = reinterpret_cast<decltype(f_mx4_unpack)>(f[7]);
+  f_mx4_product = reinterpret_cast<decltype(f_mx4_product)>(f[8]);
+  f_mx4_linear = reinterpret_cast<decltype(f_mx4_linear)>(f[9]);
+  f_block_norm = reinterpret_cast<decltype(f_block_norm)>(f[10]);
+  f_block_norm_grad = reinterpret_cast<decltype(f_block_norm_grad)>(f[11]);
+  Py_INCREF(a[kEntries]);
+  Py_XSETREF(g_dtype_code, a[kEntries]);
+  Py_INCREF(a[kEntries + 1]);
+  Py_XSETREF(g_current_stream, a[kEntries + 1]);
   Py_RETURN_NONE;
 }
 
@@ -295,7 +421,9 @@ PyObject* set_stream_source(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define HINM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HINM_METHOD(pack),    HINM_METHOD(prepare), HINM_METHOD(spmm), HINM_METHOD(spmm_vectors),
-                         HINM_METHOD(spmm_prepared), HINM_METHOD(chain), HINM_METHOD(bind), HINM_METHOD(set_stream_source),
+                         HINM_METHOD(spmm_prepared), HINM_METHOD(chain), HINM_METHOD(mx4_quantize),
+                         HINM_METHOD(mx4_unpack), HINM_METHOD(mx4_product), HINM_METHOD(mx4_linear), HINM_METHOD(block_norm),
+                         HINM_METHOD(block_norm_grad), HINM_METHOD(bind), HINM_METHOD(set_stream_source),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

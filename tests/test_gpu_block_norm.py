@@ -1,0 +1,273 @@
+"""Norms around a block and their gradients on the GPU against the binary64 oracle."""
+import numpy as np
+import pytest
+
+import hinm_synth as synth
+from oracle import block_oracle as orc
+from tests.test_oracle_block import FORMS
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+POISON = 0x1234
+EPS = 1e-5
+# fp32 sums: a value's last term passes at most some hundred additions, each 2^-24 of the magnitudes that meet
+SUM = 2.0 ** -17
+HALF_STEP = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}   # of 11 and 8 significant bits
+
+SIZES = [(1, 1), (7, 1), (64, 1), (768, 1), (4096, 1), (9000, 1), (40, 2), (33, 5), (100, 8), (257, 24), (768, 100), (129, 130),
+         (1030, 65), (4096, 40), (2100, 515), (11008, 33), (16384, 9), (24600, 3), (700, 2100)]
+
+
+def _strides(N):
+    r8 = (N + 7) // 8 * 8
+    return [(r8, r8, 0), (N, N, 0), (N + 3, r8 + 8, 1), (r8 + 16, N + 1, 8)]
+
+
+class Matrix:
+    """Rows in a buffer with a leading dimension and an offset; what lies outside them is checked."""
+
+    def __init__(self, K, N, ld, first, dtype, values=None):
+        import torch
+        self.K, self.N, self.ld, self.first, self.dtype = K, N, ld, first, dtype
+        buf = np.full(first + (K - 1) * ld + N + 8, POISON, dtype=np.uint16)
+        if values is not None:
+            bits = synth.to_bits(values.astype(np.float32), dtype)
+            for k in range(K):
+                buf[first + k * ld:first + k * ld + N] = bits[k]
+            self.wide = synth.bits_to_f32(bits, dtype).astype(np.float64)
+            # nothing outside the rows may be used: NaN there
+            outside = np.ones(buf.size, dtype=bool)
+            for k in range(K):
+                outside[first + k * ld:first + k * ld + N] = False
+            buf[outside] = 0x7FFF
+        self.t = torch.from_numpy(buf.view(np.int16)).to(DEV)
+        self.ptr = self.t.data_ptr() + 2 * first
+
+    def result(self, background=POISON):
+        host = self.t.cpu().numpy().view(np.uint16)
+        inside = np.zeros(host.size, dtype=bool)
+        rows = np.empty((self.K, self.N), dtype=np.uint16)
+        for k in range(self.K):
+            at = self.first + k * self.ld
+            rows[k] = host[at:at + self.N]
+            inside[at:at + self.N] = True
+        assert (host[~inside] == background).all(), "written outside the rows"
+        return synth.bits_to_f32(rows, self.dtype).astype(np.float64)
+
+
+def _vec(v):
+    import torch
+    return None if v is None else torch.from_numpy(np.asarray(v, dtype=np.float32)).to(DEV)
+
+
+def _f32(v):
+    return None if v is None else np.asarray(v, dtype=np.float32).astype(np.float64)
+
+
+def _guarded(n, want=True):
+    import torch
+    return torch.full((n + 16,), 7.0, dtype=torch.float32, device=DEV) if want else None
+
+
+def _values(t, n):
+    host = t.cpu().numpy()
+    assert (host[n:] == 7.0).all(), "written beyond the vector"
+    return host[:n].astype(np.float64)
+
+
+def _workspace(nbytes):
+    import torch
+    return torch.full((nbytes + 256,), 0xFF, dtype=torch.uint8, device=DEV), nbytes   # NaN in every float
+
+
+def _ptr(m):
+    return None if m is None else m.ptr
+
+
+def _inputs(K, N, form, seed):
+    rng = np.random.default_rng(seed)
+    on = lambda flag, v: v if flag else None
+    size = np.exp(0.8 * rng.standard_normal((K, 1)))
+    return {"x": rng.standard_normal((K, N)) * size, "y": on(form["block"], rng.standard_normal((K, N))),
+            "w_post": on(form["post"], 1 + 0.3 * rng.standard_normal(K)), "gate": on(form["gate"], rng.standard_normal(K)),
+            "token_gate": on(form["token"], rng.random(N)), "w_pre": on(form["pre"], 1 + 0.3 * rng.standard_normal(K))}
+
+
+def _check(name, got, want, bound):
+    finite, worst = bool(np.isfinite(got).all()), float(np.max(np.abs(got - want) - bound))
+    assert finite and worst <= 0, (name, worst)
+
+
+def _forward(K, N, dtype, form, ld_stream, ld_block, first, seed, in_place=False, want_h=True, scale=0.75):
+    import paper_2407_20496_amd as hinm
+    a = _inputs(K, N, form, seed)
+    x = Matrix(K, N, ld_stream, first, dtype, a["x"])
+    y = Matrix(K, N, ld_block, first, dtype, a["y"]) if form["block"] else None
+    h = x if in_place else Matrix(K, N, ld_stream, first, dtype) if want_h else None
+    u = None if not form["pre"] else y if in_place and y else Matrix(K, N, ld_block, first, dtype)
+    ry, rh = _guarded(N, form["post"]), _guarded(N, form["pre"])
+    vecs = [_vec(a[k]) for k in ("w_post", "gate", "token_gate", "w_pre")]
+    hinm.hinm_block_norm(K, N, dtype, scale, EPS, x.ptr, _ptr(y), *vecs, _ptr(h), ld_stream, _ptr(u), ld_block, ry, rh,
+                         *_workspace(hinm.hinm_block_norm_workspace(K, N)))
+    r = orc.block_norm(x.wide, None if y is None else y.wide, *[_f32(a[k]) for k in ("w_post", "gate", "token_gate", "w_pre")],
+                       np.float32(scale).astype(np.float64), np.float32(EPS).astype(np.float64))
+    half = HALF_STEP[dtype]
+    tiny = 2.0 ** -25 if dtype == "f16" else 0
+    if h is not None:
+        _check("h", h.result(0x7FFF if in_place else POISON), r["h"], half * np.abs(r["h"]) + SUM * r["size"] + tiny)
+    if form["post"]:
+        _check("rstd_y", _values(ry, N), r["rstd_y"], SUM * r["rstd_y"])
+    if form["pre"]:
+        # h's own error moves rstd_h by its share of the norm, which the magnitudes bound
+        of_h = np.sqrt((r["size"] ** 2).mean(axis=0) + EPS) * r["rstd_h"]
+        _check("rstd_h", _values(rh, N), r["rstd_h"], SUM * of_h * r["rstd_h"])
+        w = np.abs(_f32(a["w_pre"]))[:, None]
+        _check("u", u.result(0x7FFF if u is y else POISON), r["u"],
+               half * np.abs(r["u"]) + SUM * w * r["rstd_h"] * r["size"] * (1 + of_h) + tiny)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("K,N", SIZES)
+def test_forward(K, N, dtype):
+    form = dict(post=1, gate=1, token=N % 2, pre=1, block=1)
+    for i, (ls, lb, first) in enumerate(_strides(N)):
+        _forward(K, N, dtype, form, ls, lb, first, K + N + i)
+
+
+@pytest.mark.parametrize("K,N", [(96, 1), (300, 20), (5000, 17), (17000, 8)])
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "".join(k for k, v in f.items() if v))
+def test_forward_forms(form, K, N):
+    if not form["block"] and not form["pre"]:
+        pytest.skip("nothing to do")
+    ld = (N + 7) // 8 * 8
+    _forward(K, N, "bf16", form, ld, ld, 0, 5)
+    if form["pre"]:
+        _forward(K, N, "f16", form, ld, ld, 0, 6, want_h=False)
+
+
+@pytest.mark.parametrize("K,N", [(96, 1), (768, 70), (5000, 17), (17000, 20), (24600, 1), (24600, 9)])
+def test_forward_in_place(K, N):
+    form = dict(post=1, gate=0, token=1, pre=1, block=1)
+    for ld in ((N + 7) // 8 * 8, N):
+        _forward(K, N, "bf16", form, ld, ld, 0, 8, in_place=True)
+
+
+def test_a_token_of_zeros_and_one_that_is_no_number():
+    """All-zero columns divide by eps alone; an infinity or NaN spoils its own token only."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    for K, N in ((40, 1), (512, 12), (17000, 12)):
+        ld = (N + 7) // 8 * 8
+        x = torch.randn(K, ld, device=DEV, dtype=torch.float32).to(torch.bfloat16)
+        y = torch.randn(K, ld, device=DEV, dtype=torch.float32).to(torch.bfloat16)
+        w = torch.ones(K, device=DEV)
+        x[:, 0] = 0
+        y[:, 0] = 0
+        if N > 5:
+            y[K // 2, 3] = float("inf")
+            x[K - 1, 4] = float("nan")
+        h, u = torch.empty_like(x), torch.empty_like(x)
+        ry, rh = torch.empty(N, device=DEV), torch.empty(N, device=DEV)
+        hinm.hinm_block_norm(K, N, "bf16", 1.0, EPS, x, y, w, None, None, w, h, ld, u, ld, ry, rh,
+                             *_workspace(hinm.hinm_block_norm_workspace(K, N)))
+        assert (h[:, 0] == 0).all() and (u[:, 0] == 0).all()
+        want = 1 / np.sqrt(np.float32(EPS))
+        assert abs(ry[0].item() / want - 1) < 1e-6 and abs(rh[0].item() / want - 1) < 1e-6
+        for n in range(1, N):
+            assert torch.isnan(u[:, n]).any().item() == (n in (3, 4)), n
+
+
+def _backward(K, N, dtype, form, ld_stream, ld_block, first, seed, dh=True, wanted=True, in_place=False, scale=0.75):
+    import paper_2407_20496_amd as hinm
+    rng = np.random.default_rng(seed)
+    a = _inputs(K, N, form, seed)
+    h = Matrix(K, N, ld_stream, first, dtype, a["x"]) if form["pre"] else None
+    y = Matrix(K, N, ld_block, first, dtype, a["y"]) if form["block"] else None
+    g_h = Matrix(K, N, ld_stream, first, dtype, rng.standard_normal((K, N))) if dh else None
+    g_u = Matrix(K, N, ld_block, first, dtype, rng.standard_normal((K, N))) if form["pre"] else None
+    rstd = lambda m: (1 / np.sqrt((m.wide ** 2).mean(axis=0) + EPS)).astype(np.float32)
+    rstd_y, rstd_h = rstd(y) if form["post"] else None, rstd(h) if form["pre"] else None
+    dx = g_h if in_place and g_h else Matrix(K, N, ld_stream, first, dtype)
+    dy = None if not form["block"] else g_u if in_place and g_u else Matrix(K, N, ld_block, first, dtype)
+    out = {"dw_post": _guarded(K, form["post"] and wanted), "dgate": _guarded(K, form["gate"] and wanted),
+           "dtoken_gate": _guarded(N, form["token"] and wanted), "dw_pre": _guarded(K, form["pre"] and wanted)}
+    vecs = [_vec(a[k]) for k in ("w_post", "gate", "token_gate", "w_pre")]
+    hinm.hinm_block_norm_grad(K, N, dtype, scale, _ptr(h), _ptr(y), *vecs, _vec(rstd_y), _vec(rstd_h), _ptr(g_h), _ptr(g_u), dx.ptr,
+                              ld_stream, _ptr(dy), ld_block, out["dw_post"], out["dgate"], out["dtoken_gate"], out["dw_pre"],
+                              *_workspace(hinm.hinm_block_norm_grad_workspace(K, N)))
+    wide = lambda m: None if m is None else m.wide
+    want = orc.block_norm_grad(wide(h), wide(y), *[_f32(a[k]) for k in ("w_post", "gate", "token_gate", "w_pre")], _f32(rstd_y),
+                               _f32(rstd_h), wide(g_h), wide(g_u), np.float32(scale).astype(np.float64))
+    half, tiny = HALF_STEP[dtype], 2.0 ** -25 if dtype == "f16" else 0
+    for name, (value, size) in want.items():
+        if name in ("dx", "dy"):
+            m = dx if name == "dx" else dy
+            _check(name, m.result(0x7FFF if in_place and (m is g_h or m is g_u) else POISON), value,
+                   half * np.abs(value) + SUM * size + tiny)
+        elif out[name] is not None:
+            _check(name, _values(out[name], value.size), value, SUM * size)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("K,N", SIZES)
+def test_backward(K, N, dtype):
+    form = dict(post=1, gate=1, token=1, pre=1, block=1)
+    for i, (ls, lb, first) in enumerate(_strides(N)):
+        _backward(K, N, dtype, form, ls, lb, first, K + N + i)
+
+
+@pytest.mark.parametrize("K,N", [(96, 1), (300, 20), (5000, 17), (17000, 8)])
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "".join(k for k, v in f.items() if v))
+def test_backward_forms(form, K, N):
+    ld = (N + 7) // 8 * 8
+    _backward(K, N, "bf16", form, ld, ld, 0, 5)
+    if form["pre"]:
+        _backward(K, N, "f16", form, ld, ld, 0, 6, dh=False, wanted=False)
+
+
+@pytest.mark.parametrize("K,N", [(96, 1), (768, 70), (5000, 17), (17000, 20), (24600, 1), (24600, 9)])
+def test_backward_in_place(K, N):
+    form = dict(post=1, gate=0, token=1, pre=1, block=1)
+    for ld in ((N + 7) // 8 * 8, N):
+        _backward(K, N, "bf16", form, ld, ld, 0, 8, in_place=True)
+
+
+@pytest.mark.parametrize("K,N", [(768, 1), (768, 50), (17000, 20)])
+def test_streams_and_graph_replays(K, N):
+    """A step forward and back captured once, replayed on inputs that change, equal to the eager calls bit for bit."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    ld = (N + 7) // 8 * 8
+    new = lambda: torch.randn(K, ld, device=DEV).to(torch.float16)
+    x, y, dh, du = new(), new(), new(), new()
+    w, g = torch.rand(K, device=DEV) + 0.5, torch.rand(N, device=DEV)
+    outs = [torch.zeros_like(x) for _ in range(4)] + [torch.zeros(N, device=DEV) for _ in range(3)] + [torch.zeros(K, device=DEV)
+                                                                                                      for _ in range(2)]
+    h, u, dx, dy, ry, rh, dg, dw1, dw2 = outs
+    fw, bw = _workspace(hinm.hinm_block_norm_workspace(K, N)), _workspace(hinm.hinm_block_norm_grad_workspace(K, N))
+
+    def step():
+        hinm.hinm_block_norm(K, N, "f16", 1.0, EPS, x, y, w, None, g, w, h, ld, u, ld, ry, rh, *fw)
+        hinm.hinm_block_norm_grad(K, N, "f16", 1.0, h, y, w, None, g, w, ry, rh, dh, du, dx, ld, dy, ld, dw1, None, dg, dw2, *bw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        for t in (x, y, dh, du):
+            t.copy_(new())
+        step()
+        want = [t[:, :N].clone() if t.dim() == 2 else t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a[:, :N] if a.dim() == 2 else a, b)

@@ -1,0 +1,304 @@
+"""4-bit form and its products on the GPU against the binary64 oracle."""
+import numpy as np
+import pytest
+
+import hinm_synth as synth
+from oracle import block_oracle as orc
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+GUARD = 0x5A
+
+
+def _bits(a, dtype):
+    return synth.to_bits(np.asarray(a, dtype=np.float32), dtype)
+
+
+def _matrix(bits, ld, first=0):
+    """Device matrix with these rows at a leading dimension, `first` elements into its buffer; all other elements NaN."""
+    import torch
+    rows, cols = bits.shape
+    buf = np.full(first + (rows - 1) * ld + cols, 0x7FFF, dtype=np.uint16)
+    for r in range(rows):
+        buf[first + r * ld:first + r * ld + cols] = bits[r]
+    t = torch.from_numpy(buf.view(np.int16)).to(DEV)
+    return t, t.data_ptr() + 2 * first
+
+
+def _guarded(nbytes, align=256):
+    """Bytes with a guard behind them."""
+    import torch
+    t = torch.full((nbytes + align,), GUARD, dtype=torch.uint8, device=DEV)
+    return t
+
+
+def _form(rows, length):
+    import paper_2407_20496_amd as hinm
+    cb, sb = hinm.hinm_mx4_sizes(rows, length)
+    return _guarded(cb), _guarded(sb)
+
+
+def _host(form, rows, length):
+    c, s = (t.cpu().numpy() for t in form)
+    nc, ns = rows * orc.code_pitch(length), rows * orc.scale_pitch(length)
+    assert (c[nc:] == GUARD).all() and (s[ns:] == GUARD).all(), "written beyond the form"
+    return c[:nc].reshape(rows, -1), s[:ns].reshape(rows, -1)
+
+
+def _upload(codes, scales):
+    import torch
+    return torch.from_numpy(codes.reshape(-1)).to(DEV), torch.from_numpy(scales.reshape(-1)).to(DEV)
+
+
+def _draw(rows, cols, dtype, seed, special=True):
+    """Bit patterns of every kind of block: ordinary ones, zeros, values on and between codes, largest, smallest and subnormal
+    ones, infinities and NaN."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * np.exp(rng.standard_normal((rows, 1)))
+    for _ in range(max(1, rows * cols // 64)):
+        r, k = rng.integers(rows), rng.integers(cols)
+        n = min(32, cols - k)
+        kind = rng.integers(6)
+        if kind == 0:
+            x[r, k:k + n] = rng.choice([0.0, -0.0], n)
+        elif kind == 1:
+            x[r, k:k + n] = rng.choice([0.25, 0.5, 0.75, 1.25, 1.75, 2.5, 3.5, 4, 5, 6, 7, 7.75], n) * 2.0 ** rng.integers(-8, 8)
+        elif kind == 2:
+            x[r, k:k + n] *= 2.0 ** (-120 if dtype == "bf16" else -20)
+        elif kind == 3:
+            x[r, k:k + n] *= 2.0 ** (120 if dtype == "bf16" else 13)
+        elif kind == 4 and dtype == "bf16":
+            x[r, k:k + n] *= 2.0 ** -130
+    with np.errstate(over="ignore"):
+        b = _bits(x, dtype)
+    if special and rows * cols > 40:
+        top = 0x7F80 if dtype == "bf16" else 0x7C00
+        for pattern in (top, top | 0x8000, top | 1, 0x7FFF, 0x0001, 0x8001):
+            b[rng.integers(rows), rng.integers(cols)] = pattern
+    return b
+
+
+def _wide(bits, dtype):
+    return synth.bits_to_f32(bits, dtype).astype(np.float64)
+
+
+SIZES = [(1, 1), (1, 31), (1, 32), (2, 33), (3, 127), (2, 128), (5, 129), (4, 511), (4, 512), (3, 513), (70, 96), (65, 1000),
+         (8, 2055), (130, 40), (600, 3), (513, 1), (1030, 72)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_quantize_is_exact(rows, cols, dtype):
+    import paper_2407_20496_amd as hinm
+    bits = _draw(rows, cols, dtype, rows * 1000 + cols)
+    X = _wide(bits, dtype)
+    strides = {(cols, 0), (cols + 1, 1), ((cols + 7) // 8 * 8, 0), ((cols + 7) // 8 * 8 + 8, 8), ((cols + 7) // 8 * 8, 4)}
+    for along, Z in ((hinm.MX4_ROWS, X), (hinm.MX4_COLUMNS, np.ascontiguousarray(X.T))):
+        want = orc.quantize_rows(Z)
+        for ld, first in sorted(strides):
+            keep, src = _matrix(bits, ld, first)
+            form = _form(*Z.shape)
+            hinm.hinm_mx4_quantize(rows, cols, dtype, src, ld, along, *form)
+            codes, scales = _host(form, *Z.shape)
+            assert np.array_equal(scales, want[1]), (along, ld, first)
+            assert np.array_equal(codes, want[0]), (along, ld, first)
+            del keep
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 33), (5, 129), (4, 512), (9, 1001), (3, 2048)])
+def test_unpack_gives_the_values(rows, cols, dtype):
+    import torch
+    import paper_2407_20496_amd as hinm
+    bits = _draw(rows, cols, dtype, 7 + cols)
+    form = orc.quantize_rows(_wide(bits, dtype))
+    want = orc.values(*form, cols)
+    dev = _upload(*form)
+    for ld, first in ((cols, 0), (cols + 3, 1), ((cols + 7) // 8 * 8, 0)):
+        out = torch.full((first + rows * ld + 8,), 0x1234, dtype=torch.int16, device=DEV)
+        hinm.hinm_mx4_unpack(rows, cols, dtype, *dev, out.data_ptr() + 2 * first, ld)
+        host = out.cpu().numpy().view(np.uint16)
+        got = host[first:first + rows * ld].reshape(rows, ld)
+        back = _wide(got[:, :cols], dtype)
+        assert np.array_equal(np.isnan(back), np.isnan(want)) and np.array_equal(back[~np.isnan(want)], want[~np.isnan(want)])
+        assert (got[:, cols:] == 0x1234).all() and (host[:first] == 0x1234).all() and (host[first + rows * ld:] == 0x1234).all()
+
+
+def test_unpack_rounds_to_the_other_type():
+    """bf16's range does not fit f16: beyond it infinity, below it zero and subnormals, as any rounding to nearest."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    X = np.outer([1.0, 3.0, -6.0, 0.5], 2.0 ** np.arange(-40.0, 40.0)).T.reshape(1, -1)   # four values of each power
+    X = np.repeat(X.reshape(-1, 4), 8, axis=0).reshape(1, -1)                             # ... fill a block of 32
+    form = orc.quantize_rows(X)
+    want = orc.values(*form, X.shape[1])
+    out = torch.empty(X.shape[1], dtype=torch.float16, device=DEV)
+    hinm.hinm_mx4_unpack(1, X.shape[1], "f16", *_upload(*form), out, X.shape[1])
+    with np.errstate(over="ignore"):
+        assert np.array_equal(out.cpu().numpy(), want[0].astype(np.float16))
+
+
+def _random_form(rows, length, seed, low=118, high=130):
+    """A form with every code and scales over a range, its padding as the quantiser leaves it."""
+    rng = np.random.default_rng(seed)
+    codes = np.zeros((rows, orc.code_pitch(length)), dtype=np.uint8)
+    nib = rng.integers(0, 16, (rows, length), dtype=np.uint8)
+    np.bitwise_or.at(codes, (slice(None), np.arange(length) // 2), nib << (4 * (np.arange(length, dtype=np.uint8) % 2)))
+    scales = np.full((rows, orc.scale_pitch(length)), 127, dtype=np.uint8)
+    for j in range((length + 31) // 32):
+        scales[:, orc.scale_place(j)] = rng.integers(low, high, rows)
+    return codes, scales
+
+
+def _tolerance(size, K, want, out):
+    """fp32 sums: at most one rounding for the 32 products of a block and one for each block added, each 2^-24 of the
+    magnitudes that meet; then the rounding to 16 bits: half a step of its 8 (bf16) or 11 (f16) significant bits, in f16 at least 2^-25."""
+    t = (K / 32 + 16) * 2.0 ** -24 * size
+    if out == "f16":
+        return t + np.maximum(2.0 ** -11 * np.abs(want), 2.0 ** -25)
+    return t + (2.0 ** -8 * np.abs(want) if out == "bf16" else 0)
+
+
+PRODUCTS = [(1, 1, 1), (16, 1, 128), (17, 3, 129), (100, 16, 512), (33, 17, 1000), (40, 33, 2048), (40, 70, 640), (130, 129, 4100),
+            (64, 100, 4096), (300, 260, 640), (257, 1, 9000), (513, 30, 1537), (520, 520, 520), (1030, 770, 1160), (272, 1100, 96)]
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_product(M, N, K, out):
+    import torch
+    import paper_2407_20496_amd as hinm
+    fa, fb = _random_form(M, K, M + 2 * N + 3 * K), _random_form(N, K, 5 * M + N + K, 120, 128)
+    relu = (M + N) % 2 == 0
+    want, size = orc.product(orc.values(*fa, K), orc.values(*fb, K), relu)
+    a, b = _upload(*fa), _upload(*fb)
+    kind = torch.float32 if out == "f32" else torch.int16
+    for ld, first in ((N, 0), (N + 1, 1), ((N + 7) // 8 * 8, 0)):
+        Y = torch.full((first + M * ld + 16,), 0x4321, dtype=kind, device=DEV)
+        flags = (hinm.EPI_RELU if relu else 0) | (hinm.OUT_F32 if out == "f32" else 0)
+        hinm.hinm_mx4_product(M, N, K, "f16" if out == "f32" else out, *a, *b, Y.data_ptr() + first * Y.element_size(), ld, flags)
+        host = Y.cpu().numpy()
+        rows = host[first:first + M * ld].reshape(M, ld)
+        got = rows[:, :N].astype(np.float64) if out == "f32" else _wide(rows[:, :N].copy().view(np.uint16), out)
+        with np.errstate(over="ignore"):
+            fits = np.abs(want) < (65000 if out == "f16" else 1e30)
+        assert fits.mean() > 0.99
+        assert (np.abs(got - want) <= _tolerance(size, K, want, out))[fits].all()
+        assert (rows[:, N:] == 0x4321).all() and (host[:first] == 0x4321).all() and (host[first + M * ld:] == 0x4321).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 20, 700), (600, 600, 640)])
+def test_a_row_that_is_no_number_spoils_its_outputs_alone(M, N, K):
+    import torch
+    import paper_2407_20496_amd as hinm
+    fa, fb = _random_form(M, K, 1), _random_form(N, K, 2)
+    for f, row, block in ((fa, M - 1, 3), (fb, 5, (K - 1) // 32)):
+        f[1][row, orc.scale_place(block)] = 255
+        f[0][row, 16 * block:16 * block + 16] = 0
+    Y = torch.empty((M, N), dtype=torch.float32, device=DEV)
+    for flags in (hinm.OUT_F32, hinm.OUT_F32 | hinm.EPI_RELU):
+        hinm.hinm_mx4_product(M, N, K, "bf16", *_upload(*fa), *_upload(*fb), Y, N, flags)
+        nan = np.zeros((M, N), dtype=bool)
+        nan[M - 1], nan[:, 5] = True, True
+        assert np.array_equal(torch.isnan(Y).cpu().numpy(), nan)
+
+
+def test_scales_at_their_ends():
+    """2^-127 and 2^127 in one product: their factors cancel."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    for M, N in ((16, 4), (600, 520)):
+        K = 256
+        fa, fb = _random_form(M, K, 3, 0, 1), _random_form(N, K, 4, 254, 255)
+        want, size = orc.product(orc.values(*fa, K), orc.values(*fb, K))
+        Y = torch.empty((M, N), dtype=torch.float32, device=DEV)
+        hinm.hinm_mx4_product(M, N, K, "bf16", *_upload(*fa), *_upload(*fb), Y, N, hinm.OUT_F32)
+        assert (np.abs(Y.cpu().numpy() - want) <= _tolerance(size, K, want, "f32")).all()
+
+
+LINEARS = [(1, 1, 1, "f16"), (48, 512, 1, "bf16"), (300, 4096, 1, "bf16"), (70, 1000, 2, "f16"), (130, 2500, 3, "bf16"), (64, 700, 7, "f16"),
+           (96, 640, 16, "bf16"), (64, 333, 40, "f16"), (520, 1031, 600, "bf16")]
+
+
+@pytest.mark.parametrize("M,K,N,dtype", LINEARS)
+def test_linear_is_quantize_and_product(M, K, N, dtype):
+    import torch
+    import paper_2407_20496_amd as hinm
+    w = _upload(*_random_form(M, K, 11))
+    bits = _draw(K, N, dtype, 12, special=K * N > 4000)
+    for ld, first in ((N, 0), (N + 1, 1), ((N + 7) // 8 * 8, 0)):
+        keep, X = _matrix(bits, ld, first)
+        x = _form(N, K)
+        hinm.hinm_mx4_quantize(K, N, dtype, X, ld, hinm.MX4_COLUMNS, *x)
+        for flags, kind in ((0, torch.int16), (hinm.EPI_RELU | hinm.OUT_F32, torch.int32)):
+            want = torch.zeros((M, N), dtype=kind, device=DEV)
+            hinm.hinm_mx4_product(M, N, K, dtype, *w, *x, want, N, flags)
+            nbytes = hinm.hinm_mx4_linear_workspace(M, K, N)
+            ws = _guarded(nbytes)
+            got = torch.full((M, N), 77, dtype=kind, device=DEV)
+            hinm.hinm_mx4_linear(M, K, N, dtype, *w, X, ld, got, N, flags, ws, nbytes)
+            assert torch.equal(got, want), (ld, first, flags)
+            assert (ws[nbytes:] == GUARD).all()
+        del keep
+
+
+def test_a_training_step_of_a_4_bit_layer():
+    """Forward, input gradient and weight gradient are products of forms made along the axis that is summed over."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    M, K, N, dtype = 200, 330, 150, "bf16"
+    W, X, dY = (_draw(*s, dtype, i, special=False) for i, s in enumerate(((M, K), (K, N), (M, N))))
+    for b in (W, X, dY):
+        b[np.abs(_wide(b, dtype)) > 1e3] = 0x3F80       # sums within fp32
+    dev = {n: torch.from_numpy(b.view(np.int16)).to(DEV) for n, b in (("W", W), ("X", X), ("dY", dY))}
+    vals = {"W": _wide(W, dtype), "X": _wide(X, dtype), "dY": _wide(dY, dtype)}
+
+    def form(name, along):
+        r, c = vals[name].shape
+        f = _form(*((r, c) if along == hinm.MX4_ROWS else (c, r)))
+        hinm.hinm_mx4_quantize(r, c, dtype, dev[name], c, along, *f)
+        Z = vals[name] if along == hinm.MX4_ROWS else vals[name].T
+        return f, orc.values(*orc.quantize_rows(Z), Z.shape[1])
+    R, Cc = hinm.MX4_ROWS, hinm.MX4_COLUMNS
+    for (m, n, k), a, b in (((M, N, K), ("W", R), ("X", Cc)), ((K, N, M), ("W", Cc), ("dY", Cc)), ((M, K, N), ("dY", R), ("X", R))):
+        (fa, A), (fb, B) = form(*a), form(*b)
+        Y = torch.empty((m, n), dtype=torch.float32, device=DEV)
+        hinm.hinm_mx4_product(m, n, k, dtype, *fa, *fb, Y, n, hinm.OUT_F32)
+        want, size = orc.product(A, B)
+        assert (np.abs(Y.cpu().numpy() - want) <= _tolerance(size, k, want, "f32")).all()
+
+
+def test_streams_and_graph_replays():
+    """A side stream, and three replays of a captured linear call (first with one token, then with a batch) on inputs that
+    change between them."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    M, K, dtype = 96, 1100, "f16"
+    w = _upload(*_random_form(M, K, 21))
+    for N in (1, 24, 600):
+        X = torch.empty((K, N), dtype=torch.int16, device=DEV)
+        Y = torch.empty((M, N), dtype=torch.int16, device=DEV)
+        nbytes = hinm.hinm_mx4_linear_workspace(M, K, N)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+        call = lambda out: hinm.hinm_mx4_linear(M, K, N, dtype, *w, X, N, out, N, 0, ws, nbytes)
+        draws = [torch.from_numpy(_draw(K, N, dtype, s, special=False).view(np.int16)).to(DEV) for s in range(3)]
+        X.copy_(draws[0])
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call(Y)
+            side.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                call(Y)
+        torch.cuda.current_stream().wait_stream(side)
+        for d in draws:
+            X.copy_(d)
+            want = torch.empty_like(Y)
+            call(want)
+            Y.fill_(5)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(Y, want)
