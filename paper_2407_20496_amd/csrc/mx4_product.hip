@@ -124,7 +124,8 @@ hipError_t launch_split(const Mx4ProductArgs& a, const ProductShape& p, hipStrea
 // consecutive lanes (16 rows, one piece) read 16 different 16-byte units of 256 bytes.
 //   Waits: copies of a wave land in order.  In the middle of step s the copies of stages s + 2 and s + 3 may be outstanding,
 // all earlier ones are waited for; past the barrier stage s + 1 is there for everyone, and everyone has read stage s (its
-// LDS reads are waited for before the barrier), so its place takes stage s + 4.  Scales of group g + 1 are copied in the first
+// LDS reads are waited for before the barrier), so its place takes stage s + 4: half of its copies in the second half of step
+// s, the others in the first half of step s + 1.  Scales of group g + 1 are copied in the first
 // step of group g into the half that group g - 1 used, and have landed by its last step, before stage 4 g + 4.  Beyond the last step the last stage is
 // copied again, which keeps the count the same; nobody reads it.
 constexpr int kStages = 4;
@@ -174,11 +175,9 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     const int row = 64 * (wave * T::kScaleCopies + c) + lane;
     scales_from[c] = row < T::TM ? a_scales + min(m0 + row, p.M - 1) * sp : b_scales + min(n0 + row - T::TM, p.N - 1) * sp;
   }
-  auto copy_stage = [&](int s) {
-    const int64_t at = 64 * (int64_t)min(s, steps - 1);
-    uint8_t* to = lds + (s & (kStages - 1)) * T::kStageBytes + wave * T::kCopies * 1024;
-#pragma unroll
-    for (int c = 0; c < T::kCopies; ++c) copy16_to_lds(from[c] + at, to + 1024 * c);
+  auto copy_rows = [&](int s, int c) {  // one of the wave's copies of a stage
+    copy16_to_lds(from[c] + 64 * (int64_t)min(s, steps - 1),
+                  lds + (s & (kStages - 1)) * T::kStageBytes + (wave * T::kCopies + c) * 1024);
   };
   auto copy_scales = [&](int g) {
     const int64_t at = 16 * (int64_t)min(g, groups - 1);
@@ -197,12 +196,10 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   struct Operands {
     u32x4 a[WM], b[WN];
   };
-  auto read_half = [&](int s, int q, Operands& f) {
+  auto read_one = [&](int s, int q, int t, Operands& f) {
     const uint8_t* base = lds + (s & (kStages - 1)) * T::kStageBytes + (q ? piece1 : piece0);
-#pragma unroll
-    for (int i = 0; i < WM; ++i) f.a[i] = *reinterpret_cast<const u32x4*>(base + row_a + 2048 * i);
-#pragma unroll
-    for (int i = 0; i < WN; ++i) f.b[i] = *reinterpret_cast<const u32x4*>(base + row_b + 2048 * i);
+    if (t < WM) f.a[t] = *reinterpret_cast<const u32x4*>(base + row_a + 2048 * t);
+    else f.b[t - WM] = *reinterpret_cast<const u32x4*>(base + row_b + 2048 * (t - WM));
   };
   u32x2 scale_a[WM], scale_b[WN];  // word q: the lane's blocks 2 half + q of four steps
   auto read_scales = [&](int g) {
@@ -220,45 +217,45 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     for (int j = 0; j < WM; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
-  auto multiply = [&](auto byte, int q, const Operands& f, int from_tile, int to_tile) {
+  // Half a step: the products of one operand set, and between them, one at a time so that neither the wave's issue nor the
+  // units behind it back up, the LDS reads of the next set (from the first product on: the compiler waits there for every
+  // read before it) and half of a stage's copies.
+  auto half_step = [&](auto byte, auto which, const Operands& now, Operands& next, int read_stage, int copied_stage) {
+    constexpr int kTiles = WM * WN, kReads = WM + WN, kHalfCopies = T::kCopies / 2, q = decltype(which)::value;
 #pragma unroll
-    for (int t = 0; t < WM * WN; ++t) {
-      if (t < from_tile || t >= to_tile) continue;
+    for (int t = 0; t < kTiles; ++t) {
       const int i = t / WM, j = t % WM;
-      acc[i][j] = mfma_32x32x64<decltype(byte)::value>(f.b[i], scale_b[i][q], f.a[j], scale_a[j][q], acc[i][j]);
+      acc[i][j] = mfma_32x32x64<decltype(byte)::value>(now.b[i], scale_b[i][q], now.a[j], scale_a[j][q], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int e = t * kReads * 2 / kTiles; e < (t + 1) * kReads * 2 / kTiles && e < kReads; ++e) read_one(read_stage, 1 - q, e, next);
+#pragma unroll
+      for (int c = t * kHalfCopies / kTiles; c < (t + 1) * kHalfCopies / kTiles; ++c) copy_rows(copied_stage, (1 - q) * kHalfCopies + c);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   copy_scales(0);
 #pragma unroll
-  for (int s = 0; s < kStages; ++s) copy_stage(s);
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * T::kCopies) : "memory");
+  for (int s = 0; s < kStages; ++s)
+#pragma unroll
+    for (int c = 0; c < T::kCopies; ++c)
+      if (s < kStages - 1 || c < T::kCopies / 2) copy_rows(s, c);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * T::kCopies - T::kCopies / 2) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   Operands first, second;
-  read_half(0, 0, first);
+#pragma unroll
+  for (int t = 0; t < WM + WN; ++t) read_one(0, 0, t, first);
   read_scales(0);
 
-  // One step: the second halves' operands arrive while the first ones multiply, the next stage's first ones while the second do.
-  // Reads go out behind the first product of a half: the compiler waits there for every LDS read before it.
   auto step = [&](auto byte, int s, bool with_scales) {
-    multiply(byte, 0, first, 0, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    read_half(s, 1, second);
-    __builtin_amdgcn_sched_barrier(0);
-    multiply(byte, 0, first, 1, WM * WN);
-    __builtin_amdgcn_sched_barrier(0);
+    half_step(byte, std::integral_constant<int, 0>{}, first, second, s, s + kStages - 1);
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * T::kCopies) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    multiply(byte, 1, second, 0, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    read_half(s + 1, 0, first);
-    __builtin_amdgcn_sched_barrier(0);
     if (with_scales) copy_scales((s >> 2) + 1);
-    copy_stage(s + kStages);
-    multiply(byte, 1, second, 1, WM * WN);
-    __builtin_amdgcn_sched_barrier(0);
+    half_step(byte, std::integral_constant<int, 1>{}, second, first, s + 1, s + kStages);
   };
   int s = 0;
   for (; s + 4 <= steps; s += 4) {
