@@ -369,13 +369,13 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
  * version 1.0): 32 consecutive values of a row share a power of two, and every value is one of
  * 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives times it.
- *   codes   uint8 [rows][64 ceil(length / 128)]  value k of a row in byte k / 2, low nibble for even
- *           k; a nibble is the sign (bit 3) and the place in the list above.  Beyond `length`: zero.
- *   scales  uint8 [rows][16 ceil(length / 512)]  one byte e for 32 values: their power of two is
- *           2^(e - 127), 255 = not a number.  Block j = k / 32 of a row sits at byte
- *           16 (j / 16) + 4 (j % 4) + (j % 16) / 4: in sixteen blocks' bytes the four of every
- *           fourth block are neighbours, so one 4-byte load serves a lane of the scaled matrix
- *           instruction for 512 values.  Blocks that begin at or beyond `length`: 127.
+ *   codes   uint8 [ceil(length / 256)][rows][128]  value k of row r in line k / 256 at [r][k % 256 / 2], low
+ *           nibble for even k; a nibble is the sign (bit 3) and the place in the list above.  Zero
+ *           beyond `length`.
+ *   scales  uint8 [ceil(length / 512)][rows][16]  one byte e for 32 values: their power of two is
+ *           2^(e - 127), 255 = not a number.  The 16 blocks of 512 values: block j at byte 4 (j % 4) + j / 4
+ *           (every fourth block's bytes are neighbours, so one 4-byte load serves a lane of the scaled
+ *           matrix instruction for 512 values).  127 for blocks that begin at or beyond `length`.
  * Both 16-byte aligned.  hinm_mx4_sizes gives their sizes in bytes; either output pointer may be NULL. */
 enum { HINM_MX4_ROWS = 0, HINM_MX4_COLUMNS = 1 };
 hinm_status hinm_mx4_sizes(int32_t rows, int32_t length, size_t* code_bytes, size_t* scale_bytes);

@@ -13,11 +13,23 @@ VALUES = np.concatenate([LEVELS, -LEVELS])
 
 
 def code_pitch(length: int) -> int:
-    return (length + 127) // 128 * 64
+    """Bytes of a row's codes: whole lines of 256 values."""
+    return (length + 255) // 256 * 128
 
 
 def scale_pitch(length: int) -> int:
     return (length + 511) // 512 * 16
+
+
+def to_memory(codes: np.ndarray, scales: np.ndarray):
+    """A form with its rows one after the other, as everywhere in this module -> as it lies in memory: lines and groups first."""
+    turn = lambda a, n: np.ascontiguousarray(a.reshape(a.shape[0], -1, n).transpose(1, 0, 2)).reshape(-1)
+    return turn(codes, 128), turn(scales, 16)
+
+
+def from_memory(codes: np.ndarray, scales: np.ndarray, rows: int):
+    turn = lambda a, n: np.ascontiguousarray(a.reshape(-1, rows, n).transpose(1, 0, 2)).reshape(rows, -1)
+    return turn(codes, 128), turn(scales, 16)
 
 
 def scale_place(block: int) -> int:

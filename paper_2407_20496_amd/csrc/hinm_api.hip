@@ -89,7 +89,7 @@ struct LinearPlan {
   size_t codes, scales;  // bytes of the activations' 4-bit form, each rounded to 256
 };
 LinearPlan linear_plan(int32_t K, int32_t N) {
-  const size_t c = (size_t)N * mx4_code_pitch(K), s = (size_t)N * mx4_scale_pitch(K);
+  const size_t c = (size_t)mx4_code_bytes(N, K), s = (size_t)mx4_scale_bytes(N, K);
   return {(c + 255) & ~size_t{255}, (s + 255) & ~size_t{255}};
 }
 
@@ -678,8 +678,8 @@ hinm_status hinm_calib_mid_plan(const hinm_shape* shape, int32_t N, int32_t form
 
 hinm_status hinm_mx4_sizes(int32_t rows, int32_t length, size_t* code_bytes, size_t* scale_bytes) {
   if (rows <= 0 || length <= 0) return HINM_ERR_SHAPE;
-  if (code_bytes) *code_bytes = (size_t)rows * mx4_code_pitch(length);
-  if (scale_bytes) *scale_bytes = (size_t)rows * mx4_scale_pitch(length);
+  if (code_bytes) *code_bytes = (size_t)mx4_code_bytes(rows, length);
+  if (scale_bytes) *scale_bytes = (size_t)mx4_scale_bytes(rows, length);
   return HINM_OK;
 }
 

@@ -1,8 +1,10 @@
 // Microscaled 4-bit form (include/hinm.h): where codes and scales lie, and the conversions in both directions.
 //
 // 32 consecutive values share the power of two 2^(e - 127) (e = scale byte); a code is a sign and a place in
-// 0, .5, 1, 1.5, 2, 3, 4, 6.  Codes of a row are linear, padded to 128 values = 64 bytes, one k-step of the scaled matrix
-// instruction.  Scales are padded to 16 blocks = 16 bytes; inside them byte 4 b + s belongs to block 4 s + b.
+// 0, .5, 1, 1.5, 2, 3, 4, 6.  Lines of 256 values = 128 bytes of codes and groups of 512 values = 16 scale bytes come first
+// in the order, rows second: what a workgroup takes of neighbouring rows at one place of the summed axis is one contiguous
+// piece.  (Rows after one another instead: a group's scale bytes of 256 rows lay in 256 cache lines, which were fetched again
+// for every group.)  Byte 4 b + s of a group's scales belongs to block 4 s + b.
 //
 // Operand layout of the scaled matrix instructions on 4-bit values, established on MI355X with random codes and scales:
 // lane l of the 16x16x128 form holds row l % 16 and the 32 values of block l / 16, in order, low nibble first; of the
@@ -20,11 +22,17 @@
 
 namespace hinm {
 
-constexpr int kMx4Step = 128;    // values of a k-step: 64 bytes of codes
+constexpr int kMx4Step = 128;    // values of a 16x16x128 instruction: 64 bytes of codes
+constexpr int kMx4Line = 256;    // values of a line of codes
 constexpr int kMx4Group = 512;   // values whose 16 scale bytes lie together
 
-__host__ __device__ constexpr int64_t mx4_code_pitch(int length) { return ((int64_t)length + 127) / 128 * 64; }
-__host__ __device__ constexpr int64_t mx4_scale_pitch(int length) { return ((int64_t)length + 511) / 512 * 16; }
+__host__ __device__ constexpr int mx4_lines(int length) { return (int)(((int64_t)length + 255) / 256); }
+__host__ __device__ constexpr int mx4_groups(int length) { return (int)(((int64_t)length + 511) / 512); }
+__host__ __device__ constexpr int64_t mx4_code_bytes(int rows, int length) { return (int64_t)mx4_lines(length) * rows * 128; }
+__host__ __device__ constexpr int64_t mx4_scale_bytes(int rows, int length) { return (int64_t)mx4_groups(length) * rows * 16; }
+// where a row's line of codes and its group of scales begin
+__host__ __device__ constexpr int64_t mx4_line_at(int line, int rows, int64_t row) { return ((int64_t)line * rows + row) * 128; }
+__host__ __device__ constexpr int64_t mx4_group_at(int group, int rows, int64_t row) { return ((int64_t)group * rows + row) * 16; }
 // of block j among its group's 16
 __host__ __device__ constexpr int mx4_scale_place(int j) { return 4 * (j & 3) + (j >> 2); }
 

@@ -52,35 +52,35 @@ __global__ __launch_bounds__(512) void mx4_split_kernel(const uint8_t* a_codes, 
   const int r = lane & 15, b = lane >> 4;
   const int blocks_n = (p.N + 16 * NT - 1) / (16 * NT);
   const int m0 = (int)(blockIdx.x / blocks_n) * 16, n0 = (int)(blockIdx.x % blocks_n) * 16 * NT;
-  const int64_t cp = mx4_code_pitch(p.K), sp = mx4_scale_pitch(p.K);
-  const int steps = (p.K + kMx4Step - 1) / kMx4Step, groups = (steps + 3) / 4;
+  const int lines = mx4_lines(p.K), groups = mx4_groups(p.K);
   // rows beyond the matrices repeat the last one: what they give is not stored
   const int64_t ra = min(m0 + r, p.M - 1);
-  const uint8_t* ac = a_codes + ra * cp + 16 * b;
-  const uint8_t* as = a_scales + ra * sp + 4 * b;
+  const uint8_t* ac = a_codes + ra * 128 + 16 * b;
+  const uint8_t* as = a_scales + ra * 16 + 4 * b;
+  const int64_t a_line = (int64_t)p.M * 128, b_line = (int64_t)p.N * 128, a_group = (int64_t)p.M * 16, b_group = (int64_t)p.N * 16;
   const uint8_t *bc[NT], *bs[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int64_t rb = min(n0 + 16 * t + r, p.N - 1);
-    bc[t] = b_codes + rb * cp + 16 * b;
-    bs[t] = b_scales + rb * sp + 4 * b;
+    bc[t] = b_codes + rb * 128 + 16 * b;
+    bs[t] = b_scales + rb * 16 + 4 * b;
   }
   f32x4 acc[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) acc[t] = f32x4{0, 0, 0, 0};
   for (int g = wave; g < groups; g += waves) {
-    const uint32_t sa = *reinterpret_cast<const uint32_t*>(as + 16 * (int64_t)g);
+    const uint32_t sa = *reinterpret_cast<const uint32_t*>(as + g * a_group);
     uint32_t sb[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) sb[t] = *reinterpret_cast<const uint32_t*>(bs[t] + 16 * (int64_t)g);
+    for (int t = 0; t < NT; ++t) sb[t] = *reinterpret_cast<const uint32_t*>(bs[t] + g * b_group);
     auto step = [&](auto s_) {
       constexpr int s = decltype(s_)::value;
-      if (4 * g + s >= steps) return;
-      const int64_t at = 256 * (int64_t)g + 64 * s;
-      const u32x4 a = *reinterpret_cast<const u32x4*>(ac + at);
+      const int line = 2 * g + s / 2;
+      if (line >= lines) return;
+      const u32x4 a = *reinterpret_cast<const u32x4*>(ac + line * a_line + 64 * (s & 1));
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        acc[t] = mfma_16x16x128<s>(*reinterpret_cast<const u32x4*>(bc[t] + at), sb[t], a, sa, acc[t]);
+        acc[t] = mfma_16x16x128<s>(*reinterpret_cast<const u32x4*>(bc[t] + line * b_line + 64 * (s & 1)), sb[t], a, sa, acc[t]);
     };
     step(std::integral_constant<int, 0>{});
     step(std::integral_constant<int, 1>{});
@@ -117,27 +117,26 @@ hipError_t launch_split(const Mx4ProductArgs& a, const ProductShape& p, hipStrea
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
 // A workgroup of four waves (2 x 2) owns TM = 64 WM rows of A and TN = 64 WN rows of B; a wave owns half of each, in 32x32
-// tiles.  A stage is one k-step: 64 bytes of every row, copied straight into LDS, kStages stages in a ring; the 16 scale
-// bytes a row has for four k-steps come with every fourth stage.  A wave holds the operands of the stage it multiplies and
-// reads those of the next meanwhile.
-//   Swizzle: the four 16-byte pieces of a row sit at piece ^ (row / 4 % 4), applied on the copy's source side, so that 16
+// tiles.  A stage is 256 values = one 128-byte line of every row, copied straight into LDS, two stages in turn; the 16 scale
+// bytes a row has for 512 values come with every second stage.  A stage is four instructions for every 32x32 tile; a wave
+// reads the operands of the next one while it multiplies.  (Stages of 128 values, four in turn: copies of half lines run at
+// 20 bytes a clock and compute unit and took 885 us of 16384x16384x8192's 1176 us by themselves.)
+//   Swizzle: the eight 16-byte pieces of a row sit at piece ^ (row / 2 % 8), applied on the copy's source side, so that 16
 // consecutive lanes (16 rows, one piece) read 16 different 16-byte units of 256 bytes.
-//   Waits: copies of a wave land in order.  In the middle of step s the copies of stages s + 2 and s + 3 may be outstanding,
-// all earlier ones are waited for; past the barrier stage s + 1 is there for everyone, and everyone has read stage s (its
-// LDS reads are waited for before the barrier), so its place takes stage s + 4: half of its copies in the second half of step
-// s, the others in the first half of step s + 1.  Scales of group g + 1 are copied in the first
-// step of group g into the half that group g - 1 used, and have landed by its last step, before stage 4 g + 4.  Beyond the last step the last stage is
-// copied again, which keeps the count the same; nobody reads it.
-constexpr int kStages = 4;
+//   Waits: before the last quarter of stage p every copy of the wave's has landed, stage p + 1 among them, and its LDS reads of
+// stage p are done; past the barrier that holds for all waves, so the place of stage p takes stage p + 2: half of its copies
+// during the last quarter of p, the others during the first of p + 1.  Scales of group g + 1 (stages 2 g + 2 and 2 g + 3) are
+// copied in the last quarter of stage 2 g into the half that group g - 1 used.  Beyond the last stage the last one is
+// copied again; nobody reads it.
 
 template <int WM, int WN>
 struct TileSizes {
   static constexpr int TM = 64 * WM, TN = 64 * WN;
-  static constexpr int kStageBytes = (TM + TN) * 64;
-  static constexpr int kScaleBytes = (TM + TN) * 16;               // of a group of four steps
-  static constexpr int kCopies = (TM + TN) / 64;                   // of a wave and stage: 16 rows each
-  static constexpr int kScaleCopies = (TM + TN) / 256;             // of a wave and group: 64 rows each
-  static constexpr int kLds = kStages * kStageBytes + 2 * kScaleBytes;
+  static constexpr int kStageBytes = (TM + TN) * 128;
+  static constexpr int kScaleBytes = (TM + TN) * 16;               // of two stages
+  static constexpr int kCopies = (TM + TN) / 32;                   // of a wave and stage: 8 rows each
+  static constexpr int kScaleCopies = (TM + TN) / 256;             // of a wave and two stages: 64 rows each
+  static constexpr int kLds = 2 * (kStageBytes + kScaleBytes);
   static_assert((TM + TN) % 256 == 0 && TM % 64 == 0, "whole copies for every wave");
 };
 
@@ -147,7 +146,7 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
                                                                             void* Y, ProductShape p) {
   using T = TileSizes<WM, WN>;
   extern __shared__ __align__(16) uint8_t lds[];
-  uint8_t* const lds_scales = lds + kStages * T::kStageBytes;
+  uint8_t* const lds_scales = lds + 2 * T::kStageBytes;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // workgroups go to the eight XCDs in turn: each XCD takes a contiguous run of the list of tiles, panels of eight tiles of A
   // times all of B, so that the 32 tiles it works on share eight and four operand tiles in its L2
@@ -158,48 +157,52 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   const int panel = item / (8 * tiles_n), in_panel = item - panel * 8 * tiles_n;
   const int height = min(8, tiles_m - 8 * panel);
   const int m0 = (8 * panel + in_panel % height) * T::TM, n0 = in_panel / height * T::TN;
-  const int64_t cp = mx4_code_pitch(p.K), sp = mx4_scale_pitch(p.K);
-  const int steps = (p.K + kMx4Step - 1) / kMx4Step, groups = (steps + 3) >> 2;
+  const int stages = mx4_lines(p.K), groups = mx4_groups(p.K);
 
   // where this lane's part of each copy comes from; rows beyond the matrices repeat the last one (what they give is not stored)
   const uint8_t* from[T::kCopies];
   const uint8_t* scales_from[T::kScaleCopies];
 #pragma unroll
   for (int c = 0; c < T::kCopies; ++c) {
-    const int row = 16 * (wave * T::kCopies + c) + (lane >> 2);
-    const int piece = (lane & 3) ^ ((lane >> 4) & 3);
-    from[c] = (row < T::TM ? a_codes + min(m0 + row, p.M - 1) * cp : b_codes + min(n0 + row - T::TM, p.N - 1) * cp) + 16 * piece;
+    const int row = 8 * (wave * T::kCopies + c) + (lane >> 3);
+    const int piece = (lane & 7) ^ ((row >> 1) & 7);
+    from[c] = (row < T::TM ? a_codes + min(m0 + row, p.M - 1) * int64_t{128} : b_codes + min(n0 + row - T::TM, p.N - 1) * int64_t{128}) +
+              16 * piece;
   }
 #pragma unroll
   for (int c = 0; c < T::kScaleCopies; ++c) {
     const int row = 64 * (wave * T::kScaleCopies + c) + lane;
-    scales_from[c] = row < T::TM ? a_scales + min(m0 + row, p.M - 1) * sp : b_scales + min(n0 + row - T::TM, p.N - 1) * sp;
+    scales_from[c] = row < T::TM ? a_scales + min(m0 + row, p.M - 1) * int64_t{16} : b_scales + min(n0 + row - T::TM, p.N - 1) * int64_t{16};
   }
-  auto copy_rows = [&](int s, int c) {  // one of the wave's copies of a stage
-    copy16_to_lds(from[c] + 64 * (int64_t)min(s, steps - 1),
-                  lds + (s & (kStages - 1)) * T::kStageBytes + (wave * T::kCopies + c) * 1024);
+  auto copy_rows = [&](int stage, int c) {  // one of the wave's copies of a stage
+    // which matrix a copy belongs to is uniform: TM is a multiple of a copy's rows
+    const int64_t line = (wave * T::kCopies + c) * 8 < T::TM ? (int64_t)p.M * 128 : (int64_t)p.N * 128;
+    copy16_to_lds(from[c] + line * min(stage, stages - 1),
+                  lds + (stage & 1) * T::kStageBytes + (wave * T::kCopies + c) * 1024);
   };
   auto copy_scales = [&](int g) {
-    const int64_t at = 16 * (int64_t)min(g, groups - 1);
     uint8_t* to = lds_scales + (g & 1) * T::kScaleBytes + wave * T::kScaleCopies * 1024;
 #pragma unroll
-    for (int c = 0; c < T::kScaleCopies; ++c) copy16_to_lds(scales_from[c] + at, to + 1024 * c);
+    for (int c = 0; c < T::kScaleCopies; ++c) {
+      const int64_t group = (wave * T::kScaleCopies + c) * 64 < T::TM ? (int64_t)p.M * 16 : (int64_t)p.N * 16;
+      copy16_to_lds(scales_from[c] + group * min(g, groups - 1), to + 1024 * c);
+    }
   };
 
   const int half = lane >> 5, r = lane & 31;
   const int wave_m = (wave & 1) * 32 * WM, wave_n = (wave >> 1) * 32 * WN;
-  // byte offsets of this lane's two pieces of a row, and of its first rows
-  const int piece0 = 16 * ((2 * half) ^ ((r >> 2) & 3)), piece1 = 16 * ((2 * half + 1) ^ ((r >> 2) & 3));
-  const int row_a = (wave_m + r) * 64, row_b = (T::TM + wave_n + r) * 64;
+  // byte offset of this lane's piece of a row in the first quarter (the others differ in its bits 0 and 2), and of its first rows
+  const int piece0 = 16 * ((2 * half) ^ ((r >> 1) & 7));
+  const int row_a = (wave_m + r) * 128, row_b = (T::TM + wave_n + r) * 128;
 
-  // one operand set: piece q of this lane's blocks of a stage (the first or second instruction of a step)
+  // one operand set: what a quarter of a stage multiplies
   struct Operands {
     u32x4 a[WM], b[WN];
   };
-  auto read_one = [&](int s, int q, int t, Operands& f) {
-    const uint8_t* base = lds + (s & (kStages - 1)) * T::kStageBytes + (q ? piece1 : piece0);
-    if (t < WM) f.a[t] = *reinterpret_cast<const u32x4*>(base + row_a + 2048 * t);
-    else f.b[t - WM] = *reinterpret_cast<const u32x4*>(base + row_b + 2048 * (t - WM));
+  auto read_one = [&](int stage, int quarter, int t, Operands& f) {
+    const uint8_t* base = lds + (stage & 1) * T::kStageBytes + (piece0 ^ 16 * (4 * (quarter >> 1) + (quarter & 1)));
+    if (t < WM) f.a[t] = *reinterpret_cast<const u32x4*>(base + row_a + 4096 * t);
+    else f.b[t - WM] = *reinterpret_cast<const u32x4*>(base + row_b + 4096 * (t - WM));
   };
   u32x2 scale_a[WM], scale_b[WN];  // word q: the lane's blocks 2 half + q of four steps
   auto read_scales = [&](int g) {
@@ -217,31 +220,33 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     for (int j = 0; j < WM; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
-  // Half a step: the products of one operand set, and between them, one at a time so that neither the wave's issue nor the
-  // units behind it back up, the LDS reads of the next set (from the first product on: the compiler waits there for every
-  // read before it) and half of a stage's copies.
-  auto half_step = [&](auto byte, auto which, const Operands& now, Operands& next, int read_stage, int copied_stage) {
-    constexpr int kTiles = WM * WN, kReads = WM + WN, kHalfCopies = T::kCopies / 2, q = decltype(which)::value;
+  // A quarter of a stage: the products of one operand set, and between them, one at a time so that neither the wave's issue nor
+  // the units behind it back up, the LDS reads of the next set (from the first product on: the compiler waits there for every
+  // read before it) and, in the quarters that have them, half of a stage's copies.
+  auto quarter_stage = [&](auto byte, auto which, const Operands& now, Operands& next, int read_stage, int copied_stage) {
+    constexpr int kTiles = WM * WN, kReads = WM + WN, kHalf = T::kCopies / 2, h = decltype(which)::value;
+    constexpr bool kCopying = h == 3 || h == 0;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const int i = t / WM, j = t % WM;
-      acc[i][j] = mfma_32x32x64<decltype(byte)::value>(now.b[i], scale_b[i][q], now.a[j], scale_a[j][q], acc[i][j]);
+      acc[i][j] = mfma_32x32x64<decltype(byte)::value>(now.b[i], scale_b[i][h & 1], now.a[j], scale_a[j][h & 1], acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int e = t * kReads * 2 / kTiles; e < (t + 1) * kReads * 2 / kTiles && e < kReads; ++e) read_one(read_stage, 1 - q, e, next);
+      for (int e = t * kReads * 2 / kTiles; e < (t + 1) * kReads * 2 / kTiles && e < kReads; ++e)
+        read_one(read_stage, (h + 1) & 3, e, next);
 #pragma unroll
-      for (int c = t * kHalfCopies / kTiles; c < (t + 1) * kHalfCopies / kTiles; ++c) copy_rows(copied_stage, (1 - q) * kHalfCopies + c);
+      for (int c = t * kHalf / kTiles; kCopying && c < (t + 1) * kHalf / kTiles; ++c)
+        copy_rows(copied_stage, (h == 0 ? kHalf : 0) + c);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   copy_scales(0);
 #pragma unroll
-  for (int s = 0; s < kStages; ++s)
+  for (int c = 0; c < T::kCopies; ++c) copy_rows(0, c);
 #pragma unroll
-    for (int c = 0; c < T::kCopies; ++c)
-      if (s < kStages - 1 || c < T::kCopies / 2) copy_rows(s, c);
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kStages - 1) * T::kCopies - T::kCopies / 2) : "memory");
+  for (int c = 0; c < T::kCopies / 2; ++c) copy_rows(1, c);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::kCopies / 2) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   Operands first, second;
@@ -249,29 +254,27 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   for (int t = 0; t < WM + WN; ++t) read_one(0, 0, t, first);
   read_scales(0);
 
-  auto step = [&](auto byte, int s, bool with_scales) {
-    half_step(byte, std::integral_constant<int, 0>{}, first, second, s, s + kStages - 1);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * T::kCopies) : "memory");
+  // FIRST: the first stage of its group, with scale bytes 0 and 1; the other one has 2 and 3
+  auto stage = [&](auto is_first, int p) {
+    constexpr bool kFirst = decltype(is_first)::value;
+    constexpr std::integral_constant<int, kFirst ? 0 : 2> lower{};
+    constexpr std::integral_constant<int, kFirst ? 1 : 3> upper{};
+    quarter_stage(lower, std::integral_constant<int, 0>{}, first, second, p, p + 1);
+    quarter_stage(lower, std::integral_constant<int, 1>{}, second, first, p, 0);
+    quarter_stage(upper, std::integral_constant<int, 2>{}, first, second, p, 0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (with_scales) copy_scales((s >> 2) + 1);
-    half_step(byte, std::integral_constant<int, 1>{}, second, first, s + 1, s + kStages);
+    if (kFirst) copy_scales((p >> 1) + 1);
+    quarter_stage(upper, std::integral_constant<int, 3>{}, second, first, p + 1, p + 2);
   };
-  int s = 0;
-  for (; s + 4 <= steps; s += 4) {
-    step(std::integral_constant<int, 0>{}, s, true);
-    step(std::integral_constant<int, 1>{}, s + 1, false);
-    step(std::integral_constant<int, 2>{}, s + 2, false);
-    step(std::integral_constant<int, 3>{}, s + 3, false);
-    read_scales((s >> 2) + 1);
+  int p0 = 0;
+  for (; p0 + 2 <= stages; p0 += 2) {
+    stage(std::true_type{}, p0);
+    stage(std::false_type{}, p0 + 1);
+    read_scales((p0 >> 1) + 1);
   }
-  for (; s < steps; ++s) {  // up to three steps: the scale bytes move down instead
-    step(std::integral_constant<int, 0>{}, s, false);
-#pragma unroll
-    for (int i = 0; i < WM; ++i) scale_a[i] = u32x2{scale_a[i][0] >> 8, scale_a[i][1] >> 8};
-#pragma unroll
-    for (int i = 0; i < WN; ++i) scale_b[i] = u32x2{scale_b[i][0] >> 8, scale_b[i][1] >> 8};
-  }
+  if (p0 < stages) stage(std::true_type{}, p0);
   // every copy has landed and every wave has read its operands: the ring becomes the waves' slabs
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();

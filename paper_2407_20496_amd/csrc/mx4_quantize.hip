@@ -16,7 +16,7 @@ __device__ __forceinline__ uint32_t max_with_lane(uint32_t m) {
 }
 
 // ---- blocks along the rows --------------------------------------------------------------------------
-// A wave takes 512 consecutive values of a row (eight a lane, four lanes a block): one contiguous kilobyte in, 256 bytes of
+// A wave takes 512 consecutive values of a row (eight a lane, four lanes a block): one contiguous kilobyte in, two lines of
 // codes and the group's 16 scale bytes out.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src, int64_t ld, int rows, int cols, bool vec,
@@ -44,16 +44,15 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src,
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, low_half<DT>(v[2]) * s, high_half<DT>(v[2]) * s, 1.0f, 2);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, low_half<DT>(v[3]) * s, high_half<DT>(v[3]) * s, 1.0f, 3);
   if (e == 255) c = 0;
-  const int64_t pitch = mx4_code_pitch(cols);
-  if (k / 2 < pitch) *reinterpret_cast<uint32_t*>(codes + row * pitch + k / 2) = c;
-  if ((lane & 3) == 0)
-    scales[row * mx4_scale_pitch(cols) + 16 * g + mx4_scale_place(lane >> 2)] = (uint8_t)(beyond ? 127 : e);
+  const int line = 2 * g + (lane >> 5);
+  if (line < mx4_lines(cols)) *reinterpret_cast<uint32_t*>(codes + mx4_line_at(line, rows, row) + 4 * (lane & 31)) = c;
+  if ((lane & 3) == 0) scales[mx4_group_at(g, rows, row) + mx4_scale_place(lane >> 2)] = (uint8_t)(beyond ? 127 : e);
 }
 
 // ---- blocks down the columns ------------------------------------------------------------------------
 // A workgroup takes 64 columns x 512 rows.  A wave reads a block's 32 rows in four loads of eight 128-byte segments: lane l
 // holds columns 8 (l % 8) .. + 7 of rows 4 (l / 8) .. + 3, so it has two bytes of codes for each of its columns.  They
-// meet in LDS and leave as runs of 256 bytes a column.
+// meet in LDS and leave as two runs of 8 KB.
 constexpr int kTileCols = 64;
 constexpr int kColumnPitch = 256 + 16;  // bytes of a column's codes in LDS: the pad spreads the columns over the banks
 
@@ -106,17 +105,16 @@ __global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* s
     }
   }
   __syncthreads();
-  const int64_t pitch = mx4_code_pitch(rows);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int piece = threadIdx.x + kThreads * q;
-    const int col = piece >> 4, at = 16 * (piece & 15);
-    if (n0 + col < cols && 256 * (int64_t)g + at < pitch)
-      *reinterpret_cast<u32x4*>(codes + (int64_t)(n0 + col) * pitch + 256 * (int64_t)g + at) =
-          *reinterpret_cast<const u32x4*>(tile + col * kColumnPitch + at);
+    const int piece = threadIdx.x + kThreads * q;  // of 2 lines x 64 columns x 8
+    const int line = 2 * g + (piece >> 9), col = (piece >> 3) & 63, at = 16 * (piece & 7);
+    if (n0 + col < cols && line < mx4_lines(rows))
+      *reinterpret_cast<u32x4*>(codes + mx4_line_at(line, cols, n0 + col) + at) =
+          *reinterpret_cast<const u32x4*>(tile + col * kColumnPitch + 128 * (piece >> 9) + at);
   }
   if (threadIdx.x < kTileCols && n0 + (int)threadIdx.x < cols)
-    *reinterpret_cast<u32x4*>(scales + (int64_t)(n0 + threadIdx.x) * mx4_scale_pitch(rows) + 16 * g) =
+    *reinterpret_cast<u32x4*>(scales + mx4_group_at(g, cols, n0 + threadIdx.x)) =
         *reinterpret_cast<const u32x4*>(tile_scales + 16 * threadIdx.x);
 }
 
@@ -132,8 +130,8 @@ __global__ __launch_bounds__(kThreads) void mx4_unpack_kernel(const uint8_t* cod
   const int g = (int)(item - row * groups);
   const int k = g * kMx4Group + 8 * lane;
   if (k >= length) return;
-  const uint32_t c = *reinterpret_cast<const uint32_t*>(codes + row * mx4_code_pitch(length) + k / 2);
-  const float s = mx4_scale_value(scales[row * mx4_scale_pitch(length) + 16 * g + mx4_scale_place(lane >> 2)]);
+  const uint32_t c = *reinterpret_cast<const uint32_t*>(codes + mx4_line_at(2 * g + (lane >> 5), rows, row) + 4 * (lane & 31));
+  const float s = mx4_scale_value(scales[mx4_group_at(g, rows, row) + mx4_scale_place(lane >> 2)]);
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   f32x2 f[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
                 __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};

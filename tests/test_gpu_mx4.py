@@ -43,12 +43,12 @@ def _host(form, rows, length):
     c, s = (t.cpu().numpy() for t in form)
     nc, ns = rows * orc.code_pitch(length), rows * orc.scale_pitch(length)
     assert (c[nc:] == GUARD).all() and (s[ns:] == GUARD).all(), "written beyond the form"
-    return c[:nc].reshape(rows, -1), s[:ns].reshape(rows, -1)
+    return orc.from_memory(c[:nc], s[:ns], rows)
 
 
 def _upload(codes, scales):
     import torch
-    return torch.from_numpy(codes.reshape(-1)).to(DEV), torch.from_numpy(scales.reshape(-1)).to(DEV)
+    return tuple(torch.from_numpy(a).to(DEV) for a in orc.to_memory(codes, scales))
 
 
 def _draw(rows, cols, dtype, seed, special=True):

@@ -34,6 +34,19 @@ def test_scales_and_their_places():
     assert sorted(orc.scale_place(j) for j in range(32)) == list(range(32))
 
 
+def test_order_in_memory():
+    """Lines of codes and groups of scales first, rows second."""
+    rng = np.random.default_rng(2)
+    c, s = orc.quantize_rows(rng.standard_normal((3, 700)))
+    mc, ms = orc.to_memory(c, s)
+    for r, k in ((0, 0), (2, 255), (1, 256), (2, 699)):
+        assert mc[(k // 256 * 3 + r) * 128 + k % 256 // 2] == c[r, k // 2]
+        j = k // 32
+        assert ms[(k // 512 * 3 + r) * 16 + 4 * (j % 4) + j % 16 // 4] == s[r, orc.scale_place(j)]
+    back = orc.from_memory(mc, ms, 3)
+    assert np.array_equal(back[0], c) and np.array_equal(back[1], s)
+
+
 def test_special_blocks():
     X = np.zeros((1, 160))
     X[0, 32] = np.inf
