@@ -135,9 +135,8 @@ struct TileSizes {
   static constexpr int kStageBytes = (TM + TN) * 128;
   static constexpr int kScaleBytes = (TM + TN) * 16;               // of two stages
   static constexpr int kCopies = (TM + TN) / 32;                   // of a wave and stage: 8 rows each
-  static constexpr int kScaleCopies = (TM + TN) / 256;             // of a wave and two stages: 64 rows each
   static constexpr int kLds = 2 * (kStageBytes + kScaleBytes);
-  static_assert((TM + TN) % 256 == 0 && TM % 64 == 0, "whole copies for every wave");
+  static_assert(TM == TN && (TM == 128 || TM == 256), "whole copies for every wave");
 };
 
 template <int OUT, int WM, int WN>
@@ -159,34 +158,44 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   const int m0 = (8 * panel + in_panel % height) * T::TM, n0 = in_panel / height * T::TN;
   const int stages = mx4_lines(p.K), groups = mx4_groups(p.K);
 
-  // where this lane's part of each copy comes from; rows beyond the matrices repeat the last one (what they give is not stored)
-  const uint8_t* from[T::kCopies];
-  const uint8_t* scales_from[T::kScaleCopies];
+  // Where this lane's part of each copy comes from, from the first of the tile's rows in a line or group on; rows beyond the
+  // matrices repeat the last one (what they give is not stored).  A wave copies a quarter of A's rows, then one of B's.
+  constexpr int kOfA = T::TM / 32;
+  const int rows_a = min(T::TM, p.M - m0), rows_b = min(T::TN, p.N - n0);
+  uint32_t from[T::kCopies];
 #pragma unroll
   for (int c = 0; c < T::kCopies; ++c) {
-    const int row = 8 * (wave * T::kCopies + c) + (lane >> 3);
+    const int row = (c < kOfA ? wave * (T::TM / 4) + 8 * c : wave * (T::TN / 4) + 8 * (c - kOfA)) + (lane >> 3);
     const int piece = (lane & 7) ^ ((row >> 1) & 7);
-    from[c] = (row < T::TM ? a_codes + min(m0 + row, p.M - 1) * int64_t{128} : b_codes + min(n0 + row - T::TM, p.N - 1) * int64_t{128}) +
-              16 * piece;
+    from[c] = 128 * min(row, (c < kOfA ? rows_a : rows_b) - 1) + 16 * piece;
   }
-#pragma unroll
-  for (int c = 0; c < T::kScaleCopies; ++c) {
-    const int row = 64 * (wave * T::kScaleCopies + c) + lane;
-    scales_from[c] = row < T::TM ? a_scales + min(m0 + row, p.M - 1) * int64_t{16} : b_scales + min(n0 + row - T::TM, p.N - 1) * int64_t{16};
-  }
-  auto copy_rows = [&](int stage, int c) {  // one of the wave's copies of a stage
-    // which matrix a copy belongs to is uniform: TM is a multiple of a copy's rows
-    const int64_t line = (wave * T::kCopies + c) * 8 < T::TM ? (int64_t)p.M * 128 : (int64_t)p.N * 128;
-    copy16_to_lds(from[c] + line * min(stage, stages - 1),
-                  lds + (stage & 1) * T::kStageBytes + (wave * T::kCopies + c) * 1024);
+  struct Source {
+    __amdgpu_buffer_rsrc_t a, b;
   };
+  auto source_of = [&](int stage) {
+    const int line = min(stage, stages - 1);
+    return Source{buffer_of(a_codes + mx4_line_at(line, p.M, m0), 128u * rows_a),
+                  buffer_of(b_codes + mx4_line_at(line, p.N, n0), 128u * rows_b)};
+  };
+  auto copy_rows = [&](const Source& src, int stage, int c) {  // one of the wave's copies of a stage
+    const int row0 = c < kOfA ? wave * (T::TM / 4) + 8 * c : T::TM + wave * (T::TN / 4) + 8 * (c - kOfA);
+    copy16_to_lds(c < kOfA ? src.a : src.b, from[c], lds + (stage & 1) * T::kStageBytes + row0 * 128);
+  };
+  // scales: 64 rows a copy; with 256 rows of each matrix every wave copies both, with 128 two waves A and two B
+  constexpr bool kBoth = T::TM == 256;
+  const bool scales_of_a = kBoth || wave < 2;
+  const uint8_t* const scale_rows = scales_of_a ? a_scales + 16 * (int64_t)m0 : b_scales + 16 * (int64_t)n0;
+  const int64_t scale_group = 16 * (int64_t)(scales_of_a ? p.M : p.N);
+  const int scale_count = scales_of_a ? rows_a : rows_b;
+  const int scale_row0 = 64 * (kBoth ? wave : wave & 1);
+  uint8_t* const scale_place = lds_scales + (scales_of_a ? 0 : T::TM * 16) + scale_row0 * 16;
+  const uint32_t scale_from = 16 * min(scale_row0 + lane, scale_count - 1), scale_from_b = 16 * min(scale_row0 + lane, rows_b - 1);
   auto copy_scales = [&](int g) {
-    uint8_t* to = lds_scales + (g & 1) * T::kScaleBytes + wave * T::kScaleCopies * 1024;
-#pragma unroll
-    for (int c = 0; c < T::kScaleCopies; ++c) {
-      const int64_t group = (wave * T::kScaleCopies + c) * 64 < T::TM ? (int64_t)p.M * 16 : (int64_t)p.N * 16;
-      copy16_to_lds(scales_from[c] + group * min(g, groups - 1), to + 1024 * c);
-    }
+    const int group = min(g, groups - 1);
+    copy16_to_lds(buffer_of(scale_rows + group * scale_group, 16u * scale_count), scale_from, scale_place + (g & 1) * T::kScaleBytes);
+    if constexpr (kBoth)
+      copy16_to_lds(buffer_of(b_scales + mx4_group_at(group, p.N, n0), 16u * rows_b), scale_from_b,
+                    scale_place + T::TM * 16 + (g & 1) * T::kScaleBytes);
   };
 
   const int half = lane >> 5, r = lane & 31;
@@ -226,6 +235,7 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   auto quarter_stage = [&](auto byte, auto which, const Operands& now, Operands& next, int read_stage, int copied_stage) {
     constexpr int kTiles = WM * WN, kReads = WM + WN, kHalf = T::kCopies / 2, h = decltype(which)::value;
     constexpr bool kCopying = h == 3 || h == 0;
+    const Source src = source_of(copied_stage);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       const int i = t / WM, j = t % WM;
@@ -236,16 +246,16 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
         read_one(read_stage, (h + 1) & 3, e, next);
 #pragma unroll
       for (int c = t * kHalf / kTiles; kCopying && c < (t + 1) * kHalf / kTiles; ++c)
-        copy_rows(copied_stage, (h == 0 ? kHalf : 0) + c);
+        copy_rows(src, copied_stage, (h == 0 ? kHalf : 0) + c);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   copy_scales(0);
 #pragma unroll
-  for (int c = 0; c < T::kCopies; ++c) copy_rows(0, c);
+  for (int c = 0; c < T::kCopies; ++c) copy_rows(source_of(0), 0, c);
 #pragma unroll
-  for (int c = 0; c < T::kCopies / 2; ++c) copy_rows(1, c);
+  for (int c = 0; c < T::kCopies / 2; ++c) copy_rows(source_of(1), 1, c);
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::kCopies / 2) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
