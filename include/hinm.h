@@ -369,13 +369,16 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
  * version 1.0): 32 consecutive values of a row share a power of two, and every value is one of
  * 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives times it.
- *   codes   uint8 [ceil(length / 256)][rows][128]  value k of row r in line k / 256 at [r][k % 256 / 2], low
- *           nibble for even k; a nibble is the sign (bit 3) and the place in the list above.  Zero
+ * It lies as the scaled 32x32x64 matrix instruction takes it, in blocks of 32 rows, rb = ceil(rows / 32) of
+ * them:
+ *   codes   uint8 [ceil(length / 256)][rb][4][2][32][16]: 32 values (block p = k % 256 / 32 of a line of 256) of
+ *           row r at [k / 256][r / 32][2 (p / 4) + p % 2][p / 2 % 2][r % 32], value k in byte k % 32 / 2,
+ *           low nibble for even k; a nibble is the sign (bit 3) and the place in the list above.  Zero
  *           beyond `length`.
- *   scales  uint8 [ceil(length / 512)][rows][16]  one byte e for 32 values: their power of two is
- *           2^(e - 127), 255 = not a number.  The 16 blocks of 512 values: block j at byte 4 (j % 4) + j / 4
- *           (every fourth block's bytes are neighbours, so one 4-byte load serves a lane of the scaled
- *           matrix instruction for 512 values).  127 for blocks that begin at or beyond `length`.
+ *   scales  uint8 [ceil(length / 512)][rb][32][16]: one byte e for 32 values: their power of two is 2^(e - 127),
+ *           255 = not a number.  Block j = k % 512 / 32 of 512 values of row r at [k / 512][r / 32][r % 32]
+ *           [4 (j % 4) + j / 4].  127 for blocks that begin at or beyond `length`.
+ * Rows beyond `rows` of the last block of rows are not written and reach no result.
  * Both 16-byte aligned.  hinm_mx4_sizes gives their sizes in bytes; either output pointer may be NULL. */
 enum { HINM_MX4_ROWS = 0, HINM_MX4_COLUMNS = 1 };
 hinm_status hinm_mx4_sizes(int32_t rows, int32_t length, size_t* code_bytes, size_t* scale_bytes);

@@ -21,15 +21,23 @@ def scale_pitch(length: int) -> int:
     return (length + 511) // 512 * 16
 
 
-def to_memory(codes: np.ndarray, scales: np.ndarray):
-    """A form with its rows one after the other, as everywhere in this module -> as it lies in memory: lines and groups first."""
-    turn = lambda a, n: np.ascontiguousarray(a.reshape(a.shape[0], -1, n).transpose(1, 0, 2)).reshape(-1)
-    return turn(codes, 128), turn(scales, 16)
+def to_memory(codes: np.ndarray, scales: np.ndarray, fill: int = 0):
+    """A form with its rows one after the other, as everywhere in this module -> as it lies in memory; rows that only fill
+    the last block of 32 hold `fill` in every byte."""
+    rows = codes.shape[0]
+    rb = (rows + 31) // 32
+    grow = lambda a: np.concatenate([a, np.full((32 * rb - rows, a.shape[1]), fill, dtype=np.uint8)])
+    c = grow(codes).reshape(rb, 32, -1, 2, 2, 2, 16)     # rows, line, then the bits of p (4: a, 2: b, 1: c), 16 bytes
+    c = c.transpose(2, 0, 3, 5, 4, 1, 6)                 # [line][rb][a][c][b][row][16]
+    s = grow(scales).reshape(rb, 32, -1, 16).transpose(2, 0, 1, 3)
+    return np.ascontiguousarray(c).reshape(-1), np.ascontiguousarray(s).reshape(-1)
 
 
 def from_memory(codes: np.ndarray, scales: np.ndarray, rows: int):
-    turn = lambda a, n: np.ascontiguousarray(a.reshape(-1, rows, n).transpose(1, 0, 2)).reshape(rows, -1)
-    return turn(codes, 128), turn(scales, 16)
+    rb = (rows + 31) // 32
+    c = codes.reshape(-1, rb, 2, 2, 2, 32, 16).transpose(1, 5, 0, 2, 4, 3, 6)
+    s = scales.reshape(-1, rb, 32, 16).transpose(1, 2, 0, 3)
+    return np.ascontiguousarray(c).reshape(32 * rb, -1), np.ascontiguousarray(s).reshape(32 * rb, -1)
 
 
 def scale_place(block: int) -> int:

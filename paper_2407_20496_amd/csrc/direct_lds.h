@@ -20,13 +20,15 @@ __device__ __forceinline__ void copy4_to_lds(const void* src_lane, void* lds_wav
   __builtin_amdgcn_global_load_lds((global_void_t*)src_lane, (lds_void_t*)lds_wave_base, 4, 0, 0);
 }
 
-// The same from a buffer descriptor: every lane copies the 16 bytes at lane_offset, which must lie inside the descriptor's bytes.
+// The same from a buffer descriptor: every lane copies the 16 bytes at lane_offset + offset (the same for all lanes), which
+// must lie inside the descriptor's bytes.
 // Issuing one costs a wave next to nothing, where the form with full addresses holds it for some 20 clocks.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00027000);
 }
-__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t lane_offset, void* lds_wave_base) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void_t*)lds_wave_base, 16, (int)lane_offset, 0, 0, 0);
+__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t lane_offset, uint32_t offset,
+                                              void* lds_wave_base) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void_t*)lds_wave_base, 16, (int)lane_offset, (int)offset, 0, 0);
 }
 
 // s_waitcnt vmcnt(n) with everything else left alone (gfx9 encoding: vmcnt in bits 3:0 and 15:14,

@@ -1,18 +1,17 @@
 // Microscaled 4-bit form (include/hinm.h): where codes and scales lie, and the conversions in both directions.
 //
 // 32 consecutive values share the power of two 2^(e - 127) (e = scale byte); a code is a sign and a place in
-// 0, .5, 1, 1.5, 2, 3, 4, 6.  Lines of 256 values = 128 bytes of codes and groups of 512 values = 16 scale bytes come first
-// in the order, rows second: what a workgroup takes of neighbouring rows at one place of the summed axis is one contiguous
-// piece.  (Rows after one another instead: a group's scale bytes of 256 rows lay in 256 cache lines, which were fetched again
-// for every group.)  Byte 4 b + s of a group's scales belongs to block 4 s + b.
+// 0, .5, 1, 1.5, 2, 3, 4, 6.  The form lies in memory as the scaled 32x32x64 matrix instruction takes it: 32 rows x 64 values
+// are 1 KB, lane after lane, so that every kernel reads operands in whole contiguous kilobytes, through LDS or straight into
+// registers.
 //
-// Operand layout of the scaled matrix instructions on 4-bit values, established on MI355X with random codes and scales:
-// lane l of the 16x16x128 form holds row l % 16 and the 32 values of block l / 16, in order, low nibble first; of the
-// 32x32x64 form row l % 32 and block l / 32.  One byte of its scale register (chosen per instruction) scales the
-// lane's 32 values; 255 makes a result NaN whatever the codes.  D: lane l holds column l % 16, rows 4 (l / 16) + register
-// (16x16), or column l % 32, rows 8 (register / 4) + 4 (l / 32) + register % 4 (32x32).  Which 32 values meet is
-// free as long as both operands agree: with the scale bytes in the order above a lane's 4-byte word serves four k-steps of
-// the 16x16x128 form (block 4 s + lane / 16 in step s), and two words serve eight instructions of the 32x32x64 form.
+// Operand layout of the instruction on 4-bit values, established on MI355X with random codes and scales: lane l holds row
+// l % 32 and 32 values of block l / 32, in order, low nibble first; one byte of its scale register (chosen per instruction)
+// scales them; 255 makes a result NaN whatever the codes.  D: lane l holds column l % 32, rows 8 (register / 4) +
+// 4 (l / 32) + register % 4.  Which two blocks of a row an instruction takes is free as long as both operands agree.  Here a
+// line of 256 values = 8 blocks is four instructions, instruction i = 0..3 taking blocks 4 (i / 2) + i % 2 (lower lanes) and 2
+// further (upper lanes); 16 scale bytes of 512 values lie so that word q of a lane's two holds the bytes of its blocks in
+// instructions with i % 2 = q: byte i / 2 in the first line, 2 + i / 2 in the second.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -22,18 +21,30 @@
 
 namespace hinm {
 
-constexpr int kMx4Step = 128;    // values of a 16x16x128 instruction: 64 bytes of codes
-constexpr int kMx4Line = 256;    // values of a line of codes
+constexpr int kMx4Line = 256;    // values of a row in a line: 128 bytes of codes
 constexpr int kMx4Group = 512;   // values whose 16 scale bytes lie together
+constexpr int kMx4Rows = 32;     // rows of a block of rows
+constexpr int kMx4BlockBytes = kMx4Rows * 128;  // of a line
 
 __host__ __device__ constexpr int mx4_lines(int length) { return (int)(((int64_t)length + 255) / 256); }
 __host__ __device__ constexpr int mx4_groups(int length) { return (int)(((int64_t)length + 511) / 512); }
-__host__ __device__ constexpr int64_t mx4_code_bytes(int rows, int length) { return (int64_t)mx4_lines(length) * rows * 128; }
-__host__ __device__ constexpr int64_t mx4_scale_bytes(int rows, int length) { return (int64_t)mx4_groups(length) * rows * 16; }
-// where a row's line of codes and its group of scales begin
-__host__ __device__ constexpr int64_t mx4_line_at(int line, int rows, int64_t row) { return ((int64_t)line * rows + row) * 128; }
-__host__ __device__ constexpr int64_t mx4_group_at(int group, int rows, int64_t row) { return ((int64_t)group * rows + row) * 16; }
-// of block j among its group's 16
+__host__ __device__ constexpr int mx4_row_blocks(int rows) { return (int)(((int64_t)rows + 31) / 32); }
+__host__ __device__ constexpr int64_t mx4_code_bytes(int rows, int length) {
+  return (int64_t)mx4_lines(length) * mx4_row_blocks(rows) * kMx4BlockBytes;
+}
+__host__ __device__ constexpr int64_t mx4_scale_bytes(int rows, int length) {
+  return (int64_t)mx4_groups(length) * mx4_row_blocks(rows) * (kMx4Rows * 16);
+}
+// where a block of rows begins in a line of codes and in a group of scales
+__host__ __device__ constexpr int64_t mx4_codes_at(int line, int row_blocks, int block) {
+  return ((int64_t)line * row_blocks + block) * kMx4BlockBytes;
+}
+__host__ __device__ constexpr int64_t mx4_scales_at(int group, int row_blocks, int block) {
+  return ((int64_t)group * row_blocks + block) * (kMx4Rows * 16);
+}
+// which 512 bytes (16 of each of 32 rows) of a line's block of rows hold block p = 0..7 of 32 values
+__host__ __device__ constexpr int mx4_chunk_of(int p) { return 2 * (2 * (p >> 2) + (p & 1)) + ((p >> 1) & 1); }
+// place of the scale byte of block j = 0..15 of a group
 __host__ __device__ constexpr int mx4_scale_place(int j) { return 4 * (j & 3) + (j >> 2); }
 
 // Larger of the magnitudes in both halves (sign bits cleared): 16-bit formats order like their bit patterns, NaN highest.

@@ -16,12 +16,6 @@ __device__ __forceinline__ i32x8 operand(u32x4 v) {
 }
 constexpr int kFp4 = 4;  // operand format code of 4-bit values
 template <int BYTE>
-__device__ __forceinline__ f32x4 mfma_16x16x128(u32x4 a, uint32_t a_scale, u32x4 b, uint32_t b_scale, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), c, kFp4, kFp4, BYTE, (int)a_scale, BYTE,
-                                                          (int)b_scale);
-}
-
-template <int BYTE>
 __device__ __forceinline__ f32x16 mfma_32x32x64(u32x4 a, uint32_t a_scale, u32x4 b, uint32_t b_scale, f32x16 c) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, kFp4, kFp4, BYTE, (int)a_scale, BYTE,
                                                          (int)b_scale);
@@ -33,96 +27,199 @@ struct ProductShape {
   bool relu;
 };
 
+// Four consecutive columns of a row of Y from n on, those below N, rounded; vec: the four begin at a multiple of their size.
 template <int OUT>  // HINM_F16, HINM_BF16, 2 = float32
-__device__ __forceinline__ void store_one(void* Y, int64_t at, float v) {
-  if constexpr (OUT == 2) static_cast<float*>(Y)[at] = v;
-  else static_cast<uint16_t*>(Y)[at] = float_to_bits<OUT>(v);
-}
-
-// ---- few rows of B: the summed axis split over the waves of a workgroup ---------------------------------
-// A workgroup owns 16 rows of A and 16 NT rows of B; its waves take groups of 512 values in turn, straight from memory into
-// registers, and add their tiles in LDS in a fixed order.  B is the instructions' row operand, so that a lane ends with four
-// consecutive columns of one row of Y.
-template <int OUT, int NT>
-__global__ __launch_bounds__(512) void mx4_split_kernel(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
-                                                        const uint8_t* b_scales, void* Y, ProductShape p) {
-  extern __shared__ __align__(16) float slabs[];  // [waves][16][16 NT + 4]
-  constexpr int kPitch = 16 * NT + 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int r = lane & 15, b = lane >> 4;
-  const int blocks_n = (p.N + 16 * NT - 1) / (16 * NT);
-  const int m0 = (int)(blockIdx.x / blocks_n) * 16, n0 = (int)(blockIdx.x % blocks_n) * 16 * NT;
-  const int lines = mx4_lines(p.K), groups = mx4_groups(p.K);
-  // rows beyond the matrices repeat the last one: what they give is not stored
-  const int64_t ra = min(m0 + r, p.M - 1);
-  const uint8_t* ac = a_codes + ra * 128 + 16 * b;
-  const uint8_t* as = a_scales + ra * 16 + 4 * b;
-  const int64_t a_line = (int64_t)p.M * 128, b_line = (int64_t)p.N * 128, a_group = (int64_t)p.M * 16, b_group = (int64_t)p.N * 16;
-  const uint8_t *bc[NT], *bs[NT];
+__device__ __forceinline__ void store_four(void* Y, int64_t row_at, int n, f32x4 v, const ProductShape& p, bool vec) {
+  if (p.relu) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int64_t rb = min(n0 + 16 * t + r, p.N - 1);
-    bc[t] = b_codes + rb * 128 + 16 * b;
-    bs[t] = b_scales + rb * 16 + 4 * b;
+    for (int e = 0; e < 4; ++e) v[e] = v[e] < 0 ? 0 : v[e];  // keeps NaN
   }
-  f32x4 acc[NT];
+  if constexpr (OUT == 2) {
+    float* to = static_cast<float*>(Y) + row_at + n;
+    if (vec && n + 4 <= p.N) {
+      *reinterpret_cast<f32x4*>(to) = v;
+      return;
+    }
 #pragma unroll
-  for (int t = 0; t < NT; ++t) acc[t] = f32x4{0, 0, 0, 0};
-  for (int g = wave; g < groups; g += waves) {
-    const uint32_t sa = *reinterpret_cast<const uint32_t*>(as + g * a_group);
-    uint32_t sb[NT];
+    for (int e = 0; e < 4; ++e)
+      if (n + e < p.N) to[e] = v[e];
+  } else {
+    uint16_t* to = static_cast<uint16_t*>(Y) + row_at + n;
+    const u32x2 w = {floats_to_bits<OUT>(v[0], v[1]), floats_to_bits<OUT>(v[2], v[3])};
+    if (vec && n + 4 <= p.N) {
+      *reinterpret_cast<u32x2*>(to) = w;
+      return;
+    }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) sb[t] = *reinterpret_cast<const uint32_t*>(bs[t] + g * b_group);
-    auto step = [&](auto s_) {
-      constexpr int s = decltype(s_)::value;
-      const int line = 2 * g + s / 2;
-      if (line >= lines) return;
-      const u32x4 a = *reinterpret_cast<const u32x4*>(ac + line * a_line + 64 * (s & 1));
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        acc[t] = mfma_16x16x128<s>(*reinterpret_cast<const u32x4*>(bc[t] + line * b_line + 64 * (s & 1)), sb[t], a, sa, acc[t]);
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
-    step(std::integral_constant<int, 2>{});
-    step(std::integral_constant<int, 3>{});
-  }
-  float* slab = slabs + wave * 16 * kPitch;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(slab + r * kPitch + 16 * t + 4 * b) = acc[t];
-  __syncthreads();
-  for (int i = threadIdx.x; i < 16 * 16 * NT; i += blockDim.x) {
-    const int row = i / (16 * NT), col = i % (16 * NT);
-    if (m0 + row >= p.M || n0 + col >= p.N) continue;
-    float v = 0;
-    for (int w = 0; w < waves; ++w) v += slabs[(w * 16 + row) * kPitch + col];
-    if (p.relu) v = v < 0 ? 0 : v;  // keeps NaN
-    store_one<OUT>(Y, (int64_t)(m0 + row) * p.ldy + n0 + col, v);
+    for (int e = 0; e < 4; ++e)
+      if (n + e < p.N) to[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
   }
 }
 
-template <int OUT, int NT>
-hipError_t launch_split(const Mx4ProductArgs& a, const ProductShape& p, hipStream_t stream) {
-  const int groups = (p.K + kMx4Group - 1) / kMx4Group;
-  const int waves = groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
-  const size_t lds = (size_t)waves * 16 * (16 * NT + 4) * sizeof(float);
-  const int64_t grid = (int64_t)((p.M + 15) / 16) * ((p.N + 16 * NT - 1) / (16 * NT));
-  if (lds > 65536) {
-    const hipError_t e = raise_lds_limit<mx4_split_kernel<OUT, NT>>((int)lds);
-    if (e != hipSuccess) return e;
+// Workgroups go to the eight XCDs in turn: each XCD takes a contiguous run of a list of `items`, so that neighbours in the
+// list share operands in its L2.  -1: nothing left for this workgroup.
+__device__ __forceinline__ int item_of_workgroup(int items) {
+  const int per = gridDim.x >> 3;
+  const int item = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  return item < items ? item : -1;
+}
+uint32_t grid_of_items(int64_t items) { return (uint32_t)((items + 7) / 8 * 8); }
+
+// ---- operands straight into registers, the summed axis split over the waves ------------------------------
+// A workgroup owns 32 WM rows of A times 32 WN rows of B; its waves take lines of 256 values in turn, each for the whole tile,
+// with no barrier between them, and add their tiles in LDS in a fixed order.  The operands of a line are loaded while the
+// line before it multiplies.  B is the instruction's row operand, so that a lane ends with four consecutive columns of Y.
+//   Rows of B beyond N lie beyond the buffer descriptor's bytes for their lanes: they read as zero and cost no traffic.
+template <int OUT, int WM, int WN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (WM * WN > 8 ? 4 : 8) / WAVES > 0 ? (WM * WN > 8 ? 4 : 8) / WAVES : 1)
+void mx4_stream_kernel(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, void* Y,
+                       ProductShape p) {
+  constexpr int kPitch = 32 * WN + 4;
+  __shared__ __align__(16) float slabs[WAVES][32 * kPitch];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blocks_a = mx4_row_blocks(p.M), blocks_b = mx4_row_blocks(p.N);
+  const int tiles_m = (blocks_a + WM - 1) / WM, tiles_n = (blocks_b + WN - 1) / WN;
+  const int item = item_of_workgroup(tiles_m * tiles_n);
+  if (item < 0) return;
+  const int block_m = item / tiles_n * WM, block_n = item % tiles_n * WN;
+  const int half = lane >> 5, r = lane & 31;
+  const int lines = mx4_lines(p.K);
+  // where the tile's blocks of rows lie from its first on; beyond the matrices the last one repeats (not stored)
+  uint32_t at_a[WM], at_b[WN], scales_at_a[WM], scales_at_b[WN];
+  constexpr uint32_t kNowhere = 0x7fffff00u;
+#pragma unroll
+  for (int i = 0; i < WM; ++i) {
+    const int b = min(i, blocks_a - 1 - block_m);
+    at_a[i] = kMx4BlockBytes * b + 16 * lane;
+    scales_at_a[i] = kMx4Rows * 16 * b + 16 * r + 8 * half;
   }
-  mx4_split_kernel<OUT, NT><<<dim3((uint32_t)grid), 64 * waves, lds, stream>>>(a.a_codes, a.a_scales, a.b_codes, a.b_scales, a.Y, p);
+#pragma unroll
+  for (int i = 0; i < WN; ++i) {
+    const int b = min(i, blocks_b - 1 - block_n);
+    const bool row = 32 * (block_n + b) + r < p.N;
+    at_b[i] = row ? kMx4BlockBytes * b + 16 * lane : kNowhere;
+    scales_at_b[i] = row ? kMx4Rows * 16 * b + 16 * r + 8 * half : kNowhere;
+  }
+  struct Line {
+    u32x4 a[4][WM], b[4][WN];
+    u32x2 scale_a[WM], scale_b[WN];
+  };
+  struct Sources {
+    __amdgpu_buffer_rsrc_t a, b;
+  };
+  auto sources_of = [&](int line) {
+    return Sources{buffer_of(a_codes + mx4_codes_at(line, blocks_a, block_m), WM * kMx4BlockBytes),
+                   buffer_of(b_codes + mx4_codes_at(line, blocks_b, block_n), WN * kMx4BlockBytes)};
+  };
+  auto load_scales = [&](int line, Line& f) {
+    const __amdgpu_buffer_rsrc_t a = buffer_of(a_scales + mx4_scales_at(line >> 1, blocks_a, block_m), WM * kMx4Rows * 16);
+    const __amdgpu_buffer_rsrc_t b = buffer_of(b_scales + mx4_scales_at(line >> 1, blocks_b, block_n), WN * kMx4Rows * 16);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) f.scale_a[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(a, scales_at_a[i], 0, 0));
+#pragma unroll
+    for (int i = 0; i < WN; ++i) f.scale_b[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(b, scales_at_b[i], 0, 0));
+  };
+  auto load_step = [&](const Sources& src, int q, Line& f) {
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+      f.a[q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src.a, at_a[i], 1024 * q, 0));
+#pragma unroll
+    for (int i = 0; i < WN; ++i)
+      f.b[q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(src.b, at_b[i], 1024 * q, 0));
+  };
+  f32x16 acc[WN][WM];
+#pragma unroll
+  for (int i = 0; i < WN; ++i)
+#pragma unroll
+    for (int j = 0; j < WM; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
+  // scale words of the line that multiplies: the second line of a group has its bytes two places up
+  u32x2 scale_a[WM], scale_b[WN];
+  auto take_scales = [&](int line, const Line& f) {
+    const uint32_t down = 16 * (line & 1);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) scale_a[i] = u32x2{f.scale_a[i][0] >> down, f.scale_a[i][1] >> down};
+#pragma unroll
+    for (int i = 0; i < WN; ++i) scale_b[i] = u32x2{f.scale_b[i][0] >> down, f.scale_b[i][1] >> down};
+  };
+  auto multiply = [&](auto which, const Line& f) {
+    constexpr int q = decltype(which)::value;
+#pragma unroll
+    for (int i = 0; i < WN; ++i)
+#pragma unroll
+      for (int j = 0; j < WM; ++j)
+        acc[i][j] = mfma_32x32x64<q / 2>(f.b[q][i], scale_b[i][q & 1], f.a[q][j], scale_a[j][q & 1], acc[i][j]);
+  };
+
+  Line f;
+  if (wave < lines) {
+    const Sources src = sources_of(wave);
+    load_scales(wave, f);
+    load_step(src, 0, f);
+    load_step(src, 1, f);
+    load_step(src, 2, f);
+    load_step(src, 3, f);
+    int line = wave;
+    for (; line + WAVES < lines; line += WAVES) {
+      const Sources next = sources_of(line + WAVES);
+      take_scales(line, f);
+      load_scales(line + WAVES, f);
+      multiply(std::integral_constant<int, 0>{}, f);
+      load_step(next, 0, f);
+      multiply(std::integral_constant<int, 1>{}, f);
+      load_step(next, 1, f);
+      multiply(std::integral_constant<int, 2>{}, f);
+      load_step(next, 2, f);
+      multiply(std::integral_constant<int, 3>{}, f);
+      load_step(next, 3, f);
+    }
+    take_scales(line, f);
+    multiply(std::integral_constant<int, 0>{}, f);
+    multiply(std::integral_constant<int, 1>{}, f);
+    multiply(std::integral_constant<int, 2>{}, f);
+    multiply(std::integral_constant<int, 3>{}, f);
+  }
+  // 32 rows of Y at a time: every wave's part to its slab, then all of them added
+  constexpr int kElem = OUT == 2 ? 4 : 2;
+  const bool vec = (reinterpret_cast<uintptr_t>(Y) & (4 * kElem - 1)) == 0 && p.ldy % 4 == 0;
+  const int count = min(WAVES, lines);  // waves that had a line
+#pragma unroll
+  for (int j = 0; j < WM; ++j) {
+    if (j > 0) __syncthreads();
+    if (wave < count) {
+#pragma unroll
+      for (int i = 0; i < WN; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(slabs[wave] + r * kPitch + 32 * i + 8 * q + 4 * half) =
+              f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < 32 * 8 * WN; t += 64 * WAVES) {
+      const int row = t / (8 * WN), at = 4 * (t % (8 * WN));
+      const int m = 32 * (block_m + j) + row, n = 32 * block_n + at;
+      if (m >= p.M || n >= p.N) continue;
+      f32x4 v = *reinterpret_cast<const f32x4*>(slabs[0] + row * kPitch + at);
+      for (int w = 1; w < count; ++w) v += *reinterpret_cast<const f32x4*>(slabs[w] + row * kPitch + at);
+      store_four<OUT>(Y, (int64_t)m * p.ldy, n, v, p, vec);
+    }
+  }
+}
+
+template <int OUT, int WM, int WN, int WAVES>
+hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStream_t stream) {
+  const int64_t items = (int64_t)((p.M + 32 * WM - 1) / (32 * WM)) * ((p.N + 32 * WN - 1) / (32 * WN));
+  mx4_stream_kernel<OUT, WM, WN, WAVES><<<dim3(grid_of_items(items)), 64 * WAVES, 0, stream>>>(a.a_codes, a.a_scales, a.b_codes,
+                                                                                             a.b_scales, a.Y, p);
   return hipGetLastError();
 }
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
 // A workgroup of four waves (2 x 2) owns TM = 64 WM rows of A and TN = 64 WN rows of B; a wave owns half of each, in 32x32
-// tiles.  A stage is 256 values = one 128-byte line of every row, copied straight into LDS, two stages in turn; the 16 scale
-// bytes a row has for 512 values come with every second stage.  A stage is four instructions for every 32x32 tile; a wave
-// reads the operands of the next one while it multiplies.  (Stages of 128 values, four in turn: copies of half lines run at
-// 20 bytes a clock and compute unit and took 885 us of 16384x16384x8192's 1176 us by themselves.)
-//   Swizzle: the eight 16-byte pieces of a row sit at piece ^ (row / 2 % 8), applied on the copy's source side, so that 16
-// consecutive lanes (16 rows, one piece) read 16 different 16-byte units of 256 bytes.
+// tiles.  A stage is a line of 256 values, copied straight into LDS, two stages in turn; the 16 scale bytes a row has for 512
+// values come with every second stage.  A stage is four instructions for every 32x32 tile; a wave reads the operands of the
+// next one while it multiplies.
 //   Waits: before the last quarter of stage p every copy of the wave's has landed, stage p + 1 among them, and its LDS reads of
 // stage p are done; past the barrier that holds for all waves, so the place of stage p takes stage p + 2: half of its copies
 // during the last quarter of p, the others during the first of p + 1.  Scales of group g + 1 (stages 2 g + 2 and 2 g + 3) are
@@ -147,73 +244,69 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   extern __shared__ __align__(16) uint8_t lds[];
   uint8_t* const lds_scales = lds + 2 * T::kStageBytes;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // workgroups go to the eight XCDs in turn: each XCD takes a contiguous run of the list of tiles, panels of eight tiles of A
-  // times all of B, so that the 32 tiles it works on share eight and four operand tiles in its L2
+  // the list of tiles: panels of eight tiles of A times all of B, so that the 32 tiles an XCD works on share eight and four
+  // operand tiles
   const int tiles_m = (p.M + T::TM - 1) / T::TM, tiles_n = (p.N + T::TN - 1) / T::TN;
-  const int per = gridDim.x >> 3;
-  const int item = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if (item >= tiles_m * tiles_n) return;
+  const int item = item_of_workgroup(tiles_m * tiles_n);
+  if (item < 0) return;
   const int panel = item / (8 * tiles_n), in_panel = item - panel * 8 * tiles_n;
   const int height = min(8, tiles_m - 8 * panel);
   const int m0 = (8 * panel + in_panel % height) * T::TM, n0 = in_panel / height * T::TN;
   const int stages = mx4_lines(p.K), groups = mx4_groups(p.K);
-
-  // Where this lane's part of each copy comes from, from the first of the tile's rows in a line or group on; rows beyond the
-  // matrices repeat the last one (what they give is not stored).  A wave copies a quarter of A's rows, then one of B's.
+  // A wave copies a quarter of A's blocks of rows, then one of B's, a kilobyte at a time; blocks beyond the matrices repeat the
+  // last one (what they give is not stored).
   constexpr int kOfA = T::TM / 32;
-  const int rows_a = min(T::TM, p.M - m0), rows_b = min(T::TN, p.N - n0);
-  uint32_t from[T::kCopies];
+  const int blocks_a = mx4_row_blocks(p.M), blocks_b = mx4_row_blocks(p.N), block_m = m0 / 32, block_n = n0 / 32;
+  const uint32_t lane_at = 16 * lane;
+  uint32_t from[T::kCopies];  // uniform
 #pragma unroll
   for (int c = 0; c < T::kCopies; ++c) {
-    const int row = (c < kOfA ? wave * (T::TM / 4) + 8 * c : wave * (T::TN / 4) + 8 * (c - kOfA)) + (lane >> 3);
-    const int piece = (lane & 7) ^ ((row >> 1) & 7);
-    from[c] = 128 * min(row, (c < kOfA ? rows_a : rows_b) - 1) + 16 * piece;
+    const int kb = c < kOfA ? wave * kOfA + c : wave * (T::TN / 32) + c - kOfA;
+    from[c] = kMx4BlockBytes * min(kb >> 2, (c < kOfA ? blocks_a - block_m : blocks_b - block_n) - 1) + 1024 * (kb & 3);
   }
   struct Source {
     __amdgpu_buffer_rsrc_t a, b;
   };
   auto source_of = [&](int stage) {
     const int line = min(stage, stages - 1);
-    return Source{buffer_of(a_codes + mx4_line_at(line, p.M, m0), 128u * rows_a),
-                  buffer_of(b_codes + mx4_line_at(line, p.N, n0), 128u * rows_b)};
+    return Source{buffer_of(a_codes + mx4_codes_at(line, blocks_a, block_m), T::TM * 128),
+                  buffer_of(b_codes + mx4_codes_at(line, blocks_b, block_n), T::TN * 128)};
   };
   auto copy_rows = [&](const Source& src, int stage, int c) {  // one of the wave's copies of a stage
-    const int row0 = c < kOfA ? wave * (T::TM / 4) + 8 * c : T::TM + wave * (T::TN / 4) + 8 * (c - kOfA);
-    copy16_to_lds(c < kOfA ? src.a : src.b, from[c], lds + (stage & 1) * T::kStageBytes + row0 * 128);
+    const int kb = c < kOfA ? wave * kOfA + c : T::TM / 8 + wave * (T::TN / 32) + c - kOfA;
+    copy16_to_lds(c < kOfA ? src.a : src.b, lane_at, from[c], lds + (stage & 1) * T::kStageBytes + kb * 1024);
   };
-  // scales: 64 rows a copy; with 256 rows of each matrix every wave copies both, with 128 two waves A and two B
+  // scales: two blocks of rows a copy; with 256 rows of each matrix every wave copies both, with 128 two waves A and two B
   constexpr bool kBoth = T::TM == 256;
   const bool scales_of_a = kBoth || wave < 2;
-  const uint8_t* const scale_rows = scales_of_a ? a_scales + 16 * (int64_t)m0 : b_scales + 16 * (int64_t)n0;
-  const int64_t scale_group = 16 * (int64_t)(scales_of_a ? p.M : p.N);
-  const int scale_count = scales_of_a ? rows_a : rows_b;
-  const int scale_row0 = 64 * (kBoth ? wave : wave & 1);
-  uint8_t* const scale_place = lds_scales + (scales_of_a ? 0 : T::TM * 16) + scale_row0 * 16;
-  const uint32_t scale_from = 16 * min(scale_row0 + lane, scale_count - 1), scale_from_b = 16 * min(scale_row0 + lane, rows_b - 1);
+  const int scale_block = 2 * (kBoth ? wave : wave & 1);
+  uint8_t* const scale_place = lds_scales + (scales_of_a ? 0 : T::TM * 16) + scale_block * 512;
+  const int lane_block = scale_block + (lane >> 5);
+  const uint32_t scale_from_a = 512 * min(lane_block, blocks_a - block_m - 1) + 16 * (lane & 31);
+  const uint32_t scale_from_b = 512 * min(lane_block, blocks_b - block_n - 1) + 16 * (lane & 31);
   auto copy_scales = [&](int g) {
     const int group = min(g, groups - 1);
-    copy16_to_lds(buffer_of(scale_rows + group * scale_group, 16u * scale_count), scale_from, scale_place + (g & 1) * T::kScaleBytes);
-    if constexpr (kBoth)
-      copy16_to_lds(buffer_of(b_scales + mx4_group_at(group, p.N, n0), 16u * rows_b), scale_from_b,
-                    scale_place + T::TM * 16 + (g & 1) * T::kScaleBytes);
+    const uint8_t* of_a = a_scales + mx4_scales_at(group, blocks_a, block_m);
+    const uint8_t* of_b = b_scales + mx4_scales_at(group, blocks_b, block_n);
+    uint8_t* to = scale_place + (g & 1) * T::kScaleBytes;
+    copy16_to_lds(buffer_of(scales_of_a ? of_a : of_b, T::TM * 16), scales_of_a ? scale_from_a : scale_from_b, 0, to);
+    if constexpr (kBoth) copy16_to_lds(buffer_of(of_b, T::TN * 16), scale_from_b, 0, to + T::TM * 16);
   };
 
   const int half = lane >> 5, r = lane & 31;
   const int wave_m = (wave & 1) * 32 * WM, wave_n = (wave >> 1) * 32 * WN;
-  // byte offset of this lane's piece of a row in the first quarter (the others differ in its bits 0 and 2), and of its first rows
-  const int piece0 = 16 * ((2 * half) ^ ((r >> 1) & 7));
-  const int row_a = (wave_m + r) * 128, row_b = (T::TM + wave_n + r) * 128;
+  const int at_a = wave_m * 128 + lane_at, at_b = (T::TM + wave_n) * 128 + lane_at;
 
   // one operand set: what a quarter of a stage multiplies
   struct Operands {
     u32x4 a[WM], b[WN];
   };
   auto read_one = [&](int stage, int quarter, int t, Operands& f) {
-    const uint8_t* base = lds + (stage & 1) * T::kStageBytes + (piece0 ^ 16 * (4 * (quarter >> 1) + (quarter & 1)));
-    if (t < WM) f.a[t] = *reinterpret_cast<const u32x4*>(base + row_a + 4096 * t);
-    else f.b[t - WM] = *reinterpret_cast<const u32x4*>(base + row_b + 4096 * (t - WM));
+    const uint8_t* base = lds + (stage & 1) * T::kStageBytes + 1024 * quarter;
+    if (t < WM) f.a[t] = *reinterpret_cast<const u32x4*>(base + at_a + kMx4BlockBytes * t);
+    else f.b[t - WM] = *reinterpret_cast<const u32x4*>(base + at_b + kMx4BlockBytes * (t - WM));
   };
-  u32x2 scale_a[WM], scale_b[WN];  // word q: the lane's blocks 2 half + q of four steps
+  u32x2 scale_a[WM], scale_b[WN];  // word q: quarters with h % 2 = q, two bytes a stage
   auto read_scales = [&](int g) {
     const uint8_t* base = lds_scales + (g & 1) * T::kScaleBytes + 8 * half;
 #pragma unroll
@@ -342,7 +435,7 @@ hipError_t launch_tile(const Mx4ProductArgs& a, const ProductShape& p, hipStream
   const int64_t tiles = (int64_t)((p.M + T::TM - 1) / T::TM) * ((p.N + T::TN - 1) / T::TN);
   const hipError_t e = raise_lds_limit<mx4_tile_kernel<OUT, WM, WN>>(T::kLds);
   if (e != hipSuccess) return e;
-  mx4_tile_kernel<OUT, WM, WN><<<dim3((uint32_t)((tiles + 7) / 8 * 8)), 256, T::kLds, stream>>>(a.a_codes, a.a_scales, a.b_codes,
+  mx4_tile_kernel<OUT, WM, WN><<<dim3(grid_of_items(tiles)), 256, T::kLds, stream>>>(a.a_codes, a.a_scales, a.b_codes,
                                                                                               a.b_scales, a.Y, p);
   return hipGetLastError();
 }
@@ -352,10 +445,9 @@ hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
   if (a.M > 512 && a.N > 512) return launch_tile<OUT, 4, 4>(a, p, stream);
   if (a.M > 256 && a.N > 256) return launch_tile<OUT, 2, 2>(a, p, stream);
-  if (a.N <= 16) return launch_split<OUT, 1>(a, p, stream);
-  if (a.N <= 32) return launch_split<OUT, 2>(a, p, stream);
-  if (a.N <= 64) return launch_split<OUT, 4>(a, p, stream);
-  return launch_split<OUT, 8>(a, p, stream);
+  if (a.N <= 32) return launch_stream<OUT, 1, 1, 8>(a, p, stream);
+  if (a.N <= 64) return launch_stream<OUT, 2, 2, 8>(a, p, stream);
+  return launch_stream<OUT, 4, 4, 4>(a, p, stream);
 }
 
 }  // namespace

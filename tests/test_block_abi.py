@@ -12,8 +12,9 @@ OK, NULL, SHAPE, DTYPE, WORKSPACE, UNSUPPORTED = 0, 1, 2, 3, 4, 5
 BIG = 1 << 40
 
 
-@pytest.mark.parametrize("rows,length,want", [(1, 1, (128, 16)), (3, 256, (384, 48)), (3, 257, (768, 48)), (2, 512, (512, 32)),
-                                              (2, 513, (768, 64)), (11008, 4096, (11008 * 2048, 11008 * 128)),
+@pytest.mark.parametrize("rows,length,want", [(1, 1, (4096, 512)), (32, 256, (4096, 512)), (33, 257, (16384, 1024)),
+                                              (64, 512, (16384, 1024)), (2, 513, (12288, 1024)),
+                                              (11008, 4096, (11008 * 2048, 11008 * 128)),
                                               (1 << 20, 1 << 20, (1 << 39, 1 << 35))])
 def test_sizes(rows, length, want):
     assert hinm.hinm_mx4_sizes(rows, length) == want
@@ -72,7 +73,7 @@ def test_product_refusals(change, status):
 @pytest.mark.parametrize("change,status", [
     ({"dtype": 7}, DTYPE), ({"M": 0}, SHAPE), ({"X": None}, NULL), ({"codes": None}, NULL), ({"ldx": 7}, SHAPE), ({"ldy": 7}, SHAPE),
     ({"X": P + 1}, SHAPE), ({"flags": 8}, UNSUPPORTED), ({"ws": None}, WORKSPACE), ({"ws": P + 128}, WORKSPACE),
-    ({"bytes": 8 * 128 + 255}, WORKSPACE)])
+    ({"bytes": 4096 + 511}, WORKSPACE)])
 def test_linear_refusals(change, status):
     good = dict(M=16, K=64, N=8, dtype=1, codes=P, scales=P, X=P, ldx=8, Y=P, ldy=8, flags=0, ws=P, bytes=BIG)
     assert _refused(hinm.load_library().hinm_mx4_linear, good, **change) == status

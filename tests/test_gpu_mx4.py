@@ -41,14 +41,17 @@ def _form(rows, length):
 
 def _host(form, rows, length):
     c, s = (t.cpu().numpy() for t in form)
-    nc, ns = rows * orc.code_pitch(length), rows * orc.scale_pitch(length)
+    full = (rows + 31) // 32 * 32
+    nc, ns = full * orc.code_pitch(length), full * orc.scale_pitch(length)
     assert (c[nc:] == GUARD).all() and (s[ns:] == GUARD).all(), "written beyond the form"
-    return orc.from_memory(c[:nc], s[:ns], rows)
+    c, s = orc.from_memory(c[:nc], s[:ns], rows)
+    assert (c[rows:] == GUARD).all() and (s[rows:] == GUARD).all(), "written into rows that do not exist"
+    return c[:rows], s[:rows]
 
 
 def _upload(codes, scales):
     import torch
-    return tuple(torch.from_numpy(a).to(DEV) for a in orc.to_memory(codes, scales))
+    return tuple(torch.from_numpy(a).to(DEV) for a in orc.to_memory(codes, scales, 0xFF))
 
 
 def _draw(rows, cols, dtype, seed, special=True):

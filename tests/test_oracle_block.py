@@ -35,16 +35,20 @@ def test_scales_and_their_places():
 
 
 def test_order_in_memory():
-    """Lines of codes and groups of scales first, rows second."""
+    """Every byte where include/hinm.h says it is."""
     rng = np.random.default_rng(2)
-    c, s = orc.quantize_rows(rng.standard_normal((3, 700)))
-    mc, ms = orc.to_memory(c, s)
-    for r, k in ((0, 0), (2, 255), (1, 256), (2, 699)):
-        assert mc[(k // 256 * 3 + r) * 128 + k % 256 // 2] == c[r, k // 2]
-        j = k // 32
-        assert ms[(k // 512 * 3 + r) * 16 + 4 * (j % 4) + j % 16 // 4] == s[r, orc.scale_place(j)]
-    back = orc.from_memory(mc, ms, 3)
-    assert np.array_equal(back[0], c) and np.array_equal(back[1], s)
+    rows, length = 37, 700
+    c, s = orc.quantize_rows(rng.standard_normal((rows, length)))
+    mc, ms = orc.to_memory(c, s, 9)
+    mc, ms = mc.reshape(3, 2, 4, 2, 32, 16), ms.reshape(2, 2, 32, 16)
+    for r in (0, 5, 31, 32, 36):
+        for k in (0, 31, 32, 64, 100, 129, 200, 255, 256, 511, 600, 699):
+            p, j = k % 256 // 32, k % 512 // 32
+            assert mc[k // 256, r // 32, 2 * (p // 4) + p % 2, p // 2 % 2, r % 32, k % 32 // 2] == c[r, k // 2]
+            assert ms[k // 512, r // 32, r % 32, 4 * (j % 4) + j // 4] == s[r, orc.scale_place(k // 32)]
+    assert (mc[:, 1, :, :, 5:] == 9).all() and (ms[:, 1, 5:] == 9).all()
+    back = orc.from_memory(mc.reshape(-1), ms.reshape(-1), rows)
+    assert np.array_equal(back[0][:rows], c) and np.array_equal(back[1][:rows], s)
 
 
 def test_special_blocks():
