@@ -217,32 +217,34 @@ hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStre
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
 // A workgroup of four waves (2 x 2) owns TM = 64 WM rows of A and TN = 64 WN rows of B; a wave owns half of each, in 32x32
-// tiles.  A stage is a line of 256 values, copied straight into LDS, two stages in turn; the 16 scale bytes a row has for 512
-// values come with every second stage.  A stage is four instructions for every 32x32 tile; a wave reads the operands of the
+// tiles.  A stage is a line of 256 values, copied straight into LDS, RING (2 or 4) stages in turn; the 16 scale bytes a row has
+// for 512 values come with every second stage.  A stage is four instructions for every 32x32 tile; a wave reads the operands of the
 // next one while it multiplies.
-//   Waits: before the last quarter of stage p every copy of the wave's has landed, stage p + 1 among them, and its LDS reads of
-// stage p are done; past the barrier that holds for all waves, so the place of stage p takes stage p + 2: half of its copies
-// during the last quarter of p, the others during the first of p + 1.  Scales of group g + 1 (stages 2 g + 2 and 2 g + 3) are
-// copied in the last quarter of stage 2 g into the half that group g - 1 used.  Beyond the last stage the last one is
-// copied again; nobody reads it.
+//   Waits: copies of a wave land in order.  Before the last quarter of stage p those of stages p + 2 .. p + RING - 1 may be
+// outstanding, all earlier ones are waited for, and so are the wave's LDS reads of stage p; past the barrier that holds for all
+// waves, so stage p + 1 is there and the place of stage p takes stage p + RING: half of its copies during the last quarter of
+// p, the others during the first of p + 1.  Scales of group g + RING / 2 are copied in the last quarter of stage 2 g, ahead of
+// stage 2 g + RING, and read after stage 2 g + RING - 1; their place held group g - RING / 2.  Beyond the last stage the last
+// one is copied again; nobody reads it.
 
-template <int WM, int WN>
+template <int WM, int WN, int RING>
 struct TileSizes {
   static constexpr int TM = 64 * WM, TN = 64 * WN;
   static constexpr int kStageBytes = (TM + TN) * 128;
   static constexpr int kScaleBytes = (TM + TN) * 16;               // of two stages
   static constexpr int kCopies = (TM + TN) / 32;                   // of a wave and stage: 8 rows each
-  static constexpr int kLds = 2 * (kStageBytes + kScaleBytes);
+  static constexpr int kLds = RING * (kStageBytes + kScaleBytes);
+  static_assert(RING == 2 || RING == 4, "places by masks");
   static_assert(TM == TN && (TM == 128 || TM == 256), "whole copies for every wave");
 };
 
-template <int OUT, int WM, int WN>
+template <int OUT, int WM, int WN, int RING>
 __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(const uint8_t* a_codes, const uint8_t* a_scales,
                                                                             const uint8_t* b_codes, const uint8_t* b_scales,
                                                                             void* Y, ProductShape p) {
-  using T = TileSizes<WM, WN>;
+  using T = TileSizes<WM, WN, RING>;
   extern __shared__ __align__(16) uint8_t lds[];
-  uint8_t* const lds_scales = lds + 2 * T::kStageBytes;
+  uint8_t* const lds_scales = lds + RING * T::kStageBytes;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // the list of tiles: panels of eight tiles of A times all of B, so that the 32 tiles an XCD works on share eight and four
   // operand tiles
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   };
   auto copy_rows = [&](const Source& src, int stage, int c) {  // one of the wave's copies of a stage
     const int kb = c < kOfA ? wave * kOfA + c : T::TM / 8 + wave * (T::TN / 32) + c - kOfA;
-    copy16_to_lds(c < kOfA ? src.a : src.b, lane_at, from[c], lds + (stage & 1) * T::kStageBytes + kb * 1024);
+    copy16_to_lds(c < kOfA ? src.a : src.b, lane_at, from[c], lds + (stage & (RING - 1)) * T::kStageBytes + kb * 1024);
   };
   // scales: two blocks of rows a copy; with 256 rows of each matrix every wave copies both, with 128 two waves A and two B
   constexpr bool kBoth = T::TM == 256;
@@ -288,7 +290,7 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     const int group = min(g, groups - 1);
     const uint8_t* of_a = a_scales + mx4_scales_at(group, blocks_a, block_m);
     const uint8_t* of_b = b_scales + mx4_scales_at(group, blocks_b, block_n);
-    uint8_t* to = scale_place + (g & 1) * T::kScaleBytes;
+    uint8_t* to = scale_place + (g & (RING - 1)) * T::kScaleBytes;
     copy16_to_lds(buffer_of(scales_of_a ? of_a : of_b, T::TM * 16), scales_of_a ? scale_from_a : scale_from_b, 0, to);
     if constexpr (kBoth) copy16_to_lds(buffer_of(of_b, T::TN * 16), scale_from_b, 0, to + T::TM * 16);
   };
@@ -302,13 +304,13 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     u32x4 a[WM], b[WN];
   };
   auto read_one = [&](int stage, int quarter, int t, Operands& f) {
-    const uint8_t* base = lds + (stage & 1) * T::kStageBytes + 1024 * quarter;
+    const uint8_t* base = lds + (stage & (RING - 1)) * T::kStageBytes + 1024 * quarter;
     if (t < WM) f.a[t] = *reinterpret_cast<const u32x4*>(base + at_a + kMx4BlockBytes * t);
     else f.b[t - WM] = *reinterpret_cast<const u32x4*>(base + at_b + kMx4BlockBytes * (t - WM));
   };
   u32x2 scale_a[WM], scale_b[WN];  // word q: quarters with h % 2 = q, two bytes a stage
   auto read_scales = [&](int g) {
-    const uint8_t* base = lds_scales + (g & 1) * T::kScaleBytes + 8 * half;
+    const uint8_t* base = lds_scales + (g & (RING - 1)) * T::kScaleBytes + 8 * half;
 #pragma unroll
     for (int i = 0; i < WM; ++i) scale_a[i] = *reinterpret_cast<const u32x2*>(base + 16 * (wave_m + 32 * i + r));
 #pragma unroll
@@ -344,12 +346,15 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     }
   };
 
-  copy_scales(0);
 #pragma unroll
-  for (int c = 0; c < T::kCopies; ++c) copy_rows(source_of(0), 0, c);
+  for (int g = 0; g < RING / 2; ++g) copy_scales(g);
 #pragma unroll
-  for (int c = 0; c < T::kCopies / 2; ++c) copy_rows(source_of(1), 1, c);
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(T::kCopies / 2) : "memory");
+  for (int q = 0; q < RING; ++q) {
+    const Source src = source_of(q);
+#pragma unroll
+    for (int c = 0; c < (q < RING - 1 ? T::kCopies : T::kCopies / 2); ++c) copy_rows(src, q, c);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 2) * T::kCopies + T::kCopies / 2) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   Operands first, second;
@@ -362,14 +367,14 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     constexpr bool kFirst = decltype(is_first)::value;
     constexpr std::integral_constant<int, kFirst ? 0 : 2> lower{};
     constexpr std::integral_constant<int, kFirst ? 1 : 3> upper{};
-    quarter_stage(lower, std::integral_constant<int, 0>{}, first, second, p, p + 1);
+    quarter_stage(lower, std::integral_constant<int, 0>{}, first, second, p, p + RING - 1);
     quarter_stage(lower, std::integral_constant<int, 1>{}, second, first, p, 0);
     quarter_stage(upper, std::integral_constant<int, 2>{}, first, second, p, 0);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (kFirst) copy_scales((p >> 1) + 1);
-    quarter_stage(upper, std::integral_constant<int, 3>{}, second, first, p + 1, p + 2);
+    if (kFirst) copy_scales((p >> 1) + RING / 2);
+    quarter_stage(upper, std::integral_constant<int, 3>{}, second, first, p + 1, p + RING);
   };
   int p0 = 0;
   for (; p0 + 2 <= stages; p0 += 2) {
@@ -429,13 +434,13 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   }
 }
 
-template <int OUT, int WM, int WN>
+template <int OUT, int WM, int WN, int RING>
 hipError_t launch_tile(const Mx4ProductArgs& a, const ProductShape& p, hipStream_t stream) {
-  using T = TileSizes<WM, WN>;
+  using T = TileSizes<WM, WN, RING>;
   const int64_t tiles = (int64_t)((p.M + T::TM - 1) / T::TM) * ((p.N + T::TN - 1) / T::TN);
-  const hipError_t e = raise_lds_limit<mx4_tile_kernel<OUT, WM, WN>>(T::kLds);
+  const hipError_t e = raise_lds_limit<mx4_tile_kernel<OUT, WM, WN, RING>>(T::kLds);
   if (e != hipSuccess) return e;
-  mx4_tile_kernel<OUT, WM, WN><<<dim3(grid_of_items(tiles)), 256, T::kLds, stream>>>(a.a_codes, a.a_scales, a.b_codes,
+  mx4_tile_kernel<OUT, WM, WN, RING><<<dim3(grid_of_items(tiles)), 256, T::kLds, stream>>>(a.a_codes, a.a_scales, a.b_codes,
                                                                                               a.b_scales, a.Y, p);
   return hipGetLastError();
 }
@@ -443,8 +448,8 @@ hipError_t launch_tile(const Mx4ProductArgs& a, const ProductShape& p, hipStream
 template <int OUT>
 hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  if (a.M > 512 && a.N > 512) return launch_tile<OUT, 4, 4>(a, p, stream);
-  if (a.M > 256 && a.N > 256) return launch_tile<OUT, 2, 2>(a, p, stream);
+  if (a.M > 512 && a.N > 512) return launch_tile<OUT, 4, 4, 2>(a, p, stream);
+  if (a.M > 256 && a.N > 256) return launch_tile<OUT, 2, 2, 4>(a, p, stream);
   if (a.N <= 32) return launch_stream<OUT, 1, 1, 8>(a, p, stream);
   if (a.N <= 64) return launch_stream<OUT, 2, 2, 8>(a, p, stream);
   return launch_stream<OUT, 4, 4, 4>(a, p, stream);
