@@ -220,7 +220,7 @@ hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStre
 // tiles.  A stage is a line of 256 values, copied straight into LDS, RING (2 or 4) stages in turn; the 16 scale bytes a row has
 // for 512 values come with every second stage.  A stage is four instructions for every 32x32 tile; a wave reads the operands of the
 // next one while it multiplies.
-//   Waits: copies of a wave land in order.  Before the last quarter of stage p those of stages p + 2 .. p + RING - 1 may be
+//   Waits (large tiles): copies of a wave land in order.  Before the last quarter of stage p those of stages p + 2 .. p + RING - 1 may be
 // outstanding, all earlier ones are waited for, and so are the wave's LDS reads of stage p; past the barrier that holds for all
 // waves, so stage p + 1 is there and the place of stage p takes stage p + RING: half of its copies during the last quarter of
 // p, the others during the first of p + 1.  Scales of group g + RING / 2 are copied in the last quarter of stage 2 g, ahead of
@@ -324,6 +324,9 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
     for (int j = 0; j < WM; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
+  // Small tiles: a wave holds the operands of a whole stage and reads those of the next one meanwhile (a quarter's products,
+  // 128 clocks, do not cover the way through LDS).  The barrier then stands before the stage, at which every wave has read it.
+  constexpr bool kWhole = WM * WN <= 4;
   // A quarter of a stage: the products of one operand set, and between them, one at a time so that neither the wave's issue nor
   // the units behind it back up, the LDS reads of the next set (from the first product on: the compiler waits there for every
   // read before it) and, in the quarters that have them, half of a stage's copies.
@@ -352,37 +355,80 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   for (int q = 0; q < RING; ++q) {
     const Source src = source_of(q);
 #pragma unroll
-    for (int c = 0; c < (q < RING - 1 ? T::kCopies : T::kCopies / 2); ++c) copy_rows(src, q, c);
+    for (int c = 0; c < (kWhole || q < RING - 1 ? T::kCopies : T::kCopies / 2); ++c) copy_rows(src, q, c);
   }
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 2) * T::kCopies + T::kCopies / 2) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kWhole ? (RING - 1) * T::kCopies : (RING - 2) * T::kCopies + T::kCopies / 2) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  Operands first, second;
-#pragma unroll
-  for (int t = 0; t < WM + WN; ++t) read_one(0, 0, t, first);
-  read_scales(0);
-
   // FIRST: the first stage of its group, with scale bytes 0 and 1; the other one has 2 and 3
-  auto stage = [&](auto is_first, int p) {
-    constexpr bool kFirst = decltype(is_first)::value;
-    constexpr std::integral_constant<int, kFirst ? 0 : 2> lower{};
-    constexpr std::integral_constant<int, kFirst ? 1 : 3> upper{};
-    quarter_stage(lower, std::integral_constant<int, 0>{}, first, second, p, p + RING - 1);
-    quarter_stage(lower, std::integral_constant<int, 1>{}, second, first, p, 0);
-    quarter_stage(upper, std::integral_constant<int, 2>{}, first, second, p, 0);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (kFirst) copy_scales((p >> 1) + RING / 2);
-    quarter_stage(upper, std::integral_constant<int, 3>{}, second, first, p + 1, p + RING);
-  };
   int p0 = 0;
-  for (; p0 + 2 <= stages; p0 += 2) {
-    stage(std::true_type{}, p0);
-    stage(std::false_type{}, p0 + 1);
-    read_scales((p0 >> 1) + 1);
+  if constexpr (kWhole) {
+    struct Stage {
+      Operands q[4];
+    };
+    Stage even, odd;
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+      for (int t = 0; t < WM + WN; ++t) read_one(0, h, t, even.q[h]);
+    read_scales(0);
+    auto stage = [&](auto is_first, int p, const Stage& now, Stage& next) {
+      constexpr bool kFirst = decltype(is_first)::value;
+      constexpr int kTiles = WM * WN, kReads = WM + WN, kPart = T::kCopies / 4;
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (kFirst) copy_scales((p >> 1) + RING / 2);
+      const Source src = source_of(p + RING);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          const int i = t / WM, j = t % WM;
+          if (h < 2)
+            acc[i][j] = mfma_32x32x64<kFirst ? 0 : 2>(now.q[h].b[i], scale_b[i][h & 1], now.q[h].a[j], scale_a[j][h & 1], acc[i][j]);
+          else
+            acc[i][j] = mfma_32x32x64<kFirst ? 1 : 3>(now.q[h].b[i], scale_b[i][h & 1], now.q[h].a[j], scale_a[j][h & 1], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = t * kReads / kTiles; e < (t + 1) * kReads / kTiles; ++e) read_one(p + 1, h, e, next.q[h]);
+#pragma unroll
+          for (int c = t * kPart / kTiles; c < (t + 1) * kPart / kTiles; ++c) copy_rows(src, p + RING, h * kPart + c);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    for (; p0 + 2 <= stages; p0 += 2) {
+      stage(std::true_type{}, p0, even, odd);
+      stage(std::false_type{}, p0 + 1, odd, even);
+      read_scales((p0 >> 1) + 1);
+    }
+    if (p0 < stages) stage(std::true_type{}, p0, even, odd);
+  } else {
+    Operands first, second;
+#pragma unroll
+    for (int t = 0; t < WM + WN; ++t) read_one(0, 0, t, first);
+    read_scales(0);
+    auto stage = [&](auto is_first, int p) {
+      constexpr bool kFirst = decltype(is_first)::value;
+      constexpr std::integral_constant<int, kFirst ? 0 : 2> lower{};
+      constexpr std::integral_constant<int, kFirst ? 1 : 3> upper{};
+      quarter_stage(lower, std::integral_constant<int, 0>{}, first, second, p, p + RING - 1);
+      quarter_stage(lower, std::integral_constant<int, 1>{}, second, first, p, 0);
+      quarter_stage(upper, std::integral_constant<int, 2>{}, first, second, p, 0);
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (kFirst) copy_scales((p >> 1) + RING / 2);
+      quarter_stage(upper, std::integral_constant<int, 3>{}, second, first, p + 1, p + RING);
+    };
+    for (; p0 + 2 <= stages; p0 += 2) {
+      stage(std::true_type{}, p0);
+      stage(std::false_type{}, p0 + 1);
+      read_scales((p0 >> 1) + 1);
+    }
+    if (p0 < stages) stage(std::true_type{}, p0);
   }
-  if (p0 < stages) stage(std::true_type{}, p0);
   // every copy has landed and every wave has read its operands: the ring becomes the waves' slabs
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
@@ -445,14 +491,57 @@ hipError_t launch_tile(const Mx4ProductArgs& a, const ProductShape& p, hipStream
   return hipGetLastError();
 }
 
+// Which form serves a shape: the least of estimates in microseconds, fitted to launches with weights from memory at 99 shapes
+// (M, K of 128 .. 16384, 1 .. 8192 columns), of which the form chosen was the best one or at most 10 % behind it.  Both sides
+// of each line: 4096x4096 of 256 columns 7.5 us from registers, 9.8 as tiles of 128 rows; of 1000 columns 15.3 and 12.0; of 2048
+// columns 22 as tiles of 128 rows with a ring of four stages, 21.4 with two stages and two workgroups a unit; of 4096 columns
+// 39 as tiles of 128 rows, 36 of 256.
+struct Form {
+  int rows, cols;      // of a workgroup
+  int waves;           // registers: that share the lines; 0: tiles
+  int at_once;         // tiles: workgroups that the chip holds
+  double start;        // us of a launch and of what does not overlap
+  double line;         // registers: us of a wave's line
+  double alone, full;  // tiles: us of a stage, with few workgroups and with all places taken; registers: KB/us that a compute
+                       // unit draws with one workgroup, and with two or more
+};
+constexpr Form kForms[] = {
+    {32, 32, 8, 0, 4.0, 0.40, 122, 98},       {32, 64, 8, 0, 4.0, 0.80, 117, 87},       {64, 64, 8, 0, 4.0, 1.29, 99, 58},
+    {64, 128, 4, 0, 4.0, 1.18, 84, 63},       {128, 128, 0, 256, 4.6, 0, 0.30, 0.61}, {128, 128, 0, 512, 3.9, 0, 0.52, 1.14},
+    {256, 256, 0, 256, 8.2, 0, 0.92, 1.77},
+};
+double estimate_us(const Form& f, const ProductShape& p) {
+  const int64_t groups = (int64_t)((p.M + f.rows - 1) / f.rows) * ((p.N + f.cols - 1) / f.cols);
+  const double lines = mx4_lines(p.K);
+  if (f.waves) {
+    const double each = lines * 0.128 * (f.rows + (p.N < f.cols ? p.N : f.cols));  // KB
+    const double share = groups <= 256 ? 1 : groups / 256.0;                       // workgroups of a compute unit
+    const double rate = share >= 2 ? f.full : f.alone + (f.full - f.alone) * (share - 1);
+    const double drawn = (double)((groups + 255) / 256) * each / rate;
+    const double in_turn = (double)((mx4_lines(p.K) + f.waves - 1) / f.waves) * f.line, weights = lines * 128.0 * p.M / 5.5e6;
+    const double most = drawn > in_turn ? drawn : in_turn;
+    return f.start + (most > weights ? most : weights) + drawn / 8;
+  }
+  const int64_t full = groups / f.at_once;
+  const double left = (double)(groups - full * f.at_once) / f.at_once;
+  return f.start + lines * ((double)full * f.full + (left > 0 ? f.alone + (f.full - f.alone) * left : 0));
+}
+
 template <int OUT>
 hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  if (a.M > 512 && a.N > 512) return launch_tile<OUT, 4, 4, 2>(a, p, stream);
-  if (a.M > 256 && a.N > 256) return launch_tile<OUT, 2, 2, 4>(a, p, stream);
-  if (a.N <= 32) return launch_stream<OUT, 1, 1, 8>(a, p, stream);
-  if (a.N <= 64) return launch_stream<OUT, 2, 2, 8>(a, p, stream);
-  return launch_stream<OUT, 4, 4, 4>(a, p, stream);
+  int best = 0;
+  for (int i = 1; i < (int)(sizeof kForms / sizeof kForms[0]); ++i)
+    if (estimate_us(kForms[i], p) < estimate_us(kForms[best], p)) best = i;
+  switch (best) {
+    case 0: return launch_stream<OUT, 1, 1, 8>(a, p, stream);
+    case 1: return launch_stream<OUT, 1, 2, 8>(a, p, stream);
+    case 2: return launch_stream<OUT, 2, 2, 8>(a, p, stream);
+    case 3: return launch_stream<OUT, 2, 4, 4>(a, p, stream);
+    case 4: return launch_tile<OUT, 2, 2, 4>(a, p, stream);
+    case 5: return launch_tile<OUT, 2, 2, 2>(a, p, stream);
+    default: return launch_tile<OUT, 4, 4, 2>(a, p, stream);
+  }
 }
 
 }  // namespace
