@@ -363,8 +363,9 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
  * tokens, row-major): layers kept in microscaled 4-bit form, and the norms on both sides of the block.
  * In this part leading dimensions are any value >= the row length and 16-bit matrices need the alignment of
  * their elements only; rows that begin at multiples of 16 bytes (aligned base, leading dimension a multiple
- * of 8) are read and written in 16-byte pieces, others element by element.  Nothing beyond the row length
- * is read or written.
+ * of 8) are read and written in 16-byte pieces, others element by element.  A piece that holds at least
+ * one element of a row is read whole (what lies beyond never reaches a result); nothing beyond the
+ * row length is written.
  *
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
  * version 1.0): 32 consecutive values of a row share a power of two, and every value is one of

@@ -1,8 +1,15 @@
 // Norms on both sides of a block with gates and residual, and their gradients (include/hinm.h).
 //
-// Matrices are channels x tokens, so a norm's sums run down the columns.  A workgroup owns a strip of 64 columns (eight
-// lanes of eight) and a chunk of rows; partial sums of the chunks meet in the workspace and every later pass adds them in the
-// same order.
+// Matrices are channels x tokens, so a norm's sums run down the columns, and only a workgroup that draws whole cache lines
+// (64 columns) of many rows keeps enough of memory in flight: columns are split over workgroups.  Two launches: the first
+// adds what every column needs over its rows, by chunks; the second adds the chunks in a fixed order and writes the results.
+// The second norm's sum is there after the first launch because h is linear in x and y with factors known per column:
+//   h = s x + r t (c y)   with c = gate w_post per channel, t = token_gate, r = rstd_y per token:
+//   sum h^2 = s^2 sum x^2 + 2 s r t sum x (c y) + (r t)^2 sum (c y)^2.
+// Where the three nearly cancel (a block whose output undoes its residual) that loses digits: a column whose sum is below
+// 1/16 of its two squares is added again from h itself.  The gradients' correction S = sum_k c y d is linear in the
+// gradient d in the same way.  (One launch with the columns held in registers: strips of 8 .. 32 columns draw 16 .. 64 bytes
+// of each line, and took 55 us at 4096x4096 where two launches take less.)
 #include "eight_values.h"
 
 namespace hinm {
@@ -10,24 +17,33 @@ namespace hinm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kStrip = 64;                      // columns of a workgroup
-constexpr int kRowsAtOnce = kThreads / 8;       // rows that its lanes cover together
+constexpr int kStrip = 64;                 // columns of a workgroup: eight lanes of eight
+constexpr int kRowsAtOnce = kThreads / 8;  // rows that its lanes cover together: a round
+constexpr int kRounds = 4;                 // rounds whose loads are in flight together
+constexpr int kPatch = kRounds * kRowsAtOnce;
 constexpr int kWaves = kThreads / 64;
 
-// Rows of a chunk: at least 128, and at most 64 chunks.
-int chunk_rows(int K) {
-  const int least = (K + 63) / 64;
-  return least <= 128 ? 128 : (least + kRowsAtOnce - 1) / kRowsAtOnce * kRowsAtOnce;
-}
-int chunk_count(int K) { return (K + chunk_rows(K) - 1) / chunk_rows(K); }
 int strip_count(int N) { return (N + kStrip - 1) / kStrip; }
+// Patches of a chunk: as many as leave some 1024 workgroups, so that a workgroup's share of the chunks' sums stays small
+// beside its rows; at most 64 chunks.
+int chunk_patches(int K, int N) {
+  const int64_t patches = (K + kPatch - 1) / kPatch;
+  const int64_t per = patches * strip_count(N) / 1024, least = (patches + 63) / 64;
+  return (int)(per > least ? per : least < 1 ? 1 : least);
+}
+int chunk_count(int K, int N) {
+  const int rows = kPatch * chunk_patches(K, N);
+  return (K + rows - 1) / rows;
+}
 
-struct Strip {
-  int n0, n, left, row0, rows, chunk;  // first column; this lane's first column and how many it has; rows of the chunk
-  __device__ __forceinline__ Strip(int K, int N, int rows_per_chunk) {
+// Which strip and chunk a workgroup has.  Chunks first: neighbouring workgroups take neighbouring columns of the same rows.
+struct Place {
+  int n0, n, left, row0, rows, chunk, strip;  // first column; this lane's first column, how many it has; rows of the chunk
+  __device__ __forceinline__ Place(int K, int N, int rows_per_chunk) {
     const int strips = (N + kStrip - 1) / kStrip;
     chunk = blockIdx.x / strips;
-    n0 = (blockIdx.x - chunk * strips) * kStrip;
+    strip = blockIdx.x - chunk * strips;
+    n0 = strip * kStrip;
     n = n0 + 8 * (threadIdx.x & 7);
     left = min(8, N - n);
     row0 = chunk * rows_per_chunk;
@@ -49,34 +65,54 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[8]) {
                floats_to_bits<DT>(f[6], f[7])};
 }
 
-// Sums of the workgroup's 64 columns over its threads: `s` eight columns of this thread, the result (fixed order) in
-// total[0..63] after the call's last barrier.
-__device__ __forceinline__ void add_strip(float (&s)[8], float* by_wave, float* total) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    s[j] += __shfl_xor(s[j], 8);
-    s[j] += __shfl_xor(s[j], 16);
-    s[j] += __shfl_xor(s[j], 32);
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane < 8) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) by_wave[wave * kStrip + 8 * lane + j] = s[j];
-  }
-  __syncthreads();
-  if (threadIdx.x < kStrip) {
-    float t = 0;
-    for (int w = 0; w < kWaves; ++w) t += by_wave[w * kStrip + threadIdx.x];
-    total[threadIdx.x] = t;
-  }
-  __syncthreads();
+// Sum over a wave's lanes with the same lane % 8.
+__device__ __forceinline__ float add_lanes_by_8(float v) {
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));  // lane ^ 8
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 
-// Sum over the chunks of one column's partial sums.
-__device__ __forceinline__ float add_chunks(const float* partial, int chunks, int N, int n) {
+// QUANTITIES sums of the workgroup's 64 columns, added over its threads in a fixed order, to partial[quantity][chunk][N].
+template <int QUANTITIES>
+__device__ __forceinline__ void store_sums(float (&sum)[QUANTITIES][8], const Place& p, float* partial, int chunks, int N) {
+  __shared__ float by_wave[QUANTITIES][kWaves][kStrip];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int q = 0; q < QUANTITIES; ++q) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float t = add_lanes_by_8(sum[q][j]);
+      if (lane < 8) by_wave[q][wave][8 * lane + j] = t;
+    }
+  }
+  __syncthreads();
+  const int col = threadIdx.x & (kStrip - 1), n = p.n0 + col;
+  for (int q = threadIdx.x / kStrip; q < QUANTITIES; q += kThreads / kStrip) {
+    float t = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += by_wave[q][w][col];
+    if (n < N) partial[((int64_t)q * chunks + p.chunk) * N + n] = t;
+  }
+}
+
+// ... and their totals over the chunks, to total[quantity][64].  The caller waits at a barrier.
+template <int QUANTITIES>
+__device__ __forceinline__ void add_chunks(const float* partial, int chunks, int N, const Place& p, float (*total)[kStrip]) {
+  static_assert(QUANTITIES <= kThreads / kStrip, "a thread for each");
+  const int col = threadIdx.x & (kStrip - 1), n = p.n0 + col, q = threadIdx.x / kStrip;
+  if (q >= QUANTITIES || n >= N) return;
+  const float* at = partial + (int64_t)q * chunks * N + n;
   float t = 0;
-  for (int c = 0; c < chunks; ++c) t += partial[(int64_t)c * N + n];
-  return t;
+  int c = 0;
+  for (; c + 8 <= chunks; c += 8) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = at[(int64_t)(c + j) * N];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t += v[j];
+  }
+  for (; c < chunks; ++c) t += at[(int64_t)c * N];
+  total[q][col] = t;
 }
 
 // ---- forward ------------------------------------------------------------------------------------------
@@ -91,94 +127,241 @@ struct Forward {
   uint16_t* u;
   int64_t ld_block;
   float *rstd_y, *rstd_h;
-  float *sum_y, *sum_h;  // [chunks][N]
+  float* sums;  // [4][chunks][N]: y^2, x^2, x c y, (c y)^2
   bool vec_stream, vec_block;
 };
 
-// eight columns of h in one row
+// kRounds rows of x and y of a lane's columns, from row k on in steps of a round
+struct PatchXY {
+  u32x4 x[kRounds], y[kRounds];
+};
+__device__ __forceinline__ void load_patch(const Forward& a, const Place& p, int k, int end, PatchXY& v) {
+  const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const int r = k + i * kRowsAtOnce;
+    const bool in = r < end && p.left > 0;
+    v.x[i] = in ? load_eight(a.x + (int64_t)r * a.ld_stream + p.n, p.left, a.vec_stream) : none;
+    v.y[i] = in && a.y ? load_eight(a.y + (int64_t)r * a.ld_block + p.n, p.left, a.vec_block) : none;
+  }
+}
+__device__ __forceinline__ float channel_factor(const float* w_post, const float* gate, int k) {
+  return (w_post ? w_post[k] : 1.0f) * (gate ? gate[k] : 1.0f);
+}
+
 template <int DT>
-__device__ __forceinline__ void row_of_h(const Forward& a, int k, int n, int left, const float (&token)[8], float (&h)[8]) {
-  widen<DT>(load_eight(a.x + (int64_t)k * a.ld_stream + n, left, a.vec_stream), h);
+__global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
+  const Place p(a.K, a.N, a.rows_per_chunk);
+  float sum[4][8] = {};
+  const int end = p.row0 + p.rows;
+  for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kPatch) {
+    PatchXY v;
+    load_patch(a, p, k, end, v);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) h[j] *= a.scale;
-  if (a.y) {
-    float y[8];
-    widen<DT>(load_eight(a.y + (int64_t)k * a.ld_block + n, left, a.vec_block), y);
-    const float c = (a.w_post ? a.w_post[k] : 1.0f) * (a.gate ? a.gate[k] : 1.0f);
+    for (int i = 0; i < kRounds; ++i) {
+      const int r = k + i * kRowsAtOnce;
+      const float c = r < end ? channel_factor(a.w_post, a.gate, r) : 0.0f;
+      float x[8], y[8];
+      widen<DT>(v.x[i], x);
+      widen<DT>(v.y[i], y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] += c * (token[j] * y[j]);
-  }
-}
-
-// token_gate rstd_y of a lane's columns
-__device__ __forceinline__ void factors_of_tokens(const Forward& a, const Strip& s, const float* rstd, float (&token)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    token[j] = j < s.left && a.token_gate ? a.token_gate[s.n + j] : 1.0f;
-    if (a.w_post) token[j] *= rstd[s.n - s.n0 + j];
-  }
-}
-
-// rstd of the strip's columns from the chunks' sums, to LDS and (by the first chunk's workgroups) to memory
-__device__ __forceinline__ void finish_rstd(const Forward& a, const Strip& s, const float* sums, float* out, float* rstd) {
-  if (threadIdx.x < kStrip) {
-    const int n = s.n0 + threadIdx.x;
-    float r = 0;
-    if (n < a.N) {
-      r = 1.0f / sqrtf(add_chunks(sums, a.chunks, a.N, n) / (float)a.K + a.eps);
-      if (out && s.chunk == 0) out[n] = r;
+      for (int j = 0; j < 8; ++j) {
+        sum[0][j] += y[j] * y[j];
+        sum[1][j] += x[j] * x[j];
+        const float b = c * y[j];
+        sum[2][j] += x[j] * b;
+        sum[3][j] += b * b;
+      }
     }
-    rstd[threadIdx.x] = r;
+  }
+  store_sums<4>(sum, p, a.sums, a.chunks, a.N);
+}
+
+// What an element needs of its token.
+struct TokenFactors {
+  float branch[8], u[8];  // token_gate rstd_y; rstd_h
+};
+
+template <int DT>
+__device__ __forceinline__ void row_of_h(const Forward& a, u32x4 x, u32x4 y, float c, const float (&branch)[8], float (&h)[8]) {
+  float v[8];
+  widen<DT>(x, h);
+  widen<DT>(y, v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) h[j] = h[j] * a.scale + branch[j] * (c * v[j]);
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void block_norm_apply_kernel(Forward a) {
+  __shared__ float total[4][kStrip], branch[kStrip], root[kStrip], again[kWaves][kStrip];
+  __shared__ int cancelled;
+  const Place p(a.K, a.N, a.rows_per_chunk);
+  const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
+  PatchXY v;
+  load_patch(a, p, first, end, v);  // on their way while the sums are added
+  if (a.w_post || a.w_pre) add_chunks<4>(a.sums, a.chunks, a.N, p, total);
+  if (threadIdx.x == 0) cancelled = 0;
+  __syncthreads();
+  if (threadIdx.x < kStrip) {
+    const int n = p.n0 + threadIdx.x;
+    float b = 1, r = 0;
+    if (n < a.N) {
+      if (a.token_gate) b = a.token_gate[n];
+      if (a.w_post) {
+        const float ry = 1.0f / sqrtf(total[0][threadIdx.x] / (float)a.K + a.eps);
+        b *= ry;
+        if (a.rstd_y && p.chunk == 0) a.rstd_y[n] = ry;
+      }
+      if (a.w_pre) {
+        const float of_x = a.scale * a.scale * total[1][threadIdx.x], of_y = a.y ? b * b * total[3][threadIdx.x] : 0.0f;
+        const float sum = of_x + of_y + (a.y ? 2 * a.scale * b * total[2][threadIdx.x] : 0.0f);
+        if (sum < 0.0625f * (of_x + of_y)) cancelled = 1;
+        r = 1.0f / sqrtf(sum / (float)a.K + a.eps);
+      }
+    }
+    branch[threadIdx.x] = b;
+    root[threadIdx.x] = r;
   }
   __syncthreads();
-}
-
-// PASS 0: sums of y^2.  1: sums of h^2.  2: h and u.
-template <int DT, int PASS>
-__global__ __launch_bounds__(kThreads) void block_norm_pass_kernel(Forward a) {
-  __shared__ float by_wave[kWaves * kStrip], total[kStrip], rstd_y[kStrip], rstd_h[kStrip];
-  const Strip s(a.K, a.N, a.rows_per_chunk);
-  if constexpr (PASS > 0) {
-    if (a.w_post) finish_rstd(a, s, a.sum_y, PASS == 2 ? a.rstd_y : nullptr, rstd_y);
-    if (PASS == 2 && a.w_pre) finish_rstd(a, s, a.sum_h, a.rstd_h, rstd_h);
-  }
-  float token[8], sum[8] = {};
-  if constexpr (PASS > 0) factors_of_tokens(a, s, rstd_y, token);
-  if (s.left > 0) {
-    for (int i = threadIdx.x >> 3; i < s.rows; i += kRowsAtOnce) {
-      const int k = s.row0 + i;
-      float v[8];
-      if constexpr (PASS == 0) {
-        widen<DT>(load_eight(a.y + (int64_t)k * a.ld_block + s.n, s.left, a.vec_block), v);
-      } else {
-        row_of_h<DT>(a, k, s.n, s.left, token, v);
-      }
-      if constexpr (PASS < 2) {
+  float of_token[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += v[j] * v[j];
-      } else {
-        if (a.h) store_eight(a.h + (int64_t)k * a.ld_stream + s.n, narrow<DT>(v), s.left, a.vec_stream);
-        if (a.w_pre) {
-          const float w = a.w_pre[k];
+  for (int j = 0; j < 8; ++j) of_token[j] = branch[at + j];
+  if (cancelled) {  // the same for the whole workgroup, and for all workgroups of the strip
+    float sum[8] = {};
+    for (int k = threadIdx.x >> 3; k < a.K; k += kPatch) {
+      PatchXY w;
+      load_patch(a, p, k, a.K, w);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] *= w * rstd_h[s.n - s.n0 + j];
-          store_eight(a.u + (int64_t)k * a.ld_block + s.n, narrow<DT>(v), s.left, a.vec_block);
-        }
+      for (int i = 0; i < kRounds; ++i) {
+        const int r = k + i * kRowsAtOnce;
+        float h[8];
+        row_of_h<DT>(a, w.x[i], w.y[i], r < a.K ? channel_factor(a.w_post, a.gate, r) : 0.0f, of_token, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += h[j] * h[j];
       }
     }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float t = add_lanes_by_8(sum[j]);
+      if (lane < 8) again[wave][8 * lane + j] = t;
+    }
+    __syncthreads();
+    if (threadIdx.x < kStrip) {
+      float t = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) t += again[w][threadIdx.x];
+      root[threadIdx.x] = 1.0f / sqrtf(t / (float)a.K + a.eps);
+    }
+    __syncthreads();
   }
-  if constexpr (PASS < 2) {
-    add_strip(sum, by_wave, total);
-    const int n = s.n0 + threadIdx.x;
-    if (threadIdx.x < kStrip && n < a.N) (PASS == 0 ? a.sum_y : a.sum_h)[(int64_t)s.chunk * a.N + n] = total[threadIdx.x];
+  if (a.w_pre && a.rstd_h && p.chunk == 0 && threadIdx.x < kStrip && p.n0 + (int)threadIdx.x < a.N)
+    a.rstd_h[p.n0 + threadIdx.x] = root[threadIdx.x];
+  if (p.left <= 0) return;
+  float of_u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) of_u[j] = root[at + j];
+  for (int k = first; k < end; k += kPatch) {
+    PatchXY next;
+    if (k + kPatch < end) load_patch(a, p, k + kPatch, end, next);
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int r = k + i * kRowsAtOnce;
+      if (r >= end) break;
+      float h[8];
+      row_of_h<DT>(a, v.x[i], v.y[i], channel_factor(a.w_post, a.gate, r), of_token, h);
+      if (a.h) store_eight(a.h + (int64_t)r * a.ld_stream + p.n, narrow<DT>(h), p.left, a.vec_stream);
+      if (a.w_pre) {
+        const float w = a.w_pre[r];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] *= w * of_u[j];
+        store_eight(a.u + (int64_t)r * a.ld_block + p.n, narrow<DT>(h), p.left, a.vec_block);
+      }
+    }
+    v = next;
+  }
+}
+
+// One token without a stride: a vector, held by one workgroup of 1024 threads, eight channels a thread and round.
+constexpr int kVectorThreads = 1024;
+constexpr int kVectorMost = 2 * 8 * kVectorThreads;
+
+__device__ __forceinline__ float add_workgroup(float v, float* by_wave) {
+#pragma unroll
+  for (int q = 1; q < 64; q *= 2) v += __shfl_xor(v, q);
+  if ((threadIdx.x & 63) == 0) by_wave[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = 0;
+#pragma unroll
+  for (int w = 0; w < kVectorThreads / 64; ++w) t += by_wave[w];
+  return t;
+}
+// eight floats from k on, `valid` of them (the rest: zero); absent: ones
+__device__ __forceinline__ void load_factors(const float* p, int k, int valid, float (&f)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = p ? (j < valid ? p[k + j] : 0.0f) : 1.0f;
+}
+
+template <int DT, int ROUNDS>
+__global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forward a) {
+  __shared__ __align__(16) float by_wave[2][kVectorThreads / 64];
+  float x[ROUNDS][8], y[ROUNDS][8], c[ROUNDS][8], w[ROUNDS][8];
+  const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
+    widen<DT>(left > 0 ? load_eight(a.x + k, left, a.vec_stream) : none, x[i]);
+    widen<DT>(left > 0 && a.y ? load_eight(a.y + k, left, a.vec_block) : none, y[i]);
+    float g[8];
+    load_factors(a.w_post, k, left, c[i]);
+    load_factors(a.gate, k, left, g);
+    load_factors(a.w_pre, k, left, w[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[i][j] *= g[j];
+  }
+  float token = a.token_gate ? a.token_gate[0] : 1.0f;
+  if (a.w_post) {
+    float sum = 0;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += y[i][j] * y[i][j];
+    const float r = 1.0f / sqrtf(add_workgroup(sum, by_wave[0]) / (float)a.K + a.eps);
+    if (a.rstd_y && threadIdx.x == 0) a.rstd_y[0] = r;
+    token *= r;
+  }
+  float sum = 0;
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[i][j] = x[i][j] * a.scale + token * (c[i][j] * y[i][j]);  // h from here on
+      sum += x[i][j] * x[i][j];
+    }
+  if (a.h) {
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
+      if (left > 0) store_eight(a.h + k, narrow<DT>(x[i]), left, a.vec_stream);
+    }
+  }
+  if (!a.w_pre) return;
+  const float r = 1.0f / sqrtf(add_workgroup(sum, by_wave[1]) / (float)a.K + a.eps);
+  if (a.rstd_h && threadIdx.x == 0) a.rstd_h[0] = r;
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
+    if (left <= 0) break;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[i][j] *= w[i][j] * r;
+    store_eight(a.u + k, narrow<DT>(x[i]), left, a.vec_block);
   }
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------
-// The second norm's correction needs S = sum_k c d y with c = gate w_post and d the gradient of h, which itself holds the
-// first correction.  S is linear in d, so one pass over the inputs gives both:
+// The second norm's correction needs S = sum_k c d y with d the gradient of h, which itself holds the first correction:
 //   s1 = sum_k w_pre du h,   S = sum_k c y dh + rstd_h sum_k c y w_pre du - rstd_h^3 s1 / K sum_k c y h.
-// A second pass writes dx and dy and adds every row of its strip; a third adds the strips.
+// The second launch writes dx and dy and adds every row of its strip; a third adds the strips.
 
 struct Backward {
   int K, N, rows_per_chunk, chunks;
@@ -196,31 +379,40 @@ struct Backward {
   bool vec_stream, vec_block;
 };
 
-template <int DT>
-__device__ __forceinline__ void grad_row(const Backward& a, int k, int n, int left, float (&h)[8], float (&dh)[8], float (&g)[8],
-                                         float (&y)[8]) {
-  const int64_t at_stream = (int64_t)k * a.ld_stream + n, at_block = (int64_t)k * a.ld_block + n;
+struct PatchGrad {
+  u32x4 h[kRounds], dh[kRounds], du[kRounds], y[kRounds];
+};
+__device__ __forceinline__ void load_patch(const Backward& a, const Place& p, int k, int end, PatchGrad& v) {
   const u32x4 none = {0, 0, 0, 0};
-  widen<DT>(a.w_pre ? load_eight(a.h + at_stream, left, a.vec_stream) : none, h);
-  widen<DT>(a.dh ? load_eight(a.dh + at_stream, left, a.vec_stream) : none, dh);
-  widen<DT>(a.w_pre ? load_eight(a.du + at_block, left, a.vec_block) : none, g);
-  widen<DT>(a.y ? load_eight(a.y + at_block, left, a.vec_block) : none, y);
-}
-__device__ __forceinline__ float factor_of_channel(const Backward& a, int k) {
-  return (a.w_post ? a.w_post[k] : 1.0f) * (a.gate ? a.gate[k] : 1.0f);
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const int r = k + i * kRowsAtOnce;
+    const bool in = r < end && p.left > 0;
+    const int64_t stream = (int64_t)r * a.ld_stream + p.n, block = (int64_t)r * a.ld_block + p.n;
+    v.h[i] = in && a.w_pre ? load_eight(a.h + stream, p.left, a.vec_stream) : none;
+    v.dh[i] = in && a.dh ? load_eight(a.dh + stream, p.left, a.vec_stream) : none;
+    v.du[i] = in && a.w_pre ? load_eight(a.du + block, p.left, a.vec_block) : none;
+    v.y[i] = in && a.y ? load_eight(a.y + block, p.left, a.vec_block) : none;
+  }
 }
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward a) {
-  __shared__ float by_wave[kWaves * kStrip], total[kStrip];
-  const Strip s(a.K, a.N, a.rows_per_chunk);
+  const Place p(a.K, a.N, a.rows_per_chunk);
   float sum[4][8] = {};
-  if (s.left > 0) {
-    for (int i = threadIdx.x >> 3; i < s.rows; i += kRowsAtOnce) {
-      const int k = s.row0 + i;
+  const int end = p.row0 + p.rows;
+  for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kPatch) {
+    PatchGrad v;
+    load_patch(a, p, k, end, v);
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int r = k + i * kRowsAtOnce;
+      const float w = r < end && a.w_pre ? a.w_pre[r] : 0.0f, c = r < end ? channel_factor(a.w_post, a.gate, r) : 0.0f;
       float h[8], dh[8], g[8], y[8];
-      grad_row<DT>(a, k, s.n, s.left, h, dh, g, y);
-      const float w = a.w_pre ? a.w_pre[k] : 0.0f, c = factor_of_channel(a, k);
+      widen<DT>(v.h[i], h);
+      widen<DT>(v.dh[i], dh);
+      widen<DT>(v.du[i], g);
+      widen<DT>(v.y[i], y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         g[j] *= w;
@@ -232,132 +424,164 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward
       }
     }
   }
-  const int n = s.n0 + threadIdx.x;
-  for (int q = 0; q < 4; ++q) {
-    add_strip(sum[q], by_wave, total);
-    if (threadIdx.x < kStrip && n < a.N) a.sums[((int64_t)q * a.chunks + s.chunk) * a.N + n] = total[threadIdx.x];
-  }
+  store_sums<4>(sum, p, a.sums, a.chunks, a.N);
 }
 
 template <int DT>
-__global__ __launch_bounds__(kThreads) void block_norm_grad_rows_kernel(Backward a) {
-  __shared__ float first[kStrip], second[kStrip];  // corrections per column: rstd_h^3 s1 / K; rstd_y^2 S / K
-  const Strip s(a.K, a.N, a.rows_per_chunk);
-  const int strips = (a.N + kStrip - 1) / kStrip, strip = s.n0 / kStrip;
-  if (threadIdx.x < kStrip) {
-    const int n = s.n0 + threadIdx.x;
-    float f1 = 0, f2 = 0;
-    if (n < a.N) {
-      float t[4];
-      for (int q = 0; q < 4; ++q) t[q] = add_chunks(a.sums + (int64_t)q * a.chunks * a.N, a.chunks, a.N, n);
-      const float rh = a.w_pre ? a.rstd_h[n] : 0.0f, ry = a.w_post ? a.rstd_y[n] : 1.0f;
-      f1 = rh * rh * rh * (t[0] / (float)a.K);
-      const float S = t[1] + rh * t[2] - f1 * t[3];
-      f2 = a.w_post ? ry * ry * (S / (float)a.K) : 0.0f;
-      if (a.dtoken_gate && s.chunk == 0) a.dtoken_gate[n] = S * ry;
-    }
-    first[threadIdx.x] = f1;
-    second[threadIdx.x] = f2;
-  }
-  __syncthreads();
+__global__ __launch_bounds__(kThreads) void block_norm_grad_apply_kernel(Backward a) {
+  __shared__ float total[4][kStrip], first_of[kStrip], second_of[kStrip];  // corrections: rstd_h^3 s1 / K; rstd_y^2 S / K
+  const Place p(a.K, a.N, a.rows_per_chunk);
+  const int strips = (a.N + kStrip - 1) / kStrip;
+  const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
+  PatchGrad v;
+  load_patch(a, p, first, end, v);
+  add_chunks<4>(a.sums, a.chunks, a.N, p, total);
   float rh[8], token[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const bool in = j < s.left;
-    rh[j] = in && a.w_pre ? a.rstd_h[s.n + j] : 0.0f;
-    token[j] = !in ? 0.0f : (a.token_gate ? a.token_gate[s.n + j] : 1.0f) * (a.w_post ? a.rstd_y[s.n + j] : 1.0f);
+    const bool in = j < p.left;
+    rh[j] = in && a.w_pre ? a.rstd_h[p.n + j] : 0.0f;
+    token[j] = !in ? 0.0f : (a.token_gate ? a.token_gate[p.n + j] : 1.0f) * (a.w_post ? a.rstd_y[p.n + j] : 1.0f);
   }
-  // whole rounds of rows: the lanes of a row add their columns together
-  for (int i0 = 0; i0 < s.rows; i0 += kRowsAtOnce) {
-    const int i = i0 + (threadIdx.x >> 3), k = s.row0 + i;
-    float of_w_pre = 0, of_branch = 0;
-    if (i < s.rows && s.left > 0) {
-      float h[8], dh[8], g[8], y[8];
-      grad_row<DT>(a, k, s.n, s.left, h, dh, g, y);
-      const float w = a.w_pre ? a.w_pre[k] : 0.0f, c = factor_of_channel(a, k);
-      const int at = s.n - s.n0;
-      float dx[8], dy[8];
+  __syncthreads();
+  if (threadIdx.x < kStrip) {
+    const int n = p.n0 + threadIdx.x;
+    float f1 = 0, f2 = 0;
+    if (n < a.N) {
+      const float r = a.w_pre ? a.rstd_h[n] : 0.0f, ry = a.w_post ? a.rstd_y[n] : 1.0f;
+      f1 = r * r * r * (total[0][threadIdx.x] / (float)a.K);
+      const float S = total[1][threadIdx.x] + r * total[2][threadIdx.x] - f1 * total[3][threadIdx.x];
+      f2 = a.w_post ? ry * ry * (S / (float)a.K) : 0.0f;
+      if (a.dtoken_gate && p.chunk == 0) a.dtoken_gate[n] = S * ry;
+    }
+    first_of[threadIdx.x] = f1;
+    second_of[threadIdx.x] = f2;
+  }
+  __syncthreads();
+  float f1[8], f2[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    f1[j] = first_of[at + j];
+    f2[j] = second_of[at + j];
+  }
+  // whole patches: the lanes of a row add their columns together
+  for (int k = first; k - first < p.rows; k += kPatch) {
+    PatchGrad next;
+    if (k - first + kPatch < p.rows) load_patch(a, p, k + kPatch, end, next);
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int r = k + i * kRowsAtOnce;
+      const bool in = r < end;
+      const float w = in && a.w_pre ? a.w_pre[r] : 0.0f, c = in ? channel_factor(a.w_post, a.gate, r) : 0.0f;
+      float h[8], dh[8], g[8], y[8], of_w_pre = 0, of_branch = 0;
+      widen<DT>(v.h[i], h);
+      widen<DT>(v.dh[i], dh);
+      widen<DT>(v.du[i], g);
+      widen<DT>(v.y[i], y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         of_w_pre += g[j] * h[j] * rh[j];
-        const float d = dh[j] + w * g[j] * rh[j] - h[j] * first[at + j];
+        const float d = dh[j] + w * g[j] * rh[j] - h[j] * f1[j];
         of_branch += d * y[j] * token[j];
-        dx[j] = a.scale * d;
-        dy[j] = token[j] * (c * d - y[j] * second[at + j]);
+        dh[j] = a.scale * d;
+        y[j] = token[j] * (c * d - y[j] * f2[j]);
       }
-      if (a.dx) store_eight(a.dx + (int64_t)k * a.ld_stream + s.n, narrow<DT>(dx), s.left, a.vec_stream);
-      if (a.dy) store_eight(a.dy + (int64_t)k * a.ld_block + s.n, narrow<DT>(dy), s.left, a.vec_block);
-    }
+      if (in && p.left > 0) {
+        if (a.dx) store_eight(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left, a.vec_stream);
+        if (a.dy) store_eight(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left, a.vec_block);
+      }
 #pragma unroll
-    for (int q = 1; q < 8; q *= 2) {
-      of_w_pre += __shfl_xor(of_w_pre, q);
-      of_branch += __shfl_xor(of_branch, q);
+      for (int q = 1; q < 8; q *= 2) {
+        of_w_pre += __shfl_xor(of_w_pre, q);
+        of_branch += __shfl_xor(of_branch, q);
+      }
+      if (in && (threadIdx.x & 7) == 0) {
+        a.row_sums[(int64_t)p.strip * a.K + r] = of_w_pre;
+        a.row_sums[(int64_t)(strips + p.strip) * a.K + r] = of_branch;
+      }
     }
-    if (i < s.rows && (threadIdx.x & 7) == 0) {
-      a.row_sums[(int64_t)strip * a.K + k] = of_w_pre;
-      a.row_sums[(int64_t)(strips + strip) * a.K + k] = of_branch;
-    }
+    v = next;
   }
 }
 
+// Four threads' strips each, added in a fixed order, for 64 channels a workgroup.
 __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backward a) {
+  __shared__ float part[2][4][64];
   const int strips = (a.N + kStrip - 1) / kStrip;
-  const int k = blockIdx.x * kThreads + threadIdx.x;
-  if (k >= a.K) return;
+  const int col = threadIdx.x & 63, q = threadIdx.x >> 6, k = blockIdx.x * 64 + col;
   float of_w_pre = 0, of_branch = 0;
-  for (int t = 0; t < strips; ++t) {
-    of_w_pre += a.row_sums[(int64_t)t * a.K + k];
-    of_branch += a.row_sums[(int64_t)(strips + t) * a.K + k];
+  if (k < a.K) {
+    for (int t = q; t < strips; t += 4) {
+      of_w_pre += a.row_sums[(int64_t)t * a.K + k];
+      of_branch += a.row_sums[(int64_t)(strips + t) * a.K + k];
+    }
+  }
+  part[0][q][col] = of_w_pre;
+  part[1][q][col] = of_branch;
+  __syncthreads();
+  if (q > 0 || k >= a.K) return;
+#pragma unroll
+  for (int t = 1; t < 4; ++t) {
+    of_w_pre += part[0][t][col];
+    of_branch += part[1][t][col];
   }
   if (a.dw_pre) a.dw_pre[k] = of_w_pre;
   if (a.dw_post) a.dw_post[k] = (a.gate ? a.gate[k] : 1.0f) * of_branch;
   if (a.dgate) a.dgate[k] = (a.w_post ? a.w_post[k] : 1.0f) * of_branch;
 }
 
+bool in_pieces(const void* p, int64_t ld) { return !p || rows_in_pieces(p, ld); }
+
 }  // namespace
 
-size_t block_norm_workspace_bytes(int K, int N) { return (size_t)2 * chunk_count(K) * N * sizeof(float); }
+size_t block_norm_workspace_bytes(int K, int N) { return (size_t)4 * chunk_count(K, N) * N * sizeof(float); }
 
 template <int DT>
 static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
+  if (a.N == 1 && a.ld_stream == 1 && (a.ld_block == 1 || (!a.y && !a.w_pre)) && a.K <= kVectorMost) {
+    Forward v = a;
+    v.vec_stream = in_pieces(a.x, 8) && in_pieces(a.h, 8);
+    v.vec_block = in_pieces(a.y, 8) && in_pieces(a.u, 8);
+    if (a.K <= 8 * kVectorThreads) block_norm_vector_kernel<DT, 1><<<1, kVectorThreads, 0, stream>>>(v);
+    else block_norm_vector_kernel<DT, 2><<<1, kVectorThreads, 0, stream>>>(v);
+    return hipGetLastError();
+  }
   const dim3 grid((uint32_t)(a.chunks * strip_count(a.N)));
-  if (a.w_post) block_norm_pass_kernel<DT, 0><<<grid, kThreads, 0, stream>>>(a);
-  if (a.w_pre) block_norm_pass_kernel<DT, 1><<<grid, kThreads, 0, stream>>>(a);
-  block_norm_pass_kernel<DT, 2><<<grid, kThreads, 0, stream>>>(a);
+  if (a.w_post || a.w_pre) block_norm_sums_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
+  block_norm_apply_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
-  Forward a{b.K, b.N, chunk_rows(b.K), chunk_count(b.K), b.residual_scale, b.eps,
+  Forward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale, b.eps,
             static_cast<const uint16_t*>(b.x), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
             static_cast<uint16_t*>(b.h), b.ld_stream, static_cast<uint16_t*>(b.u), b.ld_block, b.rstd_y, b.rstd_h,
-            b.workspace, b.workspace + (int64_t)chunk_count(b.K) * b.N, false, false};
-  a.vec_stream = rows_in_pieces(a.x, a.ld_stream) && (!a.h || rows_in_pieces(a.h, a.ld_stream));
-  a.vec_block = (!a.y || rows_in_pieces(a.y, a.ld_block)) && (!a.u || rows_in_pieces(a.u, a.ld_block));
+            b.workspace, false, false};
+  a.vec_stream = in_pieces(a.x, a.ld_stream) && in_pieces(a.h, a.ld_stream);
+  a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.u, a.ld_block);
   return b.dtype == HINM_F16 ? launch_forward<HINM_F16>(a, stream) : launch_forward<HINM_BF16>(a, stream);
 }
 
 size_t block_norm_grad_workspace_bytes(int K, int N) {
-  return ((size_t)4 * chunk_count(K) * N + (size_t)2 * strip_count(N) * K) * sizeof(float);
+  return ((size_t)4 * chunk_count(K, N) * N + (size_t)2 * strip_count(N) * K) * sizeof(float);
 }
 
 template <int DT>
 static hipError_t launch_backward(const Backward& a, hipStream_t stream) {
   const dim3 grid((uint32_t)(a.chunks * strip_count(a.N)));
   block_norm_grad_sums_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
-  block_norm_grad_rows_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
+  block_norm_grad_apply_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
   if (a.dw_pre || a.dw_post || a.dgate)
-    block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(a);
+    block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_block_norm_grad(const BlockNormGradArgs& b, hipStream_t stream) {
-  Backward a{b.K, b.N, chunk_rows(b.K), chunk_count(b.K), b.residual_scale, static_cast<const uint16_t*>(b.h),
-             static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre, b.rstd_y, b.rstd_h,
-             static_cast<const uint16_t*>(b.dh), static_cast<const uint16_t*>(b.du), static_cast<uint16_t*>(b.dx), b.ld_stream,
-             static_cast<uint16_t*>(b.dy), b.ld_block, b.dw_post, b.dgate, b.dtoken_gate, b.dw_pre,
-             b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K) * b.N, false, false};
-  auto in_pieces = [](const void* p, int64_t ld) { return !p || rows_in_pieces(p, ld); };
+  Backward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale,
+             static_cast<const uint16_t*>(b.h), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
+             b.rstd_y, b.rstd_h, static_cast<const uint16_t*>(b.dh), static_cast<const uint16_t*>(b.du),
+             static_cast<uint16_t*>(b.dx), b.ld_stream, static_cast<uint16_t*>(b.dy), b.ld_block, b.dw_post, b.dgate,
+             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N, false, false};
   a.vec_stream = in_pieces(a.h, a.ld_stream) && in_pieces(a.dh, a.ld_stream) && in_pieces(a.dx, a.ld_stream);
   a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.du, a.ld_block) && in_pieces(a.dy, a.ld_block);
   return b.dtype == HINM_F16 ? launch_backward<HINM_F16>(a, stream) : launch_backward<HINM_BF16>(a, stream);

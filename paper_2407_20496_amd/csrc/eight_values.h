@@ -9,10 +9,18 @@
 
 namespace hinm {
 
-// Eight consecutive 16-bit values; `valid` of them exist (the rest reads as zero), vec: the first is 16-byte aligned.
+// Eight consecutive 16-bit values; `valid` >= 1 of them exist, the rest reads as zero.  vec: the first is 16-byte aligned; then
+// all eight are read whenever one exists (an aligned piece lies in one page) and those beyond are cleared.
 __device__ __forceinline__ u32x4 load_eight(const uint16_t* p, int valid, bool vec) {
-  if (vec && valid >= 8) return *reinterpret_cast<const u32x4*>(p);
   u32x4 v = {0, 0, 0, 0};
+  if (vec) {
+    v = *reinterpret_cast<const u32x4*>(p);
+    if (valid < 8) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] &= valid >= 2 * j + 2 ? 0xffffffffu : valid == 2 * j + 1 ? 0xffffu : 0u;
+    }
+    return v;
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     if (j < valid) v[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
