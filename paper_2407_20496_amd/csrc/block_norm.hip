@@ -8,8 +8,12 @@
 //   sum h^2 = s^2 sum x^2 + 2 s r t sum x (c y) + (r t)^2 sum (c y)^2.
 // Where the three nearly cancel (a block whose output undoes its residual) that loses digits: a column whose sum is below
 // 1/16 of its two squares is added again from h itself.  The gradients' correction S = sum_k c y d is linear in the
-// gradient d in the same way.  (One launch with the columns held in registers: strips of 8 .. 32 columns draw 16 .. 64 bytes
-// of each line, and took 55 us at 4096x4096 where two launches take less.)
+// gradient d in the same way.
+//
+// Bound by memory: read twice (the second time from the caches behind L2 where they hold it), written once.  bf16, a channel
+// factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 24 against 14, 4096x8192
+// 78 against 56, 16384x1000 (rows that share lines) 51 against 27; gradients 4096x2048 60 against 21, 4096x8192 151 against
+// 84, 16384x1000 90 against 41.
 #include "eight_values.h"
 
 namespace hinm {
@@ -21,6 +25,8 @@ constexpr int kStrip = 64;                 // columns of a workgroup: eight lane
 constexpr int kRowsAtOnce = kThreads / 8;  // rows that its lanes cover together: a round
 constexpr int kRounds = 4;                 // rounds whose loads are in flight together
 constexpr int kPatch = kRounds * kRowsAtOnce;
+constexpr int kGradRounds = 2;             // ... of the gradients' four inputs
+constexpr int kGradPatch = kGradRounds * kRowsAtOnce;
 constexpr int kWaves = kThreads / 64;
 
 int strip_count(int N) { return (N + kStrip - 1) / kStrip; }
@@ -36,13 +42,19 @@ int chunk_count(int K, int N) {
   return (K + rows - 1) / rows;
 }
 
-// Which strip and chunk a workgroup has.  Chunks first: neighbouring workgroups take neighbouring columns of the same rows.
+// Which strip and chunk a workgroup has.  Workgroups go to the eight XCDs in turn.  Rows of whole cache lines: neighbouring
+// workgroups take neighbouring strips of the same rows.  Otherwise neighbouring strips share lines and each XCD takes a
+// contiguous run of the list (chunk, strip), so that the parts of a line meet in one L2 (16384x1000: 68 -> 48 us; at
+// 4096x8192, whole lines, the run costs 87 -> 100 us).  Whole lines are also written around the caches, where the partial
+// ones wait for their other half (16384x4096: 187 -> 141 us; 11008x1571, partial lines, 67 -> 80 us).
 struct Place {
   int n0, n, left, row0, rows, chunk, strip;  // first column; this lane's first column, how many it has; rows of the chunk
-  __device__ __forceinline__ Place(int K, int N, int rows_per_chunk) {
+  __device__ __forceinline__ bool none() const { return rows <= 0; }  // beyond the list
+  __device__ __forceinline__ Place(int K, int N, int rows_per_chunk, bool whole_lines) {
     const int strips = (N + kStrip - 1) / kStrip;
-    chunk = blockIdx.x / strips;
-    strip = blockIdx.x - chunk * strips;
+    const int item = whole_lines ? (int)blockIdx.x : (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+    chunk = item / strips;
+    strip = item - chunk * strips;
     n0 = strip * kStrip;
     n = n0 + 8 * (threadIdx.x & 7);
     left = min(8, N - n);
@@ -128,12 +140,17 @@ struct Forward {
   int64_t ld_block;
   float *rstd_y, *rstd_h;
   float* sums;  // [4][chunks][N]: y^2, x^2, x c y, (c y)^2
-  bool vec_stream, vec_block;
+  bool vec_stream, vec_block, whole_lines;
 };
 
-// kRounds rows of x and y of a lane's columns, from row k on in steps of a round
+__device__ __forceinline__ float channel_factor(const float* w_post, const float* gate, int k) {
+  return (w_post ? w_post[k] : 1.0f) * (gate ? gate[k] : 1.0f);
+}
+
+// kRounds rows of x and y of a lane's columns, from row k on in steps of a round, with their channels' factors
 struct PatchXY {
   u32x4 x[kRounds], y[kRounds];
+  float c[kRounds], w[kRounds];  // gate w_post; w_pre
 };
 __device__ __forceinline__ void load_patch(const Forward& a, const Place& p, int k, int end, PatchXY& v) {
   const u32x4 none = {0, 0, 0, 0};
@@ -144,14 +161,18 @@ __device__ __forceinline__ void load_patch(const Forward& a, const Place& p, int
     v.x[i] = in ? load_eight(a.x + (int64_t)r * a.ld_stream + p.n, p.left, a.vec_stream) : none;
     v.y[i] = in && a.y ? load_eight(a.y + (int64_t)r * a.ld_block + p.n, p.left, a.vec_block) : none;
   }
-}
-__device__ __forceinline__ float channel_factor(const float* w_post, const float* gate, int k) {
-  return (w_post ? w_post[k] : 1.0f) * (gate ? gate[k] : 1.0f);
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const int r = k + i * kRowsAtOnce;
+    v.c[i] = r < end ? channel_factor(a.w_post, a.gate, r) : 0.0f;
+    v.w[i] = r < end && a.w_pre ? a.w_pre[r] : 0.0f;
+  }
 }
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
-  const Place p(a.K, a.N, a.rows_per_chunk);
+  const Place p(a.K, a.N, a.rows_per_chunk, a.whole_lines);
+  if (p.none()) return;
   float sum[4][8] = {};
   const int end = p.row0 + p.rows;
   for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kPatch) {
@@ -159,8 +180,6 @@ __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
     load_patch(a, p, k, end, v);
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
-      const int r = k + i * kRowsAtOnce;
-      const float c = r < end ? channel_factor(a.w_post, a.gate, r) : 0.0f;
       float x[8], y[8];
       widen<DT>(v.x[i], x);
       widen<DT>(v.y[i], y);
@@ -168,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
       for (int j = 0; j < 8; ++j) {
         sum[0][j] += y[j] * y[j];
         sum[1][j] += x[j] * x[j];
-        const float b = c * y[j];
+        const float b = v.c[i] * y[j];
         sum[2][j] += x[j] * b;
         sum[3][j] += b * b;
       }
@@ -191,11 +210,12 @@ __device__ __forceinline__ void row_of_h(const Forward& a, u32x4 x, u32x4 y, flo
   for (int j = 0; j < 8; ++j) h[j] = h[j] * a.scale + branch[j] * (c * v[j]);
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void block_norm_apply_kernel(Forward a) {
+template <int DT, bool LINES>
+__global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a) {
   __shared__ float total[4][kStrip], branch[kStrip], root[kStrip], again[kWaves][kStrip];
   __shared__ int cancelled;
-  const Place p(a.K, a.N, a.rows_per_chunk);
+  const Place p(a.K, a.N, a.rows_per_chunk, LINES);
+  if (p.none()) return;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchXY v;
   load_patch(a, p, first, end, v);  // on their way while the sums are added
@@ -233,9 +253,8 @@ __global__ __launch_bounds__(kThreads) void block_norm_apply_kernel(Forward a) {
       load_patch(a, p, k, a.K, w);
 #pragma unroll
       for (int i = 0; i < kRounds; ++i) {
-        const int r = k + i * kRowsAtOnce;
         float h[8];
-        row_of_h<DT>(a, w.x[i], w.y[i], r < a.K ? channel_factor(a.w_post, a.gate, r) : 0.0f, of_token, h);
+        row_of_h<DT>(a, w.x[i], w.y[i], w.c[i], of_token, h);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += h[j] * h[j];
       }
@@ -269,16 +288,109 @@ __global__ __launch_bounds__(kThreads) void block_norm_apply_kernel(Forward a) {
       const int r = k + i * kRowsAtOnce;
       if (r >= end) break;
       float h[8];
-      row_of_h<DT>(a, v.x[i], v.y[i], channel_factor(a.w_post, a.gate, r), of_token, h);
-      if (a.h) store_eight(a.h + (int64_t)r * a.ld_stream + p.n, narrow<DT>(h), p.left, a.vec_stream);
+      row_of_h<DT>(a, v.x[i], v.y[i], v.c[i], of_token, h);
+      if (a.h) store_eight<LINES>(a.h + (int64_t)r * a.ld_stream + p.n, narrow<DT>(h), p.left, a.vec_stream);
       if (a.w_pre) {
-        const float w = a.w_pre[r];
+        const float w = v.w[i];
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] *= w * of_u[j];
-        store_eight(a.u + (int64_t)r * a.ld_block + p.n, narrow<DT>(h), p.left, a.vec_block);
+        store_eight<LINES>(a.u + (int64_t)r * a.ld_block + p.n, narrow<DT>(h), p.left, a.vec_block);
       }
     }
     v = next;
+  }
+}
+
+// Few channels, or a few tokens: one launch.  A workgroup of 512 threads owns eight columns, a row a lane, and holds x and y of
+// all their rows in registers (ROUNDS rows a thread) through both sums.  It draws 16 bytes of each line, so it loses where
+// there is much to draw (4096 channels: 8 tokens 10 us against 14.5 in two launches, 64 tokens 20 against 14; 1024 channels:
+// 2048 tokens 10.6 against 12.8, 4096 tokens 16.7 against 14.8).
+constexpr int kHeldThreads = 512;
+
+// Reciprocal roots of eight columns from every thread's sums of squares.
+__device__ __forceinline__ void held_roots(float (&sum)[8], float (*by_wave)[8], float* root, const Forward& a, int n0, float* out) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+#pragma unroll
+    for (int q = 1; q < 8; q *= 2) sum[j] += __shfl_xor(sum[j], q);
+    sum[j] = add_lanes_by_8(sum[j]);
+  }
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) by_wave[threadIdx.x >> 6][j] = sum[j];
+  }
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    float t = 0;
+#pragma unroll
+    for (int w = 0; w < kHeldThreads / 64; ++w) t += by_wave[w][threadIdx.x];
+    const float r = 1.0f / sqrtf(t / (float)a.K + a.eps);
+    root[threadIdx.x] = r;
+    if (out && n0 + (int)threadIdx.x < a.N) out[n0 + threadIdx.x] = r;
+  }
+  __syncthreads();
+}
+
+template <int DT, int ROUNDS>
+__global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a) {
+  __shared__ float by_wave[kHeldThreads / 64][8], root[8];
+  // neighbouring columns, which share lines, on one XCD
+  const int n = 8 * ((int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3)), left = min(8, a.N - n);
+  if (left <= 0) return;
+  const u32x4 none = {0, 0, 0, 0};
+  u32x4 x[ROUNDS], y[ROUNDS];
+  float c[ROUNDS], w[ROUNDS];
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = threadIdx.x + i * kHeldThreads;
+    const bool in = k < a.K;
+    x[i] = in ? load_eight(a.x + (int64_t)k * a.ld_stream + n, left, a.vec_stream) : none;
+    y[i] = in && a.y ? load_eight(a.y + (int64_t)k * a.ld_block + n, left, a.vec_block) : none;
+    c[i] = in ? channel_factor(a.w_post, a.gate, k) : 0.0f;
+    w[i] = in && a.w_pre ? a.w_pre[k] : 0.0f;
+  }
+  float of_token[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) of_token[j] = a.token_gate && j < left ? a.token_gate[n + j] : 1.0f;
+  float sum[8] = {};
+  if (a.w_post) {
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      float v[8];
+      widen<DT>(y[i], v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[j] * v[j];
+    }
+    held_roots(sum, by_wave, root, a, n, a.rstd_y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) of_token[j] *= root[j];
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[j] = 0;
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = threadIdx.x + i * kHeldThreads;
+    if (k >= a.K) break;
+    float h[8];
+    row_of_h<DT>(a, x[i], y[i], c[i], of_token, h);
+    if (a.h) store_eight(a.h + (int64_t)k * a.ld_stream + n, narrow<DT>(h), left, a.vec_stream);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += h[j] * h[j];
+  }
+  if (!a.w_pre) return;
+  held_roots(sum, by_wave, root, a, n, a.rstd_h);
+  float of_u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) of_u[j] = root[j];
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = threadIdx.x + i * kHeldThreads;
+    if (k >= a.K) break;
+    float h[8];
+    row_of_h<DT>(a, x[i], y[i], c[i], of_token, h);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] *= w[i] * of_u[j];
+    store_eight(a.u + (int64_t)k * a.ld_block + n, narrow<DT>(h), left, a.vec_block);
   }
 }
 
@@ -288,7 +400,8 @@ constexpr int kVectorMost = 2 * 8 * kVectorThreads;
 
 __device__ __forceinline__ float add_workgroup(float v, float* by_wave) {
 #pragma unroll
-  for (int q = 1; q < 64; q *= 2) v += __shfl_xor(v, q);
+  for (int q = 1; q < 8; q *= 2) v += __shfl_xor(v, q);
+  v = add_lanes_by_8(v);
   if ((threadIdx.x & 63) == 0) by_wave[threadIdx.x >> 6] = v;
   __syncthreads();
   float t = 0;
@@ -298,6 +411,15 @@ __device__ __forceinline__ float add_workgroup(float v, float* by_wave) {
 }
 // eight floats from k on, `valid` of them (the rest: zero); absent: ones
 __device__ __forceinline__ void load_factors(const float* p, int k, int valid, float (&f)[8]) {
+  if (p && valid >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    const f32x4 low = *reinterpret_cast<const f32x4*>(p + k), high = *reinterpret_cast<const f32x4*>(p + k + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f[j] = low[j];
+      f[4 + j] = high[j];
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) f[j] = p ? (j < valid ? p[k + j] : 0.0f) : 1.0f;
 }
@@ -376,16 +498,17 @@ struct Backward {
   float *dw_post, *dgate, *dtoken_gate, *dw_pre;
   float* sums;      // [4][chunks][N]
   float* row_sums;  // [2][strips][K]
-  bool vec_stream, vec_block;
+  bool vec_stream, vec_block, whole_lines;
 };
 
 struct PatchGrad {
-  u32x4 h[kRounds], dh[kRounds], du[kRounds], y[kRounds];
+  u32x4 h[kGradRounds], dh[kGradRounds], du[kGradRounds], y[kGradRounds];
+  float c[kGradRounds], w[kGradRounds];
 };
 __device__ __forceinline__ void load_patch(const Backward& a, const Place& p, int k, int end, PatchGrad& v) {
   const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < kRounds; ++i) {
+  for (int i = 0; i < kGradRounds; ++i) {
     const int r = k + i * kRowsAtOnce;
     const bool in = r < end && p.left > 0;
     const int64_t stream = (int64_t)r * a.ld_stream + p.n, block = (int64_t)r * a.ld_block + p.n;
@@ -394,20 +517,25 @@ __device__ __forceinline__ void load_patch(const Backward& a, const Place& p, in
     v.du[i] = in && a.w_pre ? load_eight(a.du + block, p.left, a.vec_block) : none;
     v.y[i] = in && a.y ? load_eight(a.y + block, p.left, a.vec_block) : none;
   }
+#pragma unroll
+  for (int i = 0; i < kGradRounds; ++i) {
+    const int r = k + i * kRowsAtOnce;
+    v.c[i] = r < end ? channel_factor(a.w_post, a.gate, r) : 0.0f;
+    v.w[i] = r < end && a.w_pre ? a.w_pre[r] : 0.0f;
+  }
 }
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward a) {
-  const Place p(a.K, a.N, a.rows_per_chunk);
+  const Place p(a.K, a.N, a.rows_per_chunk, a.whole_lines);
+  if (p.none()) return;
   float sum[4][8] = {};
   const int end = p.row0 + p.rows;
-  for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kPatch) {
+  for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kGradPatch) {
     PatchGrad v;
     load_patch(a, p, k, end, v);
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
-      const int r = k + i * kRowsAtOnce;
-      const float w = r < end && a.w_pre ? a.w_pre[r] : 0.0f, c = r < end ? channel_factor(a.w_post, a.gate, r) : 0.0f;
+    for (int i = 0; i < kGradRounds; ++i) {
       float h[8], dh[8], g[8], y[8];
       widen<DT>(v.h[i], h);
       widen<DT>(v.dh[i], dh);
@@ -415,8 +543,8 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward
       widen<DT>(v.y[i], y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        g[j] *= w;
-        y[j] *= c;
+        g[j] *= v.w[i];
+        y[j] *= v.c[i];
         sum[0][j] += g[j] * h[j];
         sum[1][j] += y[j] * dh[j];
         sum[2][j] += y[j] * g[j];
@@ -427,10 +555,11 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward
   store_sums<4>(sum, p, a.sums, a.chunks, a.N);
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void block_norm_grad_apply_kernel(Backward a) {
+template <int DT, bool LINES>
+__global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Backward a) {
   __shared__ float total[4][kStrip], first_of[kStrip], second_of[kStrip];  // corrections: rstd_h^3 s1 / K; rstd_y^2 S / K
-  const Place p(a.K, a.N, a.rows_per_chunk);
+  const Place p(a.K, a.N, a.rows_per_chunk, LINES);
+  if (p.none()) return;
   const int strips = (a.N + kStrip - 1) / kStrip;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchGrad v;
@@ -465,14 +594,13 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_apply_kernel(Backwar
     f2[j] = second_of[at + j];
   }
   // whole patches: the lanes of a row add their columns together
-  for (int k = first; k - first < p.rows; k += kPatch) {
+  for (int k = first; k - first < p.rows; k += kGradPatch) {
     PatchGrad next;
-    if (k - first + kPatch < p.rows) load_patch(a, p, k + kPatch, end, next);
+    if (k - first + kGradPatch < p.rows) load_patch(a, p, k + kGradPatch, end, next);
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i) {
+    for (int i = 0; i < kGradRounds; ++i) {
       const int r = k + i * kRowsAtOnce;
       const bool in = r < end;
-      const float w = in && a.w_pre ? a.w_pre[r] : 0.0f, c = in ? channel_factor(a.w_post, a.gate, r) : 0.0f;
       float h[8], dh[8], g[8], y[8], of_w_pre = 0, of_branch = 0;
       widen<DT>(v.h[i], h);
       widen<DT>(v.dh[i], dh);
@@ -481,14 +609,14 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_apply_kernel(Backwar
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         of_w_pre += g[j] * h[j] * rh[j];
-        const float d = dh[j] + w * g[j] * rh[j] - h[j] * f1[j];
+        const float d = dh[j] + v.w[i] * g[j] * rh[j] - h[j] * f1[j];
         of_branch += d * y[j] * token[j];
         dh[j] = a.scale * d;
-        y[j] = token[j] * (c * d - y[j] * f2[j]);
+        y[j] = token[j] * (v.c[i] * d - y[j] * f2[j]);
       }
       if (in && p.left > 0) {
-        if (a.dx) store_eight(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left, a.vec_stream);
-        if (a.dy) store_eight(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left, a.vec_block);
+        if (a.dx) store_eight<LINES>(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left, a.vec_stream);
+        if (a.dy) store_eight<LINES>(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left, a.vec_block);
       }
 #pragma unroll
       for (int q = 1; q < 8; q *= 2) {
@@ -531,6 +659,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
 }
 
 bool in_pieces(const void* p, int64_t ld) { return !p || rows_in_pieces(p, ld); }
+bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld % 64 == 0); }
 
 }  // namespace
 
@@ -546,9 +675,19 @@ static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
     else block_norm_vector_kernel<DT, 2><<<1, kVectorThreads, 0, stream>>>(v);
     return hipGetLastError();
   }
-  const dim3 grid((uint32_t)(a.chunks * strip_count(a.N)));
+  const dim3 held((uint32_t)(((a.N + 7) / 8 + 7) / 8 * 8));
+  if (a.K <= 2 * kHeldThreads && (int64_t)a.K * a.N <= 3 << 20) {
+    block_norm_held_kernel<DT, 2><<<held, kHeldThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  if (a.K <= 8 * kHeldThreads && a.N <= 16) {
+    block_norm_held_kernel<DT, 8><<<held, kHeldThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
   if (a.w_post || a.w_pre) block_norm_sums_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
-  block_norm_apply_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
+  if (a.whole_lines) block_norm_apply_kernel<DT, true><<<grid, kThreads, 0, stream>>>(a);
+  else block_norm_apply_kernel<DT, false><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -556,9 +695,10 @@ hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
   Forward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale, b.eps,
             static_cast<const uint16_t*>(b.x), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
             static_cast<uint16_t*>(b.h), b.ld_stream, static_cast<uint16_t*>(b.u), b.ld_block, b.rstd_y, b.rstd_h,
-            b.workspace, false, false};
+            b.workspace, false, false, false};
   a.vec_stream = in_pieces(a.x, a.ld_stream) && in_pieces(a.h, a.ld_stream);
   a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.u, a.ld_block);
+  a.whole_lines = in_lines(a.x, a.ld_stream) && in_lines(a.h, a.ld_stream) && in_lines(a.y, a.ld_block) && in_lines(a.u, a.ld_block);
   return b.dtype == HINM_F16 ? launch_forward<HINM_F16>(a, stream) : launch_forward<HINM_BF16>(a, stream);
 }
 
@@ -568,9 +708,10 @@ size_t block_norm_grad_workspace_bytes(int K, int N) {
 
 template <int DT>
 static hipError_t launch_backward(const Backward& a, hipStream_t stream) {
-  const dim3 grid((uint32_t)(a.chunks * strip_count(a.N)));
+  const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
   block_norm_grad_sums_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
-  block_norm_grad_apply_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
+  if (a.whole_lines) block_norm_grad_apply_kernel<DT, true><<<grid, kThreads, 0, stream>>>(a);
+  else block_norm_grad_apply_kernel<DT, false><<<grid, kThreads, 0, stream>>>(a);
   if (a.dw_pre || a.dw_post || a.dgate)
     block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
@@ -581,9 +722,11 @@ hipError_t launch_block_norm_grad(const BlockNormGradArgs& b, hipStream_t stream
              static_cast<const uint16_t*>(b.h), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
              b.rstd_y, b.rstd_h, static_cast<const uint16_t*>(b.dh), static_cast<const uint16_t*>(b.du),
              static_cast<uint16_t*>(b.dx), b.ld_stream, static_cast<uint16_t*>(b.dy), b.ld_block, b.dw_post, b.dgate,
-             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N, false, false};
+             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N, false, false, false};
   a.vec_stream = in_pieces(a.h, a.ld_stream) && in_pieces(a.dh, a.ld_stream) && in_pieces(a.dx, a.ld_stream);
   a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.du, a.ld_block) && in_pieces(a.dy, a.ld_block);
+  a.whole_lines = in_lines(a.h, a.ld_stream) && in_lines(a.dh, a.ld_stream) && in_lines(a.dx, a.ld_stream) &&
+                  in_lines(a.y, a.ld_block) && in_lines(a.du, a.ld_block) && in_lines(a.dy, a.ld_block);
   return b.dtype == HINM_F16 ? launch_backward<HINM_F16>(a, stream) : launch_backward<HINM_BF16>(a, stream);
 }
 

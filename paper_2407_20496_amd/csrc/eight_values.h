@@ -26,9 +26,21 @@ __device__ __forceinline__ u32x4 load_eight(const uint16_t* p, int valid, bool v
     if (j < valid) v[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
   return v;
 }
+// PAST: whole pieces go around the caches (for rows of whole cache lines).  A template parameter: of two stores that differ in
+// this alone the compiler keeps one.
+template <bool PAST = false>
 __device__ __forceinline__ void store_eight(uint16_t* p, u32x4 v, int valid, bool vec) {
   if (vec && valid >= 8) {
-    *reinterpret_cast<u32x4*>(p) = v;
+    if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = v;
+    return;
+  }
+  if (vec) {  // a row's end: pairs, and the last one if it has none
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (valid >= 2 * j + 2) reinterpret_cast<uint32_t*>(p)[j] = v[j];
+      else if (valid == 2 * j + 1) p[2 * j] = (uint16_t)v[j];
+    }
     return;
   }
 #pragma unroll

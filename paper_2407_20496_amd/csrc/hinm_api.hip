@@ -739,11 +739,11 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
   uint8_t* x_codes = static_cast<uint8_t*>(workspace);
   uint8_t* x_scales = x_codes + p.codes;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = launch_mx4_quantize(K, N, dtype, X, ldx, true, x_codes, x_scales, s);
-  if (e != hipSuccess) return HINM_ERR_DEVICE;
   const Mx4ProductArgs a{M, N, K, dtype, codes, scales, x_codes, x_scales, Y, ldy, (flags & HINM_EPI_RELU) != 0,
                          (flags & HINM_OUT_F32) != 0};
-  return launched(launch_mx4_product(a, s));
+  if (N == 1) return launched(launch_mx4_token(a, X, ldx, s));
+  const hipError_t e = launch_mx4_quantize(K, N, dtype, X, ldx, true, x_codes, x_scales, s);
+  return launched(e == hipSuccess ? launch_mx4_product(a, s) : e);
 }
 
 hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {

@@ -67,4 +67,10 @@ __device__ __forceinline__ float mx4_scale_value(uint32_t e) {
   return __builtin_bit_cast(float, e == 255 ? 0x7fc00000u : e == 0 ? 0x00400000u : e << 23);
 }
 
+// ... of both halves with those of another lane of the row of 16, which the control word names.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with_lane(uint32_t m) {
+  return max_halves(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, CTRL, 0xf, 0xf, true));
+}
+
 }  // namespace hinm

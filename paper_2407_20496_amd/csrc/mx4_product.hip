@@ -15,9 +15,9 @@ __device__ __forceinline__ i32x8 operand(u32x4 v) {
   return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
 }
 constexpr int kFp4 = 4;  // operand format code of 4-bit values
-template <int BYTE>
+template <int BYTE_A, int BYTE_B = BYTE_A>
 __device__ __forceinline__ f32x16 mfma_32x32x64(u32x4 a, uint32_t a_scale, u32x4 b, uint32_t b_scale, f32x16 c) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, kFp4, kFp4, BYTE, (int)a_scale, BYTE,
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, kFp4, kFp4, BYTE_A, (int)a_scale, BYTE_B,
                                                          (int)b_scale);
 }
 
@@ -213,6 +213,99 @@ hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStre
   mx4_stream_kernel<OUT, WM, WN, WAVES><<<dim3(grid_of_items(items)), 64 * WAVES, 0, stream>>>(a.a_codes, a.a_scales, a.b_codes,
                                                                                              a.b_scales, a.Y, p);
   return hipGetLastError();
+}
+
+// ---- one token, quantised on the way ---------------------------------------------------------------------
+// The form above for 32 rows of A, eight waves and one row of B that comes as 16-bit values: a wave quantises the line it is
+// about to multiply, four values a lane, and passes the codes through LDS to the two lanes that hold the row.  One launch
+// where quantising apart takes two; sums in the same order, so the same result bit for bit.
+template <int OUT, int DT>
+__global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, const uint8_t* scales, const uint16_t* x, int64_t ldx,
+                                                        bool vec, void* Y, ProductShape p) {
+  constexpr int kWaves = 8, kLinePlace = 8 * 16 + 16;  // a line's codes and its eight scale bytes
+  __shared__ __align__(16) uint8_t places[kWaves][kLinePlace + 16];  // ... and zeros
+  __shared__ __align__(16) float sums[kWaves][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blocks = mx4_row_blocks(p.M), block = item_of_workgroup(blocks);
+  if (block < 0) return;
+  const int half = lane >> 5, r = lane & 31, lines = mx4_lines(p.K);
+  uint8_t* const place = places[wave];
+  struct Line {
+    u32x4 a[4];
+    u32x2 scale_a, x;
+  };
+  auto load_line = [&](int line, Line& f) {
+    const uint8_t* c = codes + mx4_codes_at(line, blocks, block) + 16 * lane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f.a[q] = *reinterpret_cast<const u32x4*>(c + 1024 * q);
+    f.scale_a = *reinterpret_cast<const u32x2*>(scales + mx4_scales_at(line >> 1, blocks, block) + 16 * r + 8 * half);
+    const int k = line * kMx4Line + 4 * lane;
+    f.x = u32x2{0, 0};
+    if (vec && k + 4 <= p.K) {
+      f.x = *reinterpret_cast<const u32x2*>(x + k);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k + j < p.K) f.x[j >> 1] |= (uint32_t)x[(k + j) * ldx] << (16 * (j & 1));
+    }
+  };
+  f32x16 acc;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) acc[q] = 0;
+  auto multiply = [&](int line, const Line& f) {
+    uint32_t m = max_halves(f.x[0] & 0x7fff7fffu, f.x[1] & 0x7fff7fffu);
+    m = max_with_lane<0xB1>(m);   // lane ^ 1
+    m = max_with_lane<0x4E>(m);   // lane ^ 2
+    m = max_with_lane<0x141>(m);  // the other four of eight
+    m = max_halves(m, m >> 16) & 0xffffu;
+    const uint32_t e = mx4_scale_of<DT>(m);
+    const float s = mx4_inverse_scale(e);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, low_half<DT>(f.x[0]) * s, high_half<DT>(f.x[0]) * s, 1.0f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, low_half<DT>(f.x[1]) * s, high_half<DT>(f.x[1]) * s, 1.0f, 1);
+    if (e == 255) c = 0;
+    // LDS operations of a wave are done in order; the compiler is held to it
+    *reinterpret_cast<uint16_t*>(place + 2 * lane) = (uint16_t)c;
+    if ((lane & 7) == 0) place[128 + (lane >> 3)] = (uint8_t)e;
+    asm volatile("" ::: "memory");
+    u32x4 b[4];
+    uint32_t scale_b[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int of = 4 * (q >> 1) + 2 * half + (q & 1);
+      b[q] = *reinterpret_cast<const u32x4*>(place + (r == 0 ? 16 * of : kLinePlace));
+      scale_b[q] = place[128 + of];
+    }
+    asm volatile("" ::: "memory");
+    const uint32_t down = 16 * (line & 1);
+    const u32x2 scale_a = {f.scale_a[0] >> down, f.scale_a[1] >> down};
+    acc = mfma_32x32x64<0, 0>(b[0], scale_b[0], f.a[0], scale_a[0], acc);
+    acc = mfma_32x32x64<0, 0>(b[1], scale_b[1], f.a[1], scale_a[1], acc);
+    acc = mfma_32x32x64<0, 1>(b[2], scale_b[2], f.a[2], scale_a[0], acc);
+    acc = mfma_32x32x64<0, 1>(b[3], scale_b[3], f.a[3], scale_a[1], acc);
+  };
+  if (lane < 4) *reinterpret_cast<uint32_t*>(place + kLinePlace + 4 * lane) = 0;
+  Line f;
+  if (wave < lines) {
+    load_line(wave, f);
+    int line = wave;
+    for (; line + kWaves < lines; line += kWaves) {
+      Line next;
+      load_line(line + kWaves, next);
+      multiply(line, f);
+      f = next;
+    }
+    multiply(line, f);
+  }
+  // D: row 0 is register 0 of the lower lanes, lane l column l of D = row l of A
+  if (half == 0) sums[wave][r] = acc[0];
+  __syncthreads();
+  const int m = 32 * block + (int)threadIdx.x;
+  if (threadIdx.x >= 32 || m >= p.M) return;
+  float v = sums[0][threadIdx.x];
+  const int count = min(kWaves, lines);
+  for (int w = 1; w < count; ++w) v += sums[w][threadIdx.x];
+  store_four<OUT>(Y, (int64_t)m * p.ldy, 0, f32x4{v, 0, 0, 0}, p, false);
 }
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
@@ -456,7 +549,7 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
         else *reinterpret_cast<u32x2*>(to) = u32x2{floats_to_bits<OUT>(v[0], v[1]), floats_to_bits<OUT>(v[2], v[3])};
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");  // LDS operations of a wave are done in order; the compiler is held to it
     constexpr int kPieces = kRowBytes / 16;
 #pragma unroll
     for (int c = 0; c < 32 * kPieces / 64; ++c) {
@@ -476,7 +569,7 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
         }
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
   }
 }
 
@@ -530,8 +623,8 @@ double estimate_us(const Form& f, const ProductShape& p) {
 template <int OUT>
 hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  int best = 0;
-  for (int i = 1; i < (int)(sizeof kForms / sizeof kForms[0]); ++i)
+  int best = 0;  // one column: as mx4_token_kernel adds it
+  for (int i = 1; a.N > 1 && i < (int)(sizeof kForms / sizeof kForms[0]); ++i)
     if (estimate_us(kForms[i], p) < estimate_us(kForms[best], p)) best = i;
   switch (best) {
     case 0: return launch_stream<OUT, 1, 1, 8>(a, p, stream);
@@ -544,11 +637,26 @@ hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   }
 }
 
+template <int OUT, int DT>
+hipError_t launch_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
+  const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
+  const bool vec = ldx == 1 && (reinterpret_cast<uintptr_t>(x) & 7) == 0;
+  mx4_token_kernel<OUT, DT><<<dim3(grid_of_items(mx4_row_blocks(a.M))), 512, 0, stream>>>(
+      a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, vec, a.Y, p);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream) {
   if (a.out_f32) return launch_out<2>(a, stream);
   return a.dtype == HINM_F16 ? launch_out<HINM_F16>(a, stream) : launch_out<HINM_BF16>(a, stream);
+}
+
+hipError_t launch_mx4_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
+  if (a.dtype == HINM_F16)
+    return a.out_f32 ? launch_token<2, HINM_F16>(a, x, ldx, stream) : launch_token<HINM_F16, HINM_F16>(a, x, ldx, stream);
+  return a.out_f32 ? launch_token<2, HINM_BF16>(a, x, ldx, stream) : launch_token<HINM_BF16, HINM_BF16>(a, x, ldx, stream);
 }
 
 }  // namespace hinm

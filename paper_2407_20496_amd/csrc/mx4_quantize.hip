@@ -14,11 +14,6 @@ constexpr int kThreads = 256;
 // the pad all of them would fall on the same banks.
 constexpr int kChunkPitch = 512 + 16;
 
-template <int CTRL>
-__device__ __forceinline__ uint32_t max_with_lane(uint32_t m) {
-  return max_halves(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, CTRL, 0xf, 0xf, true));
-}
-
 // Byte of an LDS tile that holds block j = 0..15 (512 values) of row r in a block of rows.
 __device__ __forceinline__ int lds_place(int j, int r) { return (8 * (j >> 3) + mx4_chunk_of(j & 7)) * kChunkPitch + 16 * r; }
 
