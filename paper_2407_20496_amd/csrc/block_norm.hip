@@ -639,6 +639,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
   const int col = threadIdx.x & 63, q = threadIdx.x >> 6, k = blockIdx.x * 64 + col;
   float of_w_pre = 0, of_branch = 0;
   if (k < a.K) {
+#pragma unroll 8
     for (int t = q; t < strips; t += 4) {
       of_w_pre += a.row_sums[(int64_t)t * a.K + k];
       of_branch += a.row_sums[(int64_t)(strips + t) * a.K + k];

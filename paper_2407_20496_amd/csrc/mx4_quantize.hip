@@ -14,30 +14,36 @@ constexpr int kThreads = 256;
 // the pad all of them would fall on the same banks.
 constexpr int kChunkPitch = 512 + 16;
 
-// Byte of an LDS tile that holds block j = 0..15 (512 values) of row r in a block of rows.
-__device__ __forceinline__ int lds_place(int j, int r) { return (8 * (j >> 3) + mx4_chunk_of(j & 7)) * kChunkPitch + 16 * r; }
+// Workgroups that share cache lines of the source (rows that do not begin at multiples of 128 bytes) run on one XCD, in
+// contiguous runs of the list; otherwise neighbours of the list run side by side.
+__device__ __forceinline__ int item_of_workgroup(bool whole_lines) {
+  return whole_lines ? (int)blockIdx.x : (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+}
 
 // ---- blocks along the rows --------------------------------------------------------------------------
-// A workgroup takes 32 rows x 512 values, a wave eight rows: eight loads of one contiguous kilobyte each, all in flight
-// together; a lane holds eight values, four lanes a block.
+// A workgroup takes 32 rows x 256 values, a line of a block of rows; a wave eight rows in four loads of two rows each, a lane
+// eight values, four lanes a block.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src, int64_t ld, int rows, int cols, bool vec,
-                                                            uint8_t* codes, uint8_t* scales) {
-  __shared__ __align__(16) uint8_t tile[16 * kChunkPitch];
-  __shared__ __align__(16) uint8_t tile_scales[kMx4Rows * 16];
+                                                            bool whole_lines, uint8_t* codes, uint8_t* scales) {
+  __shared__ __align__(16) uint8_t tile[8 * kChunkPitch];
+  __shared__ __align__(16) uint8_t tile_scales[kMx4Rows][8];  // byte 2 (p % 4) + p / 4 of block p
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int groups = mx4_groups(cols), blocks = mx4_row_blocks(rows);
-  const int rb = blockIdx.x / groups, g = blockIdx.x - rb * groups;
-  const int k = g * kMx4Group + 8 * lane, r0 = 8 * wave;
-  const int count = min(8, rows - rb * kMx4Rows - r0);  // this wave's rows
-  u32x4 v[8];
+  const int lines = mx4_lines(cols), blocks = mx4_row_blocks(rows);
+  const int item = item_of_workgroup(whole_lines);
+  const int rb = item / lines, line = item - rb * lines;
+  if (rb >= blocks) return;
+  const int in_line = 8 * (lane & 31), k = line * kMx4Line + in_line, p = in_line >> 5;
+  u32x4 v[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    v[i] = i < count && k < cols ? load_eight(src + (int64_t)(rb * kMx4Rows + r0 + i) * ld + k, cols - k, vec) : u32x4{0, 0, 0, 0};
+  for (int i = 0; i < 4; ++i) {
+    const int r = rb * kMx4Rows + 8 * wave + 2 * i + (lane >> 5);
+    v[i] = r < rows && k < cols ? load_eight(src + (int64_t)r * ld + k, cols - k, vec) : u32x4{0, 0, 0, 0};
+  }
   const bool beyond = (k & ~31) >= cols;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i >= count) break;
+  for (int i = 0; i < 4; ++i) {
+    const int r = 8 * wave + 2 * i + (lane >> 5);
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) m = max_halves(m, v[i][j] & 0x7fff7fffu);
@@ -52,91 +58,88 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src,
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, low_half<DT>(v[i][2]) * s, high_half<DT>(v[i][2]) * s, 1.0f, 2);
     c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, low_half<DT>(v[i][3]) * s, high_half<DT>(v[i][3]) * s, 1.0f, 3);
     if (e == 255) c = 0;
-    *reinterpret_cast<uint32_t*>(tile + lds_place(lane >> 2, r0 + i) + 4 * (lane & 3)) = c;
-    if ((lane & 3) == 0) tile_scales[16 * (r0 + i) + mx4_scale_place(lane >> 2)] = (uint8_t)(beyond ? 127 : e);
+    *reinterpret_cast<uint32_t*>(tile + mx4_chunk_of(p) * kChunkPitch + 16 * r + 4 * (lane & 3)) = c;
+    if ((lane & 3) == 0) tile_scales[r][2 * (p & 3) + (p >> 2)] = (uint8_t)(beyond ? 127 : e);
   }
   __syncthreads();
-  const int here = min(kMx4Rows, rows - rb * kMx4Rows), chunk = threadIdx.x >> 5, r = threadIdx.x & 31;
+  const int here = min(kMx4Rows, rows - rb * kMx4Rows), r = threadIdx.x & 31;
   if (r >= here) return;
-#pragma unroll
-  for (int q = 0; q < 2; ++q)
-    if (2 * g + q < mx4_lines(cols))
-      *reinterpret_cast<u32x4*>(codes + mx4_codes_at(2 * g + q, blocks, rb) + 16 * threadIdx.x) =
-          *reinterpret_cast<const u32x4*>(tile + (8 * q + chunk) * kChunkPitch + 16 * r);
-  if (chunk == 0)
-    *reinterpret_cast<u32x4*>(scales + mx4_scales_at(g, blocks, rb) + 16 * r) = *reinterpret_cast<const u32x4*>(tile_scales + 16 * r);
+  *reinterpret_cast<u32x4*>(codes + mx4_codes_at(line, blocks, rb) + 16 * threadIdx.x) =
+      *reinterpret_cast<const u32x4*>(tile + (threadIdx.x >> 5) * kChunkPitch + 16 * r);
+  // two bytes of each of four words; a group's last line writes the absent one's too
+  const int word = threadIdx.x >> 5;
+  if (word >= 4) return;
+  uint8_t* to = scales + mx4_scales_at(line >> 1, blocks, rb) + 16 * r + 4 * word;
+  const uint16_t bytes = *reinterpret_cast<const uint16_t*>(&tile_scales[r][2 * word]);
+  if (line & 1) *reinterpret_cast<uint16_t*>(to + 2) = bytes;
+  else if (line == lines - 1) *reinterpret_cast<uint32_t*>(to) = 0x7f7f0000u | bytes;
+  else *reinterpret_cast<uint16_t*>(to) = bytes;
 }
 
 // ---- blocks down the columns ------------------------------------------------------------------------
-// A workgroup takes 64 columns x 512 rows.  A wave reads a block's 32 rows in four loads of eight 128-byte segments: lane l
-// holds columns 8 (l % 8) .. + 7 of rows 4 (l / 8) .. + 3, so it has two bytes of codes for each of its columns.
-constexpr int kTileCols = 64;
+// A workgroup takes 64 columns x 128 rows, half a line; a wave a block's 32 rows, in four loads of eight 128-byte segments: lane
+// l holds columns 8 (l % 8) .. + 7 of rows 4 (l / 8) .. + 3, so it has two bytes of codes for each of its columns.  Small
+// pieces: a workgroup reads, converts and writes one after the other, and with 512 rows each, all of them did so together
+// (4096x4096: 15.2 us).
+constexpr int kTileCols = 64, kTileRows = 128;
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* src, int64_t ld, int rows, int cols, bool vec,
-                                                               uint8_t* codes, uint8_t* scales) {
-  __shared__ __align__(16) uint8_t tile[2 * 16 * kChunkPitch];  // two blocks of 32 columns
-  __shared__ __align__(16) uint8_t tile_scales[kTileCols * 16];
+                                                               bool whole_lines, uint8_t* codes, uint8_t* scales) {
+  __shared__ __align__(16) uint8_t tile[2][4 * kChunkPitch];  // two blocks of 32 columns
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tiles = (cols + kTileCols - 1) / kTileCols, blocks = mx4_row_blocks(cols);
-  const int g = blockIdx.x / tiles;
-  const int n0 = (blockIdx.x - g * tiles) * kTileCols;
-  const int c8 = lane & 7, rg = lane >> 3;
-  const int n = n0 + 8 * c8;
-  u32x4 v[4][4];
+  const int tiles = (cols + kTileCols - 1) / kTileCols, blocks = mx4_row_blocks(cols), units = 2 * mx4_lines(rows);
+  const int item = item_of_workgroup(whole_lines);
+  const int unit = item / tiles, n0 = (item - unit * tiles) * kTileCols;
+  if (unit >= units) return;
+  const int c8 = lane & 7, rg = lane >> 3, n = n0 + 8 * c8, k0 = unit * kTileRows + 32 * wave, k = k0 + 4 * rg;
+  u32x4 v[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int k = g * kMx4Group + 32 * (wave + 4 * q) + 4 * rg;
+  for (int i = 0; i < 4; ++i)
+    v[i] = k + i < rows && n < cols ? load_eight(src + (int64_t)(k + i) * ld + n, cols - n, vec) : u32x4{0, 0, 0, 0};
+  const bool beyond = k0 >= rows;
+  const int chunk = 2 * (wave & 1) + (wave >> 1);  // of block p = 4 (unit % 2) + wave, within the half line
+  // this block's byte of its word, and those of blocks that do not exist behind the last unit
+  const int step = unit & 3, fill = unit == units - 1 && step == 1 ? 2 : 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[q][i] = (k + i < rows && n < cols) ? load_eight(src + (int64_t)(k + i) * ld + n, cols - n, vec) : u32x4{0, 0, 0, 0};
-  }
+  for (int w = 0; w < 4; ++w) {
+    uint32_t m = 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int block = wave + 4 * q;
-    const bool beyond = g * kMx4Group + 32 * block >= rows;
+    for (int i = 0; i < 4; ++i) m = max_halves(m, v[i][w] & 0x7fff7fffu);
+    m = max_with_lane<0x128>(m);  // lane ^ 8
+    m = max_halves(m, (uint32_t)__shfl_xor((int)m, 16));
+    m = max_halves(m, (uint32_t)__shfl_xor((int)m, 32));
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      uint32_t m = 0;
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t e = mx4_scale_of<DT>(half ? m >> 16 : m & 0xffffu);
+      const float s = mx4_inverse_scale(e);
+      float f[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m = max_halves(m, v[q][i][w] & 0x7fff7fffu);
-      m = max_with_lane<0x128>(m);  // lane ^ 8
-      m = max_halves(m, (uint32_t)__shfl_xor((int)m, 16));
-      m = max_halves(m, (uint32_t)__shfl_xor((int)m, 32));
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const uint32_t e = mx4_scale_of<DT>(half ? m >> 16 : m & 0xffffu);
-        const float s = mx4_inverse_scale(e);
-        float f[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = (half ? high_half<DT>(v[q][i][w]) : low_half<DT>(v[q][i][w])) * s;
-        uint32_t c = 0;
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[0], f[1], 1.0f, 0);
-        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[2], f[3], 1.0f, 1);
-        if (e == 255) c = 0;
-        const int col = 8 * c8 + 2 * w + half;
-        *reinterpret_cast<uint16_t*>(tile + (col >> 5) * 16 * kChunkPitch + lds_place(block, col & 31) + 2 * rg) = (uint16_t)c;
-        if (rg == 0) tile_scales[16 * col + mx4_scale_place(block)] = (uint8_t)(beyond ? 127 : e);
+      for (int i = 0; i < 4; ++i) f[i] = (half ? high_half<DT>(v[i][w]) : low_half<DT>(v[i][w])) * s;
+      uint32_t c = 0;
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[0], f[1], 1.0f, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[2], f[3], 1.0f, 1);
+      if (e == 255) c = 0;
+      const int col = 8 * c8 + 2 * w + half;
+      *reinterpret_cast<uint16_t*>(&tile[col >> 5][chunk * kChunkPitch + 16 * (col & 31) + 2 * rg]) = (uint16_t)c;
+      if (rg == 2 * w + half && n0 + col < cols) {
+        uint8_t* to = scales + mx4_scales_at(unit >> 2, blocks, (n0 + col) >> 5) + 16 * (col & 31) + 4 * wave + step;
+        to[0] = (uint8_t)(beyond ? 127 : e);
+        for (int q = 1; q <= fill; ++q) to[q] = 127;
       }
     }
   }
   __syncthreads();
-  const int chunk = threadIdx.x >> 5, r = threadIdx.x & 31;
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    if (n0 + 32 * b + r >= cols) continue;
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-      if (2 * g + q < mx4_lines(rows))
-        *reinterpret_cast<u32x4*>(codes + mx4_codes_at(2 * g + q, blocks, n0 / 32 + b) + 16 * threadIdx.x) =
-            *reinterpret_cast<const u32x4*>(tile + (16 * b + 8 * q + chunk) * kChunkPitch + 16 * r);
-    if (chunk == 0)
-      *reinterpret_cast<u32x4*>(scales + mx4_scales_at(g, blocks, n0 / 32 + b) + 16 * r) =
-          *reinterpret_cast<const u32x4*>(tile_scales + 16 * (32 * b + r));
-  }
+  const int b = threadIdx.x >> 7, r = threadIdx.x & 31;
+  if (n0 + 32 * b + r >= cols) return;
+  *reinterpret_cast<u32x4*>(codes + mx4_codes_at(unit >> 1, blocks, n0 / 32 + b) + 2048 * (unit & 1) + 16 * (threadIdx.x & 127)) =
+      *reinterpret_cast<const u32x4*>(&tile[b][((threadIdx.x >> 5) & 3) * kChunkPitch + 16 * r]);
 }
 
 // ---- back -------------------------------------------------------------------------------------------
+// Byte of an LDS tile that holds block j = 0..15 (512 values) of row r in a block of rows.
+__device__ __forceinline__ int lds_place(int j, int r) { return (8 * (j >> 3) + mx4_chunk_of(j & 7)) * kChunkPitch + 16 * r; }
+
 template <int DT>
 __global__ __launch_bounds__(kThreads) void mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int length,
                                                               uint16_t* dst, int64_t ld, bool vec) {
@@ -180,15 +183,15 @@ hipError_t launch_mx4_quantize(int rows, int cols, int dtype, const void* src, i
   if (columns && cols == 1 && ld == 1) return launch_mx4_quantize(1, rows, dtype, src, rows, false, codes, scales, stream);
   const uint16_t* p = static_cast<const uint16_t*>(src);
   const bool vec = rows_in_pieces(src, ld) || (rows == 1 && (reinterpret_cast<uintptr_t>(src) & 15) == 0);
-  if (columns) {
-    const dim3 grid((uint32_t)((int64_t)((cols + kTileCols - 1) / kTileCols) * mx4_groups(rows)));
-    if (dtype == HINM_F16) mx4_columns_kernel<HINM_F16><<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, vec, codes, scales);
-    else mx4_columns_kernel<HINM_BF16><<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, vec, codes, scales);
-  } else {
-    const dim3 grid((uint32_t)((int64_t)mx4_row_blocks(rows) * mx4_groups(cols)));
-    if (dtype == HINM_F16) mx4_rows_kernel<HINM_F16><<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, vec, codes, scales);
-    else mx4_rows_kernel<HINM_BF16><<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, vec, codes, scales);
-  }
+  const bool whole_lines = (reinterpret_cast<uintptr_t>(src) & 127) == 0 && ld % 64 == 0;
+  const int64_t items = columns ? (int64_t)((cols + kTileCols - 1) / kTileCols) * 2 * mx4_lines(rows)
+                                : (int64_t)mx4_row_blocks(rows) * mx4_lines(cols);
+  const dim3 grid((uint32_t)((items + 7) / 8 * 8));
+  auto launch = [&](auto kernel) {
+    kernel<<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, vec, whole_lines, codes, scales);
+  };
+  if (columns) launch(dtype == HINM_F16 ? mx4_columns_kernel<HINM_F16> : mx4_columns_kernel<HINM_BF16>);
+  else launch(dtype == HINM_F16 ? mx4_rows_kernel<HINM_F16> : mx4_rows_kernel<HINM_BF16>);
   return hipGetLastError();
 }
 
