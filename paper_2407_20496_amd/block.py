@@ -1,0 +1,139 @@
+"""A transformer's feed-forward block between its norms, on channels x tokens matrices, over the C-ABI entry points.
+
+    h = a x + gate . norm(layers(u)) w_post        u_next = norm(h) w_next
+
+Layers come in either compressed form: prepared HiNM layers (`Layer`, run by hinm_chain) or 4-bit ones (`Mx4Layer`, run by
+hinm_mx4_linear).  This module holds buffers and hands arrays from one call to the next; everything that is computed runs in
+the library's kernels, on the current stream.  PyTorch is used for device memory only.
+
+    up, down = mx4_layer(W_up, flags=hb.EPI_RELU), mx4_layer(W_down)
+    block = FeedForward([up, down], tokens, w_post, w_next=w_next_block)
+    u = block_input(x, w_pre, tokens)
+    x, u = block(x, u)            # and on to the next block with these
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Optional, Sequence, Tuple, Union
+
+import torch
+
+from . import binding as hb
+
+
+@dataclass
+class Mx4Layer:
+    """Weights [M][K] in microscaled 4-bit form; flags as for hinm_mx4_linear (EPI_RELU between layers)."""
+    M: int
+    K: int
+    dtype: object
+    codes: torch.Tensor
+    scales: torch.Tensor
+    flags: int = 0
+
+
+def mx4_form(rows: int, length: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Memory for codes and scales of `rows` rows of `length` values."""
+    cb, sb = hb.hinm_mx4_sizes(rows, length)
+    return torch.empty(cb, dtype=torch.uint8, device=device), torch.empty(sb, dtype=torch.uint8, device=device)
+
+
+def mx4_layer(W: torch.Tensor, flags: int = 0) -> Mx4Layer:
+    """Dense 16-bit weights [M][K] (rows may be strided) to a 4-bit layer."""
+    M, K = W.shape
+    if W.stride(1) != 1 and K > 1:
+        raise ValueError("weights must be contiguous along their rows")
+    codes, scales = mx4_form(M, K, W.device)
+    hb.hinm_mx4_quantize(M, K, W.dtype, W, max(W.stride(0), K), hb.MX4_ROWS, codes, scales)
+    return Mx4Layer(M, K, W.dtype, codes, scales, flags)
+
+
+def mx4_linear_grad(W: torch.Tensor, X: torch.Tensor, dY: torch.Tensor, tokens: Optional[int] = None,
+                    want_input: bool = True, want_weights: bool = True):
+    """Gradients of Y = W X where every product is taken on 4-bit operands, each quantised along the axis that is summed over
+    and rounded as if the quantisation were not there (straight through): (dX like X, dW float32 [M][K]).
+    W [M][K], X [K][ld], dY [M][ld], contiguous, `tokens` <= ld columns in use."""
+    M, K = W.shape
+    N = X.shape[1] if tokens is None else tokens
+    dev, dtype = W.device, W.dtype
+    dX = dW = None
+    if want_input:
+        across_w, across_dy = mx4_form(K, M, dev), mx4_form(N, M, dev)
+        hb.hinm_mx4_quantize(M, K, dtype, W, K, hb.MX4_COLUMNS, *across_w)
+        hb.hinm_mx4_quantize(M, N, dtype, dY, dY.shape[1], hb.MX4_COLUMNS, *across_dy)
+        dX = torch.empty_like(X)
+        hb.hinm_mx4_product(K, N, M, dtype, *across_w, *across_dy, dX, X.shape[1])
+    if want_weights:
+        along_dy, along_x = mx4_form(M, N, dev), mx4_form(K, N, dev)
+        hb.hinm_mx4_quantize(M, N, dtype, dY, dY.shape[1], hb.MX4_ROWS, *along_dy)
+        hb.hinm_mx4_quantize(K, N, dtype, X, X.shape[1], hb.MX4_ROWS, *along_x)
+        dW = torch.empty((M, K), dtype=torch.float32, device=dev)
+        hb.hinm_mx4_product(M, K, N, dtype, *along_dy, *along_x, dW, K, hb.OUT_F32)
+    return dX, dW
+
+
+def leading_dimension(tokens: int) -> int:
+    """Columns of a buffer for `tokens` tokens: whole 16-byte pieces, or one alone."""
+    return tokens if tokens == 1 else (tokens + 7) // 8 * 8
+
+
+def _workspace(nbytes: int, device) -> torch.Tensor:
+    return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+
+
+def block_input(x: torch.Tensor, w_pre: torch.Tensor, tokens: int, eps: float = 1e-6) -> torch.Tensor:
+    """u = norm(x) w_pre: what the first block's layers take.  x [K][ld] 16-bit."""
+    K, ld = x.shape
+    u = torch.empty_like(x)
+    nbytes = hb.hinm_block_norm_workspace(K, tokens)
+    hb.hinm_block_norm(K, tokens, x.dtype, 1.0, eps, x, None, None, None, None, w_pre, None, ld, u, ld, None, None,
+                       _workspace(nbytes, x.device), nbytes)
+    return u
+
+
+class FeedForward:
+    """One block for a fixed number of tokens: its layers, norms and buffers."""
+
+    def __init__(self, layers: Sequence[Union[Mx4Layer, hb.Layer]], tokens: int, w_post: Optional[torch.Tensor],
+                 gate: Optional[torch.Tensor] = None, w_next: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
+                 eps: float = 1e-6, device="cuda"):
+        layers = list(layers)
+        if not layers or any(a.M != b.K for a, b in zip(layers, layers[1:])) or layers[-1].M != layers[0].K:
+            raise ValueError("layers must follow one another and lead back to the block's channels")
+        self.in_4_bits = all(isinstance(l, Mx4Layer) for l in layers)
+        if not self.in_4_bits and any(isinstance(l, Mx4Layer) for l in layers):
+            raise ValueError("one block's layers come in one form")
+        self.layers, self.tokens, self.ld = layers, tokens, leading_dimension(tokens)
+        self.w_post, self.gate, self.w_next = w_post, gate, w_next
+        self.residual_scale, self.eps = residual_scale, eps
+        self.K, self.dtype = layers[0].K, layers[0].dtype
+        kind = {hb.F16: torch.float16, hb.BF16: torch.bfloat16}[hb._dtype_code(self.dtype)]
+        new = lambda rows: torch.empty((rows, self.ld), dtype=kind, device=device)
+        self.y = new(self.K)
+        if self.in_4_bits:
+            self.between = [new(l.M) for l in layers[:-1]]
+            self.scratch_bytes = max(hb.hinm_mx4_linear_workspace(l.M, l.K, tokens) for l in layers)
+        else:
+            self.scratch_bytes = hb.hinm_chain_sizes(layers, tokens)
+        self.scratch = _workspace(self.scratch_bytes, device)
+        self.norm_bytes = hb.hinm_block_norm_workspace(self.K, tokens)
+        self.norm_workspace = _workspace(self.norm_bytes, device)
+
+    def run_layers(self, u: torch.Tensor) -> torch.Tensor:
+        """y = layers(u), in the block's own buffer."""
+        N, ld = self.tokens, self.ld
+        if not self.in_4_bits:
+            hb.hinm_chain(self.layers, N, u, ld, self.y, ld, self.scratch, self.scratch_bytes)
+            return self.y
+        for l, out in zip(self.layers, self.between + [self.y]):
+            hb.hinm_mx4_linear(l.M, l.K, N, l.dtype, l.codes, l.scales, u, ld, out, ld, l.flags, self.scratch,
+                               self.scratch_bytes)
+            u = out
+        return u
+
+    def __call__(self, x: torch.Tensor, u: torch.Tensor, token_gate: Optional[torch.Tensor] = None):
+        """(h, u_next) in place of (x, u); u_next is u untouched where no norm follows."""
+        y = self.run_layers(u)
+        hb.hinm_block_norm(self.K, self.tokens, self.dtype, self.residual_scale, self.eps, x, y, self.w_post, self.gate,
+                           token_gate, self.w_next, x, self.ld, u, self.ld, None, None, self.norm_workspace, self.norm_bytes)
+        return x, u
