@@ -365,7 +365,8 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
  * their elements only; rows that begin at multiples of 16 bytes (aligned base, leading dimension a multiple
  * of 8) are read and written in 16-byte pieces, others element by element.  A piece that holds at least
  * one element of a row is read whole (what lies beyond never reaches a result); nothing beyond the
- * row length is written.
+ * row length is written.  Sizes above 2^30, more than 2^22 tokens of a norm, and calls of more than some
+ * 2^22 workgroups (32 x 256 values or 128 x 128 outputs each) return HINM_ERR_UNSUPPORTED.
  *
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
  * version 1.0): 32 consecutive values of a row share a power of two, and every value is one of

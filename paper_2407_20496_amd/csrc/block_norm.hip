@@ -6,9 +6,9 @@
 // The second norm's sum is there after the first launch because h is linear in x and y with factors known per column:
 //   h = s x + r t (c y)   with c = gate w_post per channel, t = token_gate, r = rstd_y per token:
 //   sum h^2 = s^2 sum x^2 + 2 s r t sum x (c y) + (r t)^2 sum (c y)^2.
-// Where the three nearly cancel (a block whose output undoes its residual) that loses digits: a column whose sum is below
-// 1/16 of its two squares is added again from h itself.  The gradients' correction S = sum_k c y d is linear in the
-// gradient d in the same way.
+// The three may cancel (a block whose output undoes its residual), so they are added in binary64: the products of two floats
+// are exact there and the sum keeps its digits down to 2^-50 of what cancels; what h itself loses is its own rounding.  The
+// gradients' correction S = sum_k c y d is linear in the gradient d in the same way.
 //
 // Bound by memory: read twice (the second time from the caches behind L2 where they hold it), written once.  bf16, a channel
 // factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 24 against 14, 4096x8192
@@ -77,30 +77,80 @@ __device__ __forceinline__ u32x4 narrow(const float (&f)[8]) {
                floats_to_bits<DT>(f[6], f[7])};
 }
 
+// Sum over each eight neighbouring lanes.
+template <int CTRL>
+__device__ __forceinline__ float plus_moved(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float add_eight_lanes(float v) {
+  v = plus_moved<0xB1>(v);      // lane ^ 1
+  v = plus_moved<0x4E>(v);      // lane ^ 2
+  return plus_moved<0x141>(v);  // the other four
+}
+
 // Sum over a wave's lanes with the same lane % 8.
 __device__ __forceinline__ float add_lanes_by_8(float v) {
-  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));  // lane ^ 8
+  v = plus_moved<0x128>(v);  // lane ^ 8
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
 
+// Eight values of every lane, added over the lanes with the same lane % 8 and left one to a lane: value j = lane / 8 with its
+// three bits turned round (lane / 32 the highest).  Each step adds what two halves of the lanes hold of half of the values:
+// swaps of register halves, no LDS.
+template <int LANES>  // 32: the upper lanes of a with the lower ones of b; 16: odd rows of 16 of a with even ones of b
+__device__ __forceinline__ void swap_lanes(uint32_t& a, uint32_t& b) {
+  typedef unsigned pair __attribute__((ext_vector_type(2)));
+  pair r;
+  if constexpr (LANES == 32) r = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(a, b, false, false));
+  else r = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(a, b, false, false));
+  a = r[0];
+  b = r[1];
+}
+template <int LANES>
+__device__ __forceinline__ float swapped_sum(float a, float b) {
+  uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+  swap_lanes<LANES>(x, y);
+  return __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+}
+template <int LANES>
+__device__ __forceinline__ double swapped_sum(double a, double b) {
+  u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
+  uint32_t x0 = x[0], x1 = x[1], y0 = y[0], y1 = y[1];
+  swap_lanes<LANES>(x0, y0);
+  swap_lanes<LANES>(x1, y1);
+  return __builtin_bit_cast(double, (u32x2{x0, x1})) + __builtin_bit_cast(double, (u32x2{y0, y1}));
+}
+__device__ __forceinline__ uint32_t from_lane_8(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true); }
+__device__ __forceinline__ float from_lane_8(float v) { return __builtin_bit_cast(float, from_lane_8(__builtin_bit_cast(uint32_t, v))); }
+__device__ __forceinline__ double from_lane_8(double v) {
+  const u32x2 x = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(double, (u32x2{from_lane_8(x[0]), from_lane_8(x[1])}));
+}
+template <class T>
+__device__ __forceinline__ T add_columns(const T (&v)[8]) {
+  T w[4], x[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = swapped_sum<32>(v[i], v[i + 4]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) x[i] = swapped_sum<16>(w[i], w[i + 2]);
+  const bool second = threadIdx.x & 8;
+  const T kept = second ? x[1] : x[0], given = second ? x[0] : x[1];
+  return kept + from_lane_8(given);
+}
+
 // QUANTITIES sums of the workgroup's 64 columns, added over its threads in a fixed order, to partial[quantity][chunk][N].
-template <int QUANTITIES>
-__device__ __forceinline__ void store_sums(float (&sum)[QUANTITIES][8], const Place& p, float* partial, int chunks, int N) {
-  __shared__ float by_wave[QUANTITIES][kWaves][kStrip];
+template <int QUANTITIES, class T>
+__device__ __forceinline__ void store_sums(const T (&sum)[QUANTITIES][8], const Place& p, T* partial, int chunks, int N) {
+  __shared__ T by_wave[QUANTITIES][kWaves][kStrip];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int j = 4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1);
 #pragma unroll
-  for (int q = 0; q < QUANTITIES; ++q) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float t = add_lanes_by_8(sum[q][j]);
-      if (lane < 8) by_wave[q][wave][8 * lane + j] = t;
-    }
-  }
+  for (int q = 0; q < QUANTITIES; ++q) by_wave[q][wave][8 * (lane & 7) + j] = add_columns(sum[q]);
   __syncthreads();
   const int col = threadIdx.x & (kStrip - 1), n = p.n0 + col;
   for (int q = threadIdx.x / kStrip; q < QUANTITIES; q += kThreads / kStrip) {
-    float t = 0;
+    T t = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) t += by_wave[q][w][col];
     if (n < N) partial[((int64_t)q * chunks + p.chunk) * N + n] = t;
@@ -108,16 +158,16 @@ __device__ __forceinline__ void store_sums(float (&sum)[QUANTITIES][8], const Pl
 }
 
 // ... and their totals over the chunks, to total[quantity][64].  The caller waits at a barrier.
-template <int QUANTITIES>
-__device__ __forceinline__ void add_chunks(const float* partial, int chunks, int N, const Place& p, float (*total)[kStrip]) {
+template <int QUANTITIES, class T>
+__device__ __forceinline__ void add_chunks(const T* partial, int chunks, int N, const Place& p, T (*total)[kStrip]) {
   static_assert(QUANTITIES <= kThreads / kStrip, "a thread for each");
   const int col = threadIdx.x & (kStrip - 1), n = p.n0 + col, q = threadIdx.x / kStrip;
   if (q >= QUANTITIES || n >= N) return;
-  const float* at = partial + (int64_t)q * chunks * N + n;
-  float t = 0;
+  const T* at = partial + (int64_t)q * chunks * N + n;
+  T t = 0;
   int c = 0;
   for (; c + 8 <= chunks; c += 8) {
-    float v[8];
+    T v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = at[(int64_t)(c + j) * N];
 #pragma unroll
@@ -139,7 +189,7 @@ struct Forward {
   uint16_t* u;
   int64_t ld_block;
   float *rstd_y, *rstd_h;
-  float* sums;  // [4][chunks][N]: y^2, x^2, x c y, (c y)^2
+  double* sums;  // [4][chunks][N]: y^2, x^2, x c y, (c y)^2
   bool vec_stream, vec_block, whole_lines;
 };
 
@@ -173,7 +223,8 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
   const Place p(a.K, a.N, a.rows_per_chunk, a.whole_lines);
   if (p.none()) return;
-  float sum[4][8] = {};
+  double sum[4][8] = {};
+  float y_squares[8] = {};  // nothing cancels there
   const int end = p.row0 + p.rows;
   for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kPatch) {
     PatchXY v;
@@ -185,21 +236,18 @@ __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
       widen<DT>(v.y[i], y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        sum[0][j] += y[j] * y[j];
-        sum[1][j] += x[j] * x[j];
-        const float b = v.c[i] * y[j];
-        sum[2][j] += x[j] * b;
+        const double wide = x[j], b = v.c[i] * y[j];  // c y is rounded to a float as in h
+        y_squares[j] += y[j] * y[j];
+        sum[1][j] += wide * wide;
+        sum[2][j] += wide * b;
         sum[3][j] += b * b;
       }
     }
   }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[0][j] = y_squares[j];
   store_sums<4>(sum, p, a.sums, a.chunks, a.N);
 }
-
-// What an element needs of its token.
-struct TokenFactors {
-  float branch[8], u[8];  // token_gate rstd_y; rstd_h
-};
 
 template <int DT>
 __device__ __forceinline__ void row_of_h(const Forward& a, u32x4 x, u32x4 y, float c, const float (&branch)[8], float (&h)[8]) {
@@ -212,15 +260,14 @@ __device__ __forceinline__ void row_of_h(const Forward& a, u32x4 x, u32x4 y, flo
 
 template <int DT, bool LINES>
 __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a) {
-  __shared__ float total[4][kStrip], branch[kStrip], root[kStrip], again[kWaves][kStrip];
-  __shared__ int cancelled;
+  __shared__ double total[4][kStrip];
+  __shared__ float branch[kStrip], root[kStrip];
   const Place p(a.K, a.N, a.rows_per_chunk, LINES);
   if (p.none()) return;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchXY v;
   load_patch(a, p, first, end, v);  // on their way while the sums are added
   if (a.w_post || a.w_pre) add_chunks<4>(a.sums, a.chunks, a.N, p, total);
-  if (threadIdx.x == 0) cancelled = 0;
   __syncthreads();
   if (threadIdx.x < kStrip) {
     const int n = p.n0 + threadIdx.x;
@@ -228,15 +275,17 @@ __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a
     if (n < a.N) {
       if (a.token_gate) b = a.token_gate[n];
       if (a.w_post) {
-        const float ry = 1.0f / sqrtf(total[0][threadIdx.x] / (float)a.K + a.eps);
+        const float ry = 1.0f / sqrtf((float)(total[0][threadIdx.x] / a.K) + a.eps);
         b *= ry;
         if (a.rstd_y && p.chunk == 0) a.rstd_y[n] = ry;
       }
       if (a.w_pre) {
-        const float of_x = a.scale * a.scale * total[1][threadIdx.x], of_y = a.y ? b * b * total[3][threadIdx.x] : 0.0f;
-        const float sum = of_x + of_y + (a.y ? 2 * a.scale * b * total[2][threadIdx.x] : 0.0f);
-        if (sum < 0.0625f * (of_x + of_y)) cancelled = 1;
-        r = 1.0f / sqrtf(sum / (float)a.K + a.eps);
+        const double s = a.scale;
+        double sum = s * s * total[1][threadIdx.x];
+        if (a.y) sum += 2 * s * b * total[2][threadIdx.x] + (double)b * b * total[3][threadIdx.x];
+        if (sum < 0) sum = 0;  // all of it cancelled
+        r = 1.0f / sqrtf((float)(sum / a.K) + a.eps);
+        if (a.rstd_h && p.chunk == 0) a.rstd_h[n] = r;
       }
     }
     branch[threadIdx.x] = b;
@@ -246,36 +295,6 @@ __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a
   float of_token[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) of_token[j] = branch[at + j];
-  if (cancelled) {  // the same for the whole workgroup, and for all workgroups of the strip
-    float sum[8] = {};
-    for (int k = threadIdx.x >> 3; k < a.K; k += kPatch) {
-      PatchXY w;
-      load_patch(a, p, k, a.K, w);
-#pragma unroll
-      for (int i = 0; i < kRounds; ++i) {
-        float h[8];
-        row_of_h<DT>(a, w.x[i], w.y[i], w.c[i], of_token, h);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += h[j] * h[j];
-      }
-    }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float t = add_lanes_by_8(sum[j]);
-      if (lane < 8) again[wave][8 * lane + j] = t;
-    }
-    __syncthreads();
-    if (threadIdx.x < kStrip) {
-      float t = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) t += again[w][threadIdx.x];
-      root[threadIdx.x] = 1.0f / sqrtf(t / (float)a.K + a.eps);
-    }
-    __syncthreads();
-  }
-  if (a.w_pre && a.rstd_h && p.chunk == 0 && threadIdx.x < kStrip && p.n0 + (int)threadIdx.x < a.N)
-    a.rstd_h[p.n0 + threadIdx.x] = root[threadIdx.x];
   if (p.left <= 0) return;
   float of_u[8];
 #pragma unroll
@@ -309,16 +328,9 @@ constexpr int kHeldThreads = 512;
 
 // Reciprocal roots of eight columns from every thread's sums of squares.
 __device__ __forceinline__ void held_roots(float (&sum)[8], float (*by_wave)[8], float* root, const Forward& a, int n0, float* out) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-#pragma unroll
-    for (int q = 1; q < 8; q *= 2) sum[j] += __shfl_xor(sum[j], q);
-    sum[j] = add_lanes_by_8(sum[j]);
-  }
-  if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) by_wave[threadIdx.x >> 6][j] = sum[j];
-  }
+  const int lane = threadIdx.x & 63;
+  const float t = add_eight_lanes(add_columns(sum));
+  if ((lane & 7) == 0) by_wave[threadIdx.x >> 6][4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] = t;
   __syncthreads();
   if (threadIdx.x < 8) {
     float t = 0;
@@ -399,9 +411,7 @@ constexpr int kVectorThreads = 1024;
 constexpr int kVectorMost = 2 * 8 * kVectorThreads;
 
 __device__ __forceinline__ float add_workgroup(float v, float* by_wave) {
-#pragma unroll
-  for (int q = 1; q < 8; q *= 2) v += __shfl_xor(v, q);
-  v = add_lanes_by_8(v);
+  v = add_lanes_by_8(add_eight_lanes(v));
   if ((threadIdx.x & 63) == 0) by_wave[threadIdx.x >> 6] = v;
   __syncthreads();
   float t = 0;
@@ -618,11 +628,8 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
         if (a.dx) store_eight<LINES>(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left, a.vec_stream);
         if (a.dy) store_eight<LINES>(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left, a.vec_block);
       }
-#pragma unroll
-      for (int q = 1; q < 8; q *= 2) {
-        of_w_pre += __shfl_xor(of_w_pre, q);
-        of_branch += __shfl_xor(of_branch, q);
-      }
+      of_w_pre = add_eight_lanes(of_w_pre);
+      of_branch = add_eight_lanes(of_branch);
       if (in && (threadIdx.x & 7) == 0) {
         a.row_sums[(int64_t)p.strip * a.K + r] = of_w_pre;
         a.row_sums[(int64_t)(strips + p.strip) * a.K + r] = of_branch;
@@ -664,7 +671,7 @@ bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintp
 
 }  // namespace
 
-size_t block_norm_workspace_bytes(int K, int N) { return (size_t)4 * chunk_count(K, N) * N * sizeof(float); }
+size_t block_norm_workspace_bytes(int K, int N) { return (size_t)4 * chunk_count(K, N) * N * sizeof(double); }
 
 template <int DT>
 static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
@@ -696,7 +703,7 @@ hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
   Forward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale, b.eps,
             static_cast<const uint16_t*>(b.x), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
             static_cast<uint16_t*>(b.h), b.ld_stream, static_cast<uint16_t*>(b.u), b.ld_block, b.rstd_y, b.rstd_h,
-            b.workspace, false, false, false};
+            reinterpret_cast<double*>(b.workspace), false, false, false};
   a.vec_stream = in_pieces(a.x, a.ld_stream) && in_pieces(a.h, a.ld_stream);
   a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.u, a.ld_block);
   a.whole_lines = in_lines(a.x, a.ld_stream) && in_lines(a.h, a.ld_stream) && in_lines(a.y, a.ld_block) && in_lines(a.u, a.ld_block);

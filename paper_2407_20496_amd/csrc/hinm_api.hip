@@ -68,6 +68,10 @@ size_t elem_bytes_out(uint32_t flags) { return (flags & HINM_OUT_F32) ? 4 : 2; }
 bool known_dtype(int32_t d) { return d == HINM_F16 || d == HINM_BF16; }
 hinm_status launched(hipError_t e) { return e == hipSuccess ? HINM_OK : HINM_ERR_DEVICE; }
 
+// What sizes may be (index arithmetic in 32 bits beside it), and the workgroups of a launch (of up to 512 threads).
+constexpr int32_t kMostSize = 1 << 30;
+constexpr int64_t kMostGroups = 1 << 22;
+
 // rows of `length` values in 4-bit form
 hinm_status check_form(const uint8_t* codes, const uint8_t* scales) {
   if (!codes || !scales) return HINM_ERR_NULL;
@@ -80,8 +84,9 @@ hinm_status check_product(int32_t M, int32_t N, int32_t K, int32_t dtype, const 
   if (!Y) return HINM_ERR_NULL;
   if (ldy < N || !aligned(Y, (flags & HINM_OUT_F32) ? 4 : 2)) return HINM_ERR_SHAPE;
   if (flags & ~(uint32_t)(HINM_EPI_RELU | HINM_OUT_F32)) return HINM_ERR_UNSUPPORTED;
-  // workgroups of one launch: at least one for 16 x 128 outputs
-  if ((((int64_t)M + 15) / 16) * (((int64_t)N + 127) / 128) >= (int64_t{1} << 22)) return HINM_ERR_UNSUPPORTED;
+  // workgroups of one launch: 32 rows for one column, otherwise at most 128 x 128 outputs
+  if (M > kMostSize || N > kMostSize || K > kMostSize) return HINM_ERR_UNSUPPORTED;
+  if (N == 1 ? M / 32 >= kMostGroups : (int64_t)((M + 127) / 128) * ((N + 127) / 128) >= kMostGroups) return HINM_ERR_UNSUPPORTED;
   return HINM_OK;
 }
 
@@ -93,13 +98,13 @@ LinearPlan linear_plan(int32_t K, int32_t N) {
   return {(c + 255) & ~size_t{255}, (s + 255) & ~size_t{255}};
 }
 
-// a workgroup's strip is 64 tokens and a launch holds at most 64 of them a strip
+// a workgroup has 64 tokens, and some 64 of them the chunks of such a strip
 constexpr int32_t kMostTokens = 1 << 22;
 
 hinm_status check_norm(int32_t K, int32_t N, int32_t dtype) {
   if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
   if (K <= 0 || N <= 0) return HINM_ERR_SHAPE;
-  return N > kMostTokens ? HINM_ERR_UNSUPPORTED : HINM_OK;
+  return N > kMostTokens || K > kMostSize ? HINM_ERR_UNSUPPORTED : HINM_OK;
 }
 
 // ---- hinm_pack_static: the score workspace of the pack kernels in a file-scope device array -------------
@@ -692,6 +697,10 @@ hinm_status hinm_mx4_quantize(int32_t rows, int32_t cols, int32_t dtype, const v
   if (st != HINM_OK) return st;
   if (ld < cols || !aligned(src, 2)) return HINM_ERR_SHAPE;
   if (along != HINM_MX4_ROWS && along != HINM_MX4_COLUMNS) return HINM_ERR_UNSUPPORTED;
+  if (rows > kMostSize || cols > kMostSize) return HINM_ERR_UNSUPPORTED;
+  const int64_t pieces = along == HINM_MX4_ROWS ? (int64_t)mx4_row_blocks(rows) * mx4_lines(cols)
+                                                : (int64_t)((cols + 63) / 64) * 2 * mx4_lines(rows);
+  if (pieces >= 2 * kMostGroups) return HINM_ERR_UNSUPPORTED;
   return launched(launch_mx4_quantize(rows, cols, dtype, src, ld, along == HINM_MX4_COLUMNS, codes, scales,
                                       static_cast<hipStream_t>(stream)));
 }
@@ -704,6 +713,8 @@ hinm_status hinm_mx4_unpack(int32_t rows, int32_t length, int32_t dtype, const u
   const hinm_status st = check_form(codes, scales);
   if (st != HINM_OK) return st;
   if (ld < length || !aligned(dst, 2)) return HINM_ERR_SHAPE;
+  if (rows > kMostSize || length > kMostSize || (int64_t)mx4_row_blocks(rows) * mx4_groups(length) >= 2 * kMostGroups)
+    return HINM_ERR_UNSUPPORTED;
   return launched(launch_mx4_unpack(rows, length, dtype, codes, scales, dst, ld, static_cast<hipStream_t>(stream)));
 }
 
@@ -721,6 +732,7 @@ hinm_status hinm_mx4_product(int32_t M, int32_t N, int32_t K, int32_t dtype, con
 hinm_status hinm_mx4_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes) {
   if (!workspace_bytes) return HINM_ERR_NULL;
   if (M <= 0 || K <= 0 || N <= 0) return HINM_ERR_SHAPE;
+  if (M > kMostSize || K > kMostSize || N > kMostSize) return HINM_ERR_UNSUPPORTED;
   const LinearPlan p = linear_plan(K, N);
   *workspace_bytes = p.codes + p.scales;
   return HINM_OK;

@@ -71,8 +71,7 @@ uint32_t grid_of_items(int64_t items) { return (uint32_t)((items + 7) / 8 * 8); 
 // line before it multiplies.  B is the instruction's row operand, so that a lane ends with four consecutive columns of Y.
 //   Rows of B beyond N lie beyond the buffer descriptor's bytes for their lanes: they read as zero and cost no traffic.
 template <int OUT, int WM, int WN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (WM * WN > 8 ? 4 : 8) / WAVES > 0 ? (WM * WN > 8 ? 4 : 8) / WAVES : 1)
-void mx4_stream_kernel(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, void* Y,
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, void* Y,
                        ProductShape p) {
   constexpr int kPitch = 32 * WN + 4;
   __shared__ __align__(16) float slabs[WAVES][32 * kPitch];
@@ -603,10 +602,12 @@ constexpr Form kForms[] = {
     {64, 128, 4, 0, 4.0, 1.18, 84, 63},       {128, 128, 0, 256, 4.6, 0, 0.30, 0.61}, {128, 128, 0, 512, 3.9, 0, 0.52, 1.14},
     {256, 256, 0, 256, 8.2, 0, 0.92, 1.77},
 };
+constexpr int64_t kMostGroups = 1 << 22;  // of up to 512 threads in a launch
 double estimate_us(const Form& f, const ProductShape& p) {
   const int64_t groups = (int64_t)((p.M + f.rows - 1) / f.rows) * ((p.N + f.cols - 1) / f.cols);
   const double lines = mx4_lines(p.K);
   if (f.waves) {
+    if (groups > kMostGroups) return 1e30;
     const double each = lines * 0.128 * (f.rows + (p.N < f.cols ? p.N : f.cols));  // KB
     const double share = groups <= 256 ? 1 : groups / 256.0;                       // workgroups of a compute unit
     const double rate = share >= 2 ? f.full : f.alone + (f.full - f.alone) * (share - 1);

@@ -35,6 +35,8 @@ def test_bad_sizes():
     assert lib.hinm_block_norm_workspace(0, 1, C.byref(n)) == SHAPE
     assert lib.hinm_block_norm_grad_workspace(1, -1, C.byref(n)) == SHAPE
     assert lib.hinm_block_norm_workspace(1, (1 << 22) + 1, C.byref(n)) == UNSUPPORTED
+    assert lib.hinm_block_norm_grad_workspace((1 << 30) + 1, 1, C.byref(n)) == UNSUPPORTED
+    assert lib.hinm_mx4_linear_workspace(1, (1 << 30) + 1, 1, C.byref(n)) == UNSUPPORTED
 
 
 def _refused(call, good, **changes):
@@ -46,7 +48,8 @@ def _refused(call, good, **changes):
 @pytest.mark.parametrize("change,status", [
     ({"dtype": 2}, DTYPE), ({"rows": 0}, SHAPE), ({"cols": -1}, SHAPE), ({"src": None}, NULL), ({"codes": None}, NULL),
     ({"scales": None}, NULL), ({"ld": 63}, SHAPE), ({"src": P + 1}, SHAPE), ({"codes": P + 8}, SHAPE), ({"scales": P + 4}, SHAPE),
-    ({"along": 2}, UNSUPPORTED), ({"along": -1}, UNSUPPORTED)])
+    ({"along": 2}, UNSUPPORTED), ({"along": -1}, UNSUPPORTED), ({"rows": (1 << 30) + 1}, UNSUPPORTED), ({"rows": 1 << 30}, UNSUPPORTED),
+    ({"rows": 1 << 30, "cols": 1, "ld": 2, "along": 1}, UNSUPPORTED), ({"rows": 1, "cols": (1 << 30) + 1, "ld": BIG}, UNSUPPORTED)])
 def test_quantize_refusals(change, status):
     good = dict(rows=32, cols=64, dtype=0, src=P, ld=64, along=0, codes=P, scales=P)
     assert _refused(hinm.load_library().hinm_mx4_quantize, good, **change) == status
@@ -54,7 +57,8 @@ def test_quantize_refusals(change, status):
 
 @pytest.mark.parametrize("change,status", [
     ({"dtype": -1}, DTYPE), ({"rows": 0}, SHAPE), ({"length": 0}, SHAPE), ({"dst": None}, NULL), ({"codes": None}, NULL),
-    ({"ld": 63}, SHAPE), ({"dst": P + 1}, SHAPE), ({"codes": P + 1}, SHAPE)])
+    ({"ld": 63}, SHAPE), ({"dst": P + 1}, SHAPE), ({"codes": P + 1}, SHAPE), ({"rows": 1 << 30}, UNSUPPORTED),
+    ({"length": (1 << 30) + 1, "ld": BIG}, UNSUPPORTED)])
 def test_unpack_refusals(change, status):
     good = dict(rows=32, length=64, dtype=0, codes=P, scales=P, dst=P, ld=64)
     assert _refused(hinm.load_library().hinm_mx4_unpack, good, **change) == status
@@ -64,7 +68,8 @@ def test_unpack_refusals(change, status):
     ({"dtype": 7}, DTYPE), ({"M": 0}, SHAPE), ({"N": 0}, SHAPE), ({"K": -4}, SHAPE), ({"ac": None}, NULL), ({"asc": None}, NULL),
     ({"bc": None}, NULL), ({"bs": None}, NULL), ({"Y": None}, NULL), ({"ldy": 7}, SHAPE), ({"bc": P + 8}, SHAPE), ({"Y": P + 1}, SHAPE),
     ({"flags": 4}, UNSUPPORTED), ({"flags": 0x100}, UNSUPPORTED), ({"flags": 2, "Y": P + 2}, SHAPE),
-    ({"M": (1 << 31) - 1, "N": (1 << 31) - 1, "ldy": BIG}, UNSUPPORTED)])
+    ({"M": (1 << 31) - 1, "N": (1 << 31) - 1, "ldy": BIG}, UNSUPPORTED), ({"M": 1 << 30, "N": 1, "ldy": 1}, UNSUPPORTED),
+    ({"K": (1 << 30) + 1}, UNSUPPORTED), ({"M": 1 << 20, "N": 1 << 20, "ldy": BIG}, UNSUPPORTED)])
 def test_product_refusals(change, status):
     good = dict(M=16, N=8, K=64, dtype=1, ac=P, asc=P, bc=P, bs=P, Y=P, ldy=8, flags=0)
     assert _refused(hinm.load_library().hinm_mx4_product, good, **change) == status

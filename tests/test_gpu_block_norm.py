@@ -271,3 +271,60 @@ def test_streams_and_graph_replays(K, N):
         torch.cuda.synchronize()
         for a, b in zip(outs, want):
             assert torch.equal(a[:, :N] if a.dim() == 2 else a, b)
+
+
+@pytest.mark.parametrize("K,N,in_place", [(300, 20, False), (5000, 70, False), (5000, 70, True), (20000, 17, True), (300, 1, True)])
+def test_a_block_that_undoes_its_residual(K, N, in_place):
+    """h = x + y with y = -x in every third token, all but one channel in every third, and something else in the rest: the sum of
+    h^2 must not be what is left of two large sums."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    ld = (N + 7) // 8 * 8
+    rng = np.random.default_rng(K)
+    x = Matrix(K, N, ld, 0, "bf16", rng.standard_normal((K, N)) * np.exp(rng.standard_normal((K, 1))))
+    other = -x.wide
+    other[K // 2, 1::3] += 2.0 ** -6 * np.abs(other[K // 2, 1::3]) + 2.0 ** -8
+    other[:, 2::3] = rng.standard_normal(other[:, 2::3].shape)
+    y = Matrix(K, N, ld, 0, "bf16", other)
+    w = (1 + 0.3 * rng.standard_normal(K)).astype(np.float32)
+    h = x if in_place else Matrix(K, N, ld, 0, "bf16")
+    u = y if in_place else Matrix(K, N, ld, 0, "bf16")
+    rh = _guarded(N)
+    want = orc.block_norm(x.wide, y.wide, None, None, None, _f32(w), 1.0, np.float32(EPS).astype(np.float64))
+    hinm.hinm_block_norm(K, N, "bf16", 1.0, EPS, x.ptr, y.ptr, None, None, None, _vec(w), h.ptr, ld, u.ptr, ld, None, rh,
+                         *_workspace(hinm.hinm_block_norm_workspace(K, N)))
+    # x and y are exact here and their sum in fp32 is too, or rounded by 2^-24 of itself: nothing is lost
+    assert (np.abs(_values(rh, N) - want["rstd_h"]) <= SUM * want["rstd_h"]).all()
+    background = 0x7FFF if in_place else POISON
+    _check("h", h.result(background), want["h"], HALF_STEP["bf16"] * np.abs(want["h"]))
+    _check("u", u.result(background), want["u"], HALF_STEP["bf16"] * np.abs(want["u"]) * 1.01 + 1e-30)
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements a matrix: some columns, forward and back, against binary64."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    K, N = 40000, 54000
+    new = lambda: torch.randn(K, N, device=DEV, dtype=torch.bfloat16)
+    x, y = new(), new()
+    h, u = torch.empty_like(x), torch.empty_like(x)
+    w, rh, ry = torch.rand(K, device=DEV) + 0.5, torch.empty(N, device=DEV), torch.empty(N, device=DEV)
+    hinm.hinm_block_norm(K, N, "bf16", 1.0, EPS, x, y, w, None, None, w, h, N, u, N, ry, rh,
+                         *_workspace(hinm.hinm_block_norm_workspace(K, N)))
+    cols = [0, 7, 26999, 53992, N - 1]
+    wd = w.cpu().numpy().astype(np.float64)
+    take = lambda t: t[:, cols].float().cpu().numpy().astype(np.float64)
+    r = orc.block_norm(take(x), take(y), wd, None, None, wd, 1.0, EPS)
+    _check("h", take(h), r["h"], HALF_STEP["bf16"] * np.abs(r["h"]) + SUM * r["size"])
+    of_h = np.sqrt((r["size"] ** 2).mean(axis=0) + EPS) * r["rstd_h"]
+    _check("u", take(u), r["u"], HALF_STEP["bf16"] * np.abs(r["u"]) + SUM * wd[:, None] * r["rstd_h"] * r["size"] * (1 + of_h))
+    dx, dy = torch.empty_like(x), x           # x has done its work
+    dw = torch.empty(K, device=DEV)
+    hinm.hinm_block_norm_grad(K, N, "bf16", 1.0, h, y, w, None, None, w, ry, rh, u, u, dx, N, dy, N, dw, None, None, None,
+                              *_workspace(hinm.hinm_block_norm_grad_workspace(K, N)))
+    f = lambda t: t[cols].cpu().numpy().astype(np.float64)
+    g = orc.block_norm_grad(take(h), take(y), wd, None, None, wd, f(ry), f(rh), take(u), take(u), 1.0)
+    for name, got in (("dx", dx), ("dy", dy)):
+        value, size = g[name]
+        _check(name, take(got), value, HALF_STEP["bf16"] * np.abs(value) + SUM * size)
+    assert torch.isfinite(dw).all()

@@ -305,3 +305,32 @@ def test_streams_and_graph_replays():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(Y, want)
+
+
+def test_offsets_beyond_32_bits():
+    """A matrix of more than 2^31 values, quantised both ways and back, and a product with as many outputs: last rows and columns."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    rows, cols = 66000, 33000
+    W = torch.randn(rows, cols, device=DEV, dtype=torch.bfloat16)
+    for along, shape in ((hinm.MX4_ROWS, (rows, cols)), (hinm.MX4_COLUMNS, (cols, rows))):
+        cb, sb = hinm.hinm_mx4_sizes(*shape)
+        form = torch.empty(cb, dtype=torch.uint8, device=DEV), torch.empty(sb, dtype=torch.uint8, device=DEV)
+        hinm.hinm_mx4_quantize(rows, cols, "bf16", W, cols, along, *form)
+        back = torch.empty(shape, dtype=torch.bfloat16, device=DEV)
+        hinm.hinm_mx4_unpack(*shape, "bf16", *form, back, shape[1])
+        for r in (0, shape[0] // 2 + 5, shape[0] - 1):
+            line = (W[r] if along == hinm.MX4_ROWS else W[:, r]).float().cpu().numpy().astype(np.float64)[None]
+            want = orc.values(*orc.quantize_rows(line), shape[1])
+            assert np.array_equal(back[r].float().cpu().numpy().astype(np.float64), want[0]), (along, r)
+        del form, back
+    del W
+    M, N, K = 47000, 46500, 64
+    fa, fb = _random_form(M, K, 1), _random_form(N, K, 2)
+    Y = torch.empty((M, N), dtype=torch.bfloat16, device=DEV)
+    hinm.hinm_mx4_product(M, N, K, "bf16", *_upload(*fa), *_upload(*fb), Y, N)
+    pick = lambda f, i: tuple(t[i] for t in f)
+    m, n = [0, 23456, M - 1], np.arange(N - 300, N)
+    want, size = orc.product(orc.values(*pick(fa, m), K), orc.values(*pick(fb, n), K))
+    got = Y[m][:, N - 300:].float().cpu().numpy().astype(np.float64)
+    assert (np.abs(got - want) <= _tolerance(size, K, want, "bf16")).all()
