@@ -42,6 +42,12 @@ int chunk_count(int K, int N) {
   return (K + rows - 1) / rows;
 }
 
+// What a kernel knows of its matrices' rows: whole cache lines; pieces of 16 bytes at multiples of 16; nothing (the registers
+// that a row's end at any address takes cost the other two their occupancy: 4096x2048 24 -> 27 us).
+enum Layout { kLines, kPieces, kAny };
+template <Layout L>
+__device__ __forceinline__ Pieces known(Pieces rows) { return L == kAny ? rows : kAligned; }
+
 // Which strip and chunk a workgroup has.  Workgroups go to the eight XCDs in turn.  Rows of whole cache lines: neighbouring
 // workgroups take neighbouring strips of the same rows.  Otherwise neighbouring strips share lines and each XCD takes a
 // contiguous run of the list (chunk, strip), so that the parts of a line meet in one L2 (16384x1000: 68 -> 48 us; at
@@ -190,7 +196,8 @@ struct Forward {
   int64_t ld_block;
   float *rstd_y, *rstd_h;
   double* sums;  // [4][chunks][N]: y^2, x^2, x c y, (c y)^2
-  bool vec_stream, vec_block, whole_lines;
+  Pieces stream, block;
+  Layout layout;
 };
 
 __device__ __forceinline__ float channel_factor(const float* w_post, const float* gate, int k) {
@@ -202,14 +209,15 @@ struct PatchXY {
   u32x4 x[kRounds], y[kRounds];
   float c[kRounds], w[kRounds];  // gate w_post; w_pre
 };
+template <Layout L>
 __device__ __forceinline__ void load_patch(const Forward& a, const Place& p, int k, int end, PatchXY& v) {
   const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
     const int r = k + i * kRowsAtOnce;
     const bool in = r < end && p.left > 0;
-    v.x[i] = in ? load_eight(a.x + (int64_t)r * a.ld_stream + p.n, p.left, a.vec_stream) : none;
-    v.y[i] = in && a.y ? load_eight(a.y + (int64_t)r * a.ld_block + p.n, p.left, a.vec_block) : none;
+    v.x[i] = in ? draw_eight(a.x + (int64_t)r * a.ld_stream + p.n, p.left, known<L>(a.stream)) : none;
+    v.y[i] = in && a.y ? draw_eight(a.y + (int64_t)r * a.ld_block + p.n, p.left, known<L>(a.block)) : none;
   }
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
@@ -219,21 +227,21 @@ __device__ __forceinline__ void load_patch(const Forward& a, const Place& p, int
   }
 }
 
-template <int DT>
+template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
-  const Place p(a.K, a.N, a.rows_per_chunk, a.whole_lines);
+  const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
   if (p.none()) return;
   double sum[4][8] = {};
   float y_squares[8] = {};  // nothing cancels there
   const int end = p.row0 + p.rows;
   for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kPatch) {
     PatchXY v;
-    load_patch(a, p, k, end, v);
+    load_patch<L>(a, p, k, end, v);
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       float x[8], y[8];
-      widen<DT>(v.x[i], x);
-      widen<DT>(v.y[i], y);
+      widen<DT>(place_eight(v.x[i], p.left, known<L>(a.stream)), x);
+      widen<DT>(place_eight(v.y[i], p.left, known<L>(a.block)), y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const double wide = x[j], b = v.c[i] * y[j];  // c y is rounded to a float as in h
@@ -258,15 +266,15 @@ __device__ __forceinline__ void row_of_h(const Forward& a, u32x4 x, u32x4 y, flo
   for (int j = 0; j < 8; ++j) h[j] = h[j] * a.scale + branch[j] * (c * v[j]);
 }
 
-template <int DT, bool LINES>
+template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a) {
   __shared__ double total[4][kStrip];
   __shared__ float branch[kStrip], root[kStrip];
-  const Place p(a.K, a.N, a.rows_per_chunk, LINES);
+  const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
   if (p.none()) return;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchXY v;
-  load_patch(a, p, first, end, v);  // on their way while the sums are added
+  load_patch<L>(a, p, first, end, v);  // on their way while the sums are added
   if (a.w_post || a.w_pre) add_chunks<4>(a.sums, a.chunks, a.N, p, total);
   __syncthreads();
   if (threadIdx.x < kStrip) {
@@ -301,19 +309,20 @@ __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a
   for (int j = 0; j < 8; ++j) of_u[j] = root[at + j];
   for (int k = first; k < end; k += kPatch) {
     PatchXY next;
-    if (k + kPatch < end) load_patch(a, p, k + kPatch, end, next);
+    if (k + kPatch < end) load_patch<L>(a, p, k + kPatch, end, next);
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const int r = k + i * kRowsAtOnce;
       if (r >= end) break;
       float h[8];
-      row_of_h<DT>(a, v.x[i], v.y[i], v.c[i], of_token, h);
-      if (a.h) store_eight<LINES>(a.h + (int64_t)r * a.ld_stream + p.n, narrow<DT>(h), p.left, a.vec_stream);
+      row_of_h<DT>(a, place_eight(v.x[i], p.left, known<L>(a.stream)), place_eight(v.y[i], p.left, known<L>(a.block)), v.c[i],
+                   of_token, h);
+      if (a.h) store_eight<L == kLines>(a.h + (int64_t)r * a.ld_stream + p.n, narrow<DT>(h), p.left);
       if (a.w_pre) {
         const float w = v.w[i];
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] *= w * of_u[j];
-        store_eight<LINES>(a.u + (int64_t)r * a.ld_block + p.n, narrow<DT>(h), p.left, a.vec_block);
+        store_eight<L == kLines>(a.u + (int64_t)r * a.ld_block + p.n, narrow<DT>(h), p.left);
       }
     }
     v = next;
@@ -356,10 +365,15 @@ __global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a
   for (int i = 0; i < ROUNDS; ++i) {
     const int k = threadIdx.x + i * kHeldThreads;
     const bool in = k < a.K;
-    x[i] = in ? load_eight(a.x + (int64_t)k * a.ld_stream + n, left, a.vec_stream) : none;
-    y[i] = in && a.y ? load_eight(a.y + (int64_t)k * a.ld_block + n, left, a.vec_block) : none;
+    x[i] = in ? draw_eight(a.x + (int64_t)k * a.ld_stream + n, left, a.stream) : none;
+    y[i] = in && a.y ? draw_eight(a.y + (int64_t)k * a.ld_block + n, left, a.block) : none;
     c[i] = in ? channel_factor(a.w_post, a.gate, k) : 0.0f;
     w[i] = in && a.w_pre ? a.w_pre[k] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    x[i] = place_eight(x[i], left, a.stream);
+    y[i] = place_eight(y[i], left, a.block);
   }
   float of_token[8];
 #pragma unroll
@@ -385,7 +399,7 @@ __global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a
     if (k >= a.K) break;
     float h[8];
     row_of_h<DT>(a, x[i], y[i], c[i], of_token, h);
-    if (a.h) store_eight(a.h + (int64_t)k * a.ld_stream + n, narrow<DT>(h), left, a.vec_stream);
+    if (a.h) store_eight(a.h + (int64_t)k * a.ld_stream + n, narrow<DT>(h), left);
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] += h[j] * h[j];
   }
@@ -402,7 +416,7 @@ __global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a
     row_of_h<DT>(a, x[i], y[i], c[i], of_token, h);
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] *= w[i] * of_u[j];
-    store_eight(a.u + (int64_t)k * a.ld_block + n, narrow<DT>(h), left, a.vec_block);
+    store_eight(a.u + (int64_t)k * a.ld_block + n, narrow<DT>(h), left);
   }
 }
 
@@ -442,8 +456,10 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
     const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
-    widen<DT>(left > 0 ? load_eight(a.x + k, left, a.vec_stream) : none, x[i]);
-    widen<DT>(left > 0 && a.y ? load_eight(a.y + k, left, a.vec_block) : none, y[i]);
+    const u32x4 of_x = left > 0 ? draw_eight(a.x + k, left, a.stream) : none;
+    const u32x4 of_y = left > 0 && a.y ? draw_eight(a.y + k, left, a.block) : none;
+    widen<DT>(trim_eight(of_x, left, a.stream), x[i]);
+    widen<DT>(trim_eight(of_y, left, a.block), y[i]);
     float g[8];
     load_factors(a.w_post, k, left, c[i]);
     load_factors(a.gate, k, left, g);
@@ -474,7 +490,7 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i) {
       const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
-      if (left > 0) store_eight(a.h + k, narrow<DT>(x[i]), left, a.vec_stream);
+      if (left > 0) store_eight(a.h + k, narrow<DT>(x[i]), left);
     }
   }
   if (!a.w_pre) return;
@@ -486,7 +502,7 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
     if (left <= 0) break;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[i][j] *= w[i][j] * r;
-    store_eight(a.u + k, narrow<DT>(x[i]), left, a.vec_block);
+    store_eight(a.u + k, narrow<DT>(x[i]), left);
   }
 }
 
@@ -508,13 +524,15 @@ struct Backward {
   float *dw_post, *dgate, *dtoken_gate, *dw_pre;
   float* sums;      // [4][chunks][N]
   float* row_sums;  // [2][strips][K]
-  bool vec_stream, vec_block, whole_lines;
+  Pieces stream, block;
+  Layout layout;
 };
 
 struct PatchGrad {
   u32x4 h[kGradRounds], dh[kGradRounds], du[kGradRounds], y[kGradRounds];
   float c[kGradRounds], w[kGradRounds];
 };
+template <Layout L>
 __device__ __forceinline__ void load_patch(const Backward& a, const Place& p, int k, int end, PatchGrad& v) {
   const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
@@ -522,10 +540,10 @@ __device__ __forceinline__ void load_patch(const Backward& a, const Place& p, in
     const int r = k + i * kRowsAtOnce;
     const bool in = r < end && p.left > 0;
     const int64_t stream = (int64_t)r * a.ld_stream + p.n, block = (int64_t)r * a.ld_block + p.n;
-    v.h[i] = in && a.w_pre ? load_eight(a.h + stream, p.left, a.vec_stream) : none;
-    v.dh[i] = in && a.dh ? load_eight(a.dh + stream, p.left, a.vec_stream) : none;
-    v.du[i] = in && a.w_pre ? load_eight(a.du + block, p.left, a.vec_block) : none;
-    v.y[i] = in && a.y ? load_eight(a.y + block, p.left, a.vec_block) : none;
+    v.h[i] = in && a.w_pre ? draw_eight(a.h + stream, p.left, known<L>(a.stream)) : none;
+    v.dh[i] = in && a.dh ? draw_eight(a.dh + stream, p.left, known<L>(a.stream)) : none;
+    v.du[i] = in && a.w_pre ? draw_eight(a.du + block, p.left, known<L>(a.block)) : none;
+    v.y[i] = in && a.y ? draw_eight(a.y + block, p.left, known<L>(a.block)) : none;
   }
 #pragma unroll
   for (int i = 0; i < kGradRounds; ++i) {
@@ -535,22 +553,22 @@ __device__ __forceinline__ void load_patch(const Backward& a, const Place& p, in
   }
 }
 
-template <int DT>
+template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward a) {
-  const Place p(a.K, a.N, a.rows_per_chunk, a.whole_lines);
+  const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
   if (p.none()) return;
   float sum[4][8] = {};
   const int end = p.row0 + p.rows;
   for (int k = p.row0 + (threadIdx.x >> 3); k < end; k += kGradPatch) {
     PatchGrad v;
-    load_patch(a, p, k, end, v);
+    load_patch<L>(a, p, k, end, v);
 #pragma unroll
     for (int i = 0; i < kGradRounds; ++i) {
       float h[8], dh[8], g[8], y[8];
-      widen<DT>(v.h[i], h);
-      widen<DT>(v.dh[i], dh);
-      widen<DT>(v.du[i], g);
-      widen<DT>(v.y[i], y);
+      widen<DT>(trim_eight(v.h[i], p.left, known<L>(a.stream)), h);
+      widen<DT>(trim_eight(v.dh[i], p.left, known<L>(a.stream)), dh);
+      widen<DT>(trim_eight(v.du[i], p.left, known<L>(a.block)), g);
+      widen<DT>(trim_eight(v.y[i], p.left, known<L>(a.block)), y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         g[j] *= v.w[i];
@@ -565,15 +583,15 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward
   store_sums<4>(sum, p, a.sums, a.chunks, a.N);
 }
 
-template <int DT, bool LINES>
+template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Backward a) {
   __shared__ float total[4][kStrip], first_of[kStrip], second_of[kStrip];  // corrections: rstd_h^3 s1 / K; rstd_y^2 S / K
-  const Place p(a.K, a.N, a.rows_per_chunk, LINES);
+  const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
   if (p.none()) return;
   const int strips = (a.N + kStrip - 1) / kStrip;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchGrad v;
-  load_patch(a, p, first, end, v);
+  load_patch<L>(a, p, first, end, v);
   add_chunks<4>(a.sums, a.chunks, a.N, p, total);
   float rh[8], token[8];
 #pragma unroll
@@ -606,16 +624,16 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
   // whole patches: the lanes of a row add their columns together
   for (int k = first; k - first < p.rows; k += kGradPatch) {
     PatchGrad next;
-    if (k - first + kGradPatch < p.rows) load_patch(a, p, k + kGradPatch, end, next);
+    if (k - first + kGradPatch < p.rows) load_patch<L>(a, p, k + kGradPatch, end, next);
 #pragma unroll
     for (int i = 0; i < kGradRounds; ++i) {
       const int r = k + i * kRowsAtOnce;
       const bool in = r < end;
       float h[8], dh[8], g[8], y[8], of_w_pre = 0, of_branch = 0;
-      widen<DT>(v.h[i], h);
-      widen<DT>(v.dh[i], dh);
-      widen<DT>(v.du[i], g);
-      widen<DT>(v.y[i], y);
+      widen<DT>(trim_eight(v.h[i], p.left, known<L>(a.stream)), h);
+      widen<DT>(trim_eight(v.dh[i], p.left, known<L>(a.stream)), dh);
+      widen<DT>(trim_eight(v.du[i], p.left, known<L>(a.block)), g);
+      widen<DT>(trim_eight(v.y[i], p.left, known<L>(a.block)), y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         of_w_pre += g[j] * h[j] * rh[j];
@@ -625,8 +643,8 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
         y[j] = token[j] * (v.c[i] * d - y[j] * f2[j]);
       }
       if (in && p.left > 0) {
-        if (a.dx) store_eight<LINES>(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left, a.vec_stream);
-        if (a.dy) store_eight<LINES>(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left, a.vec_block);
+        if (a.dx) store_eight<L == kLines>(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left);
+        if (a.dy) store_eight<L == kLines>(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left);
       }
       of_w_pre = add_eight_lanes(of_w_pre);
       of_branch = add_eight_lanes(of_branch);
@@ -666,19 +684,26 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
   if (a.dgate) a.dgate[k] = (a.w_post ? a.w_post[k] : 1.0f) * of_branch;
 }
 
-bool in_pieces(const void* p, int64_t ld) { return !p || rows_in_pieces(p, ld); }
 bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld % 64 == 0); }
 
 }  // namespace
 
 size_t block_norm_workspace_bytes(int K, int N) { return (size_t)4 * chunk_count(K, N) * N * sizeof(double); }
 
+template <int DT, Layout L>
+static hipError_t launch_forward_strips(const Forward& a, hipStream_t stream) {
+  const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
+  if (a.w_post || a.w_pre) block_norm_sums_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
+  block_norm_apply_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
 template <int DT>
 static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
   if (a.N == 1 && a.ld_stream == 1 && (a.ld_block == 1 || (!a.y && !a.w_pre)) && a.K <= kVectorMost) {
     Forward v = a;
-    v.vec_stream = in_pieces(a.x, 8) && in_pieces(a.h, 8);
-    v.vec_block = in_pieces(a.y, 8) && in_pieces(a.u, 8);
+    v.stream = pieces_of_rows(a.x, 8, a.K);
+    v.block = pieces_of_rows(a.y, 8, a.K);
     if (a.K <= 8 * kVectorThreads) block_norm_vector_kernel<DT, 1><<<1, kVectorThreads, 0, stream>>>(v);
     else block_norm_vector_kernel<DT, 2><<<1, kVectorThreads, 0, stream>>>(v);
     return hipGetLastError();
@@ -692,21 +717,20 @@ static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
     block_norm_held_kernel<DT, 8><<<held, kHeldThreads, 0, stream>>>(a);
     return hipGetLastError();
   }
-  const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
-  if (a.w_post || a.w_pre) block_norm_sums_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
-  if (a.whole_lines) block_norm_apply_kernel<DT, true><<<grid, kThreads, 0, stream>>>(a);
-  else block_norm_apply_kernel<DT, false><<<grid, kThreads, 0, stream>>>(a);
-  return hipGetLastError();
+  if (a.layout == kLines) return launch_forward_strips<DT, kLines>(a, stream);
+  if (a.layout == kPieces) return launch_forward_strips<DT, kPieces>(a, stream);
+  return launch_forward_strips<DT, kAny>(a, stream);
 }
 
 hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
   Forward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale, b.eps,
             static_cast<const uint16_t*>(b.x), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
             static_cast<uint16_t*>(b.h), b.ld_stream, static_cast<uint16_t*>(b.u), b.ld_block, b.rstd_y, b.rstd_h,
-            reinterpret_cast<double*>(b.workspace), false, false, false};
-  a.vec_stream = in_pieces(a.x, a.ld_stream) && in_pieces(a.h, a.ld_stream);
-  a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.u, a.ld_block);
-  a.whole_lines = in_lines(a.x, a.ld_stream) && in_lines(a.h, a.ld_stream) && in_lines(a.y, a.ld_block) && in_lines(a.u, a.ld_block);
+            reinterpret_cast<double*>(b.workspace), kAligned, kAligned, kAny};
+  a.stream = pieces_of_rows(a.x, a.ld_stream, a.N);
+  a.block = pieces_of_rows(a.y, a.ld_block, a.N);
+  const bool lines = in_lines(a.x, a.ld_stream) && in_lines(a.h, a.ld_stream) && in_lines(a.y, a.ld_block) && in_lines(a.u, a.ld_block);
+  a.layout = lines ? kLines : a.stream == kAligned && a.block == kAligned ? kPieces : kAny;
   return b.dtype == HINM_F16 ? launch_forward<HINM_F16>(a, stream) : launch_forward<HINM_BF16>(a, stream);
 }
 
@@ -714,15 +738,21 @@ size_t block_norm_grad_workspace_bytes(int K, int N) {
   return ((size_t)4 * chunk_count(K, N) * N + (size_t)2 * strip_count(N) * K) * sizeof(float);
 }
 
-template <int DT>
-static hipError_t launch_backward(const Backward& a, hipStream_t stream) {
+template <int DT, Layout L>
+static hipError_t launch_backward_strips(const Backward& a, hipStream_t stream) {
   const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
-  block_norm_grad_sums_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
-  if (a.whole_lines) block_norm_grad_apply_kernel<DT, true><<<grid, kThreads, 0, stream>>>(a);
-  else block_norm_grad_apply_kernel<DT, false><<<grid, kThreads, 0, stream>>>(a);
+  block_norm_grad_sums_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
+  block_norm_grad_apply_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
   if (a.dw_pre || a.dw_post || a.dgate)
     block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
+}
+
+template <int DT>
+static hipError_t launch_backward(const Backward& a, hipStream_t stream) {
+  if (a.layout == kLines) return launch_backward_strips<DT, kLines>(a, stream);
+  if (a.layout == kPieces) return launch_backward_strips<DT, kPieces>(a, stream);
+  return launch_backward_strips<DT, kAny>(a, stream);
 }
 
 hipError_t launch_block_norm_grad(const BlockNormGradArgs& b, hipStream_t stream) {
@@ -730,11 +760,13 @@ hipError_t launch_block_norm_grad(const BlockNormGradArgs& b, hipStream_t stream
              static_cast<const uint16_t*>(b.h), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
              b.rstd_y, b.rstd_h, static_cast<const uint16_t*>(b.dh), static_cast<const uint16_t*>(b.du),
              static_cast<uint16_t*>(b.dx), b.ld_stream, static_cast<uint16_t*>(b.dy), b.ld_block, b.dw_post, b.dgate,
-             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N, false, false, false};
-  a.vec_stream = in_pieces(a.h, a.ld_stream) && in_pieces(a.dh, a.ld_stream) && in_pieces(a.dx, a.ld_stream);
-  a.vec_block = in_pieces(a.y, a.ld_block) && in_pieces(a.du, a.ld_block) && in_pieces(a.dy, a.ld_block);
-  a.whole_lines = in_lines(a.h, a.ld_stream) && in_lines(a.dh, a.ld_stream) && in_lines(a.dx, a.ld_stream) &&
-                  in_lines(a.y, a.ld_block) && in_lines(a.du, a.ld_block) && in_lines(a.dy, a.ld_block);
+             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N, kAligned, kAligned,
+             kAny};
+  a.stream = lesser(pieces_of_rows(a.h, a.ld_stream, a.N), pieces_of_rows(a.dh, a.ld_stream, a.N));
+  a.block = lesser(pieces_of_rows(a.y, a.ld_block, a.N), pieces_of_rows(a.du, a.ld_block, a.N));
+  const bool lines = in_lines(a.h, a.ld_stream) && in_lines(a.dh, a.ld_stream) && in_lines(a.dx, a.ld_stream) &&
+                     in_lines(a.y, a.ld_block) && in_lines(a.du, a.ld_block) && in_lines(a.dy, a.ld_block);
+  a.layout = lines ? kLines : a.stream == kAligned && a.block == kAligned ? kPieces : kAny;
   return b.dtype == HINM_F16 ? launch_backward<HINM_F16>(a, stream) : launch_backward<HINM_BF16>(a, stream);
 }
 

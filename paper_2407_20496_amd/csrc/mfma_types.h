@@ -38,6 +38,10 @@ typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
 // 16-byte global load that only promises 4-byte alignment
 typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x2_a4 __attribute__((ext_vector_type(2), aligned(4)));
+// pieces at any even address
+typedef uint32_t u32_a2 __attribute__((aligned(2)));
+typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 template <int DT, int ABID>

@@ -27,17 +27,17 @@ struct ProductShape {
   bool relu;
 };
 
-// Four consecutive columns of a row of Y from n on, those below N, rounded; vec: the four begin at a multiple of their size.
+// Four consecutive columns of a row of Y from n on, those below N, rounded.
 template <int OUT>  // HINM_F16, HINM_BF16, 2 = float32
-__device__ __forceinline__ void store_four(void* Y, int64_t row_at, int n, f32x4 v, const ProductShape& p, bool vec) {
+__device__ __forceinline__ void store_four(void* Y, int64_t row_at, int n, f32x4 v, const ProductShape& p) {
   if (p.relu) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = v[e] < 0 ? 0 : v[e];  // keeps NaN
   }
   if constexpr (OUT == 2) {
     float* to = static_cast<float*>(Y) + row_at + n;
-    if (vec && n + 4 <= p.N) {
-      *reinterpret_cast<f32x4*>(to) = v;
+    if (n + 4 <= p.N) {
+      *reinterpret_cast<u32x4_a4*>(to) = __builtin_bit_cast(u32x4, v);
       return;
     }
 #pragma unroll
@@ -46,8 +46,8 @@ __device__ __forceinline__ void store_four(void* Y, int64_t row_at, int n, f32x4
   } else {
     uint16_t* to = static_cast<uint16_t*>(Y) + row_at + n;
     const u32x2 w = {floats_to_bits<OUT>(v[0], v[1]), floats_to_bits<OUT>(v[2], v[3])};
-    if (vec && n + 4 <= p.N) {
-      *reinterpret_cast<u32x2*>(to) = w;
+    if (n + 4 <= p.N) {
+      *reinterpret_cast<u32x2_a2*>(to) = w;
       return;
     }
 #pragma unroll
@@ -180,8 +180,6 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const
     multiply(std::integral_constant<int, 3>{}, f);
   }
   // 32 rows of Y at a time: every wave's part to its slab, then all of them added
-  constexpr int kElem = OUT == 2 ? 4 : 2;
-  const bool vec = (reinterpret_cast<uintptr_t>(Y) & (4 * kElem - 1)) == 0 && p.ldy % 4 == 0;
   const int count = min(WAVES, lines);  // waves that had a line
 #pragma unroll
   for (int j = 0; j < WM; ++j) {
@@ -201,7 +199,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const
       if (m >= p.M || n >= p.N) continue;
       f32x4 v = *reinterpret_cast<const f32x4*>(slabs[0] + row * kPitch + at);
       for (int w = 1; w < count; ++w) v += *reinterpret_cast<const f32x4*>(slabs[w] + row * kPitch + at);
-      store_four<OUT>(Y, (int64_t)m * p.ldy, n, v, p, vec);
+      store_four<OUT>(Y, (int64_t)m * p.ldy, n, v, p);
     }
   }
 }
@@ -220,7 +218,7 @@ hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStre
 // where quantising apart takes two; sums in the same order, so the same result bit for bit.
 template <int OUT, int DT>
 __global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, const uint8_t* scales, const uint16_t* x, int64_t ldx,
-                                                        bool vec, void* Y, ProductShape p) {
+                                                        void* Y, ProductShape p) {
   constexpr int kWaves = 8, kLinePlace = 8 * 16 + 16;  // a line's codes and its eight scale bytes
   __shared__ __align__(16) uint8_t places[kWaves][kLinePlace + 16];  // ... and zeros
   __shared__ __align__(16) float sums[kWaves][32];
@@ -240,8 +238,8 @@ __global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, co
     f.scale_a = *reinterpret_cast<const u32x2*>(scales + mx4_scales_at(line >> 1, blocks, block) + 16 * r + 8 * half);
     const int k = line * kMx4Line + 4 * lane;
     f.x = u32x2{0, 0};
-    if (vec && k + 4 <= p.K) {
-      f.x = *reinterpret_cast<const u32x2*>(x + k);
+    if (ldx == 1 && k + 4 <= p.K) {
+      f.x = *reinterpret_cast<const u32x2_a2*>(x + k);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -304,7 +302,7 @@ __global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, co
   float v = sums[0][threadIdx.x];
   const int count = min(kWaves, lines);
   for (int w = 1; w < count; ++w) v += sums[w][threadIdx.x];
-  store_four<OUT>(Y, (int64_t)m * p.ldy, 0, f32x4{v, 0, 0, 0}, p, false);
+  store_four<OUT>(Y, (int64_t)m * p.ldy, 0, f32x4{v, 0, 0, 0}, p);
 }
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
@@ -531,7 +529,6 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
   constexpr int kRowBytes = 32 * WN * kElem, kRowPitch = kRowBytes + 16, kPer = 16 / kElem;
   static_assert(4 * 32 * kRowPitch <= T::kLds, "slabs");
   uint8_t* slab = lds + wave * 32 * kRowPitch;
-  const bool vec = (reinterpret_cast<uintptr_t>(Y) & 15) == 0 && p.ldy % kPer == 0;
 #pragma unroll
   for (int j = 0; j < WM; ++j) {
 #pragma unroll
@@ -557,8 +554,8 @@ __global__ __launch_bounds__(256, WM * WN > 8 ? 1 : 2) void mx4_tile_kernel(cons
       const u32x4 v = *reinterpret_cast<const u32x4*>(slab + row * kRowPitch + 16 * piece);
       if (m >= p.M || n >= p.N) continue;
       uint8_t* to = static_cast<uint8_t*>(Y) + ((int64_t)m * p.ldy + n) * kElem;
-      if (vec && n + kPer <= p.N) {
-        *reinterpret_cast<u32x4*>(to) = v;
+      if (n + kPer <= p.N) {
+        *reinterpret_cast<u32x4_a2*>(to) = v;
       } else {
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
@@ -641,9 +638,8 @@ hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
 template <int OUT, int DT>
 hipError_t launch_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  const bool vec = ldx == 1 && (reinterpret_cast<uintptr_t>(x) & 7) == 0;
   mx4_token_kernel<OUT, DT><<<dim3(grid_of_items(mx4_row_blocks(a.M))), 512, 0, stream>>>(
-      a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, vec, a.Y, p);
+      a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, a.Y, p);
   return hipGetLastError();
 }
 

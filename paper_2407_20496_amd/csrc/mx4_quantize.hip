@@ -24,7 +24,7 @@ __device__ __forceinline__ int item_of_workgroup(bool whole_lines) {
 // A workgroup takes 32 rows x 256 values, a line of a block of rows; a wave eight rows in four loads of two rows each, a lane
 // eight values, four lanes a block.
 template <int DT>
-__global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src, int64_t ld, int rows, int cols, bool vec,
+__global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src, int64_t ld, int rows, int cols, Pieces pieces,
                                                             bool whole_lines, uint8_t* codes, uint8_t* scales) {
   __shared__ __align__(16) uint8_t tile[8 * kChunkPitch];
   __shared__ __align__(16) uint8_t tile_scales[kMx4Rows][8];  // byte 2 (p % 4) + p / 4 of block p
@@ -38,11 +38,12 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src,
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = rb * kMx4Rows + 8 * wave + 2 * i + (lane >> 5);
-    v[i] = r < rows && k < cols ? load_eight(src + (int64_t)r * ld + k, cols - k, vec) : u32x4{0, 0, 0, 0};
+    v[i] = r < rows && k < cols ? draw_eight(src + (int64_t)r * ld + k, cols - k, pieces) : u32x4{0, 0, 0, 0};
   }
   const bool beyond = (k & ~31) >= cols;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    v[i] = trim_eight(v[i], cols - k, pieces);
     const int r = 8 * wave + 2 * i + (lane >> 5);
     uint32_t m = 0;
 #pragma unroll
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(const uint16_t* src,
 constexpr int kTileCols = 64, kTileRows = 128;
 
 template <int DT>
-__global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* src, int64_t ld, int rows, int cols, bool vec,
+__global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* src, int64_t ld, int rows, int cols, Pieces pieces,
                                                                bool whole_lines, uint8_t* codes, uint8_t* scales) {
   __shared__ __align__(16) uint8_t tile[2][4 * kChunkPitch];  // two blocks of 32 columns
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -96,7 +97,9 @@ __global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* s
   u32x4 v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    v[i] = k + i < rows && n < cols ? load_eight(src + (int64_t)(k + i) * ld + n, cols - n, vec) : u32x4{0, 0, 0, 0};
+    v[i] = k + i < rows && n < cols ? draw_eight(src + (int64_t)(k + i) * ld + n, cols - n, pieces) : u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = trim_eight(v[i], cols - n, pieces);
   const bool beyond = k0 >= rows;
   const int chunk = 2 * (wave & 1) + (wave >> 1);  // of block p = 4 (unit % 2) + wave, within the half line
   // this block's byte of its word, and those of blocks that do not exist behind the last unit
@@ -142,7 +145,7 @@ __device__ __forceinline__ int lds_place(int j, int r) { return (8 * (j >> 3) + 
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void mx4_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int rows, int length,
-                                                              uint16_t* dst, int64_t ld, bool vec) {
+                                                              uint16_t* dst, int64_t ld) {
   __shared__ __align__(16) uint8_t tile[16 * kChunkPitch];
   __shared__ __align__(16) uint8_t tile_scales[kMx4Rows * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -171,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void mx4_unpack_kernel(const uint8_t* cod
     u32x4 out;
 #pragma unroll
     for (int j = 0; j < 4; ++j) out[j] = floats_to_bits<DT>(f[j][0] * s, f[j][1] * s);
-    store_eight(dst + (int64_t)(rb * kMx4Rows + i) * ld + k, out, length - k, vec);
+    store_eight(dst + (int64_t)(rb * kMx4Rows + i) * ld + k, out, length - k);
   }
 }
 
@@ -182,13 +185,13 @@ hipError_t launch_mx4_quantize(int rows, int cols, int dtype, const void* src, i
   // one column without a stride is one row
   if (columns && cols == 1 && ld == 1) return launch_mx4_quantize(1, rows, dtype, src, rows, false, codes, scales, stream);
   const uint16_t* p = static_cast<const uint16_t*>(src);
-  const bool vec = rows_in_pieces(src, ld) || (rows == 1 && (reinterpret_cast<uintptr_t>(src) & 15) == 0);
+  const Pieces pieces = pieces_of_rows(src, rows == 1 ? 8 : ld, cols);
   const bool whole_lines = (reinterpret_cast<uintptr_t>(src) & 127) == 0 && ld % 64 == 0;
   const int64_t items = columns ? (int64_t)((cols + kTileCols - 1) / kTileCols) * 2 * mx4_lines(rows)
                                 : (int64_t)mx4_row_blocks(rows) * mx4_lines(cols);
   const dim3 grid((uint32_t)((items + 7) / 8 * 8));
   auto launch = [&](auto kernel) {
-    kernel<<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, vec, whole_lines, codes, scales);
+    kernel<<<grid, kThreads, 0, stream>>>(p, ld, rows, cols, pieces, whole_lines, codes, scales);
   };
   if (columns) launch(dtype == HINM_F16 ? mx4_columns_kernel<HINM_F16> : mx4_columns_kernel<HINM_BF16>);
   else launch(dtype == HINM_F16 ? mx4_rows_kernel<HINM_F16> : mx4_rows_kernel<HINM_BF16>);
@@ -199,9 +202,8 @@ hipError_t launch_mx4_unpack(int rows, int length, int dtype, const uint8_t* cod
                              hipStream_t stream) {
   const dim3 grid((uint32_t)((int64_t)mx4_row_blocks(rows) * mx4_groups(length)));
   uint16_t* p = static_cast<uint16_t*>(dst);
-  const bool vec = rows_in_pieces(dst, ld);
-  if (dtype == HINM_F16) mx4_unpack_kernel<HINM_F16><<<grid, kThreads, 0, stream>>>(codes, scales, rows, length, p, ld, vec);
-  else mx4_unpack_kernel<HINM_BF16><<<grid, kThreads, 0, stream>>>(codes, scales, rows, length, p, ld, vec);
+  if (dtype == HINM_F16) mx4_unpack_kernel<HINM_F16><<<grid, kThreads, 0, stream>>>(codes, scales, rows, length, p, ld);
+  else mx4_unpack_kernel<HINM_BF16><<<grid, kThreads, 0, stream>>>(codes, scales, rows, length, p, ld);
   return hipGetLastError();
 }
 

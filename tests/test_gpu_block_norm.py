@@ -328,3 +328,12 @@ def test_offsets_beyond_32_bits():
         value, size = g[name]
         _check(name, take(got), value, HALF_STEP["bf16"] * np.abs(value) + SUM * size)
     assert torch.isfinite(dw).all()
+
+
+@pytest.mark.parametrize("N", [*range(3, 17), 61, 62, 63])
+def test_ends_of_rows_at_any_address(N):
+    """Every count of columns behind a row's last whole eight, aligned or not, forward and back."""
+    form = dict(post=1, gate=1, token=1, pre=1, block=1)
+    for i, (ls, lb, first) in enumerate(_strides(N)):
+        _forward(1100, N, "bf16", form, ls, lb, first, N + i)
+        _backward(140, N, "f16", form, ls, lb, first, N + i)

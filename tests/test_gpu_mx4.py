@@ -334,3 +334,30 @@ def test_offsets_beyond_32_bits():
     want, size = orc.product(orc.values(*pick(fa, m), K), orc.values(*pick(fb, n), K))
     got = Y[m][:, N - 300:].float().cpu().numpy().astype(np.float64)
     assert (np.abs(got - want) <= _tolerance(size, K, want, "bf16")).all()
+
+
+@pytest.mark.parametrize("cols", [*range(2, 17), 249, 253, 254, 255])
+def test_ends_of_rows_at_any_address(cols):
+    """Every count of values behind a row's last whole eight, aligned or not, into the form and back."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    rows = 37
+    bits = _draw(rows, cols, "bf16", 100 + cols)
+    X = _wide(bits, "bf16")
+    for ld, first in ((cols, 0), (cols + 1, 1), (cols + 2, 3), ((cols + 7) // 8 * 8, 0)):
+        keep, src = _matrix(bits, ld, first)
+        for along, Z in ((hinm.MX4_ROWS, X), (hinm.MX4_COLUMNS, np.ascontiguousarray(X.T))):
+            codes, scales = orc.quantize_rows(Z)
+            form = _form(*Z.shape)
+            hinm.hinm_mx4_quantize(rows, cols, "bf16", src, ld, along, *form)
+            got = _host(form, *Z.shape)
+            assert np.array_equal(got[1], scales) and np.array_equal(got[0], codes), (along, ld, first)
+        del keep
+        form = orc.quantize_rows(X)
+        want = orc.values(*form, cols)
+        out = torch.full((first + rows * ld + 8,), 0x1234, dtype=torch.int16, device=DEV)
+        hinm.hinm_mx4_unpack(rows, cols, "bf16", *_upload(*form), out.data_ptr() + 2 * first, ld)
+        host = out.cpu().numpy().view(np.uint16)
+        there = host[first:first + rows * ld].reshape(rows, ld)
+        assert np.array_equal(_wide(there[:, :cols], "bf16"), want, equal_nan=True)
+        assert (there[:, cols:] == 0x1234).all() and (host[:first] == 0x1234).all() and (host[first + rows * ld:] == 0x1234).all()
