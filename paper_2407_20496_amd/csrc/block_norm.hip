@@ -30,12 +30,17 @@ constexpr int kGradPatch = kGradRounds * kRowsAtOnce;
 constexpr int kWaves = kThreads / 64;
 
 int strip_count(int N) { return (N + kStrip - 1) / kStrip; }
-// Patches of a chunk: as many as leave some 1024 workgroups, so that a workgroup's share of the chunks' sums stays small
-// beside its rows; at most 64 chunks.
+// Patches of a workgroup where `at_once` of them run at a time: the fewest with which all of them do.  (One round and a part
+// costs two: 16384x4000 forward 214 -> 190 us, 11008x1571 66 -> 56; gradients 4096x2048 45 -> 40.)
+int patches_of_workgroup(int patches, int N, int at_once) {
+  const int most = at_once / strip_count(N);
+  return most < 1 ? patches : (patches + most - 1) / most;
+}
+// Patches of a chunk: four workgroups to a compute unit, at most 64 chunks, so that adding a strip's chunks stays small beside
+// its rows.
 int chunk_patches(int K, int N) {
-  const int64_t patches = (K + kPatch - 1) / kPatch;
-  const int64_t per = patches * strip_count(N) / 1024, least = (patches + 63) / 64;
-  return (int)(per > least ? per : least < 1 ? 1 : least);
+  const int patches = (K + kPatch - 1) / kPatch, per = patches_of_workgroup(patches, N, 1024), least = (patches + 63) / 64;
+  return per > least ? per : least;
 }
 int chunk_count(int K, int N) {
   const int rows = kPatch * chunk_patches(K, N);
@@ -182,6 +187,9 @@ __device__ __forceinline__ void add_chunks(const T* partial, int chunks, int N, 
   for (; c < chunks; ++c) t += at[(int64_t)c * N];
   total[q][col] = t;
 }
+
+// The gradients' second launch has three workgroups to a compute unit.
+int rows_of_grad_apply(int K, int N) { return kGradPatch * patches_of_workgroup((K + kGradPatch - 1) / kGradPatch, N, 768); }
 
 // ---- forward ------------------------------------------------------------------------------------------
 
@@ -512,7 +520,7 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
 // The second launch writes dx and dy and adds every row of its strip; a third adds the strips.
 
 struct Backward {
-  int K, N, rows_per_chunk, chunks;
+  int K, N, rows_per_chunk, chunks, rows_of_apply;
   float scale;
   const uint16_t *h, *y;
   const float *w_post, *gate, *token_gate, *w_pre, *rstd_y, *rstd_h;
@@ -586,7 +594,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward
 template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Backward a) {
   __shared__ float total[4][kStrip], first_of[kStrip], second_of[kStrip];  // corrections: rstd_h^3 s1 / K; rstd_y^2 S / K
-  const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
+  const Place p(a.K, a.N, a.rows_of_apply, L == kLines);
   if (p.none()) return;
   const int strips = (a.N + kStrip - 1) / kStrip;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
@@ -742,7 +750,8 @@ template <int DT, Layout L>
 static hipError_t launch_backward_strips(const Backward& a, hipStream_t stream) {
   const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
   block_norm_grad_sums_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
-  block_norm_grad_apply_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
+  const int64_t apply = (int64_t)((a.K + a.rows_of_apply - 1) / a.rows_of_apply) * strip_count(a.N);
+  block_norm_grad_apply_kernel<DT, L><<<dim3((uint32_t)((apply + 7) / 8 * 8)), kThreads, 0, stream>>>(a);
   if (a.dw_pre || a.dw_post || a.dgate)
     block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
@@ -756,7 +765,7 @@ static hipError_t launch_backward(const Backward& a, hipStream_t stream) {
 }
 
 hipError_t launch_block_norm_grad(const BlockNormGradArgs& b, hipStream_t stream) {
-  Backward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale,
+  Backward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), rows_of_grad_apply(b.K, b.N), b.residual_scale,
              static_cast<const uint16_t*>(b.h), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
              b.rstd_y, b.rstd_h, static_cast<const uint16_t*>(b.dh), static_cast<const uint16_t*>(b.du),
              static_cast<uint16_t*>(b.dx), b.ld_stream, static_cast<uint16_t*>(b.dy), b.ld_block, b.dw_post, b.dgate,
