@@ -88,6 +88,7 @@ template <int DT>
 __global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* src, int64_t ld, int rows, int cols, Pieces pieces,
                                                                bool whole_lines, uint8_t* codes, uint8_t* scales) {
   __shared__ __align__(16) uint8_t tile[2][4 * kChunkPitch];  // two blocks of 32 columns
+  __shared__ uint8_t tile_scales[4 * kTileCols];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tiles = (cols + kTileCols - 1) / kTileCols, blocks = mx4_row_blocks(cols), units = 2 * mx4_lines(rows);
   const int item = item_of_workgroup(whole_lines);
@@ -102,8 +103,6 @@ __global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* s
   for (int i = 0; i < 4; ++i) v[i] = trim_eight(v[i], cols - n, pieces);
   const bool beyond = k0 >= rows;
   const int chunk = 2 * (wave & 1) + (wave >> 1);  // of block p = 4 (unit % 2) + wave, within the half line
-  // this block's byte of its word, and those of blocks that do not exist behind the last unit
-  const int step = unit & 3, fill = unit == units - 1 && step == 1 ? 2 : 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     uint32_t m = 0;
@@ -125,14 +124,17 @@ __global__ __launch_bounds__(kThreads) void mx4_columns_kernel(const uint16_t* s
       if (e == 255) c = 0;
       const int col = 8 * c8 + 2 * w + half;
       *reinterpret_cast<uint16_t*>(&tile[col >> 5][chunk * kChunkPitch + 16 * (col & 31) + 2 * rg]) = (uint16_t)c;
-      if (rg == 2 * w + half && n0 + col < cols) {
-        uint8_t* to = scales + mx4_scales_at(unit >> 2, blocks, (n0 + col) >> 5) + 16 * (col & 31) + 4 * wave + step;
-        to[0] = (uint8_t)(beyond ? 127 : e);
-        for (int q = 1; q <= fill; ++q) to[q] = 127;
-      }
+      if (rg == 2 * w + half) tile_scales[4 * col + wave] = (uint8_t)(beyond ? 127 : e);
     }
   }
   __syncthreads();
+  // a byte of each of a column's four words; the last unit writes those of blocks that do not exist too
+  const int col = threadIdx.x >> 2, step = unit & 3;
+  if (n0 + col < cols) {
+    uint8_t* to = scales + mx4_scales_at(unit >> 2, blocks, (n0 + col) >> 5) + 16 * (col & 31) + 4 * (threadIdx.x & 3) + step;
+    to[0] = tile_scales[threadIdx.x];
+    for (int q = 1; q <= (unit == units - 1 && step == 1 ? 2 : 0); ++q) to[q] = 127;
+  }
   const int b = threadIdx.x >> 7, r = threadIdx.x & 31;
   if (n0 + 32 * b + r >= cols) return;
   *reinterpret_cast<u32x4*>(codes + mx4_codes_at(unit >> 1, blocks, n0 / 32 + b) + 2048 * (unit & 1) + 16 * (threadIdx.x & 127)) =
