@@ -517,7 +517,8 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
 // ---- gradients ----------------------------------------------------------------------------------------
 // The second norm's correction needs S = sum_k c d y with d the gradient of h, which itself holds the first correction:
 //   s1 = sum_k w_pre du h,   S = sum_k c y dh + rstd_h sum_k c y w_pre du - rstd_h^3 s1 / K sum_k c y h.
-// The second launch writes dx and dy and adds every row of its strip; a third adds the strips.
+// The second launch writes dx and dy and adds every row of its strip; where there are several, a third adds them (4096x3
+// 14.7 -> 12 us without it).
 
 struct Backward {
   int K, N, rows_per_chunk, chunks, rows_of_apply;
@@ -535,6 +536,13 @@ struct Backward {
   Pieces stream, block;
   Layout layout;
 };
+
+// Channel k's, from its sums over all tokens of du h rstd_h and of d y rstd_y token_gate.
+__device__ __forceinline__ void store_weight_gradients(const Backward& a, int k, float of_w_pre, float of_branch) {
+  if (a.dw_pre) a.dw_pre[k] = of_w_pre;
+  if (a.dw_post) a.dw_post[k] = (a.gate ? a.gate[k] : 1.0f) * of_branch;
+  if (a.dgate) a.dgate[k] = (a.w_post ? a.w_post[k] : 1.0f) * of_branch;
+}
 
 struct PatchGrad {
   u32x4 h[kGradRounds], dh[kGradRounds], du[kGradRounds], y[kGradRounds];
@@ -657,8 +665,12 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
       of_w_pre = add_eight_lanes(of_w_pre);
       of_branch = add_eight_lanes(of_branch);
       if (in && (threadIdx.x & 7) == 0) {
-        a.row_sums[(int64_t)p.strip * a.K + r] = of_w_pre;
-        a.row_sums[(int64_t)(strips + p.strip) * a.K + r] = of_branch;
+        if (strips == 1) {
+          store_weight_gradients(a, r, of_w_pre, of_branch);
+        } else {
+          a.row_sums[(int64_t)p.strip * a.K + r] = of_w_pre;
+          a.row_sums[(int64_t)(strips + p.strip) * a.K + r] = of_branch;
+        }
       }
     }
     v = next;
@@ -687,9 +699,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
     of_w_pre += part[0][t][col];
     of_branch += part[1][t][col];
   }
-  if (a.dw_pre) a.dw_pre[k] = of_w_pre;
-  if (a.dw_post) a.dw_post[k] = (a.gate ? a.gate[k] : 1.0f) * of_branch;
-  if (a.dgate) a.dgate[k] = (a.w_post ? a.w_post[k] : 1.0f) * of_branch;
+  store_weight_gradients(a, k, of_w_pre, of_branch);
 }
 
 bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld % 64 == 0); }
@@ -752,7 +762,7 @@ static hipError_t launch_backward_strips(const Backward& a, hipStream_t stream) 
   block_norm_grad_sums_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
   const int64_t apply = (int64_t)((a.K + a.rows_of_apply - 1) / a.rows_of_apply) * strip_count(a.N);
   block_norm_grad_apply_kernel<DT, L><<<dim3((uint32_t)((apply + 7) / 8 * 8)), kThreads, 0, stream>>>(a);
-  if (a.dw_pre || a.dw_post || a.dgate)
+  if (strip_count(a.N) > 1 && (a.dw_pre || a.dw_post || a.dgate))
     block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
