@@ -169,6 +169,7 @@ __device__ __forceinline__ void store_sums(const T (&sum)[QUANTITIES][8], const 
 }
 
 // ... and their totals over the chunks, to total[quantity][64].  The caller waits at a barrier.
+constexpr int kChunksAtOnce = 8;
 template <int QUANTITIES, class T>
 __device__ __forceinline__ void add_chunks(const T* partial, int chunks, int N, const Place& p, T (*total)[kStrip]) {
   static_assert(QUANTITIES <= kThreads / kStrip, "a thread for each");
@@ -176,25 +177,24 @@ __device__ __forceinline__ void add_chunks(const T* partial, int chunks, int N, 
   if (q >= QUANTITIES || n >= N) return;
   const T* at = partial + (int64_t)q * chunks * N + n;
   T t = 0;
-  int c = 0;
-  for (; c + 8 <= chunks; c += 8) {
-    T v[8];
+  for (int c = 0; c < chunks; c += kChunksAtOnce) {
+    T v[kChunksAtOnce];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = at[(int64_t)(c + j) * N];
+    for (int j = 0; j < kChunksAtOnce; ++j) v[j] = at[(int64_t)min(c + j, chunks - 1) * N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t += v[j];
+    for (int j = 0; j < kChunksAtOnce; ++j) t += c + j < chunks ? v[j] : T(0);
   }
-  for (; c < chunks; ++c) t += at[(int64_t)c * N];
   total[q][col] = t;
 }
 
-// The gradients' second launch has three workgroups to a compute unit.
+// Rows of a workgroup in the second launches: the gradients' has three to a compute unit.
+int rows_of_apply(int K, int N) { return kPatch * patches_of_workgroup((K + kPatch - 1) / kPatch, N, 1024); }
 int rows_of_grad_apply(int K, int N) { return kGradPatch * patches_of_workgroup((K + kGradPatch - 1) / kGradPatch, N, 768); }
 
 // ---- forward ------------------------------------------------------------------------------------------
 
 struct Forward {
-  int K, N, rows_per_chunk, chunks;
+  int K, N, rows_per_chunk, chunks, rows_of_apply;
   float scale, eps;
   const uint16_t *x, *y;
   const float *w_post, *gate, *token_gate, *w_pre;
@@ -278,7 +278,7 @@ template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a) {
   __shared__ double total[4][kStrip];
   __shared__ float branch[kStrip], root[kStrip];
-  const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
+  const Place p(a.K, a.N, a.rows_of_apply, L == kLines);
   if (p.none()) return;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchXY v;
@@ -702,6 +702,8 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
   store_weight_gradients(a, k, of_w_pre, of_branch);
 }
 
+// Workgroups for the list (chunk, strip), a multiple of the XCDs.
+dim3 grid_of(int chunks, int N) { return dim3((uint32_t)(((int64_t)chunks * strip_count(N) + 7) / 8 * 8)); }
 bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld % 64 == 0); }
 
 }  // namespace
@@ -710,9 +712,8 @@ size_t block_norm_workspace_bytes(int K, int N) { return (size_t)4 * chunk_count
 
 template <int DT, Layout L>
 static hipError_t launch_forward_strips(const Forward& a, hipStream_t stream) {
-  const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
-  if (a.w_post || a.w_pre) block_norm_sums_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
-  block_norm_apply_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
+  if (a.w_post || a.w_pre) block_norm_sums_kernel<DT, L><<<grid_of(a.chunks, a.N), kThreads, 0, stream>>>(a);
+  block_norm_apply_kernel<DT, L><<<grid_of((a.K + a.rows_of_apply - 1) / a.rows_of_apply, a.N), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -741,7 +742,7 @@ static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
 }
 
 hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
-  Forward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), b.residual_scale, b.eps,
+  Forward a{b.K, b.N, kPatch * chunk_patches(b.K, b.N), chunk_count(b.K, b.N), rows_of_apply(b.K, b.N), b.residual_scale, b.eps,
             static_cast<const uint16_t*>(b.x), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
             static_cast<uint16_t*>(b.h), b.ld_stream, static_cast<uint16_t*>(b.u), b.ld_block, b.rstd_y, b.rstd_h,
             reinterpret_cast<double*>(b.workspace), kAligned, kAligned, kAny};
@@ -758,10 +759,8 @@ size_t block_norm_grad_workspace_bytes(int K, int N) {
 
 template <int DT, Layout L>
 static hipError_t launch_backward_strips(const Backward& a, hipStream_t stream) {
-  const dim3 grid((uint32_t)((a.chunks * strip_count(a.N) + 7) / 8 * 8));
-  block_norm_grad_sums_kernel<DT, L><<<grid, kThreads, 0, stream>>>(a);
-  const int64_t apply = (int64_t)((a.K + a.rows_of_apply - 1) / a.rows_of_apply) * strip_count(a.N);
-  block_norm_grad_apply_kernel<DT, L><<<dim3((uint32_t)((apply + 7) / 8 * 8)), kThreads, 0, stream>>>(a);
+  block_norm_grad_sums_kernel<DT, L><<<grid_of(a.chunks, a.N), kThreads, 0, stream>>>(a);
+  block_norm_grad_apply_kernel<DT, L><<<grid_of((a.K + a.rows_of_apply - 1) / a.rows_of_apply, a.N), kThreads, 0, stream>>>(a);
   if (strip_count(a.N) > 1 && (a.dw_pre || a.dw_post || a.dgate))
     block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
   return hipGetLastError();
