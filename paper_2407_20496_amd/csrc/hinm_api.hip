@@ -753,7 +753,7 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const Mx4ProductArgs a{M, N, K, dtype, codes, scales, x_codes, x_scales, Y, ldy, (flags & HINM_EPI_RELU) != 0,
                          (flags & HINM_OUT_F32) != 0};
-  if (N == 1) return launched(launch_mx4_token(a, X, ldx, s));
+  if (mx4_quantises_on_the_way(a)) return launched(launch_mx4_on_the_way(a, X, ldx, s));
   const hipError_t e = launch_mx4_quantize(K, N, dtype, X, ldx, true, x_codes, x_scales, s);
   return launched(e == hipSuccess ? launch_mx4_product(a, s) : e);
 }

@@ -304,8 +304,10 @@ struct Mx4ProductArgs {
   bool out_f32;
 };
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream);
-// N = 1, B given as 16-bit values of stride ldx (b_codes and b_scales are not used): the product with their 4-bit form
-hipError_t launch_mx4_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream);
+// B given as 16-bit values [K][N] of stride ldx (b_codes and b_scales are not used): the product with their 4-bit form in one
+// launch, for the shapes that are faster so
+bool mx4_quantises_on_the_way(const Mx4ProductArgs& a);
+hipError_t launch_mx4_on_the_way(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream);
 
 // ---- norms around a block (block_norm.hip) -------------------------------------------------------------------
 struct BlockNormArgs {

@@ -70,10 +70,25 @@ uint32_t grid_of_items(int64_t items) { return (uint32_t)((items + 7) / 8 * 8); 
 // with no barrier between them, and add their tiles in LDS in a fixed order.  The operands of a line are loaded while the
 // line before it multiplies.  B is the instruction's row operand, so that a lane ends with four consecutive columns of Y.
 //   Rows of B beyond N lie beyond the buffer descriptor's bytes for their lanes: they read as zero and cost no traffic.
+constexpr int slab_pitch(int WN) { return 32 * WN + 4; }
+template <int OUT, int WN, int WAVES>
+__device__ __forceinline__ void add_slabs(const float (*slabs)[32 * slab_pitch(WN)], int count, int block_m, int block_n, void* Y,
+                                          const ProductShape& p) {
+  for (int t = threadIdx.x; t < 32 * 8 * WN; t += 64 * WAVES) {
+    const int row = t / (8 * WN), at = 4 * (t % (8 * WN));
+    const int m = 32 * block_m + row, n = 32 * block_n + at;
+    if (m >= p.M || n >= p.N) continue;
+    f32x4 v = *reinterpret_cast<const f32x4*>(slabs[0] + row * slab_pitch(WN) + at);
+    for (int w = 1; w < count; ++w) v += *reinterpret_cast<const f32x4*>(slabs[w] + row * slab_pitch(WN) + at);
+    store_four<OUT>(Y, (int64_t)m * p.ldy, n, v, p);
+  }
+}
+
 template <int OUT, int WM, int WN, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, void* Y,
-                       ProductShape p) {
-  constexpr int kPitch = 32 * WN + 4;
+__global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const uint8_t* a_codes, const uint8_t* a_scales,
+                                                                           const uint8_t* b_codes, const uint8_t* b_scales,
+                                                                           void* Y, ProductShape p) {
+  constexpr int kPitch = slab_pitch(WN);
   __shared__ __align__(16) float slabs[WAVES][32 * kPitch];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int blocks_a = mx4_row_blocks(p.M), blocks_b = mx4_row_blocks(p.N);
@@ -193,14 +208,7 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const
               f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     }
     __syncthreads();
-    for (int t = threadIdx.x; t < 32 * 8 * WN; t += 64 * WAVES) {
-      const int row = t / (8 * WN), at = 4 * (t % (8 * WN));
-      const int m = 32 * (block_m + j) + row, n = 32 * block_n + at;
-      if (m >= p.M || n >= p.N) continue;
-      f32x4 v = *reinterpret_cast<const f32x4*>(slabs[0] + row * kPitch + at);
-      for (int w = 1; w < count; ++w) v += *reinterpret_cast<const f32x4*>(slabs[w] + row * kPitch + at);
-      store_four<OUT>(Y, (int64_t)m * p.ldy, n, v, p);
-    }
+    add_slabs<OUT, WN, WAVES>(slabs, count, block_m + j, block_n, Y, p);
   }
 }
 
@@ -303,6 +311,112 @@ __global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, co
   const int count = min(kWaves, lines);
   for (int w = 1; w < count; ++w) v += sums[w][threadIdx.x];
   store_four<OUT>(Y, (int64_t)m * p.ldy, 0, f32x4{v, 0, 0, 0}, p);
+}
+
+// ---- a few tokens, quantised on the way ------------------------------------------------------------------
+// The same for 2 .. 32 tokens in P = 1, 2 or 4 pieces of a row of X, at most 4096 / P channels.  The waves first quantise all of X
+// into LDS, in passes of 256 / P channels: a lane takes four channels of eight tokens, as the kernel that quantises columns, so
+// eight lanes hold a block.  Every workgroup does that, which pays for small X only: 16 passes are where it draws level on
+// the device (8192x256 of 16 tokens 5.9 -> 3.7 us, 4096x1024 of 8 tokens 6.6 -> 4.4, 4096x2048 of 16 tokens 7.2 and 7.3), and a
+// launch less is 2.6 us of the caller's time.  Tokens that do not exist come out of what happens to lie there: a row of the
+// instruction's operand has no part in another row's result.
+constexpr int kFewPasses = 16;
+template <int OUT, int DT, int P>
+__global__ __launch_bounds__(512) void mx4_few_kernel(const uint8_t* codes, const uint8_t* scales, const uint16_t* x, int64_t ldx,
+                                                      Pieces pieces, void* Y, ProductShape p) {
+  constexpr int kWaves = 8, kTokens = 8 * P, kLanes = 64 / P, kPitch = slab_pitch(1), kRounds = kFewPasses / kWaves;
+  __shared__ __align__(16) uint8_t x_codes[kFewPasses * 1024];  // [block][token][16]
+  __shared__ uint8_t x_scales[kFewPasses * 64];                 // [block][token]
+  __shared__ __align__(16) float slabs[kWaves][32 * kPitch];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blocks = mx4_row_blocks(p.M), block = item_of_workgroup(blocks);
+  if (block < 0) return;
+  const int half = lane >> 5, r = lane & 31, lines = mx4_lines(p.K);
+  const int n = 8 * (lane / kLanes), left = p.N - n, k4 = 4 * (lane % kLanes);  // this lane's tokens; its channels of a pass
+  u32x4 v[kRounds][4];
+#pragma unroll
+  for (int s = 0; s < kRounds; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = 4 * kLanes * (wave + kWaves * s) + k4 + i;
+      v[s][i] = k < p.K && left > 0 ? draw_eight(x + (int64_t)k * ldx + n, left, pieces) : u32x4{0, 0, 0, 0};
+    }
+  struct Line {
+    u32x4 a[4];
+    u32x2 scale_a;
+  };
+  auto load_line = [&](int line, Line& f) {
+    const uint8_t* c = codes + mx4_codes_at(line, blocks, block) + 16 * lane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f.a[q] = *reinterpret_cast<const u32x4*>(c + 1024 * q);
+    f.scale_a = *reinterpret_cast<const u32x2*>(scales + mx4_scales_at(line >> 1, blocks, block) + 16 * r + 8 * half);
+  };
+  Line f;
+  if (wave < lines) load_line(wave, f);
+#pragma unroll
+  for (int s = 0; s < kRounds; ++s) {
+    const int pass = wave + kWaves * s, k = 4 * kLanes * pass + k4, in_block = (k >> 2) & 7;
+    if (pass >= lines * P) break;
+    uint8_t* const to = x_codes + ((k >> 5) * kTokens + n) * 16 + 2 * in_block;
+    uint8_t* const to_scale = x_scales + (k >> 5) * kTokens + n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[s][i] = place_eight(v[s][i], left, pieces);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = max_halves(m, v[s][i][w] & 0x7fff7fffu);
+      m = max_with_lane<0xB1>(m);   // lane ^ 1
+      m = max_with_lane<0x4E>(m);   // lane ^ 2
+      m = max_with_lane<0x141>(m);  // the other four of eight
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t e = mx4_scale_of<DT>(h ? m >> 16 : m & 0xffffu);
+        const float inverse = mx4_inverse_scale(e);
+        float g[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = (h ? high_half<DT>(v[s][i][w]) : low_half<DT>(v[s][i][w])) * inverse;
+        uint32_t c = 0;
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, g[0], g[1], 1.0f, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, g[2], g[3], 1.0f, 1);
+        if (e == 255) c = 0;
+        *reinterpret_cast<uint16_t*>(to + 16 * (2 * w + h)) = (uint16_t)c;
+        if (in_block == 2 * w + h) to_scale[2 * w + h] = (uint8_t)e;
+      }
+    }
+  }
+  __syncthreads();
+  f32x16 acc;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) acc[q] = 0;
+  auto multiply = [&](int line, const Line& f) {
+    u32x4 b[4];
+    uint32_t scale_b[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = (8 * line + 4 * (q >> 1) + 2 * half + (q & 1)) * kTokens + (r & (kTokens - 1));
+      b[q] = *reinterpret_cast<const u32x4*>(x_codes + 16 * at);
+      scale_b[q] = x_scales[at];
+    }
+    const uint32_t down = 16 * (line & 1);
+    const u32x2 scale_a = {f.scale_a[0] >> down, f.scale_a[1] >> down};
+    acc = mfma_32x32x64<0, 0>(b[0], scale_b[0], f.a[0], scale_a[0], acc);
+    acc = mfma_32x32x64<0, 0>(b[1], scale_b[1], f.a[1], scale_a[1], acc);
+    acc = mfma_32x32x64<0, 1>(b[2], scale_b[2], f.a[2], scale_a[0], acc);
+    acc = mfma_32x32x64<0, 1>(b[3], scale_b[3], f.a[3], scale_a[1], acc);
+  };
+  if (wave < lines) {
+    Line next;
+    if (wave + kWaves < lines) load_line(wave + kWaves, next);
+    multiply(wave, f);
+    if (wave + kWaves < lines) multiply(wave + kWaves, next);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(slabs[wave] + r * kPitch + 8 * q + 4 * half) =
+          f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+  }
+  __syncthreads();
+  add_slabs<OUT, 1, kWaves>(slabs, min(kWaves, lines), block, 0, Y, p);
 }
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
@@ -618,13 +732,17 @@ double estimate_us(const Form& f, const ProductShape& p) {
   return f.start + lines * ((double)full * f.full + (left > 0 ? f.alone + (f.full - f.alone) * left : 0));
 }
 
+int form_of(const ProductShape& p) {
+  int best = 0;  // one column: as mx4_token_kernel adds it
+  for (int i = 1; p.N > 1 && i < (int)(sizeof kForms / sizeof kForms[0]); ++i)
+    if (estimate_us(kForms[i], p) < estimate_us(kForms[best], p)) best = i;
+  return best;
+}
+
 template <int OUT>
 hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  int best = 0;  // one column: as mx4_token_kernel adds it
-  for (int i = 1; a.N > 1 && i < (int)(sizeof kForms / sizeof kForms[0]); ++i)
-    if (estimate_us(kForms[i], p) < estimate_us(kForms[best], p)) best = i;
-  switch (best) {
+  switch (form_of(p)) {
     case 0: return launch_stream<OUT, 1, 1, 8>(a, p, stream);
     case 1: return launch_stream<OUT, 1, 2, 8>(a, p, stream);
     case 2: return launch_stream<OUT, 2, 2, 8>(a, p, stream);
@@ -643,14 +761,39 @@ hipError_t launch_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hip
   return hipGetLastError();
 }
 
+template <int OUT, int DT>
+hipError_t launch_few(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
+  const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
+  const dim3 grid(grid_of_items(mx4_row_blocks(a.M)));
+  const Pieces pieces = pieces_of_rows(x, ldx, a.N);
+  auto launch = [&](auto kernel) {
+    kernel<<<grid, 512, 0, stream>>>(a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, pieces, a.Y, p);
+  };
+  if (a.N <= 8) launch(mx4_few_kernel<OUT, DT, 1>);
+  else if (a.N <= 16) launch(mx4_few_kernel<OUT, DT, 2>);
+  else launch(mx4_few_kernel<OUT, DT, 4>);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+bool mx4_quantises_on_the_way(const Mx4ProductArgs& a) {
+  if (a.N == 1) return true;
+  const int pieces = a.N <= 8 ? 1 : a.N <= 16 ? 2 : 4;
+  return a.N <= 32 && mx4_lines(a.K) * pieces <= kFewPasses && form_of(ProductShape{a.M, a.N, a.K, a.ldy, a.relu}) == 0;
+}
 
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream) {
   if (a.out_f32) return launch_out<2>(a, stream);
   return a.dtype == HINM_F16 ? launch_out<HINM_F16>(a, stream) : launch_out<HINM_BF16>(a, stream);
 }
 
-hipError_t launch_mx4_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
+hipError_t launch_mx4_on_the_way(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
+  if (a.N > 1) {
+    if (a.dtype == HINM_F16)
+      return a.out_f32 ? launch_few<2, HINM_F16>(a, x, ldx, stream) : launch_few<HINM_F16, HINM_F16>(a, x, ldx, stream);
+    return a.out_f32 ? launch_few<2, HINM_BF16>(a, x, ldx, stream) : launch_few<HINM_BF16, HINM_BF16>(a, x, ldx, stream);
+  }
   if (a.dtype == HINM_F16)
     return a.out_f32 ? launch_token<2, HINM_F16>(a, x, ldx, stream) : launch_token<HINM_F16, HINM_F16>(a, x, ldx, stream);
   return a.out_f32 ? launch_token<2, HINM_BF16>(a, x, ldx, stream) : launch_token<HINM_BF16, HINM_BF16>(a, x, ldx, stream);

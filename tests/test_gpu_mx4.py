@@ -361,3 +361,27 @@ def test_ends_of_rows_at_any_address(cols):
         there = host[first:first + rows * ld].reshape(rows, ld)
         assert np.array_equal(_wide(there[:, :cols], "bf16"), want, equal_nan=True)
         assert (there[:, cols:] == 0x1234).all() and (host[:first] == 0x1234).all() and (host[first + rows * ld:] == 0x1234).all()
+
+
+@pytest.mark.parametrize("N,K", [(2, 1), (2, 4096), (3, 4097), (5, 255), (8, 3841), (8, 4096), (9, 2048), (9, 2049), (13, 700), (16, 257), (16, 1793),
+                                 (17, 1024), (17, 1025), (24, 31), (25, 769), (31, 513), (32, 1000), (33, 500)])
+def test_few_tokens_are_quantised_as_apart(N, K):
+    """Both sides of the sizes up to which a call quantises on its way: equal to the two calls bit for bit."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    for M, dtype in ((1, "bf16"), (70, "f16"), (1000, "bf16")):
+        w = _upload(*_random_form(M, K, 3 * M + K))
+        bits = _draw(K, N, dtype, 21 + N, special=K * N > 4000)
+        for ld, first in ((N, 0), (N + 1, 1), ((N + 7) // 8 * 8, 0)):
+            keep, X = _matrix(bits, ld, first)
+            x = _form(N, K)
+            hinm.hinm_mx4_quantize(K, N, dtype, X, ld, hinm.MX4_COLUMNS, *x)
+            nbytes = hinm.hinm_mx4_linear_workspace(M, K, N)
+            ws = _guarded(nbytes)
+            for flags, kind in ((0, torch.int16), (hinm.EPI_RELU | hinm.OUT_F32, torch.int32)):
+                want = torch.full((M, N + 3), 5, dtype=kind, device=DEV)
+                got = want.clone()
+                hinm.hinm_mx4_product(M, N, K, dtype, *w, *x, want, N + 3, flags)
+                hinm.hinm_mx4_linear(M, K, N, dtype, *w, X, ld, got, N + 3, flags, ws, nbytes)
+                assert torch.equal(got, want), (M, ld, first, flags)
+            del keep
