@@ -694,11 +694,11 @@ hipError_t launch_tile(const Mx4ProductArgs& a, const ProductShape& p, hipStream
   return hipGetLastError();
 }
 
-// Which form serves a shape: the least of estimates in microseconds, fitted to launches with weights from memory at 99 shapes
-// (M, K of 128 .. 16384, 1 .. 8192 columns), of which the form chosen was the best one or at most 10 % behind it.  Both sides
+// Which form serves a shape: the least of estimates in microseconds, fitted to launches with weights from memory at 134
+// shapes (M, K of 128 .. 16384, 1 .. 8192 columns), of which the form chosen was the best one or at most 10 % behind it.  Both sides
 // of each line: 4096x4096 of 256 columns 7.5 us from registers, 9.8 as tiles of 128 rows; of 1000 columns 15.3 and 12.0; of 2048
 // columns 22 as tiles of 128 rows with a ring of four stages, 21.4 with two stages and two workgroups a unit; of 4096 columns
-// 39 as tiles of 128 rows, 36 of 256.
+// 40 as tiles of 128 rows, 37 of 256; 8254x1280 of 3533 columns, where writing counts, 32 and 34.
 struct Form {
   int rows, cols;      // of a workgroup
   int waves;           // registers: that share the lines; 0: tiles
@@ -707,14 +707,16 @@ struct Form {
   double line;         // registers: us of a wave's line
   double alone, full;  // tiles: us of a stage, with few workgroups and with all places taken; registers: KB/us that a compute
                        // unit draws with one workgroup, and with two or more
+  double writing;      // tiles: us that all places take to write 16-bit results while nothing multiplies
 };
 constexpr Form kForms[] = {
-    {32, 32, 8, 0, 4.0, 0.40, 122, 98},       {32, 64, 8, 0, 4.0, 0.80, 117, 87},       {64, 64, 8, 0, 4.0, 1.29, 99, 58},
-    {64, 128, 4, 0, 4.0, 1.18, 84, 63},       {128, 128, 0, 256, 4.6, 0, 0.30, 0.61}, {128, 128, 0, 512, 3.9, 0, 0.52, 1.14},
-    {256, 256, 0, 256, 8.2, 0, 0.92, 1.77},
+    {32, 32, 8, 0, 4.0, 0.40, 122, 98, 0},           {32, 64, 8, 0, 4.0, 0.80, 117, 87, 0},
+    {64, 64, 8, 0, 4.0, 1.29, 99, 58, 0},            {64, 128, 4, 0, 4.0, 1.18, 84, 63, 0},
+    {128, 128, 0, 256, 4.6, 0, 0.30, 0.61, 1.0}, {128, 128, 0, 512, 3.9, 0, 0.52, 1.14, 1.5},
+    {256, 256, 0, 256, 8.2, 0, 0.92, 1.77, 4.0},
 };
 constexpr int64_t kMostGroups = 1 << 22;  // of up to 512 threads in a launch
-double estimate_us(const Form& f, const ProductShape& p) {
+double estimate_us(const Form& f, const ProductShape& p, bool out_f32) {
   const int64_t groups = (int64_t)((p.M + f.rows - 1) / f.rows) * ((p.N + f.cols - 1) / f.cols);
   const double lines = mx4_lines(p.K);
   if (f.waves) {
@@ -729,20 +731,21 @@ double estimate_us(const Form& f, const ProductShape& p) {
   }
   const int64_t full = groups / f.at_once;
   const double left = (double)(groups - full * f.at_once) / f.at_once;
-  return f.start + lines * ((double)full * f.full + (left > 0 ? f.alone + (f.full - f.alone) * left : 0));
+  const double rounds = (double)groups / f.at_once, written = rounds > 0.5 ? (rounds - 0.5) * (out_f32 ? 2 : 1) : 0;
+  return f.start + lines * ((double)full * f.full + (left > 0 ? f.alone + (f.full - f.alone) * left : 0)) + f.writing * written;
 }
 
-int form_of(const ProductShape& p) {
+int form_of(const ProductShape& p, bool out_f32) {
   int best = 0;  // one column: as mx4_token_kernel adds it
   for (int i = 1; p.N > 1 && i < (int)(sizeof kForms / sizeof kForms[0]); ++i)
-    if (estimate_us(kForms[i], p) < estimate_us(kForms[best], p)) best = i;
+    if (estimate_us(kForms[i], p, out_f32) < estimate_us(kForms[best], p, out_f32)) best = i;
   return best;
 }
 
 template <int OUT>
 hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  switch (form_of(p)) {
+  switch (form_of(p, OUT == 2)) {
     case 0: return launch_stream<OUT, 1, 1, 8>(a, p, stream);
     case 1: return launch_stream<OUT, 1, 2, 8>(a, p, stream);
     case 2: return launch_stream<OUT, 2, 2, 8>(a, p, stream);
@@ -780,7 +783,7 @@ hipError_t launch_few(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipSt
 bool mx4_quantises_on_the_way(const Mx4ProductArgs& a) {
   if (a.N == 1) return true;
   const int pieces = a.N <= 8 ? 1 : a.N <= 16 ? 2 : 4;
-  return a.N <= 32 && mx4_lines(a.K) * pieces <= kFewPasses && form_of(ProductShape{a.M, a.N, a.K, a.ldy, a.relu}) == 0;
+  return a.N <= 32 && mx4_lines(a.K) * pieces <= kFewPasses && form_of(ProductShape{a.M, a.N, a.K, a.ldy, a.relu}, a.out_f32) == 0;
 }
 
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream) {
