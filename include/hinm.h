@@ -361,11 +361,11 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
 /* ---- around the compressed layers: 4-bit layers and a block's norms ------------------------------
  * What a transformer's feed-forward block needs beside HiNM layers, on the same matrices (channels x
  * tokens, row-major): layers kept in microscaled 4-bit form, and the norms on both sides of the block.
- * In this part leading dimensions are any value >= the row length and 16-bit matrices need the alignment of
- * their elements only; rows that begin at multiples of 16 bytes (aligned base, leading dimension a multiple
- * of 8) are read and written in 16-byte pieces, others element by element.  A piece that holds at least
- * one element of a row is read whole (what lies beyond never reaches a result); nothing beyond the
- * row length is written.  Sizes above 2^30, more than 2^22 tokens of a norm, and calls of more than some
+ * In this part leading dimensions are any value >= the row length and matrices need the alignment of
+ * their elements only.  Rows are read and written in 16-byte pieces.  Where they begin at multiples of 16
+ * bytes (aligned base, leading dimension a multiple of 8) a piece that holds at least one element of a
+ * row is read whole (what lies beyond never reaches a result); otherwise nothing beyond a row is read.
+ * Nothing beyond the row length is written.  Sizes above 2^30, more than 2^22 tokens of a norm, and calls of more than some
  * 2^22 workgroups (32 x 256 values or 128 x 128 outputs each) return HINM_ERR_UNSUPPORTED.
  *
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
@@ -411,7 +411,7 @@ hinm_status hinm_mx4_product(int32_t M, int32_t N, int32_t K, int32_t dtype, con
 
 /* A 4-bit layer on 16-bit activations: Y [M][N] = W X with W in 4-bit form (M rows of length K) and X [K][N]
  * quantised along its columns on the way; the result is that of hinm_mx4_quantize and hinm_mx4_product, bit for
- * bit.  workspace: hinm_mx4_linear_workspace bytes of device memory, 256-byte aligned. */
+ * bit.  One token, and up to 32 through a small layer, take one launch, others two.  workspace: hinm_mx4_linear_workspace bytes of device memory, 256-byte aligned. */
 hinm_status hinm_mx4_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const uint8_t* codes,
                             const uint8_t* scales, const void* X, int64_t ldx, void* Y, int64_t ldy,
@@ -428,7 +428,8 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
  * block (u and rstd_h are left alone and may be NULL); rstd_y / rstd_h not wanted; h not wanted (then w_pre and u
  * are needed).  u is computed from h before its rounding.  x and h have leading dimension ld_stream, y
  * and u ld_block.  h may be x and u may be y; apart from that outputs must not overlap inputs.  Sums
- * in fp32 in a fixed order.  workspace: hinm_block_norm_workspace bytes, 256-byte aligned. */
+ * in a fixed order, in fp32, and in binary64 where terms of h may cancel.
+ * workspace: hinm_block_norm_workspace bytes, 256-byte aligned. */
 hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_block_norm(int32_t K, int32_t N, int32_t dtype, float residual_scale, float eps,
                             const void* x, const void* y, const float* w_post, const float* gate,

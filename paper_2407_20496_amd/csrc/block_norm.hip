@@ -11,9 +11,9 @@
 // gradients' correction S = sum_k c y d is linear in the gradient d in the same way.
 //
 // Bound by memory: read twice (the second time from the caches behind L2 where they hold it), written once.  bf16, a channel
-// factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 24 against 14, 4096x8192
-// 78 against 56, 16384x1000 (rows that share lines) 51 against 27; gradients 4096x2048 60 against 21, 4096x8192 151 against
-// 84, 16384x1000 90 against 41.
+// factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 23 against 14, 4096x8192
+// 77 against 56, 16384x1000 (rows that share lines) 53 against 27; gradients 4096x2048 40 against 21, 4096x8192 139 against
+// 84, 16384x1000 84 against 41.  Kernels alone: 4096x8192 sums at 5.1 TB/s, results at 6.0; gradients at 4.8 and 4.9.
 #include "eight_values.h"
 
 namespace hinm {
@@ -344,7 +344,8 @@ __global__ __launch_bounds__(kThreads, 4) void block_norm_apply_kernel(Forward a
 constexpr int kHeldThreads = 512;
 
 // Reciprocal roots of eight columns from every thread's sums of squares.
-__device__ __forceinline__ void held_roots(float (&sum)[8], float (*by_wave)[8], float* root, const Forward& a, int n0, float* out) {
+__device__ __forceinline__ void held_roots(float (&sum)[8], float (*by_wave)[8], float* root, const Forward& a, int n0,
+                                           float* out) {
   const int lane = threadIdx.x & 63;
   const float t = add_eight_lanes(add_columns(sum));
   if ((lane & 7) == 0) by_wave[threadIdx.x >> 6][4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] = t;
@@ -428,7 +429,8 @@ __global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a
   }
 }
 
-// One token without a stride: a vector, held by one workgroup of 1024 threads, eight channels a thread and round.
+// One token without a stride: a vector, held by one workgroup of 1024 threads, eight channels a thread and round.  4096 channels
+// take 3.7 us, two trips to memory and two barriers, of which a launch is most.
 constexpr int kVectorThreads = 1024;
 constexpr int kVectorMost = 2 * 8 * kVectorThreads;
 
@@ -677,7 +679,7 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
   }
 }
 
-// Four threads' strips each, added in a fixed order, for 64 channels a workgroup.
+// Four threads' strips each, added in a fixed order, for 64 channels a workgroup: 3 to 5 us, a launch and one trip to memory.
 __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backward a) {
   __shared__ float part[2][4][64];
   const int strips = (a.N + kStrip - 1) / kStrip;
@@ -748,7 +750,8 @@ hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
             reinterpret_cast<double*>(b.workspace), kAligned, kAligned, kAny};
   a.stream = pieces_of_rows(a.x, a.ld_stream, a.N);
   a.block = pieces_of_rows(a.y, a.ld_block, a.N);
-  const bool lines = in_lines(a.x, a.ld_stream) && in_lines(a.h, a.ld_stream) && in_lines(a.y, a.ld_block) && in_lines(a.u, a.ld_block);
+  const bool lines = in_lines(a.x, a.ld_stream) && in_lines(a.h, a.ld_stream) && in_lines(a.y, a.ld_block) &&
+                     in_lines(a.u, a.ld_block);
   a.layout = lines ? kLines : a.stream == kAligned && a.block == kAligned ? kPieces : kAny;
   return b.dtype == HINM_F16 ? launch_forward<HINM_F16>(a, stream) : launch_forward<HINM_BF16>(a, stream);
 }

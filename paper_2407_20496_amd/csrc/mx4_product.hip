@@ -70,10 +70,13 @@ uint32_t grid_of_items(int64_t items) { return (uint32_t)((items + 7) / 8 * 8); 
 // with no barrier between them, and add their tiles in LDS in a fixed order.  The operands of a line are loaded while the
 // line before it multiplies.  B is the instruction's row operand, so that a lane ends with four consecutive columns of Y.
 //   Rows of B beyond N lie beyond the buffer descriptor's bytes for their lanes: they read as zero and cost no traffic.
+//   Few columns are bound by A's 17/32 bytes a value, which every workgroup has under way at once: 4096x11008 of 16 columns
+// 6.3 us (3.8 TB/s; 128 workgroups), 16384x11008 of 8, quantising included, 23 us (4.2 TB/s); more columns by what a compute unit
+// draws from L2: 4096x4096 of 256 7.4 us.
 constexpr int slab_pitch(int WN) { return 32 * WN + 4; }
 template <int OUT, int WN, int WAVES>
-__device__ __forceinline__ void add_slabs(const float (*slabs)[32 * slab_pitch(WN)], int count, int block_m, int block_n, void* Y,
-                                          const ProductShape& p) {
+__device__ __forceinline__ void add_slabs(const float (*slabs)[32 * slab_pitch(WN)], int count, int block_m, int block_n,
+                                          void* Y, const ProductShape& p) {
   for (int t = threadIdx.x; t < 32 * 8 * WN; t += 64 * WAVES) {
     const int row = t / (8 * WN), at = 4 * (t % (8 * WN));
     const int m = 32 * block_m + row, n = 32 * block_n + at;
@@ -223,7 +226,8 @@ hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStre
 // ---- one token, quantised on the way ---------------------------------------------------------------------
 // The form above for 32 rows of A, eight waves and one row of B that comes as 16-bit values: a wave quantises the line it is
 // about to multiply, four values a lane, and passes the codes through LDS to the two lanes that hold the row.  One launch
-// where quantising apart takes two; sums in the same order, so the same result bit for bit.
+// where quantising apart takes two; sums in the same order, so the same result bit for bit.  11008x4096: 6.0 us, 4.0 TB/s of
+// weights; a launch's start and the trip to memory are half of it.
 template <int OUT, int DT>
 __global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, const uint8_t* scales, const uint16_t* x, int64_t ldx,
                                                         void* Y, ProductShape p) {
@@ -430,6 +434,10 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(const uint8_t* codes, cons
 // p, the others during the first of p + 1.  Scales of group g + RING / 2 are copied in the last quarter of stage 2 g, ahead of
 // stage 2 g + RING, and read after stage 2 g + RING - 1; their place held group g - RING / 2.  Beyond the last stage the last
 // one is copied again; nobody reads it.
+//   What bounds it: 16384x16384x8192 takes 0.93 to 1.0 ms, 4.4 to 4.7 PFLOP/s, at a clock that the power limit holds at 1.5 to
+// 1.6 GHz (a loop of nothing but the instruction reaches 6.3 PFLOP/s on such operands, 8.7 on zeros).  Tiles of 128 rows draw
+// 36 KB a stage and unit from L2, 15 TB/s over the chip: 4096x4096 of 1000 columns 13.4 us (2.5 PFLOP/s), of 2048 22 us (3.1);
+// with operands of zeros 18.5.  Tiles of 256x128 measured the same there (22.2) and less elsewhere.
 
 template <int WM, int WN, int RING>
 struct TileSizes {
