@@ -430,7 +430,8 @@ __global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a
 }
 
 // One token without a stride: a vector, held by one workgroup of 1024 threads, eight channels a thread and round.  4096 channels
-// take 3.7 us, two trips to memory and two barriers, of which a launch is most.
+// take 3.7 us on the device, most of it a launch; a call 8.0 against 12.2 with the kernel above, 16384 channels 7.4 against 19.9
+// in two launches.
 constexpr int kVectorThreads = 1024;
 constexpr int kVectorMost = 2 * 8 * kVectorThreads;
 

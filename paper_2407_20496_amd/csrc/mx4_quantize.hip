@@ -18,7 +18,8 @@ constexpr int kThreads = 256;
 constexpr int kChunkPitch = 512 + 16;
 
 // Workgroups that share cache lines of the source (rows that do not begin at multiples of 128 bytes) run on one XCD, in
-// contiguous runs of the list; otherwise neighbours of the list run side by side.
+// contiguous runs of the list; otherwise neighbours of the list run side by side (down the columns 11008x1571 14.3 -> 12.4 us and
+// 11008x4095 30.9 -> 24.9 in runs; whole lines, 11008x4096 along the rows, 22.7 -> 23.4).
 __device__ __forceinline__ int item_of_workgroup(bool whole_lines) {
   return whole_lines ? (int)blockIdx.x : (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
 }
