@@ -429,54 +429,67 @@ __global__ __launch_bounds__(kHeldThreads) void block_norm_held_kernel(Forward a
   }
 }
 
-// One token without a stride: a vector, held by one workgroup of 1024 threads, eight channels a thread and round.  4096 channels
-// take 3.7 us on the device, most of it a launch; a call 8.0 against 12.2 with the kernel above, 16384 channels 7.4 against 19.9
-// in two launches.
-constexpr int kVectorThreads = 1024;
-constexpr int kVectorMost = 2 * 8 * kVectorThreads;
+// One token without a stride: a vector, held by one workgroup, eight channels a thread and round.  Most of it is a launch and one
+// trip to memory, so nothing stands between the loads: WHOLE, whole pieces at multiples of 16 bytes (channels and factors),
+// has no row's end to look after (4096 channels in a graph 3.5 us without, 2.7 with; on 1024 threads for 512 3.9 and 3.5).  A
+// call: 4096 channels 12.2 us with the kernel above and 8.0 here, 16384 channels 19.9 in two launches and 7.4.
+constexpr int kVectorMost = 2 * 8 * 1024;  // channels
 
+template <int THREADS>
 __device__ __forceinline__ float add_workgroup(float v, float* by_wave) {
   v = add_lanes_by_8(add_eight_lanes(v));
   if ((threadIdx.x & 63) == 0) by_wave[threadIdx.x >> 6] = v;
   __syncthreads();
   float t = 0;
 #pragma unroll
-  for (int w = 0; w < kVectorThreads / 64; ++w) t += by_wave[w];
+  for (int w = 0; w < THREADS / 64; ++w) t += by_wave[w];
   return t;
 }
-// eight floats from k on, `valid` of them (the rest: zero); absent: ones
+// eight floats from k on, `valid` of them (the rest: zero); absent: ones.  WHOLE: all eight exist, at a multiple of 16 bytes
+template <bool WHOLE>
 __device__ __forceinline__ void load_factors(const float* p, int k, int valid, float (&f)[8]) {
-  if (p && valid >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    const f32x4 low = *reinterpret_cast<const f32x4*>(p + k), high = *reinterpret_cast<const f32x4*>(p + k + 4);
+  f32x4 low = {1, 1, 1, 1}, high = {1, 1, 1, 1};
+  if (p && (WHOLE || (valid >= 8 && (reinterpret_cast<uintptr_t>(p) & 15) == 0))) {
+    low = *reinterpret_cast<const f32x4*>(p + k);
+    high = *reinterpret_cast<const f32x4*>(p + k + 4);
+  } else if (!WHOLE && p) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      f[j] = low[j];
-      f[4 + j] = high[j];
+      low[j] = j < valid ? p[k + j] : 0.0f;
+      high[j] = j + 4 < valid ? p[k + j + 4] : 0.0f;
     }
-    return;
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f[j] = p ? (j < valid ? p[k + j] : 0.0f) : 1.0f;
+  for (int j = 0; j < 4; ++j) {
+    f[j] = low[j];
+    f[4 + j] = high[j];
+  }
 }
 
-template <int DT, int ROUNDS>
-__global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forward a) {
-  __shared__ __align__(16) float by_wave[2][kVectorThreads / 64];
-  float x[ROUNDS][8], y[ROUNDS][8], c[ROUNDS][8], w[ROUNDS][8];
+template <int DT, int THREADS, int ROUNDS, bool WHOLE>
+__global__ __launch_bounds__(THREADS) void block_norm_vector_kernel(Forward a) {
+  __shared__ __align__(16) float by_wave[2][THREADS / 64];
+  float x[ROUNDS][8], y[ROUNDS][8], c[ROUNDS][8], g[ROUNDS][8], w[ROUNDS][8];
+  u32x4 of_x[ROUNDS], of_y[ROUNDS];
   const u32x4 none = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
-    const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
-    const u32x4 of_x = left > 0 ? draw_eight(a.x + k, left, a.stream) : none;
-    const u32x4 of_y = left > 0 && a.y ? draw_eight(a.y + k, left, a.block) : none;
-    widen<DT>(trim_eight(of_x, left, a.stream), x[i]);
-    widen<DT>(trim_eight(of_y, left, a.block), y[i]);
-    float g[8];
-    load_factors(a.w_post, k, left, c[i]);
-    load_factors(a.gate, k, left, g);
-    load_factors(a.w_pre, k, left, w[i]);
+    const int k = 8 * (threadIdx.x + i * THREADS), left = a.K - k;
+    const int at = WHOLE && left <= 0 ? 0 : k;  // threads beyond the vector read its beginning, and drop it
+    of_x[i] = WHOLE ? draw_eight(a.x + at, 8, kAligned) : left > 0 ? draw_eight(a.x + k, left, a.stream) : none;
+    of_y[i] = none;
+    if (a.y) of_y[i] = WHOLE ? draw_eight(a.y + at, 8, kAligned) : left > 0 ? draw_eight(a.y + k, left, a.block) : none;
+    load_factors<WHOLE>(a.w_post, at, left, c[i]);
+    load_factors<WHOLE>(a.gate, at, left, g[i]);
+    load_factors<WHOLE>(a.w_pre, at, left, w[i]);
+  }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c[i][j] *= g[j];
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int left = a.K - 8 * (int)(threadIdx.x + i * THREADS);
+    widen<DT>(WHOLE ? (left > 0 ? of_x[i] : none) : trim_eight(of_x[i], left, a.stream), x[i]);
+    widen<DT>(WHOLE ? (left > 0 ? of_y[i] : none) : trim_eight(of_y[i], left, a.block), y[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[i][j] *= g[i][j];
   }
   float token = a.token_gate ? a.token_gate[0] : 1.0f;
   if (a.w_post) {
@@ -485,7 +498,7 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
     for (int i = 0; i < ROUNDS; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum += y[i][j] * y[i][j];
-    const float r = 1.0f / sqrtf(add_workgroup(sum, by_wave[0]) / (float)a.K + a.eps);
+    const float r = 1.0f / sqrtf(add_workgroup<THREADS>(sum, by_wave[0]) / (float)a.K + a.eps);
     if (a.rstd_y && threadIdx.x == 0) a.rstd_y[0] = r;
     token *= r;
   }
@@ -500,16 +513,16 @@ __global__ __launch_bounds__(kVectorThreads) void block_norm_vector_kernel(Forwa
   if (a.h) {
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i) {
-      const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
+      const int k = 8 * (threadIdx.x + i * THREADS), left = a.K - k;
       if (left > 0) store_eight(a.h + k, narrow<DT>(x[i]), left);
     }
   }
   if (!a.w_pre) return;
-  const float r = 1.0f / sqrtf(add_workgroup(sum, by_wave[1]) / (float)a.K + a.eps);
+  const float r = 1.0f / sqrtf(add_workgroup<THREADS>(sum, by_wave[1]) / (float)a.K + a.eps);
   if (a.rstd_h && threadIdx.x == 0) a.rstd_h[0] = r;
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
-    const int k = 8 * (threadIdx.x + i * kVectorThreads), left = a.K - k;
+    const int k = 8 * (threadIdx.x + i * THREADS), left = a.K - k;
     if (left <= 0) break;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[i][j] *= w[i][j] * r;
@@ -707,6 +720,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
 
 // Workgroups for the list (chunk, strip), a multiple of the XCDs.
 dim3 grid_of(int chunks, int N) { return dim3((uint32_t)(((int64_t)chunks * strip_count(N) + 7) / 8 * 8)); }
+bool at_16_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld % 64 == 0); }
 
 }  // namespace
@@ -720,14 +734,23 @@ static hipError_t launch_forward_strips(const Forward& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int DT, bool WHOLE>
+static void launch_vector(const Forward& a, hipStream_t stream) {
+  if (a.K <= 4096) block_norm_vector_kernel<DT, 512, 1, WHOLE><<<1, 512, 0, stream>>>(a);
+  else if (a.K <= 8192) block_norm_vector_kernel<DT, 1024, 1, WHOLE><<<1, 1024, 0, stream>>>(a);
+  else block_norm_vector_kernel<DT, 1024, 2, WHOLE><<<1, 1024, 0, stream>>>(a);
+}
+
 template <int DT>
 static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
   if (a.N == 1 && a.ld_stream == 1 && (a.ld_block == 1 || (!a.y && !a.w_pre)) && a.K <= kVectorMost) {
     Forward v = a;
     v.stream = pieces_of_rows(a.x, 8, a.K);
     v.block = pieces_of_rows(a.y, 8, a.K);
-    if (a.K <= 8 * kVectorThreads) block_norm_vector_kernel<DT, 1><<<1, kVectorThreads, 0, stream>>>(v);
-    else block_norm_vector_kernel<DT, 2><<<1, kVectorThreads, 0, stream>>>(v);
+    const bool whole = a.K % 8 == 0 && v.stream == kAligned && v.block == kAligned && at_16_bytes(a.w_post) &&
+                       at_16_bytes(a.gate) && at_16_bytes(a.w_pre);
+    if (whole) launch_vector<DT, true>(v, stream);
+    else launch_vector<DT, false>(v, stream);
     return hipGetLastError();
   }
   const dim3 held((uint32_t)(((a.N + 7) / 8 + 7) / 8 * 8));
