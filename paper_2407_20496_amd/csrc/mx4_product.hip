@@ -318,12 +318,15 @@ __global__ __launch_bounds__(512) void mx4_token_kernel(const uint8_t* codes, co
 }
 
 // ---- a few tokens, quantised on the way ------------------------------------------------------------------
-// The same for 2 .. 32 tokens in P = 1, 2 or 4 pieces of a row of X, at most 4096 / P channels.  The waves first quantise all of X
-// into LDS, in passes of 256 / P channels: a lane takes four channels of eight tokens, as the kernel that quantises columns, so
-// eight lanes hold a block.  Every workgroup does that, which pays for small X only: 16 passes are where it draws level on
-// the device (8192x256 of 16 tokens 5.9 -> 3.7 us, 4096x1024 of 8 tokens 6.6 -> 4.4, 4096x2048 of 16 tokens 7.2 and 7.3), and a
-// launch less is 2.6 us of the caller's time.  Tokens that do not exist come out of what happens to lie there: a row of the
-// instruction's operand has no part in another row's result.
+// The same for 32 tokens a workgroup, or all of 2 .. 31, in P = 1, 2 or 4 pieces of a row of X, at most 4096 / P channels.  The
+// waves first quantise those tokens into LDS, in passes of 256 / P channels: a lane takes four channels of eight tokens, as the
+// kernel that quantises columns, so eight lanes hold a block.  Every workgroup does that, which pays for small products only,
+// but there a launch less is 2.6 us of the caller's time.  On the device, in a graph, us in two launches and here:
+//   up to 32 tokens, 16 passes: 8192x256 of 16 5.9 and 3.7, 4096x1024 of 8 6.6 and 4.4, 4096x2048 of 16 7.2 and 7.3;
+//   more, by workgroups (at most 768, which run at once) and lines: 752 of one line 6.7 and 6.9, 512 of two 6.5 and 5.9, 611 of
+//   two 6.7 and 8.1, 256 of four 6.9 and 7.0, 329 of four 6.8 and 8.7; 512x500 of 200 tokens 6.2 and 4.2.
+// The forms that would serve such products apart (64x128 and smaller) add their lines in the same order.  Tokens that do not
+// exist come out of what happens to lie there: a row of the instruction's operand has no part in another row's result.
 constexpr int kFewPasses = 16;
 template <int OUT, int DT, int P>
 __global__ __launch_bounds__(512) void mx4_few_kernel(const uint8_t* codes, const uint8_t* scales, const uint16_t* x, int64_t ldx,
@@ -333,17 +336,19 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(const uint8_t* codes, cons
   __shared__ uint8_t x_scales[kFewPasses * 64];                 // [block][token]
   __shared__ __align__(16) float slabs[kWaves][32 * kPitch];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int blocks = mx4_row_blocks(p.M), block = item_of_workgroup(blocks);
-  if (block < 0) return;
+  const int blocks = mx4_row_blocks(p.M), blocks_n = (p.N + 31) / 32;
+  const int item = item_of_workgroup(blocks * blocks_n);
+  if (item < 0) return;
+  const int block = item / blocks_n, block_n = item - block * blocks_n;
   const int half = lane >> 5, r = lane & 31, lines = mx4_lines(p.K);
-  const int n = 8 * (lane / kLanes), left = p.N - n, k4 = 4 * (lane % kLanes);  // this lane's tokens; its channels of a pass
+  const int n = 8 * (lane / kLanes), left = p.N - 32 * block_n - n, k4 = 4 * (lane % kLanes);  // this lane's tokens; its channels of a pass
   u32x4 v[kRounds][4];
 #pragma unroll
   for (int s = 0; s < kRounds; ++s)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int k = 4 * kLanes * (wave + kWaves * s) + k4 + i;
-      v[s][i] = k < p.K && left > 0 ? draw_eight(x + (int64_t)k * ldx + n, left, pieces) : u32x4{0, 0, 0, 0};
+      v[s][i] = k < p.K && left > 0 ? draw_eight(x + (int64_t)k * ldx + 32 * block_n + n, left, pieces) : u32x4{0, 0, 0, 0};
     }
   struct Line {
     u32x4 a[4];
@@ -420,7 +425,7 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(const uint8_t* codes, cons
           f32x4{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
   }
   __syncthreads();
-  add_slabs<OUT, 1, kWaves>(slabs, min(kWaves, lines), block, 0, Y, p);
+  add_slabs<OUT, 1, kWaves>(slabs, min(kWaves, lines), block, block_n, Y, p);
 }
 
 // ---- many rows of both: tiles through LDS ---------------------------------------------------------------
@@ -775,7 +780,7 @@ hipError_t launch_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hip
 template <int OUT, int DT>
 hipError_t launch_few(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
-  const dim3 grid(grid_of_items(mx4_row_blocks(a.M)));
+  const dim3 grid(grid_of_items((int64_t)mx4_row_blocks(a.M) * ((a.N + 31) / 32)));
   const Pieces pieces = pieces_of_rows(x, ldx, a.N);
   auto launch = [&](auto kernel) {
     kernel<<<grid, 512, 0, stream>>>(a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, pieces, a.Y, p);
@@ -791,7 +796,10 @@ hipError_t launch_few(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipSt
 bool mx4_quantises_on_the_way(const Mx4ProductArgs& a) {
   if (a.N == 1) return true;
   const int pieces = a.N <= 8 ? 1 : a.N <= 16 ? 2 : 4;
-  return a.N <= 32 && mx4_lines(a.K) * pieces <= kFewPasses && form_of(ProductShape{a.M, a.N, a.K, a.ldy, a.relu}, a.out_f32) == 0;
+  const int64_t lines = mx4_lines(a.K), groups = (int64_t)mx4_row_blocks(a.M) * ((a.N + 31) / 32);
+  if (lines * pieces > kFewPasses) return false;
+  const int form = form_of(ProductShape{a.M, a.N, a.K, a.ldy, a.relu}, a.out_f32);
+  return a.N <= 32 ? form == 0 : form <= 3 && groups <= 768 && groups * lines <= 1024;
 }
 
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream) {

@@ -385,3 +385,27 @@ def test_few_tokens_are_quantised_as_apart(N, K):
                 hinm.hinm_mx4_linear(M, K, N, dtype, *w, X, ld, got, N + 3, flags, ws, nbytes)
                 assert torch.equal(got, want), (M, ld, first, flags)
             del keep
+
+
+@pytest.mark.parametrize("M,N,K", [(500, 40, 1000), (1500, 200, 500), (1500, 230, 500), (4096, 100, 256), (4096, 64, 1024), (100, 700, 1024),
+                                   (33, 1500, 513), (70, 1001, 130), (31, 1031, 777), (1, 353, 999), (2049, 97, 257)])
+def test_small_products_are_quantised_as_apart(M, N, K):
+    """More tokens than a workgroup takes: equal to the two calls bit for bit, whichever way they go."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    dtype = "f16" if M % 2 else "bf16"
+    w = _upload(*_random_form(M, K, 5 * M + K))
+    bits = _draw(K, N, dtype, 31 + N)
+    for ld, first in ((N + 1, 1), ((N + 7) // 8 * 8, 0)):
+        keep, X = _matrix(bits, ld, first)
+        x = _form(N, K)
+        hinm.hinm_mx4_quantize(K, N, dtype, X, ld, hinm.MX4_COLUMNS, *x)
+        nbytes = hinm.hinm_mx4_linear_workspace(M, K, N)
+        ws = _guarded(nbytes)
+        for flags, kind in ((0, torch.int16), (hinm.EPI_RELU | hinm.OUT_F32, torch.int32)):
+            want = torch.full((M, N + 5), 5, dtype=kind, device=DEV)
+            got = want.clone()
+            hinm.hinm_mx4_product(M, N, K, dtype, *w, *x, want, N + 5, flags)
+            hinm.hinm_mx4_linear(M, K, N, dtype, *w, X, ld, got, N + 5, flags, ws, nbytes)
+            assert torch.equal(got, want), (ld, first, flags)
+        del keep
