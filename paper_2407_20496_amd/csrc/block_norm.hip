@@ -534,7 +534,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_vector_kernel(Forward a) {
 // The second norm's correction needs S = sum_k c d y with d the gradient of h, which itself holds the first correction:
 //   s1 = sum_k w_pre du h,   S = sum_k c y dh + rstd_h sum_k c y w_pre du - rstd_h^3 s1 / K sum_k c y h.
 // The second launch writes dx and dy and adds every row of its strip; where there are several, a third adds them (4096x3
-// 14.7 -> 12 us without it).
+// 14.7 -> 12 us without it).  Few channels or tokens: one launch, and one that adds the strips where there are several.
 
 struct Backward {
   int K, N, rows_per_chunk, chunks, rows_of_apply;
@@ -548,7 +548,8 @@ struct Backward {
   int64_t ld_block;
   float *dw_post, *dgate, *dtoken_gate, *dw_pre;
   float* sums;      // [4][chunks][N]
-  float* row_sums;  // [2][strips][K]
+  float* row_sums;  // [2][row_strips][K]
+  int row_strips;   // of 64 columns, or of eight
   Pieces stream, block;
   Layout layout;
 };
@@ -558,6 +559,16 @@ __device__ __forceinline__ void store_weight_gradients(const Backward& a, int k,
   if (a.dw_pre) a.dw_pre[k] = of_w_pre;
   if (a.dw_post) a.dw_post[k] = (a.gate ? a.gate[k] : 1.0f) * of_branch;
   if (a.dgate) a.dgate[k] = (a.w_post ? a.w_post[k] : 1.0f) * of_branch;
+}
+
+// ... of a strip's columns
+__device__ __forceinline__ void store_row_sums(const Backward& a, int strip, int k, float of_w_pre, float of_branch) {
+  if (a.row_strips == 1) {
+    store_weight_gradients(a, k, of_w_pre, of_branch);
+  } else {
+    a.row_sums[(int64_t)strip * a.K + k] = of_w_pre;
+    a.row_sums[(int64_t)(a.row_strips + strip) * a.K + k] = of_branch;
+  }
 }
 
 struct PatchGrad {
@@ -585,6 +596,57 @@ __device__ __forceinline__ void load_patch(const Backward& a, const Place& p, in
   }
 }
 
+// A row's part of a column's four sums.
+template <int DT>
+__device__ __forceinline__ void add_grad_sums(u32x4 of_h, u32x4 of_dh, u32x4 of_du, u32x4 of_y, float c, float w,
+                                              float (&sum)[4][8]) {
+  float h[8], dh[8], g[8], y[8];
+  widen<DT>(of_h, h);
+  widen<DT>(of_dh, dh);
+  widen<DT>(of_du, g);
+  widen<DT>(of_y, y);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    g[j] *= w;
+    y[j] *= c;
+    sum[0][j] += g[j] * h[j];
+    sum[1][j] += y[j] * dh[j];
+    sum[2][j] += y[j] * g[j];
+    sum[3][j] += y[j] * h[j];
+  }
+}
+// From their totals: the factors of h and of y in the corrections, rstd_h^3 s1 / K and rstd_y^2 S / K.  first: the one that
+// writes the token's gradient.
+__device__ __forceinline__ void corrections(const Backward& a, int n, bool first, float s0, float s1, float s2, float s3, float& f1,
+                                            float& f2) {
+  f1 = f2 = 0;
+  if (n >= a.N) return;
+  const float r = a.w_pre ? a.rstd_h[n] : 0.0f, ry = a.w_post ? a.rstd_y[n] : 1.0f;
+  f1 = r * r * r * (s0 / (float)a.K);
+  const float S = s1 + r * s2 - f1 * s3;
+  f2 = a.w_post ? ry * ry * (S / (float)a.K) : 0.0f;
+  if (a.dtoken_gate && first) a.dtoken_gate[n] = S * ry;
+}
+// A row's results and its eight columns' part of the channel's two sums.
+template <int DT>
+__device__ __forceinline__ void grad_row(const Backward& a, u32x4 of_h, u32x4 of_dh, u32x4 of_du, u32x4 of_y, float c, float w,
+                                         const float (&rh)[8], const float (&token)[8], const float (&f1)[8], const float (&f2)[8],
+                                         float (&dx)[8], float (&dy)[8], float& of_w_pre, float& of_branch) {
+  float h[8], g[8];
+  widen<DT>(of_h, h);
+  widen<DT>(of_dh, dx);
+  widen<DT>(of_du, g);
+  widen<DT>(of_y, dy);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    of_w_pre += g[j] * h[j] * rh[j];
+    const float d = dx[j] + w * g[j] * rh[j] - h[j] * f1[j];
+    of_branch += d * dy[j] * token[j];
+    dx[j] = a.scale * d;
+    dy[j] = token[j] * (c * d - dy[j] * f2[j]);
+  }
+}
+
 template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward a) {
   const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
@@ -595,22 +657,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_sums_kernel(Backward
     PatchGrad v;
     load_patch<L>(a, p, k, end, v);
 #pragma unroll
-    for (int i = 0; i < kGradRounds; ++i) {
-      float h[8], dh[8], g[8], y[8];
-      widen<DT>(trim_eight(v.h[i], p.left, known<L>(a.stream)), h);
-      widen<DT>(trim_eight(v.dh[i], p.left, known<L>(a.stream)), dh);
-      widen<DT>(trim_eight(v.du[i], p.left, known<L>(a.block)), g);
-      widen<DT>(trim_eight(v.y[i], p.left, known<L>(a.block)), y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        g[j] *= v.w[i];
-        y[j] *= v.c[i];
-        sum[0][j] += g[j] * h[j];
-        sum[1][j] += y[j] * dh[j];
-        sum[2][j] += y[j] * g[j];
-        sum[3][j] += y[j] * h[j];
-      }
-    }
+    for (int i = 0; i < kGradRounds; ++i)
+      add_grad_sums<DT>(trim_eight(v.h[i], p.left, known<L>(a.stream)), trim_eight(v.dh[i], p.left, known<L>(a.stream)),
+                        trim_eight(v.du[i], p.left, known<L>(a.block)), trim_eight(v.y[i], p.left, known<L>(a.block)), v.c[i],
+                        v.w[i], sum);
   }
   store_sums<4>(sum, p, a.sums, a.chunks, a.N);
 }
@@ -620,7 +670,6 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
   __shared__ float total[4][kStrip], first_of[kStrip], second_of[kStrip];  // corrections: rstd_h^3 s1 / K; rstd_y^2 S / K
   const Place p(a.K, a.N, a.rows_of_apply, L == kLines);
   if (p.none()) return;
-  const int strips = (a.N + kStrip - 1) / kStrip;
   const int end = p.row0 + p.rows, first = p.row0 + (threadIdx.x >> 3), at = 8 * (threadIdx.x & 7);
   PatchGrad v;
   load_patch<L>(a, p, first, end, v);
@@ -634,15 +683,9 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
   }
   __syncthreads();
   if (threadIdx.x < kStrip) {
-    const int n = p.n0 + threadIdx.x;
-    float f1 = 0, f2 = 0;
-    if (n < a.N) {
-      const float r = a.w_pre ? a.rstd_h[n] : 0.0f, ry = a.w_post ? a.rstd_y[n] : 1.0f;
-      f1 = r * r * r * (total[0][threadIdx.x] / (float)a.K);
-      const float S = total[1][threadIdx.x] + r * total[2][threadIdx.x] - f1 * total[3][threadIdx.x];
-      f2 = a.w_post ? ry * ry * (S / (float)a.K) : 0.0f;
-      if (a.dtoken_gate && p.chunk == 0) a.dtoken_gate[n] = S * ry;
-    }
+    float f1, f2;
+    corrections(a, p.n0 + (int)threadIdx.x, p.chunk == 0, total[0][threadIdx.x], total[1][threadIdx.x], total[2][threadIdx.x],
+                total[3][threadIdx.x], f1, f2);
     first_of[threadIdx.x] = f1;
     second_of[threadIdx.x] = f2;
   }
@@ -661,49 +704,105 @@ __global__ __launch_bounds__(kThreads, 3) void block_norm_grad_apply_kernel(Back
     for (int i = 0; i < kGradRounds; ++i) {
       const int r = k + i * kRowsAtOnce;
       const bool in = r < end;
-      float h[8], dh[8], g[8], y[8], of_w_pre = 0, of_branch = 0;
-      widen<DT>(trim_eight(v.h[i], p.left, known<L>(a.stream)), h);
-      widen<DT>(trim_eight(v.dh[i], p.left, known<L>(a.stream)), dh);
-      widen<DT>(trim_eight(v.du[i], p.left, known<L>(a.block)), g);
-      widen<DT>(trim_eight(v.y[i], p.left, known<L>(a.block)), y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        of_w_pre += g[j] * h[j] * rh[j];
-        const float d = dh[j] + v.w[i] * g[j] * rh[j] - h[j] * f1[j];
-        of_branch += d * y[j] * token[j];
-        dh[j] = a.scale * d;
-        y[j] = token[j] * (v.c[i] * d - y[j] * f2[j]);
-      }
+      float dx[8], dy[8], of_w_pre = 0, of_branch = 0;
+      grad_row<DT>(a, trim_eight(v.h[i], p.left, known<L>(a.stream)), trim_eight(v.dh[i], p.left, known<L>(a.stream)),
+                   trim_eight(v.du[i], p.left, known<L>(a.block)), trim_eight(v.y[i], p.left, known<L>(a.block)), v.c[i], v.w[i],
+                   rh, token, f1, f2, dx, dy, of_w_pre, of_branch);
       if (in && p.left > 0) {
-        if (a.dx) store_eight<L == kLines>(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dh), p.left);
-        if (a.dy) store_eight<L == kLines>(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(y), p.left);
+        if (a.dx) store_eight<L == kLines>(a.dx + (int64_t)r * a.ld_stream + p.n, narrow<DT>(dx), p.left);
+        if (a.dy) store_eight<L == kLines>(a.dy + (int64_t)r * a.ld_block + p.n, narrow<DT>(dy), p.left);
       }
       of_w_pre = add_eight_lanes(of_w_pre);
       of_branch = add_eight_lanes(of_branch);
       if (in && (threadIdx.x & 7) == 0) {
-        if (strips == 1) {
-          store_weight_gradients(a, r, of_w_pre, of_branch);
-        } else {
-          a.row_sums[(int64_t)p.strip * a.K + r] = of_w_pre;
-          a.row_sums[(int64_t)(strips + p.strip) * a.K + r] = of_branch;
-        }
+        store_row_sums(a, p.strip, r, of_w_pre, of_branch);
       }
     }
     v = next;
   }
 }
 
-// Four threads' strips each, added in a fixed order, for 64 channels a workgroup: 3 to 5 us, a launch and one trip to memory.
+// Few channels or tokens: the sums and the results in one launch, as block_norm_held_kernel.
+template <int DT, int ROUNDS>
+__global__ __launch_bounds__(kHeldThreads) void block_norm_grad_held_kernel(Backward a) {
+  __shared__ float by_wave[4][kHeldThreads / 64][8], first_of[8], second_of[8];
+  const int strip = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+  const int n = 8 * strip, left = min(8, a.N - n);
+  if (left <= 0) return;
+  const u32x4 none = {0, 0, 0, 0};
+  u32x4 h[ROUNDS], dh[ROUNDS], du[ROUNDS], y[ROUNDS];
+  float c[ROUNDS], w[ROUNDS];
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = threadIdx.x + i * kHeldThreads;
+    const bool in = k < a.K;
+    const int64_t stream = (int64_t)k * a.ld_stream + n, block = (int64_t)k * a.ld_block + n;
+    h[i] = in && a.w_pre ? draw_eight(a.h + stream, left, a.stream) : none;
+    dh[i] = in && a.dh ? draw_eight(a.dh + stream, left, a.stream) : none;
+    du[i] = in && a.w_pre ? draw_eight(a.du + block, left, a.block) : none;
+    y[i] = in && a.y ? draw_eight(a.y + block, left, a.block) : none;
+    c[i] = in ? channel_factor(a.w_post, a.gate, k) : 0.0f;
+    w[i] = in && a.w_pre ? a.w_pre[k] : 0.0f;
+  }
+  float rh[8], token[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    rh[j] = j < left && a.w_pre ? a.rstd_h[n + j] : 0.0f;
+    token[j] = j >= left ? 0.0f : (a.token_gate ? a.token_gate[n + j] : 1.0f) * (a.w_post ? a.rstd_y[n + j] : 1.0f);
+  }
+  float sum[4][8] = {};
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    h[i] = trim_eight(h[i], left, a.stream);
+    dh[i] = trim_eight(dh[i], left, a.stream);
+    du[i] = trim_eight(du[i], left, a.block);
+    y[i] = trim_eight(y[i], left, a.block);
+    add_grad_sums<DT>(h[i], dh[i], du[i], y[i], c[i], w[i], sum);
+  }
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float t = add_eight_lanes(add_columns(sum[q]));
+    if ((lane & 7) == 0) by_wave[q][threadIdx.x >> 6][4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] = t;
+  }
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    float t[4] = {};
+#pragma unroll
+    for (int v = 0; v < kHeldThreads / 64; ++v)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) t[q] += by_wave[q][v][threadIdx.x];
+    corrections(a, n + (int)threadIdx.x, true, t[0], t[1], t[2], t[3], first_of[threadIdx.x], second_of[threadIdx.x]);
+  }
+  __syncthreads();
+  float f1[8], f2[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    f1[j] = first_of[j];
+    f2[j] = second_of[j];
+  }
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int k = threadIdx.x + i * kHeldThreads;
+    if (k >= a.K) break;
+    float dx[8], dy[8], of_w_pre = 0, of_branch = 0;
+    grad_row<DT>(a, h[i], dh[i], du[i], y[i], c[i], w[i], rh, token, f1, f2, dx, dy, of_w_pre, of_branch);
+    if (a.dx) store_eight(a.dx + (int64_t)k * a.ld_stream + n, narrow<DT>(dx), left);
+    if (a.dy) store_eight(a.dy + (int64_t)k * a.ld_block + n, narrow<DT>(dy), left);
+    store_row_sums(a, strip, k, of_w_pre, of_branch);
+  }
+}
+
+// Strips added in a fixed order, sixteen threads a channel: 3 us, a launch and a trip or two to memory.
 __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backward a) {
-  __shared__ float part[2][4][64];
-  const int strips = (a.N + kStrip - 1) / kStrip;
-  const int col = threadIdx.x & 63, q = threadIdx.x >> 6, k = blockIdx.x * 64 + col;
+  __shared__ float part[2][16][16];
+  const int col = threadIdx.x & 15, q = threadIdx.x >> 4, k = blockIdx.x * 16 + col;
   float of_w_pre = 0, of_branch = 0;
   if (k < a.K) {
 #pragma unroll 8
-    for (int t = q; t < strips; t += 4) {
+    for (int t = q; t < a.row_strips; t += 16) {
       of_w_pre += a.row_sums[(int64_t)t * a.K + k];
-      of_branch += a.row_sums[(int64_t)(strips + t) * a.K + k];
+      of_branch += a.row_sums[(int64_t)(a.row_strips + t) * a.K + k];
     }
   }
   part[0][q][col] = of_w_pre;
@@ -711,7 +810,7 @@ __global__ __launch_bounds__(kThreads) void block_norm_grad_weights_kernel(Backw
   __syncthreads();
   if (q > 0 || k >= a.K) return;
 #pragma unroll
-  for (int t = 1; t < 4; ++t) {
+  for (int t = 1; t < 16; ++t) {
     of_w_pre += part[0][t][col];
     of_branch += part[1][t][col];
   }
@@ -780,21 +879,43 @@ hipError_t launch_block_norm(const BlockNormArgs& b, hipStream_t stream) {
   return b.dtype == HINM_F16 ? launch_forward<HINM_F16>(a, stream) : launch_forward<HINM_BF16>(a, stream);
 }
 
+// Rounds of the kernel that holds all rows, or 0 (us in two launches and three, and there): one launch for up to eight tokens
+// (256x1 16.7 and 8.5, 2048x8 12.2 and 9.0); two for few channels and not too much to draw in pieces of 16 bytes (768x200 14.6 and
+// 11.5, 768x1000 15.1 and 14.1, 1024x1000 15.1 and 15.8, 768x4096 20 and 26), nor too many strips to add (64x4096 14.7
+// and 12.1, 64x16000 15.6 and 37).
+static int grad_rounds_held(int K, int N) {
+  if (N <= 8) return K <= 2 * kHeldThreads ? 2 : K <= 4 * kHeldThreads ? 4 : 0;
+  return K <= 2 * kHeldThreads && N <= 4096 && (int64_t)K * N <= 3 << 18 ? 2 : 0;
+}
 size_t block_norm_grad_workspace_bytes(int K, int N) {
+  if (grad_rounds_held(K, N)) return N <= 8 ? 0 : (size_t)2 * ((N + 7) / 8) * K * sizeof(float);
   return ((size_t)4 * chunk_count(K, N) * N + (size_t)2 * strip_count(N) * K) * sizeof(float);
+}
+
+static hipError_t launch_grad_weights(const Backward& a, hipStream_t stream) {
+  if (a.row_strips > 1 && (a.dw_pre || a.dw_post || a.dgate))
+    block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 15) / 16)), kThreads, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 template <int DT, Layout L>
 static hipError_t launch_backward_strips(const Backward& a, hipStream_t stream) {
   block_norm_grad_sums_kernel<DT, L><<<grid_of(a.chunks, a.N), kThreads, 0, stream>>>(a);
   block_norm_grad_apply_kernel<DT, L><<<grid_of((a.K + a.rows_of_apply - 1) / a.rows_of_apply, a.N), kThreads, 0, stream>>>(a);
-  if (strip_count(a.N) > 1 && (a.dw_pre || a.dw_post || a.dgate))
-    block_norm_grad_weights_kernel<<<dim3((uint32_t)((a.K + 63) / 64)), kThreads, 0, stream>>>(a);
-  return hipGetLastError();
+  return launch_grad_weights(a, stream);
 }
 
 template <int DT>
 static hipError_t launch_backward(const Backward& a, hipStream_t stream) {
+  if (const int rounds = grad_rounds_held(a.K, a.N)) {
+    Backward held = a;
+    held.row_strips = (a.N + 7) / 8;
+    held.row_sums = a.sums;
+    const dim3 grid((uint32_t)((held.row_strips + 7) / 8 * 8));
+    if (rounds == 2) block_norm_grad_held_kernel<DT, 2><<<grid, kHeldThreads, 0, stream>>>(held);
+    else block_norm_grad_held_kernel<DT, 4><<<grid, kHeldThreads, 0, stream>>>(held);
+    return launch_grad_weights(held, stream);
+  }
   if (a.layout == kLines) return launch_backward_strips<DT, kLines>(a, stream);
   if (a.layout == kPieces) return launch_backward_strips<DT, kPieces>(a, stream);
   return launch_backward_strips<DT, kAny>(a, stream);
@@ -805,8 +926,8 @@ hipError_t launch_block_norm_grad(const BlockNormGradArgs& b, hipStream_t stream
              static_cast<const uint16_t*>(b.h), static_cast<const uint16_t*>(b.y), b.w_post, b.gate, b.token_gate, b.w_pre,
              b.rstd_y, b.rstd_h, static_cast<const uint16_t*>(b.dh), static_cast<const uint16_t*>(b.du),
              static_cast<uint16_t*>(b.dx), b.ld_stream, static_cast<uint16_t*>(b.dy), b.ld_block, b.dw_post, b.dgate,
-             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N, kAligned, kAligned,
-             kAny};
+             b.dtoken_gate, b.dw_pre, b.workspace, b.workspace + (int64_t)4 * chunk_count(b.K, b.N) * b.N,
+             strip_count(b.N), kAligned, kAligned, kAny};
   a.stream = lesser(pieces_of_rows(a.h, a.ld_stream, a.N), pieces_of_rows(a.dh, a.ld_stream, a.N));
   a.block = lesser(pieces_of_rows(a.y, a.ld_block, a.N), pieces_of_rows(a.du, a.ld_block, a.N));
   const bool lines = in_lines(a.h, a.ld_stream) && in_lines(a.dh, a.ld_stream) && in_lines(a.dx, a.ld_stream) &&

@@ -337,3 +337,19 @@ def test_ends_of_rows_at_any_address(N):
     for i, (ls, lb, first) in enumerate(_strides(N)):
         _forward(1100, N, "bf16", form, ls, lb, first, N + i)
         _backward(140, N, "f16", form, ls, lb, first, N + i)
+
+
+@pytest.mark.parametrize("K,N", [(1025, 1), (1500, 3), (2048, 8), (2049, 8), (2048, 9), (1024, 768), (1024, 769), (191, 4096), (190, 4097), (512, 64),
+                                 (513, 65), (3, 200)])
+def test_gradients_at_the_ends_of_their_forms(K, N):
+    form = dict(post=1, gate=1, token=1, pre=1, block=1)
+    for i, (ls, lb, first) in enumerate(_strides(N)):
+        _backward(K, N, "bf16" if i % 2 else "f16", form, ls, lb, first, K + N + i)
+    _backward(K, N, "bf16", form, N, N, 0, 9, in_place=True)
+
+
+@pytest.mark.parametrize("N", [*range(9, 17), 61, 62, 63])
+def test_ends_of_rows_of_gradients_in_strips(N):
+    form = dict(post=1, gate=1, token=1, pre=1, block=1)
+    for i, (ls, lb, first) in enumerate(_strides(N)):
+        _backward(1100, N, "f16", form, ls, lb, first, N + i)
