@@ -32,6 +32,32 @@ class Mx4Layer:
     flags: int = 0
 
 
+_TORCH_DTYPE = {hb.F16: torch.float16, hb.BF16: torch.bfloat16}
+
+
+def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dtype=None, device=None) -> int:
+    """Leading dimension of a 16-bit [K][>= tokens] matrix whose rows lie apart; ValueError for anything else (the library
+    is told addresses and cannot see it)."""
+    if t.dim() != 2 or t.shape[1] < tokens or (K is not None and t.shape[0] != K):
+        raise ValueError(f"{what}: [{'channels' if K is None else K}][at least {tokens}] wanted, not {list(t.shape)}")
+    if t.dtype != (dtype or t.dtype) or t.dtype not in _TORCH_DTYPE.values():
+        raise ValueError(f"{what}: {dtype or 'float16 or bfloat16'} wanted, not {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what}: on {t.device}, not on {device}")
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError(f"{what}: rows of consecutive values apart from each other wanted, not strides {t.stride()}")
+    return t.stride(0) if rows > 1 else cols
+
+
+def _factors(t: Optional[torch.Tensor], what: str, n: int, device) -> None:
+    """A float32 vector of n consecutive values, or none."""
+    if t is None:
+        return
+    if t.shape != (n,) or t.dtype != torch.float32 or (n > 1 and t.stride(0) != 1) or t.device != device:
+        raise ValueError(f"{what}: {n} consecutive float32 on {device} wanted, not {list(t.shape)} {t.dtype} on {t.device}")
+
+
 def mx4_form(rows: int, length: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
     """Memory for codes and scales of `rows` rows of `length` values."""
     cb, sb = hb.hinm_mx4_sizes(rows, length)
@@ -82,17 +108,23 @@ def _workspace(nbytes: int, device) -> torch.Tensor:
 
 
 def block_input(x: torch.Tensor, w_pre: torch.Tensor, tokens: int, eps: float = 1e-6) -> torch.Tensor:
-    """u = norm(x) w_pre: what the first block's layers take.  x [K][ld] 16-bit."""
-    K, ld = x.shape
-    u = torch.empty_like(x)
+    """u = norm(x) w_pre: what the first block's layers take.  x [K][>= tokens] 16-bit, in rows of any pitch; u has x's shape,
+    contiguous (a FeedForward takes it where that is [K][leading_dimension(tokens)])."""
+    ld = _pitch(x, "x", tokens)
+    K = x.shape[0]
+    _factors(w_pre, "w_pre", K, x.device)
+    u = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     nbytes = hb.hinm_block_norm_workspace(K, tokens)
-    hb.hinm_block_norm(K, tokens, x.dtype, 1.0, eps, x, None, None, None, None, w_pre, None, ld, u, ld, None, None,
+    hb.hinm_block_norm(K, tokens, x.dtype, 1.0, eps, x, None, None, None, None, w_pre, None, ld, u, x.shape[1], None, None,
                        _workspace(nbytes, x.device), nbytes)
     return u
 
 
 class FeedForward:
-    """One block for a fixed number of tokens: its layers, norms and buffers."""
+    """One block for a fixed number of tokens: its layers, norms and buffers.
+
+    x is [K][>= tokens] in rows of any pitch, u [K][>= tokens] in rows of leading_dimension(tokens), which is the pitch of the
+    block's own buffers too; both of the layers' type, on the block's device.  Other arrays raise ValueError."""
 
     def __init__(self, layers: Sequence[Union[Mx4Layer, hb.Layer]], tokens: int, w_post: Optional[torch.Tensor],
                  gate: Optional[torch.Tensor] = None, w_next: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
@@ -103,13 +135,18 @@ class FeedForward:
         self.in_4_bits = all(isinstance(l, Mx4Layer) for l in layers)
         if not self.in_4_bits and any(isinstance(l, Mx4Layer) for l in layers):
             raise ValueError("one block's layers come in one form")
+        if len({hb._dtype_code(l.dtype) for l in layers}) > 1:
+            raise ValueError("one block's layers have one type")
         self.layers, self.tokens, self.ld = layers, tokens, leading_dimension(tokens)
         self.w_post, self.gate, self.w_next = w_post, gate, w_next
         self.residual_scale, self.eps = residual_scale, eps
         self.K, self.dtype = layers[0].K, layers[0].dtype
-        kind = {hb.F16: torch.float16, hb.BF16: torch.bfloat16}[hb._dtype_code(self.dtype)]
-        new = lambda rows: torch.empty((rows, self.ld), dtype=kind, device=device)
+        new = lambda rows: torch.empty((rows, self.ld), dtype=_TORCH_DTYPE[hb._dtype_code(self.dtype)], device=device)
         self.y = new(self.K)
+        for what, t in (("w_post", w_post), ("gate", gate), ("w_next", w_next)):
+            _factors(t, what, self.K, self.y.device)
+        if self.in_4_bits and any(t.device != self.y.device for l in layers for t in (l.codes, l.scales)):
+            raise ValueError(f"the layers' weights are not on {self.y.device}")
         if self.in_4_bits:
             self.between = [new(l.M) for l in layers[:-1]]
             self.scratch_bytes = max(hb.hinm_mx4_linear_workspace(l.M, l.K, tokens) for l in layers)
@@ -122,6 +159,8 @@ class FeedForward:
     def run_layers(self, u: torch.Tensor) -> torch.Tensor:
         """y = layers(u), in the block's own buffer."""
         N, ld = self.tokens, self.ld
+        if _pitch(u, "u", N, self.K, self.y.dtype, self.y.device) != ld:
+            raise ValueError(f"u: rows of {ld} = leading_dimension({N}) values wanted, not strides {u.stride()}")
         if not self.in_4_bits:
             hb.hinm_chain(self.layers, N, u, ld, self.y, ld, self.scratch, self.scratch_bytes)
             return self.y
@@ -133,7 +172,9 @@ class FeedForward:
 
     def __call__(self, x: torch.Tensor, u: torch.Tensor, token_gate: Optional[torch.Tensor] = None):
         """(h, u_next) in place of (x, u); u_next is u untouched where no norm follows."""
+        ld_stream = _pitch(x, "x", self.tokens, self.K, self.y.dtype, self.y.device)
+        _factors(token_gate, "token_gate", self.tokens, self.y.device)
         y = self.run_layers(u)
         hb.hinm_block_norm(self.K, self.tokens, self.dtype, self.residual_scale, self.eps, x, y, self.w_post, self.gate,
-                           token_gate, self.w_next, x, self.ld, u, self.ld, None, None, self.norm_workspace, self.norm_bytes)
+                           token_gate, self.w_next, x, ld_stream, u, self.ld, None, None, self.norm_workspace, self.norm_bytes)
         return x, u

@@ -1,0 +1,114 @@
+"""What block.py takes and refuses, on the CPU: the library's calls are recorded instead of made, and a refusal has to come
+before the first of them."""
+import pytest
+import torch
+
+import paper_2407_20496_amd as hinm
+from paper_2407_20496_amd import block as blk
+
+LAUNCHES = ("hinm_mx4_quantize", "hinm_mx4_product", "hinm_mx4_linear", "hinm_block_norm", "hinm_chain")
+K, M, N, LD = 32, 64, 20, 24
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    for name in LAUNCHES:
+        monkeypatch.setattr(blk.hb, name, lambda *a, _n=name, **k: made.append((_n, a)))
+    return made
+
+
+def _layer(m, k, dtype=torch.float16, flags=0):
+    return blk.Mx4Layer(m, k, dtype, *blk.mx4_form(m, k, "cpu"), flags)
+
+
+def _block(dtype=torch.float16, **more):
+    return blk.FeedForward([_layer(M, K, dtype), _layer(K, M, dtype)], N, torch.ones(K), w_next=torch.ones(K), device="cpu", **more)
+
+
+def _new(rows=K, cols=LD, dtype=torch.float16):
+    return torch.zeros((rows, cols), dtype=dtype)
+
+
+BAD_ROWS = {"narrower than the tokens": lambda: _new(cols=N - 1), "too few channels": lambda: _new(rows=K - 1),
+            "too many channels": lambda: _new(rows=K + 1), "another type": lambda: _new(dtype=torch.bfloat16),
+            "float32": lambda: _new(dtype=torch.float32), "a vector": lambda: _new().reshape(-1),
+            "columns apart": lambda: _new(cols=2 * LD)[:, ::2], "transposed": lambda: _new(rows=LD, cols=K).t(),
+            "one row for all": lambda: _new(rows=1).expand(K, LD), "overlapping rows": lambda: torch.zeros(K * LD, dtype=torch.float16).as_strided((K, LD), (8, 1)),
+            "another device": lambda: torch.zeros((K, LD), dtype=torch.float16, device="meta")}
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS.values(), ids=BAD_ROWS)
+def test_a_block_refuses_other_arrays(bad, calls):
+    block = _block()
+    for x, u in ((bad(), _new()), (_new(), bad())):
+        with pytest.raises(ValueError):
+            block(x, u)
+    with pytest.raises(ValueError):
+        block.run_layers(bad())
+    assert not calls
+
+
+@pytest.mark.parametrize("cols", [N, 32])
+def test_a_block_refuses_another_pitch_of_its_input(cols, calls):
+    """The layers' input shares its pitch with the block's own output."""
+    block = _block()
+    with pytest.raises(ValueError):
+        block(_new(), _new(cols=cols))
+    with pytest.raises(ValueError):
+        block.run_layers(_new(cols=cols))
+    assert not calls
+
+
+@pytest.mark.parametrize("x,pitch", [(_new(), LD), (_new(cols=N), N), (_new(cols=40), 40), (_new(cols=64)[:, :LD], 64),
+                                     (_new(cols=64)[:, 8:8 + N], 64)])
+def test_a_block_takes_the_pitch_of_its_stream(x, pitch, calls):
+    _block()(x, _new())
+    name, args = calls[-1]
+    assert name == "hinm_block_norm" and args[5] is x and args[11] is x and args[12] == pitch and args[14] == LD
+
+
+def test_a_wider_view_is_as_good_as_a_buffer_of_the_blocks_pitch(calls):
+    u = _new(cols=LD)[:, :N]
+    assert _block().run_layers(u) is not None and calls[0][0] == "hinm_mx4_linear" and calls[0][1][7] == LD
+
+
+BAD_VECTORS = {"float64": torch.ones(K, dtype=torch.float64), "short": torch.ones(K - 1), "long": torch.ones(K + 1),
+               "apart": torch.ones(2 * K)[::2], "one for all": torch.ones(1).expand(K), "a matrix": torch.ones(K, 1),
+               "another device": torch.ones(K, device="meta")}
+
+
+@pytest.mark.parametrize("bad", BAD_VECTORS.values(), ids=BAD_VECTORS)
+def test_a_block_refuses_other_factors(bad, calls):
+    layers = [_layer(M, K), _layer(K, M)]
+    for w_post, gate, w_next in ((bad, None, None), (None, bad, None), (None, None, bad)):
+        with pytest.raises(ValueError):
+            blk.FeedForward(layers, N, w_post, gate, w_next, device="cpu")
+    with pytest.raises(ValueError):
+        blk.block_input(_new(), bad, N)
+    with pytest.raises(ValueError):
+        _block()(_new(), _new(), token_gate=bad)      # as many as tokens are wanted, and no fewer
+    assert not calls
+
+
+def test_a_blocks_layers_share_their_type_and_device():
+    with pytest.raises(ValueError):
+        blk.FeedForward([_layer(M, K), _layer(K, M, torch.bfloat16)], N, None, device="cpu")
+    with pytest.raises(ValueError):
+        blk.FeedForward([_layer(M, K), _layer(K, M)], N, None, device="meta")
+    assert blk.FeedForward([_layer(M, K, "f16"), _layer(K, M, hinm.F16)], N, None, device="cpu").y.dtype == torch.float16
+
+
+@pytest.mark.parametrize("bad", [k for k in BAD_ROWS if "channels" not in k and k not in ("another type", "another device")])
+def test_a_blocks_input_refuses_other_arrays(bad, calls):
+    x = BAD_ROWS[bad]()
+    with pytest.raises(ValueError):
+        blk.block_input(x, torch.ones(K), N)
+    assert not calls
+
+
+@pytest.mark.parametrize("x,pitch", [(_new(), LD), (_new(cols=N), N), (_new(cols=64)[:, :LD], 64), (_new(cols=1), 1)])
+def test_a_blocks_input_has_the_shape_of_its_stream(x, pitch, calls):
+    u = blk.block_input(x, torch.ones(K), min(N, x.shape[1]))
+    args = calls[-1][1]
+    assert u.shape == x.shape and u.is_contiguous() and args[5] is x and args[12] == pitch and args[14] == x.shape[1]
