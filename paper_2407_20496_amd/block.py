@@ -35,19 +35,25 @@ class Mx4Layer:
 _TORCH_DTYPE = {hb.F16: torch.float16, hb.BF16: torch.bfloat16}
 
 
-def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dtype=None, device=None) -> int:
-    """Leading dimension of a 16-bit [K][>= tokens] matrix whose rows lie apart; ValueError for anything else (the library
-    is told addresses and cannot see it)."""
-    if t.dim() != 2 or t.shape[1] < tokens or (K is not None and t.shape[0] != K):
-        raise ValueError(f"{what}: [{'channels' if K is None else K}][at least {tokens}] wanted, not {list(t.shape)}")
-    if t.dtype != (dtype or t.dtype) or t.dtype not in _TORCH_DTYPE.values():
-        raise ValueError(f"{what}: {dtype or 'float16 or bfloat16'} wanted, not {t.dtype}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what}: on {t.device}, not on {device}")
+def _row_pitch(t: torch.Tensor, what: str) -> int:
+    """Leading dimension of a 16-bit matrix whose rows of consecutive values lie apart; ValueError for anything else (the
+    library is told addresses and cannot see it)."""
+    if t.dim() != 2 or t.dtype not in _TORCH_DTYPE.values():
+        raise ValueError(f"{what}: a float16 or bfloat16 matrix wanted, not {t.dtype} {list(t.shape)}")
     rows, cols = t.shape
     if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
         raise ValueError(f"{what}: rows of consecutive values apart from each other wanted, not strides {t.stride()}")
     return t.stride(0) if rows > 1 else cols
+
+
+def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dtype=None, device=None) -> int:
+    """... of a [K][>= tokens] one."""
+    ld = _row_pitch(t, what)
+    if t.shape[1] < tokens or (K is not None and t.shape[0] != K):
+        raise ValueError(f"{what}: [{'channels' if K is None else K}][at least {tokens}] wanted, not {list(t.shape)}")
+    if (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device):
+        raise ValueError(f"{what}: {dtype} on {device} wanted, not {t.dtype} on {t.device}")
+    return ld
 
 
 def _factors(t: Optional[torch.Tensor], what: str, n: int, device) -> None:
@@ -65,12 +71,11 @@ def mx4_form(rows: int, length: int, device) -> Tuple[torch.Tensor, torch.Tensor
 
 
 def mx4_layer(W: torch.Tensor, flags: int = 0) -> Mx4Layer:
-    """Dense 16-bit weights [M][K] (rows may be strided) to a 4-bit layer."""
+    """Dense 16-bit weights [M][K] (rows may lie apart) to a 4-bit layer."""
+    ld = _row_pitch(W, "weights")
     M, K = W.shape
-    if W.stride(1) != 1 and K > 1:
-        raise ValueError("weights must be contiguous along their rows")
     codes, scales = mx4_form(M, K, W.device)
-    hb.hinm_mx4_quantize(M, K, W.dtype, W, max(W.stride(0), K), hb.MX4_ROWS, codes, scales)
+    hb.hinm_mx4_quantize(M, K, W.dtype, W, ld, hb.MX4_ROWS, codes, scales)
     return Mx4Layer(M, K, W.dtype, codes, scales, flags)
 
 

@@ -112,3 +112,24 @@ def test_a_blocks_input_has_the_shape_of_its_stream(x, pitch, calls):
     u = blk.block_input(x, torch.ones(K), min(N, x.shape[1]))
     args = calls[-1][1]
     assert u.shape == x.shape and u.is_contiguous() and args[5] is x and args[12] == pitch and args[14] == x.shape[1]
+
+
+def _strided(rows, cols, *strides):
+    return torch.zeros(rows * cols + 64 * sum(strides), dtype=torch.bfloat16).as_strided((rows, cols), strides)
+
+
+@pytest.mark.parametrize("W", [torch.zeros(1, K, dtype=torch.bfloat16).expand(M, K), _strided(M, K, 8, 1), _strided(M, K, K - 1, 1),
+                               _strided(M, K, 1, M), _strided(M, K, 2 * K, 2), torch.zeros(M * K, dtype=torch.bfloat16),
+                               torch.zeros(M, K, 1, dtype=torch.bfloat16), torch.zeros(M, K)],
+                         ids=["one row for all", "overlapping", "overlapping by one", "transposed", "columns apart", "a vector", "a cube", "float32"])
+def test_a_layer_refuses_weights_that_do_not_lie_row_by_row(W, calls):
+    with pytest.raises(ValueError):
+        blk.mx4_layer(W)
+    assert not calls
+
+
+@pytest.mark.parametrize("W,pitch", [(_strided(M, K, K, 1), K), (_strided(M, K, K + 5, 1), K + 5), (_strided(1, K, 0, 1), K), (_strided(1, K, 7, 1), K),
+                                     (_strided(M, 1, 3, 5), 3)])
+def test_a_layer_takes_the_pitch_of_its_weights(W, pitch, calls):
+    layer = blk.mx4_layer(W)
+    assert (layer.M, layer.K) == W.shape and calls[0][1][3] is W and calls[0][1][4] == pitch
