@@ -83,21 +83,24 @@ def mx4_linear_grad(W: torch.Tensor, X: torch.Tensor, dY: torch.Tensor, tokens: 
                     want_input: bool = True, want_weights: bool = True):
     """Gradients of Y = W X where every product is taken on 4-bit operands, each quantised along the axis that is summed over
     and rounded as if the quantisation were not there (straight through): (dX like X, dW float32 [M][K]).
-    W [M][K], X [K][ld], dY [M][ld], contiguous, `tokens` <= ld columns in use."""
+    W [M][K], X [K][>= tokens], dY [M][>= tokens] of one type on one device, in rows of any pitch (others raise ValueError);
+    `tokens` columns are in use (all of X's where it is not given), and dX's columns beyond them are left as they are allocated."""
+    ld_w = _row_pitch(W, "W")
     M, K = W.shape
-    N = X.shape[1] if tokens is None else tokens
     dev, dtype = W.device, W.dtype
+    N = tokens if tokens is not None else X.shape[-1]
+    ld_x, ld_dy = _pitch(X, "X", N, K, dtype, dev), _pitch(dY, "dY", N, M, dtype, dev)
     dX = dW = None
     if want_input:
         across_w, across_dy = mx4_form(K, M, dev), mx4_form(N, M, dev)
-        hb.hinm_mx4_quantize(M, K, dtype, W, K, hb.MX4_COLUMNS, *across_w)
-        hb.hinm_mx4_quantize(M, N, dtype, dY, dY.shape[1], hb.MX4_COLUMNS, *across_dy)
-        dX = torch.empty_like(X)
+        hb.hinm_mx4_quantize(M, K, dtype, W, ld_w, hb.MX4_COLUMNS, *across_w)
+        hb.hinm_mx4_quantize(M, N, dtype, dY, ld_dy, hb.MX4_COLUMNS, *across_dy)
+        dX = torch.empty(X.shape, dtype=dtype, device=dev)
         hb.hinm_mx4_product(K, N, M, dtype, *across_w, *across_dy, dX, X.shape[1])
     if want_weights:
         along_dy, along_x = mx4_form(M, N, dev), mx4_form(K, N, dev)
-        hb.hinm_mx4_quantize(M, N, dtype, dY, dY.shape[1], hb.MX4_ROWS, *along_dy)
-        hb.hinm_mx4_quantize(K, N, dtype, X, X.shape[1], hb.MX4_ROWS, *along_x)
+        hb.hinm_mx4_quantize(M, N, dtype, dY, ld_dy, hb.MX4_ROWS, *along_dy)
+        hb.hinm_mx4_quantize(K, N, dtype, X, ld_x, hb.MX4_ROWS, *along_x)
         dW = torch.empty((M, K), dtype=torch.float32, device=dev)
         hb.hinm_mx4_product(M, K, N, dtype, *along_dy, *along_x, dW, K, hb.OUT_F32)
     return dX, dW

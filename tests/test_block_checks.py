@@ -133,3 +133,44 @@ def test_a_layer_refuses_weights_that_do_not_lie_row_by_row(W, calls):
 def test_a_layer_takes_the_pitch_of_its_weights(W, pitch, calls):
     layer = blk.mx4_layer(W)
     assert (layer.M, layer.K) == W.shape and calls[0][1][3] is W and calls[0][1][4] == pitch
+
+
+BF16 = torch.bfloat16
+GOOD = {"W": lambda: _new(M, K, BF16), "X": lambda: _new(K, LD, BF16), "dY": lambda: _new(M, LD, BF16)}
+BAD = {"W": {"float32": lambda: _new(M, K, torch.float32), "another type": lambda: _new(M, K), "transposed": lambda: _new(K, M, BF16).t(),
+             "one row for all": lambda: _new(1, K, BF16).expand(M, K), "columns apart": lambda: _new(M, 2 * K, BF16)[:, ::2],
+             "a vector": lambda: _new(M, K, BF16).reshape(-1), "another device": lambda: _new(M, K, BF16).to("meta")},
+       "X": {"another type": lambda: _new(K, LD), "too few channels": lambda: _new(K - 1, LD, BF16), "too many channels": lambda: _new(M, LD, BF16),
+             "narrower than the tokens": lambda: _new(K, N - 1, BF16), "transposed": lambda: _new(LD, K, BF16).t(),
+             "overlapping": lambda: _strided(K, LD, 8, 1), "another device": lambda: _new(K, LD, BF16).to("meta")},
+       "dY": {"another type": lambda: _new(M, LD), "too few rows": lambda: _new(K, LD, BF16), "too many rows": lambda: _new(M + 1, LD, BF16),
+              "narrower than the tokens": lambda: _new(M, N - 1, BF16), "columns apart": lambda: _new(M, 2 * LD, BF16)[:, ::2],
+              "another device": lambda: _new(M, LD, BF16).to("meta")}}
+
+
+@pytest.mark.parametrize("which,what", [(k, w) for k, v in BAD.items() for w in v])
+def test_a_layers_gradients_refuse_other_arrays(which, what, calls):
+    given = {k: v() for k, v in GOOD.items()}
+    given[which] = BAD[which][what]()
+    with pytest.raises(ValueError):
+        blk.mx4_linear_grad(**given, tokens=N)
+    assert not calls
+
+
+def test_a_layers_gradients_refuse_as_many_tokens_as_there_are_in_one_array_only(calls):
+    with pytest.raises(ValueError):
+        blk.mx4_linear_grad(GOOD["W"](), _new(K, 2 * LD, BF16), GOOD["dY"]())
+    assert not calls
+
+
+@pytest.mark.parametrize("cols_w,cols_x,cols_dy", [(K, LD, LD), (K + 3, LD, LD), (K, 40, LD), (K, LD, 64), (2 * K, N, 41)])
+def test_a_layers_gradients_take_the_pitch_of_each_array(cols_w, cols_x, cols_dy, calls):
+    W, X, dY = _new(M, cols_w, BF16)[:, :K], _new(K, cols_x, BF16)[:, :N], _new(M, cols_dy, BF16)[:, :N]
+    dX, dW = blk.mx4_linear_grad(W, X, dY)
+    assert dX.shape == X.shape and dX.is_contiguous() and dW.shape == W.shape
+    quantised = {(a[3].data_ptr(), a[5]): a[:5] for n, a in calls if n == "hinm_mx4_quantize"}
+    assert quantised[W.data_ptr(), hinm.MX4_COLUMNS] == (M, K, BF16, W, cols_w)
+    assert quantised[X.data_ptr(), hinm.MX4_ROWS] == (K, N, BF16, X, cols_x)
+    assert quantised[dY.data_ptr(), hinm.MX4_COLUMNS] == quantised[dY.data_ptr(), hinm.MX4_ROWS] == (M, N, BF16, dY, cols_dy)
+    products = [(a[:3], a[8], a[9]) for n, a in calls if n == "hinm_mx4_product"]
+    assert products == [((K, N, M), dX, N), ((M, K, N), dW, K)]

@@ -37,3 +37,20 @@ def test_a_stream_of_another_pitch(form, K, M, N, width, first):
     want = orc.block_norm(_wide(x, N), None, None, None, None, f64(w_next), 1.0, np.float32(EPS))["u"]
     assert t.shape == x.shape
     _close(_wide(t, N), want, np.abs(want), "bf16", K)
+
+
+def test_gradients_of_a_layer_from_slices_of_larger_arrays():
+    """The same values at other pitches: the same gradients, bit for bit."""
+    import torch
+    from paper_2407_20496_amd import block as blk
+    M, K, N = 130, 200, 51
+    rng = np.random.default_rng(6)
+    draw = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(torch.bfloat16).to(DEV)
+    W, X, dY = draw(M, K + 9)[:, 3:3 + K], draw(K, 64)[:, :N], draw(M, N + 2)[:, 1:1 + N]
+    got = blk.mx4_linear_grad(W, X, dY)
+    want = blk.mx4_linear_grad(W.contiguous(), X.contiguous(), dY.contiguous())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    layer, same = blk.mx4_layer(W), blk.mx4_layer(W.contiguous())
+    held = torch.arange(32 * ((M + 31) // 32), device=DEV).reshape(-1, 32) < M          # rows that exist
+    codes = lambda l: l.codes.reshape(-1, held.shape[0], 8, 32, 16).transpose(2, 3)[:, held]
+    assert torch.equal(codes(layer), codes(same))
