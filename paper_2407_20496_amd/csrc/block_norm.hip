@@ -622,9 +622,10 @@ __device__ __forceinline__ void corrections(const Backward& a, int n, bool first
   f1 = f2 = 0;
   if (n >= a.N) return;
   const float r = a.w_pre ? a.rstd_h[n] : 0.0f, ry = a.w_post ? a.rstd_y[n] : 1.0f;
-  f1 = r * r * r * (s0 / (float)a.K);
+  // one factor after the other: the cube of a reciprocal root leaves float32 where the root of a token of 10^13 does not
+  f1 = r * (r * (r * (s0 / (float)a.K)));
   const float S = s1 + r * s2 - f1 * s3;
-  f2 = a.w_post ? ry * ry * (S / (float)a.K) : 0.0f;
+  f2 = a.w_post ? ry * (ry * (S / (float)a.K)) : 0.0f;
   if (a.dtoken_gate && first) a.dtoken_gate[n] = S * ry;
 }
 // A row's results and its eight columns' part of the channel's two sums.
