@@ -7,8 +7,9 @@
 //   h = s x + r t (c y)   with c = gate w_post per channel, t = token_gate, r = rstd_y per token:
 //   sum h^2 = s^2 sum x^2 + 2 s r t sum x (c y) + (r t)^2 sum (c y)^2.
 // The three may cancel (a block whose output undoes its residual), so they are added in binary64: the products of two floats
-// are exact there and the sum keeps its digits down to 2^-50 of what cancels; what h itself loses is its own rounding.  The
-// gradients' correction S = sum_k c y d is linear in the gradient d in the same way.
+// are exact there and the sum keeps its digits down to 2^-50 of what cancels; what h itself loses is its own rounding.
+// Infinities do not meet in these sums as they do in h, so the cross term leaves them out (cross_of_finite).  The gradients'
+// correction S = sum_k c y d is linear in the gradient d in the same way.
 //
 // Bound by memory: read twice (the second time from the caches behind L2 where they hold it), written once.  bf16, a channel
 // factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 23 against 14, 4096x8192
@@ -235,6 +236,31 @@ __device__ __forceinline__ void load_patch(const Forward& a, const Place& p, int
   }
 }
 
+// A thread's sums x c y once more, for columns that hold what is not finite: over elements of which both are.  An infinity in x or
+// in c y is in its own square's sum, which makes sum h^2 infinite as h is; only where both are infinite and of opposite signs in
+// h, h is not a number, and neither is its sum.  (With the products the sum would hold inf - inf, or 0 inf, where h has none.)
+template <int DT, Layout L>
+__device__ __forceinline__ void cross_of_finite(const Forward& a, const Place& p, double (&squares)[8], double (&cross)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) cross[j] = 0;
+#pragma unroll 1
+  for (int k = p.row0 + (threadIdx.x >> 3); k < p.row0 + p.rows; k += kRowsAtOnce) {
+    const float c = channel_factor(a.w_post, a.gate, k);
+    float x[8], y[8];
+    widen<DT>(place_eight(draw_eight(a.x + (int64_t)k * a.ld_stream + p.n, p.left, known<L>(a.stream)), p.left, known<L>(a.stream)), x);
+    widen<DT>(place_eight(draw_eight(a.y + (int64_t)k * a.ld_block + p.n, p.left, known<L>(a.block)), p.left, known<L>(a.block)), y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float b = c * y[j];
+      const bool x_finite = fabsf(x[j]) < INFINITY, b_finite = fabsf(b) < INFINITY;
+      if (x_finite && b_finite) cross[j] += (double)x[j] * b;
+      if (x_finite || b_finite || j >= p.left) continue;
+      const float t = a.token_gate ? a.token_gate[p.n + j] : 1.0f;
+      if ((x[j] < 0) ^ (b < 0) ^ (a.scale < 0) ^ (t < 0)) squares[j] = NAN;
+    }
+  }
+}
+
 template <int DT, Layout L>
 __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
   const Place p(a.K, a.N, a.rows_per_chunk, L == kLines);
@@ -260,6 +286,10 @@ __global__ __launch_bounds__(kThreads) void block_norm_sums_kernel(Forward a) {
       }
     }
   }
+  bool finite = true;  // squares of floats and sums of them are, in binary64
+#pragma unroll
+  for (int j = 0; j < 8; ++j) finite = finite && (j >= p.left || sum[1][j] + sum[3][j] < INFINITY);
+  if (a.y && !finite) cross_of_finite<DT, L>(a, p, sum[1], sum[2]);
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[0][j] = y_squares[j];
   store_sums<4>(sum, p, a.sums, a.chunks, a.N);

@@ -37,3 +37,60 @@ def test_gradients_of_large_and_small_tokens(K, N, ld):
             _check(name, got, value, HALF_STEP["bf16"] * np.abs(value) + SUM * magnitude + 2.0 ** -134)
         else:
             _check(name, _values(out[name], value.size), value, SUM * magnitude)
+
+
+INF, NAN = float("inf"), float("nan")
+# (x in row 7, x in row 200, y in row 7, y in row 200, row 250: gate zero there; token gate); None: as drawn
+TOKENS = [(None, None, None, None, None, 1), (INF, None, None, None, None, 1), (-INF, None, None, None, None, -0.5), (INF, None, 0, None, None, 1),
+          (INF, -INF, None, None, None, 1), (None, None, INF, None, None, 1), (INF, None, -INF, None, None, 1), (INF, None, INF, None, None, 1),
+          (INF, None, None, -INF, None, 1), (NAN, None, None, None, None, 1), (None, None, None, NAN, None, 1), (None, None, INF, None, None, 0),
+          (INF, None, INF, None, None, -1), (INF, None, -INF, None, None, -1), (None, None, None, None, ("y", INF), 1),
+          (None, None, None, None, ("x", -INF), 1), (INF, INF, -INF, INF, None, 1), (-INF, INF, INF, -INF, None, -2), (INF, None, 0, None, None, 0)]
+
+
+def _same(name, got, want, bound):
+    """Infinities and NaN in the same places, everything else within the bound; exact where the magnitudes are infinite."""
+    bound = np.where(np.isfinite(bound), bound, 0)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), (name, np.argwhere(np.isnan(got) != np.isnan(want))[:4])
+    plain = np.isfinite(want)
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]) and (np.abs(got - want)[plain] <= bound[plain]).all(), name
+
+
+@pytest.mark.parametrize("scale", [1.0, -0.75, 0.0])
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("K,ld,in_place", [(300, 24, False), (1100, 24, False), (1100, 19, False), (1100, 64, False), (1100, 64, True), (9000, 24, True),
+                                           (9000, 1, False)])
+def test_infinities_are_those_of_the_formula(K, ld, in_place, post, scale):
+    """One launch that holds the tokens, two in every layout, and tokens one by one (ld = 1) agree on what an infinity does."""
+    import paper_2407_20496_amd as hinm
+    rng = np.random.default_rng(K)
+    N = len(TOKENS)
+    x, y = rng.standard_normal((2, K, N))
+    for n, (x7, x200, y7, y200, at_zero, _) in enumerate(TOKENS):
+        for a, row, v in ((x, 7, x7), (x, 200, x200), (y, 7, y7), (y, 200, y200)):
+            if v is not None:
+                a[row, n] = v
+        if at_zero:
+            (x if at_zero[0] == "x" else y)[250, n] = at_zero[1]
+    token_gate = np.array([t[5] for t in TOKENS], dtype=np.float32)
+    gate, w = rng.standard_normal(K).astype(np.float32), (1 + 0.3 * rng.standard_normal(K)).astype(np.float32)
+    gate[7], gate[200], gate[250] = 1.5, 0.5, 0
+    w_post = w[::-1].copy() if post else None
+    eps = np.float32(1e-5)
+    for cols in ([slice(n, n + 1) for n in range(N)] if ld == 1 else [slice(0, N)]):
+        n = x[:, cols].shape[1]
+        X, Y = Matrix(K, n, ld, 0, "bf16", x[:, cols]), Matrix(K, n, ld, 0, "bf16", y[:, cols])
+        h, u = (X, Y) if in_place else (Matrix(K, n, ld, 0, "bf16"), Matrix(K, n, ld, 0, "bf16"))
+        ry, rh = _guarded(n, post), _guarded(n)
+        hinm.hinm_block_norm(K, n, "bf16", scale, float(eps), X.ptr, Y.ptr, _vec(w_post), _vec(gate), _vec(token_gate[cols]), _vec(w), h.ptr, ld,
+                             u.ptr, ld, ry, rh, *_workspace(hinm.hinm_block_norm_workspace(K, n)))
+        with np.errstate(all="ignore"):
+            want = orc.block_norm(X.wide, Y.wide, _f32(w_post), _f32(gate), _f32(token_gate[cols]), _f32(w), scale, float(eps))
+            of_h = np.sqrt((want["size"] ** 2).mean(axis=0) + eps) * want["rstd_h"]
+            background = 0x7FFF if in_place else 0x1234
+            _same("h", h.result(background), want["h"], HALF_STEP["bf16"] * np.abs(want["h"]) + SUM * want["size"])
+            _same("rstd_h", _values(rh, n), want["rstd_h"], SUM * of_h * want["rstd_h"])
+            _same("u", u.result(background), want["u"],
+                  HALF_STEP["bf16"] * np.abs(want["u"]) + SUM * np.abs(w)[:, None] * want["rstd_h"] * want["size"] * (1 + of_h))
+            if post:
+                _same("rstd_y", _values(ry, n), want["rstd_y"], SUM * want["rstd_y"])
