@@ -78,6 +78,12 @@ hinm_status check_form(const uint8_t* codes, const uint8_t* scales) {
   return aligned(codes, 16) && aligned(scales, 16) ? HINM_OK : HINM_ERR_SHAPE;
 }
 
+// workgroups that quantise a matrix: 32 x 256 values along the rows, 128 x 64 down the columns
+bool too_many_to_quantize(int32_t rows, int32_t cols, bool columns) {
+  const int64_t pieces = columns ? (int64_t)((cols + 63) / 64) * 2 * mx4_lines(rows) : (int64_t)mx4_row_blocks(rows) * mx4_lines(cols);
+  return pieces >= 2 * kMostGroups;
+}
+
 hinm_status check_product(int32_t M, int32_t N, int32_t K, int32_t dtype, const void* Y, int64_t ldy, uint32_t flags) {
   if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
   if (M <= 0 || N <= 0 || K <= 0) return HINM_ERR_SHAPE;
@@ -697,10 +703,7 @@ hinm_status hinm_mx4_quantize(int32_t rows, int32_t cols, int32_t dtype, const v
   if (st != HINM_OK) return st;
   if (ld < cols || !aligned(src, 2)) return HINM_ERR_SHAPE;
   if (along != HINM_MX4_ROWS && along != HINM_MX4_COLUMNS) return HINM_ERR_UNSUPPORTED;
-  if (rows > kMostSize || cols > kMostSize) return HINM_ERR_UNSUPPORTED;
-  const int64_t pieces = along == HINM_MX4_ROWS ? (int64_t)mx4_row_blocks(rows) * mx4_lines(cols)
-                                                : (int64_t)((cols + 63) / 64) * 2 * mx4_lines(rows);
-  if (pieces >= 2 * kMostGroups) return HINM_ERR_UNSUPPORTED;
+  if (rows > kMostSize || cols > kMostSize || too_many_to_quantize(rows, cols, along == HINM_MX4_COLUMNS)) return HINM_ERR_UNSUPPORTED;
   return launched(launch_mx4_quantize(rows, cols, dtype, src, ld, along == HINM_MX4_COLUMNS, codes, scales,
                                       static_cast<hipStream_t>(stream)));
 }
@@ -754,6 +757,7 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
   const Mx4ProductArgs a{M, N, K, dtype, codes, scales, x_codes, x_scales, Y, ldy, (flags & HINM_EPI_RELU) != 0,
                          (flags & HINM_OUT_F32) != 0};
   if (mx4_quantises_on_the_way(a)) return launched(launch_mx4_on_the_way(a, X, ldx, s));
+  if (too_many_to_quantize(K, N, true)) return HINM_ERR_UNSUPPORTED;
   const hipError_t e = launch_mx4_quantize(K, N, dtype, X, ldx, true, x_codes, x_scales, s);
   return launched(e == hipSuccess ? launch_mx4_product(a, s) : e);
 }
