@@ -365,8 +365,9 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
  * their elements only.  Rows are read and written in 16-byte pieces.  Where they begin at multiples of 16
  * bytes (aligned base, leading dimension a multiple of 8) a piece that holds at least one element of a
  * row is read whole (what lies beyond never reaches a result); otherwise nothing beyond a row is read.
- * Nothing beyond the row length is written.  Sizes above 2^30, more than 2^22 tokens of a norm, and calls of more than some
- * 2^22 workgroups (32 x 256 values or 128 x 128 outputs each) return HINM_ERR_UNSUPPORTED.
+ * Nothing beyond the row length is written.  Sizes above 2^30, more than 2^22 tokens of a norm, calls of more than some
+ * 2^22 workgroups (32 x 256 values or 128 x 128 outputs each), and a norm's gradients of channels from 2^27 on over more than 64
+ * tokens return HINM_ERR_UNSUPPORTED.
  *
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
  * version 1.0): 32 consecutive values of a row share a power of two, and every value is one of

@@ -815,6 +815,8 @@ hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float resi
   for (const float* p : {w_post, gate, token_gate, w_pre, rstd_y, rstd_h, const_cast<const float*>(dw_post),
                          const_cast<const float*>(dgate), const_cast<const float*>(dtoken_gate), const_cast<const float*>(dw_pre)})
     if (!aligned(p, 4)) return HINM_ERR_SHAPE;
+  // channels' gradients of several strips of tokens are added by workgroups of 1024 threads, 32 channels each
+  if (K >= 32 * kMostGroups && N > 64 && (dw_post || dgate || dw_pre)) return HINM_ERR_UNSUPPORTED;
   const size_t need = block_norm_grad_workspace_bytes(K, N);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
   const BlockNormGradArgs a{K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh, du, dx,
