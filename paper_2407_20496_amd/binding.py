@@ -399,10 +399,15 @@ def hinm_spmm_prepared_plan(M, K, V, Kv, dtype, N, ldx, ldy, flags=0) -> Tuple[s
 
 # ---- around the compressed layers: 4-bit layers and a block's norms -------------------------------
 
+def _size(v) -> int:
+    """The nearest value of 32 bits, which the library refuses where v has more (ctypes would cut them off)."""
+    return max(-1 << 31, min(int(v), (1 << 31) - 1))
+
+
 def hinm_mx4_sizes(rows, length) -> Tuple[int, int]:
     """(code_bytes, scale_bytes) of `rows` rows of `length` values in 4-bit form."""
     out = [C.c_size_t(0) for _ in range(2)]
-    _check(load_library().hinm_mx4_sizes(int(rows), int(length), *[C.byref(o) for o in out]), "hinm_mx4_sizes")
+    _check(load_library().hinm_mx4_sizes(_size(rows), _size(length), *[C.byref(o) for o in out]), "hinm_mx4_sizes")
     return tuple(int(o.value) for o in out)
 
 
@@ -432,7 +437,7 @@ def hinm_mx4_product(M, N, K, dtype, a_codes, a_scales, b_codes, b_scales, Y, ld
 
 def hinm_mx4_linear_workspace(M, K, N) -> int:
     out = C.c_size_t(0)
-    _check(load_library().hinm_mx4_linear_workspace(int(M), int(K), int(N), C.byref(out)), "hinm_mx4_linear_workspace")
+    _check(load_library().hinm_mx4_linear_workspace(_size(M), _size(K), _size(N), C.byref(out)), "hinm_mx4_linear_workspace")
     return int(out.value)
 
 
@@ -447,7 +452,7 @@ def hinm_mx4_linear(M, K, N, dtype, codes, scales, X, ldx, Y, ldy, flags=0, work
 
 def hinm_block_norm_workspace(K, N) -> int:
     out = C.c_size_t(0)
-    _check(load_library().hinm_block_norm_workspace(int(K), int(N), C.byref(out)), "hinm_block_norm_workspace")
+    _check(load_library().hinm_block_norm_workspace(_size(K), _size(N), C.byref(out)), "hinm_block_norm_workspace")
     return int(out.value)
 
 
@@ -463,7 +468,7 @@ def hinm_block_norm(K, N, dtype, residual_scale, eps, x, y, w_post, gate, token_
 
 def hinm_block_norm_grad_workspace(K, N) -> int:
     out = C.c_size_t(0)
-    _check(load_library().hinm_block_norm_grad_workspace(int(K), int(N), C.byref(out)), "hinm_block_norm_grad_workspace")
+    _check(load_library().hinm_block_norm_grad_workspace(_size(K), _size(N), C.byref(out)), "hinm_block_norm_grad_workspace")
     return int(out.value)
 
 

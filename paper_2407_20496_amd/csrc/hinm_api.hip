@@ -689,6 +689,7 @@ hinm_status hinm_calib_mid_plan(const hinm_shape* shape, int32_t N, int32_t form
 
 hinm_status hinm_mx4_sizes(int32_t rows, int32_t length, size_t* code_bytes, size_t* scale_bytes) {
   if (rows <= 0 || length <= 0) return HINM_ERR_SHAPE;
+  if (rows > kMostSize || length > kMostSize) return HINM_ERR_UNSUPPORTED;
   if (code_bytes) *code_bytes = (size_t)mx4_code_bytes(rows, length);
   if (scale_bytes) *scale_bytes = (size_t)mx4_scale_bytes(rows, length);
   return HINM_OK;

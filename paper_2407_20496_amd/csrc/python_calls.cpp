@@ -79,12 +79,30 @@ bool to_ptrs(PyObject* const* a, int n, void** out) {
     if (!to_ptr(a[i], &out[i])) return false;
   return true;
 }
+// The nearest value that fits: what 32 bits do not hold, the library refuses as out of range, and must not see as what is
+// left of it.
+bool to_nearest(PyObject* o, int64_t low, int64_t high, int64_t* out) {
+  PyObject* n = PyNumber_Long(o);
+  if (!n) return false;
+  int beyond;
+  const long long v = PyLong_AsLongLongAndOverflow(n, &beyond);
+  Py_DECREF(n);
+  if (v == -1 && PyErr_Occurred()) return false;
+  *out = beyond > 0 || v > high ? high : beyond < 0 || v < low ? low : (int64_t)v;
+  return true;
+}
 bool to_sizes(PyObject* const* a, int n, int32_t* out) {
   for (int i = 0; i < n; ++i) {
     int64_t v;
-    if (!to_i64(a[i], &v)) return false;
+    if (!to_nearest(a[i], INT32_MIN, INT32_MAX, &v)) return false;
     out[i] = (int32_t)v;
   }
+  return true;
+}
+bool to_flags(PyObject* o, uint32_t* out) {
+  int64_t v;
+  if (!to_nearest(o, -1, UINT32_MAX, &v)) return false;
+  *out = (uint32_t)v;
   return true;
 }
 
@@ -322,13 +340,14 @@ PyObject* mx4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* mx4_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t d[3], dtype;
   void *p[5], *stream;
-  int64_t ldy, flags;
+  int64_t ldy;
+  uint32_t flags;
   if (!takes(n, 12) || !to_sizes(a, 3, d) || !to_dtype(a[3], &dtype) || !to_ptrs(a + 4, 5, p) || !to_i64(a[9], &ldy) ||
-      !to_i64(a[10], &flags) || !to_stream(a[11], &stream))
+      !to_flags(a[10], &flags) || !to_stream(a[11], &stream))
     return nullptr;
   return status_of([&] {
     return f_mx4_product(d[0], d[1], d[2], dtype, static_cast<uint8_t*>(p[0]), static_cast<uint8_t*>(p[1]),
-                         static_cast<uint8_t*>(p[2]), static_cast<uint8_t*>(p[3]), p[4], ldy, (uint32_t)flags, stream);
+                         static_cast<uint8_t*>(p[2]), static_cast<uint8_t*>(p[3]), p[4], ldy, flags, stream);
   });
 }
 
@@ -336,14 +355,15 @@ PyObject* mx4_product(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int32_t d[3], dtype;
   void *form[2], *x, *y, *ws, *stream;
-  int64_t ldx, ldy, flags, bytes;
+  int64_t ldx, ldy, bytes;
+  uint32_t flags;
   if (!takes(n, 14) || !to_sizes(a, 3, d) || !to_dtype(a[3], &dtype) || !to_ptrs(a + 4, 2, form) || !to_ptr(a[6], &x) ||
-      !to_i64(a[7], &ldx) || !to_ptr(a[8], &y) || !to_i64(a[9], &ldy) || !to_i64(a[10], &flags) || !to_ptr(a[11], &ws) ||
+      !to_i64(a[7], &ldx) || !to_ptr(a[8], &y) || !to_i64(a[9], &ldy) || !to_flags(a[10], &flags) || !to_ptr(a[11], &ws) ||
       !to_i64(a[12], &bytes) || !to_stream(a[13], &stream))
     return nullptr;
   return status_of([&] {
     return f_mx4_linear(d[0], d[1], d[2], dtype, static_cast<uint8_t*>(form[0]), static_cast<uint8_t*>(form[1]), x, ldx, y, ldy,
-                        (uint32_t)flags, ws, (size_t)bytes, stream);
+                        flags, ws, (size_t)bytes, stream);
   });
 }
 
