@@ -432,7 +432,7 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
  * in a fixed order, in fp32, and in binary64 where terms of h may cancel.  Infinities and NaN do to a token what they do in
  * these formulas, whatever stands beside it; a token whose root mean square passes 10^17 may count as infinite, as its sum of
  * squares is held in fp32 where one launch holds it.
- * workspace: hinm_block_norm_workspace bytes, 256-byte aligned. */
+ * workspace: hinm_block_norm_workspace bytes, 256-byte aligned; where few channels or tokens need 0, it may be NULL. */
 hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_block_norm(int32_t K, int32_t N, int32_t dtype, float residual_scale, float eps,
                             const void* x, const void* y, const float* w_post, const float* gate,
@@ -452,7 +452,7 @@ hinm_status hinm_block_norm(int32_t K, int32_t N, int32_t dtype, float residual_
  * no block, only dx and dw_pre.  Outputs may be NULL where they are not wanted; dw_post, dgate, dtoken_gate and
  * dw_pre (float32, overwritten) only where their input is given.  dx may be dh and dy may be du; h, dh and dx
  * have leading dimension ld_stream, y, du and dy ld_block.  Sums in fp32 in a fixed order.
- * workspace: hinm_block_norm_grad_workspace bytes, 256-byte aligned. */
+ * workspace: hinm_block_norm_grad_workspace bytes, 256-byte aligned; where few channels or tokens need 0, it may be NULL. */
 hinm_status hinm_block_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float residual_scale, const void* h,
                                  const void* y, const float* w_post, const float* gate, const float* token_gate,

@@ -857,7 +857,14 @@ bool in_lines(const void* p, int64_t ld) { return !p || ((reinterpret_cast<uintp
 
 }  // namespace
 
-size_t block_norm_workspace_bytes(int K, int N) { return (size_t)4 * chunk_count(K, N) * N * sizeof(double); }
+// Rounds of the forward kernel that holds all rows, or 0.
+static int rounds_held(int K, int N) {
+  if (K <= 2 * kHeldThreads && (int64_t)K * N <= 3 << 20) return 2;
+  return K <= 8 * kHeldThreads && N <= 16 ? 8 : 0;
+}
+size_t block_norm_workspace_bytes(int K, int N) {
+  return rounds_held(K, N) ? 0 : (size_t)4 * chunk_count(K, N) * N * sizeof(double);
+}
 
 template <int DT, Layout L>
 static hipError_t launch_forward_strips(const Forward& a, hipStream_t stream) {
@@ -885,13 +892,10 @@ static hipError_t launch_forward(const Forward& a, hipStream_t stream) {
     else launch_vector<DT, false>(v, stream);
     return hipGetLastError();
   }
-  const dim3 held((uint32_t)(((a.N + 7) / 8 + 7) / 8 * 8));
-  if (a.K <= 2 * kHeldThreads && (int64_t)a.K * a.N <= 3 << 20) {
-    block_norm_held_kernel<DT, 2><<<held, kHeldThreads, 0, stream>>>(a);
-    return hipGetLastError();
-  }
-  if (a.K <= 8 * kHeldThreads && a.N <= 16) {
-    block_norm_held_kernel<DT, 8><<<held, kHeldThreads, 0, stream>>>(a);
+  if (const int rounds = rounds_held(a.K, a.N)) {
+    const dim3 held((uint32_t)(((a.N + 7) / 8 + 7) / 8 * 8));
+    if (rounds == 2) block_norm_held_kernel<DT, 2><<<held, kHeldThreads, 0, stream>>>(a);
+    else block_norm_held_kernel<DT, 8><<<held, kHeldThreads, 0, stream>>>(a);
     return hipGetLastError();
   }
   if (a.layout == kLines) return launch_forward_strips<DT, kLines>(a, stream);

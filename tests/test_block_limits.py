@@ -67,3 +67,33 @@ def test_calls_refuse_flags_that_32_bits_do_not_hold(flags):
         with pytest.raises(hinm.HinmError) as e:
             call()
         assert e.value.status == UNSUPPORTED
+
+
+HELD = [(1, 1), (768, 1), (4096, 1), (4096, 16), (768, 4096), (1024, 100)]
+IN_TWO = [(4097, 1), (4097, 16), (4096, 17), (768, 4097), (1025, 17), (16384, 4096)]
+
+
+def test_a_norm_in_one_launch_asks_for_no_workspace():
+    assert [hinm.hinm_block_norm_workspace(*s) for s in HELD] == [0] * len(HELD)
+    assert all(hinm.hinm_block_norm_workspace(*s) > 0 for s in IN_TWO)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("K,N", HELD)
+def test_a_norm_in_one_launch_takes_no_workspace(K, N):
+    import numpy as np
+    import torch
+    from oracle import block_oracle as orc
+    from tests.test_gpu_block_norm import HALF_STEP, SUM
+    ld = (N + 7) // 8 * 8
+    x, y = (torch.randn(K, ld, device="cuda:0").to(torch.bfloat16) for _ in range(2))
+    w = torch.rand(K, device="cuda:0") + 0.5
+    h, u = torch.empty_like(x), torch.empty_like(x)
+    hinm.hinm_block_norm(K, N, "bf16", 1.0, 1e-5, x, y, w, None, None, w, h, ld, u, ld)
+    wide = lambda t: t[:, :N].float().cpu().numpy().astype(np.float64)
+    wd = w.cpu().numpy().astype(np.float64)
+    want = orc.block_norm(wide(x), wide(y), wd, None, None, wd, 1.0, 1e-5)
+    assert (np.abs(wide(h) - want["h"]) <= HALF_STEP["bf16"] * np.abs(want["h"]) + SUM * want["size"]).all()
+    of_h = np.sqrt((want["size"] ** 2).mean(axis=0) + 1e-5) * want["rstd_h"]
+    assert (np.abs(wide(u) - want["u"]) <= HALF_STEP["bf16"] * np.abs(want["u"])
+            + SUM * wd[:, None] * want["rstd_h"] * want["size"] * (1 + of_h)).all()
