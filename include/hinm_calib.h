@@ -87,6 +87,11 @@ hinm_status hinm_calib_tile_part(const hinm_shape* shape, int32_t N, const void*
  * columns serves it, as text; empty if another kernel does.  Needs no device. */
 hinm_status hinm_calib_mid_plan(const hinm_shape* shape, int32_t N, int32_t form, char* text, size_t text_bytes);
 
+/* The launches of hinm_mx4_product (quantize = 0) or of hinm_mx4_linear (quantize = 1) for these sizes and flags, as text.  Needs
+ * no device; returns what such a call would for valid pointers. */
+hinm_status hinm_calib_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t dtype, uint32_t flags, int32_t quantize, char* text,
+                                size_t text_bytes);
+
 #ifdef __cplusplus
 }
 #endif

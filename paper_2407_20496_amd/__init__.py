@@ -21,5 +21,5 @@ from .binding import (  # noqa: F401
     hinm_block_norm_workspace, hinm_block_norm, hinm_block_norm_grad_workspace, hinm_block_norm_grad,
     hinm_status_str, hinm_version,
     calib_symbols, hinm_calib_copy, hinm_calib_fill, hinm_calib_read, hinm_calib_scatter_rows, hinm_calib_smfmac,
-    hinm_calib_empty, hinm_calib_lds_stream, hinm_calib_gather_stream, hinm_calib_tile_part, hinm_calib_mid_plan,
+    hinm_calib_empty, hinm_calib_lds_stream, hinm_calib_gather_stream, hinm_calib_tile_part, hinm_calib_mid_plan, hinm_calib_mx4_plan,
 )

@@ -52,7 +52,7 @@ def calib_symbols() -> Tuple[str, ...]:
     """Entry points include/hinm_calib.h declares (measurement aids)."""
     return ("hinm_calib_copy", "hinm_calib_fill", "hinm_calib_read", "hinm_calib_scatter_rows", "hinm_calib_smfmac",
             "hinm_calib_empty", "hinm_calib_lds_stream", "hinm_calib_gather_stream", "hinm_calib_tile_part",
-            "hinm_calib_mid_plan")
+            "hinm_calib_mid_plan", "hinm_calib_mx4_plan")
 
 
 def load_library():
@@ -141,6 +141,7 @@ def load_library():
     lib.hinm_calib_gather_stream.argtypes = [C.c_void_p, C.c_size_t, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                              C.c_int32, C.c_void_p]
     lib.hinm_calib_tile_part.argtypes = [sp, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
+    lib.hinm_calib_mx4_plan.argtypes = [i32, i32, i32, i32, C.c_uint32, i32, C.c_char_p, sz]
     lib.hinm_calib_mid_plan.argtypes = [sp, C.c_int32, C.c_int32, C.c_char_p, C.c_size_t]
     for name in calib_symbols():
         getattr(lib, name).restype = C.c_int
@@ -543,6 +544,14 @@ def hinm_calib_mid_plan(M, K, V, Kv, dtype, N, form) -> str:
     buf = C.create_string_buffer(256)
     _check(load_library().hinm_calib_mid_plan(C.byref(_shape(M, K, V, Kv, dtype)), int(N), int(form), buf, len(buf)),
            "hinm_calib_mid_plan")
+    return buf.value.decode()
+
+
+def hinm_calib_mx4_plan(M, N, K, dtype, flags=0, quantize=False) -> str:
+    """The launches of hinm_mx4_product, or with `quantize` of hinm_mx4_linear, for these sizes."""
+    buf = C.create_string_buffer(512)
+    _check(load_library().hinm_calib_mx4_plan(_size(M), _size(N), _size(K), _dtype_code(dtype), int(flags), int(bool(quantize)), buf,
+                                              len(buf)), "hinm_calib_mx4_plan")
     return buf.value.decode()
 
 

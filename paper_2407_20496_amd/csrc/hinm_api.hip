@@ -763,6 +763,22 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
   return launched(e == hipSuccess ? launch_mx4_product(a, s) : e);
 }
 
+hinm_status hinm_calib_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t dtype, uint32_t flags, int32_t quantize, char* text,
+                                size_t text_bytes) {
+  if (!text || text_bytes == 0) return HINM_ERR_NULL;
+  text[0] = 0;
+  void* const fake = reinterpret_cast<void*>(uintptr_t{1} << 20);  // never dereferenced
+  const hinm_status st = check_product(M, N, K, dtype, fake, N, flags);
+  if (st != HINM_OK) return st;
+  LaunchPlan plan{text, text_bytes};
+  const Mx4ProductArgs a{M, N, K, dtype, nullptr, nullptr, nullptr, nullptr, fake, N, (flags & HINM_EPI_RELU) != 0,
+                         (flags & HINM_OUT_F32) != 0, &plan};
+  if (quantize && mx4_quantises_on_the_way(a)) return launched(launch_mx4_on_the_way(a, fake, N, nullptr));
+  if (quantize && too_many_to_quantize(K, N, true)) return HINM_ERR_UNSUPPORTED;
+  if (quantize) plan_record(&plan, "mx4_columns_kernel<DT=%d>", dtype);
+  return launched(launch_mx4_product(a, nullptr));
+}
+
 hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {
   if (!workspace_bytes) return HINM_ERR_NULL;
   const hinm_status st = check_norm(K, N, HINM_F16);

@@ -302,6 +302,7 @@ struct Mx4ProductArgs {
   int64_t ldy;
   bool relu;
   bool out_f32;
+  LaunchPlan* plan = nullptr;  // set: record what would be launched instead
 };
 hipError_t launch_mx4_product(const Mx4ProductArgs& a, hipStream_t stream);
 // B given as 16-bit values [K][N] of stride ldx (b_codes and b_scales are not used): the product with their 4-bit form in one

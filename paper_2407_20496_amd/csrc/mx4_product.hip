@@ -218,6 +218,10 @@ __global__ __launch_bounds__(64 * WAVES, 8 / WAVES) void mx4_stream_kernel(const
 template <int OUT, int WM, int WN, int WAVES>
 hipError_t launch_stream(const Mx4ProductArgs& a, const ProductShape& p, hipStream_t stream) {
   const int64_t items = (int64_t)((p.M + 32 * WM - 1) / (32 * WM)) * ((p.N + 32 * WN - 1) / (32 * WN));
+  if (a.plan) {
+    plan_record(a.plan, "mx4_stream_kernel<OUT=%d,WM=%d,WN=%d,WAVES=%d> grid=%u block=%d", OUT, WM, WN, WAVES, grid_of_items(items), 64 * WAVES);
+    return hipSuccess;
+  }
   mx4_stream_kernel<OUT, WM, WN, WAVES><<<dim3(grid_of_items(items)), 64 * WAVES, 0, stream>>>(a.a_codes, a.a_scales, a.b_codes,
                                                                                              a.b_scales, a.Y, p);
   return hipGetLastError();
@@ -700,6 +704,10 @@ template <int OUT, int WM, int WN, int RING>
 hipError_t launch_tile(const Mx4ProductArgs& a, const ProductShape& p, hipStream_t stream) {
   using T = TileSizes<WM, WN, RING>;
   const int64_t tiles = (int64_t)((p.M + T::TM - 1) / T::TM) * ((p.N + T::TN - 1) / T::TN);
+  if (a.plan) {
+    plan_record(a.plan, "mx4_tile_kernel<OUT=%d,WM=%d,WN=%d,RING=%d> grid=%u block=256 lds=%d", OUT, WM, WN, RING, grid_of_items(tiles), T::kLds);
+    return hipSuccess;
+  }
   const hipError_t e = raise_lds_limit<mx4_tile_kernel<OUT, WM, WN, RING>>(T::kLds);
   if (e != hipSuccess) return e;
   mx4_tile_kernel<OUT, WM, WN, RING><<<dim3(grid_of_items(tiles)), 256, T::kLds, stream>>>(a.a_codes, a.a_scales, a.b_codes,
@@ -772,6 +780,10 @@ hipError_t launch_out(const Mx4ProductArgs& a, hipStream_t stream) {
 template <int OUT, int DT>
 hipError_t launch_token(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
+  if (a.plan) {
+    plan_record(a.plan, "mx4_token_kernel<OUT=%d,DT=%d> grid=%u block=512", OUT, DT, grid_of_items(mx4_row_blocks(a.M)));
+    return hipSuccess;
+  }
   mx4_token_kernel<OUT, DT><<<dim3(grid_of_items(mx4_row_blocks(a.M))), 512, 0, stream>>>(
       a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, a.Y, p);
   return hipGetLastError();
@@ -781,6 +793,10 @@ template <int OUT, int DT>
 hipError_t launch_few(const Mx4ProductArgs& a, const void* x, int64_t ldx, hipStream_t stream) {
   const ProductShape p{a.M, a.N, a.K, a.ldy, a.relu};
   const dim3 grid(grid_of_items((int64_t)mx4_row_blocks(a.M) * ((a.N + 31) / 32)));
+  if (a.plan) {
+    plan_record(a.plan, "mx4_few_kernel<OUT=%d,DT=%d,P=%d> grid=%u block=512", OUT, DT, a.N <= 8 ? 1 : a.N <= 16 ? 2 : 4, grid.x);
+    return hipSuccess;
+  }
   const Pieces pieces = pieces_of_rows(x, ldx, a.N);
   auto launch = [&](auto kernel) {
     kernel<<<grid, 512, 0, stream>>>(a.a_codes, a.a_scales, static_cast<const uint16_t*>(x), ldx, pieces, a.Y, p);
