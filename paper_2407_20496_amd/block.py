@@ -153,8 +153,10 @@ class FeedForward:
         self.y = new(self.K)
         for what, t in (("w_post", w_post), ("gate", gate), ("w_next", w_next)):
             _factors(t, what, self.K, self.y.device)
-        if self.in_4_bits and any(t.device != self.y.device for l in layers for t in (l.codes, l.scales)):
-            raise ValueError(f"the layers' weights are not on {self.y.device}")
+        for l in layers if self.in_4_bits else ():
+            for t, n in zip((l.codes, l.scales), hb.hinm_mx4_sizes(l.M, l.K)):
+                if t.dtype != torch.uint8 or t.numel() < n or not t.is_contiguous() or t.device != self.y.device:
+                    raise ValueError(f"weights: {n} bytes on {self.y.device} wanted, not {t.dtype} {list(t.shape)} on {t.device}")
         if self.in_4_bits:
             self.between = [new(l.M) for l in layers[:-1]]
             self.scratch_bytes = max(hb.hinm_mx4_linear_workspace(l.M, l.K, tokens) for l in layers)

@@ -174,3 +174,12 @@ def test_a_layers_gradients_take_the_pitch_of_each_array(cols_w, cols_x, cols_dy
     assert quantised[dY.data_ptr(), hinm.MX4_COLUMNS] == quantised[dY.data_ptr(), hinm.MX4_ROWS] == (M, N, BF16, dY, cols_dy)
     products = [(a[:3], a[8], a[9]) for n, a in calls if n == "hinm_mx4_product"]
     assert products == [((K, N, M), dX, N), ((M, K, N), dW, K)]
+
+
+@pytest.mark.parametrize("which", ["codes", "scales"])
+def test_a_block_refuses_layers_with_less_memory_than_their_form_has(which):
+    for cut in (lambda t: t[:-1], lambda t: t.view(torch.int16), lambda t: t.repeat(2)[::2]):
+        short = _layer(M, K)
+        setattr(short, which, cut(getattr(short, which)))
+        with pytest.raises(ValueError):
+            blk.FeedForward([short, _layer(K, M)], N, None, device="cpu")
