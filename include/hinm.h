@@ -412,7 +412,8 @@ hinm_status hinm_mx4_product(int32_t M, int32_t N, int32_t K, int32_t dtype, con
 
 /* A 4-bit layer on 16-bit activations: Y [M][N] = W X with W in 4-bit form (M rows of length K) and X [K][N]
  * quantised along its columns on the way; the result is that of hinm_mx4_quantize and hinm_mx4_product, bit for
- * bit.  One token and small products take one launch, others two.  workspace: hinm_mx4_linear_workspace bytes of device memory, 256-byte aligned. */
+ * bit.  One token and small products take one launch, others two.  Y must not overlap X.  workspace:
+ * hinm_mx4_linear_workspace bytes of device memory, 256-byte aligned. */
 hinm_status hinm_mx4_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const uint8_t* codes,
                             const uint8_t* scales, const void* X, int64_t ldx, void* Y, int64_t ldy,

@@ -12,9 +12,9 @@
 // correction S = sum_k c y d is linear in the gradient d in the same way.
 //
 // Bound by memory: read twice (the second time from the caches behind L2 where they hold it), written once.  bf16, a channel
-// factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 23 against 14, 4096x8192
-// 77 against 56, 16384x1000 (rows that share lines) 53 against 27; gradients 4096x2048 40 against 21, 4096x8192 139 against
-// 84, 16384x1000 84 against 41.  Kernels alone: 4096x8192 sums at 5.1 TB/s, results at 6.0; gradients at 4.8 and 4.9.
+// factor and a token's gate, us against what reading and writing once takes at 4.8 TB/s: 4096x2048 23.5 against 14, 4096x8192
+// 76 against 56, 16384x1000 (rows that share lines) 53 against 27; gradients 4096x2048 38 against 21, 4096x8192 138 against
+// 84, 16384x1000 85 against 41.  Kernels alone: 4096x8192 sums at 5.1 TB/s, results at 6.0; gradients at 4.8 and 4.9.
 #include "eight_values.h"
 
 namespace hinm {

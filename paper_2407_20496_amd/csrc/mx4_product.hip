@@ -444,9 +444,11 @@ __global__ __launch_bounds__(512) void mx4_few_kernel(const uint8_t* codes, cons
 // stage 2 g + RING, and read after stage 2 g + RING - 1; their place held group g - RING / 2.  Beyond the last stage the last
 // one is copied again; nobody reads it.
 //   What bounds it: 16384x16384x8192 takes 0.93 to 1.0 ms, 4.4 to 4.7 PFLOP/s, at a clock that the power limit holds at 1.5 to
-// 1.6 GHz (a loop of nothing but the instruction reaches 6.3 PFLOP/s on such operands, 8.7 on zeros).  Tiles of 128 rows draw
-// 36 KB a stage and unit from L2, 15 TB/s over the chip: 4096x4096 of 1000 columns 13.4 us (2.5 PFLOP/s), of 2048 22 us (3.1);
-// with operands of zeros 18.5.  Tiles of 256x128 measured the same there (22.2) and less elsewhere.
+// 1.6 GHz (a loop of nothing but the instruction reaches 6.3 PFLOP/s on such operands, 8.7 on zeros).  Tiles of 128 rows wait:
+// a stage is 512 clocks of products and takes some 1400, as one wave a SIMD stands at its copies, the barrier and its LDS reads in
+// turn (matrix units busy 36 % of its life; 36 KB a stage and unit are half of what L2 gives): 4096x4096 of 1000 columns 13.4 to
+// 15.8 us (2.1 to 2.5 PFLOP/s).  Two workgroups a unit, 2048 columns: busy half of the time, 23 us (3.0); with operands of zeros
+// 18.5.  Tiles of 256x128 measured the same there (22.2) and less elsewhere.
 
 template <int WM, int WN, int RING>
 struct TileSizes {
