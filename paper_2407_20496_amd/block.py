@@ -48,6 +48,10 @@ def _row_pitch(t: torch.Tensor, what: str) -> int:
 
 def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dtype=None, device=None) -> int:
     """... of a [K][>= tokens] one."""
+    if K is not None and t.dim() == 2 and t.dtype is dtype and t.device == device:  # a step pays for this: 0.8 us here, 2.1 below
+        (rows, cols), (ld, step) = t.shape, t.stride()
+        if rows == K > 1 and cols >= tokens and ld >= cols and step == 1:
+            return ld
     ld = _row_pitch(t, what)
     if t.shape[1] < tokens or (K is not None and t.shape[0] != K):
         raise ValueError(f"{what}: [{'channels' if K is None else K}][at least {tokens}] wanted, not {list(t.shape)}")
