@@ -430,9 +430,9 @@ hinm_status hinm_mx4_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, cons
  * block (u and rstd_h are left alone and may be NULL); rstd_y / rstd_h not wanted; h not wanted (then w_pre and u
  * are needed).  u is computed from h before its rounding.  x and h have leading dimension ld_stream, y
  * and u ld_block.  h may be x and u may be y; apart from that outputs must not overlap inputs.  Sums
- * in a fixed order, in fp32, and in binary64 where terms of h may cancel.  Infinities and NaN do to a token what they do in
- * these formulas, whatever stands beside it; a token whose root mean square passes 10^17 may count as infinite, as its sum of
- * squares is held in fp32 where one launch holds it.
+ * in a fixed order, in fp32, and in binary64 where terms of h may cancel.  Infinities and NaN of x and y do to a token
+ * what they do in these formulas, whatever stands beside it.  Squares of y, and of h where one launch holds a token, are summed
+ * in fp32: a token's root mean square may be at most 10^17 and, where eps is 0, at least 10^-17.
  * workspace: hinm_block_norm_workspace bytes, 256-byte aligned; where few channels or tokens need 0, it may be NULL. */
 hinm_status hinm_block_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_block_norm(int32_t K, int32_t N, int32_t dtype, float residual_scale, float eps,
