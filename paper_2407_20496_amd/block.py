@@ -47,11 +47,13 @@ def _row_pitch(t: torch.Tensor, what: str) -> int:
 
 
 def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dtype=None, device=None) -> int:
-    """... of a [K][>= tokens] one."""
+    """... of a [K][>= tokens] one; one token may be a vector."""
     if K is not None and t.dim() == 2 and t.dtype is dtype and t.device == device:  # a step pays for this: 0.8 us here, 2.1 below
         (rows, cols), (ld, step) = t.shape, t.stride()
         if rows == K > 1 and cols >= tokens and ld >= cols and step == 1:
             return ld
+    if t.dim() == 1 and tokens == 1:
+        t = t.unsqueeze(1)
     ld = _row_pitch(t, what)
     if t.shape[1] < tokens or (K is not None and t.shape[0] != K):
         raise ValueError(f"{what}: [{'channels' if K is None else K}][at least {tokens}] wanted, not {list(t.shape)}")
@@ -61,10 +63,8 @@ def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dty
 
 
 def _factors(t: Optional[torch.Tensor], what: str, n: int, device) -> None:
-    """A float32 vector of n consecutive values, or none."""
-    if t is None:
-        return
-    if t.shape != (n,) or t.dtype != torch.float32 or (n > 1 and t.stride(0) != 1) or t.device != device:
+    """n float32 values or more, one after the other, or none at all."""
+    if t is not None and (t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous() or t.device != device):
         raise ValueError(f"{what}: {n} consecutive float32 on {device} wanted, not {list(t.shape)} {t.dtype} on {t.device}")
 
 

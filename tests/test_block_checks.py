@@ -73,9 +73,8 @@ def test_a_wider_view_is_as_good_as_a_buffer_of_the_blocks_pitch(calls):
     assert _block().run_layers(u) is not None and calls[0][0] == "hinm_mx4_linear" and calls[0][1][7] == LD
 
 
-BAD_VECTORS = {"float64": torch.ones(K, dtype=torch.float64), "short": torch.ones(K - 1), "long": torch.ones(K + 1),
-               "apart": torch.ones(2 * K)[::2], "one for all": torch.ones(1).expand(K), "a matrix": torch.ones(K, 1),
-               "another device": torch.ones(K, device="meta")}
+BAD_VECTORS = {"float64": torch.ones(K, dtype=torch.float64), "bfloat16": torch.ones(K, dtype=torch.bfloat16), "short": torch.ones(N - 1),
+               "apart": torch.ones(2 * K)[::2], "one for all": torch.ones(1).expand(K), "another device": torch.ones(K, device="meta")}
 
 
 @pytest.mark.parametrize("bad", BAD_VECTORS.values(), ids=BAD_VECTORS)
@@ -87,8 +86,23 @@ def test_a_block_refuses_other_factors(bad, calls):
     with pytest.raises(ValueError):
         blk.block_input(_new(), bad, N)
     with pytest.raises(ValueError):
-        _block()(_new(), _new(), token_gate=bad)      # as many as tokens are wanted, and no fewer
+        _block()(_new(), _new(), token_gate=bad)
     assert not calls
+
+
+def test_a_block_takes_factors_of_any_shape_and_room_for_more_tokens(calls):
+    block = blk.FeedForward([_layer(M, K), _layer(K, M)], N, torch.ones(K, 1), torch.ones(1, K), torch.ones(K), device="cpu")
+    block(_new(), _new(), token_gate=torch.ones(N + 5))
+    assert calls[-1][0] == "hinm_block_norm"
+
+
+@pytest.mark.parametrize("x,pitch", [(_new(cols=1), 1), (_new(cols=1).reshape(-1), 1), (_new()[:, 3:4], LD), (_new()[:, 3], LD)])
+def test_one_token_may_be_a_vector(x, pitch, calls):
+    block = blk.FeedForward([_layer(M, K), _layer(K, M)], 1, torch.ones(K), w_next=torch.ones(K), device="cpu")
+    u = _new(cols=1).reshape(x.shape)
+    assert block(x, u)[1] is u and calls[-1][1][12] == pitch and calls[-1][1][14] == 1
+    with pytest.raises(ValueError):
+        block(x[1:], u)
 
 
 def test_a_blocks_layers_share_their_type_and_device():
