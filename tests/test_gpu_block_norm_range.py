@@ -94,3 +94,29 @@ def test_infinities_are_those_of_the_formula(K, ld, in_place, post, scale):
                   HALF_STEP["bf16"] * np.abs(want["u"]) + SUM * np.abs(w)[:, None] * want["rstd_h"] * want["size"] * (1 + of_h))
             if post:
                 _same("rstd_y", _values(ry, n), want["rstd_y"], SUM * want["rstd_y"])
+
+
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("K,N,ld", [(300, 9, 16), (3000, 9, 16), (1100, 27, 32), (1100, 27, 27), (1100, 81, 128), (5000, 1, 1)])
+def test_large_and_small_tokens(K, N, ld, post):
+    """Down to 1e-17 without eps, up to 1e17, in every kernel."""
+    import paper_2407_20496_amd as hinm
+    rng = np.random.default_rng(K + N)
+    sizes = [1e17, 1e-17, 1e15, 1e-13, 1.0, 1e13, 1e5, 1e-5, 3e-15]
+    for first in range(len(sizes) if N == 1 else 1):
+        size = np.array([sizes[(first + n) % len(sizes)] for n in range(N)])
+        x, y = (Matrix(K, N, ld, 0, "bf16", rng.standard_normal((K, N)) * size) for _ in range(2))
+        h, u = Matrix(K, N, ld, 0, "bf16"), Matrix(K, N, ld, 0, "bf16")
+        w_post, w_pre = (1 + 0.3 * rng.standard_normal((2, K))).astype(np.float32)
+        ry, rh = _guarded(N, post), _guarded(N)
+        given = w_post if post else None
+        hinm.hinm_block_norm(K, N, "bf16", 0.75, 0.0, x.ptr, y.ptr, _vec(given), None, None, _vec(w_pre), h.ptr, ld, u.ptr, ld, ry, rh,
+                             *_workspace(hinm.hinm_block_norm_workspace(K, N)))
+        want = orc.block_norm(x.wide, y.wide, _f32(given), None, None, _f32(w_pre), 0.75, 0.0)
+        of_h = np.sqrt((want["size"] ** 2).mean(axis=0)) * want["rstd_h"]
+        _check("h", h.result(), want["h"], HALF_STEP["bf16"] * np.abs(want["h"]) + SUM * want["size"])
+        _check("rstd_h", _values(rh, N), want["rstd_h"], SUM * of_h * want["rstd_h"])
+        _check("u", u.result(), want["u"], HALF_STEP["bf16"] * np.abs(want["u"])
+               + SUM * np.abs(_f32(w_pre))[:, None] * want["rstd_h"] * want["size"] * (1 + of_h))
+        if post:
+            _check("rstd_y", _values(ry, N), want["rstd_y"], SUM * want["rstd_y"])
