@@ -86,6 +86,10 @@ typedef enum { HINM_F16 = 0, HINM_BF16 = 1 } hinm_dtype;
 enum {
   HINM_EPI_RELU = 1u,         /* y = max(y, 0) before rounding (used between chained layers) */
   HINM_OUT_F32 = 2u,          /* Y is float32 [M][N]: the un-rounded accumulators (verification mode) */
+  /* hinm_linear and hinm_linear_grad only, at most one of them and HINM_EPI_RELU */
+  HINM_EPI_GELU = 4u,         /* z Phi(z), Phi the normal distribution's probability of less than z */
+  HINM_EPI_GELU_TANH = 8u,    /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+  HINM_EPI_SILU = 16u,        /* z / (1 + exp(-z)) */
   /* kernel choice; default (none set) picks by shape */
   HINM_KERNEL_REFERENCE = 0x100u, /* one thread per output element, plain FMA; any V */
   HINM_KERNEL_SMFMAC = 0x200u,    /* a sparse-MFMA kernel: 32x32 tiles (V in {32,64,96,128}, Kv % 32 == 0,
@@ -461,6 +465,67 @@ hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float resi
                                  const void* du, void* dx, int64_t ld_stream, void* dy, int64_t ld_block,
                                  float* dw_post, float* dgate, float* dtoken_gate, float* dw_pre,
                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- dense layers and layer norm ------------------------------------------------------------------
+ * What stands beside compressed layers in the networks they come from: layers that stay in 16 bits (also a
+ * layer's weights before it is pruned, or unpacked for fine-tuning), with what follows the product in its
+ * epilogue, and layer norm; forward, and the gradients of a training step.  Matrices, leading dimensions,
+ * alignment and what is read beyond a row are those of the part above: any leading dimension >= the row
+ * length, any alignment of an element.  Rows at multiples of 16 bytes (aligned base, leading dimension a
+ * multiple of 8) are the fast case.
+ *
+ * Z = W X + bias, Y = act(Z) + residual: W [M][K], X [K][N], Z, Y and residual [M][N], 16-bit; bias float32
+ * [M].  Products are summed in fp32 and everything up to Y is computed from these sums; Y and Z are each
+ * rounded once, to nearest-even, Y float32 with HINM_OUT_F32.  act by flags: none, HINM_EPI_RELU (which keeps
+ * NaN), _GELU, _GELU_TANH or _SILU.  bias, residual and Z may be NULL: none, none, not wanted.  Z and Y have
+ * leading dimension ldy.  residual may be Y with ldr = ldy (the sum in place) unless HINM_OUT_F32; apart from
+ * that outputs must not overlap inputs or each other.  Sums in a fixed order: the same call gives the same
+ * bits.  Sizes above 2^30 and products of more than some 2^22 workgroups (64 x 64 results each) return
+ * HINM_ERR_UNSUPPORTED.  workspace: hinm_linear_workspace bytes, 256-byte aligned; where that is 0 it may be NULL. */
+hinm_status hinm_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw, const void* X,
+                        int64_t ldx, const float* bias, const void* residual, int64_t ldr, void* Z, void* Y,
+                        int64_t ldy, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of hinm_linear from dY [M][N] (of Y; it is the residual's gradient as it stands):
+ *   dZ = dY act'(Z),   dX = W^T dZ,   dW = dZ X^T,   dbias = sum_n dZ.
+ * act by flags, Z as hinm_linear left it; without an activation Z is not read and dZ is dY.  relu' is 1 above
+ * zero and 0 elsewhere.  dZ is rounded to dtype ahead of the products, whose operands the matrix cores take in 16
+ * bits; dbias (float32 [M]) is summed from the values before that.  dX [K][N] has leading dimension ldx, as X;
+ * dW [M][K] ldw, as W, in dtype, float32 with HINM_OUT_F32; Z and dY have ldy.  dX, dW and dbias may be NULL
+ * where they are not wanted (one of them is): W is needed for dX, X for dW.  Outputs must not overlap inputs
+ * or each other.  Sums in a fixed order.  workspace: hinm_linear_grad_workspace bytes, 256-byte aligned; where
+ * that is 0 it may be NULL. */
+hinm_status hinm_linear_grad_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw, const void* X,
+                             int64_t ldx, const void* Z, const void* dY, int64_t ldy, void* dX, void* dW, float* dbias,
+                             uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Layer norm over the K channels of each of N tokens:
+ *   mean[n] = mean_k x[k][n],   rstd[n] = (mean_k (x[k][n] - mean[n])^2 + eps)^-1/2,
+ *   u[k][n] = w[k] rstd[n] (x[k][n] - mean[n]) + b[k].
+ * x, u 16-bit; w, b float32 [K], NULL = one and zero; mean, rstd float32 [N] outputs, NULL where not wanted.
+ * u may be x with ldu = ldx; apart from that outputs must not overlap inputs.  Sums in a fixed order, in binary64
+ * or of a column that one workgroup holds, whose deviations are squared in fp32: a token's deviations may be at most 10^17.
+ * A token that holds an infinity or a NaN has NaN results, the others theirs.  Sizes as for hinm_block_norm.  workspace:
+ * hinm_layer_norm_workspace bytes, 256-byte aligned; where few channels or tokens need 0, it may be NULL. */
+hinm_status hinm_layer_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_layer_norm(int32_t K, int32_t N, int32_t dtype, float eps, const void* x, int64_t ldx, const float* w,
+                            const float* b, void* u, int64_t ldu, float* mean, float* rstd, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Gradients of hinm_layer_norm from x, mean and rstd (as it took and left them) and du, the gradient of u; with
+ * xn = (x - mean) rstd and g = w du:
+ *   dx = dh + rstd (g - mean_k g - xn mean_k (g xn)),   dw = sum_n du xn,   db = sum_n du.
+ * dh [K][N], the gradient that reaches x beside the norm (a residual stream's), may be NULL: none.  dx, dw and db
+ * (float32 [K], overwritten) may be NULL where they are not wanted (one of them is).  dh and dx have leading
+ * dimension ldx, du ldu.  dx may be dh, or du with ldu = ldx; apart from that outputs must not overlap inputs.  Sums in
+ * fp32 in a fixed order.  workspace: hinm_layer_norm_grad_workspace bytes, 256-byte aligned; where few channels or
+ * tokens need 0, it may be NULL. */
+hinm_status hinm_layer_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
+hinm_status hinm_layer_norm_grad(int32_t K, int32_t N, int32_t dtype, const void* x, int64_t ldx, const float* w,
+                                 const float* mean, const float* rstd, const void* du, int64_t ldu, const void* dh,
+                                 void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes, void* stream);
 
 const char* hinm_status_str(hinm_status s);
 

@@ -9,6 +9,7 @@ from typing import Optional, Sequence, Tuple
 F16, BF16 = 0, 1
 MX4_ROWS, MX4_COLUMNS = 0, 1
 EPI_RELU, OUT_F32 = 1, 2
+EPI_GELU, EPI_GELU_TANH, EPI_SILU = 4, 8, 16
 KERNEL_REFERENCE, KERNEL_SMFMAC, KERNEL_GEMV = 0x100, 0x200, 0x400
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -45,14 +46,16 @@ def exported_symbols() -> Tuple[str, ...]:
             "hinm_spmm_prepared_workspace", "hinm_spmm_prepared", "hinm_spmm_prepared_plan", "hinm_chain_sizes",
             "hinm_chain", "hinm_mx4_sizes", "hinm_mx4_quantize", "hinm_mx4_unpack", "hinm_mx4_product",
             "hinm_mx4_linear_workspace", "hinm_mx4_linear", "hinm_block_norm_workspace", "hinm_block_norm",
-            "hinm_block_norm_grad_workspace", "hinm_block_norm_grad", "hinm_status_str", "hinm_version") + calib_symbols()
+            "hinm_block_norm_grad_workspace", "hinm_block_norm_grad", "hinm_linear_workspace", "hinm_linear",
+            "hinm_linear_grad_workspace", "hinm_linear_grad", "hinm_layer_norm_workspace", "hinm_layer_norm",
+            "hinm_layer_norm_grad_workspace", "hinm_layer_norm_grad", "hinm_status_str", "hinm_version") + calib_symbols()
 
 
 def calib_symbols() -> Tuple[str, ...]:
     """Entry points include/hinm_calib.h declares (measurement aids)."""
     return ("hinm_calib_copy", "hinm_calib_fill", "hinm_calib_read", "hinm_calib_scatter_rows", "hinm_calib_smfmac",
             "hinm_calib_empty", "hinm_calib_lds_stream", "hinm_calib_gather_stream", "hinm_calib_tile_part",
-            "hinm_calib_mid_plan", "hinm_calib_mx4_plan")
+            "hinm_calib_mid_plan", "hinm_calib_mx4_plan", "hinm_calib_linear_plan")
 
 
 def load_library():
@@ -126,9 +129,18 @@ def load_library():
     lib.hinm_block_norm_grad_workspace.argtypes = [i32, i32, szp]
     lib.hinm_block_norm_grad.argtypes = [i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
                                          vp, vp, sz, vp]
+    lib.hinm_linear_workspace.argtypes = [i32, i32, i32, szp]
+    lib.hinm_linear.argtypes = [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, C.c_uint32, vp, sz, vp]
+    lib.hinm_linear_grad_workspace.argtypes = [i32, i32, i32, szp]
+    lib.hinm_linear_grad.argtypes = [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, C.c_uint32, vp, sz, vp]
+    lib.hinm_layer_norm_workspace.argtypes = [i32, i32, szp]
+    lib.hinm_layer_norm.argtypes = [i32, i32, i32, f32, vp, i64, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.hinm_layer_norm_grad_workspace.argtypes = [i32, i32, szp]
+    lib.hinm_layer_norm_grad.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
     for name in ("hinm_mx4_sizes", "hinm_mx4_quantize", "hinm_mx4_unpack", "hinm_mx4_product", "hinm_mx4_linear_workspace",
                  "hinm_mx4_linear", "hinm_block_norm_workspace", "hinm_block_norm", "hinm_block_norm_grad_workspace",
-                 "hinm_block_norm_grad"):
+                 "hinm_block_norm_grad", "hinm_linear_workspace", "hinm_linear", "hinm_linear_grad_workspace", "hinm_linear_grad",
+                 "hinm_layer_norm_workspace", "hinm_layer_norm", "hinm_layer_norm_grad_workspace", "hinm_layer_norm_grad"):
         getattr(lib, name).restype = C.c_int
     lib.hinm_calib_copy.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p]
     lib.hinm_calib_fill.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.c_void_p]
@@ -142,6 +154,7 @@ def load_library():
                                              C.c_int32, C.c_void_p]
     lib.hinm_calib_tile_part.argtypes = [sp, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p]
     lib.hinm_calib_mx4_plan.argtypes = [i32, i32, i32, i32, C.c_uint32, i32, C.c_char_p, sz]
+    lib.hinm_calib_linear_plan.argtypes = [i32, i32, i32, i32, i32, i32, C.c_char_p, sz]
     lib.hinm_calib_mid_plan.argtypes = [sp, C.c_int32, C.c_int32, C.c_char_p, C.c_size_t]
     for name in calib_symbols():
         getattr(lib, name).restype = C.c_int
@@ -157,7 +170,7 @@ def load_library():
     _calls.bind(*[C.cast(getattr(lib, f), C.c_void_p).value for f in
                   ("hinm_pack", "hinm_prepare", "hinm_spmm", "hinm_spmm_vectors", "hinm_spmm_prepared", "hinm_chain",
                    "hinm_mx4_quantize", "hinm_mx4_unpack", "hinm_mx4_product", "hinm_mx4_linear", "hinm_block_norm",
-                   "hinm_block_norm_grad")],
+                   "hinm_block_norm_grad", "hinm_linear", "hinm_linear_grad", "hinm_layer_norm", "hinm_layer_norm_grad")],
                 _dtype_code, _stream)
     _native = _calls
     _lib = lib
@@ -485,6 +498,71 @@ def hinm_block_norm_grad(K, N, dtype, residual_scale, h, y, w_post, gate, token_
         raise HinmError(status, "hinm_block_norm_grad")
 
 
+# ---- dense layers and layer norm -------------------------------------------------------------------
+
+def hinm_linear_workspace(M, K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_linear_workspace(_size(M), _size(K), _size(N), C.byref(out)), "hinm_linear_workspace")
+    return int(out.value)
+
+
+def hinm_linear(M, K, N, dtype, W, ldw, X, ldx, bias, residual, ldr, Z, Y, ldy, flags=0, workspace=None, workspace_bytes=0,
+                stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.linear(M, K, N, dtype, W, ldw, X, ldx, bias, residual, ldr, Z, Y, ldy, flags, workspace, workspace_bytes,
+                            stream)
+    if status:
+        raise HinmError(status, "hinm_linear")
+
+
+def hinm_linear_grad_workspace(M, K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_linear_grad_workspace(_size(M), _size(K), _size(N), C.byref(out)), "hinm_linear_grad_workspace")
+    return int(out.value)
+
+
+def hinm_linear_grad(M, K, N, dtype, W, ldw, X, ldx, Z, dY, ldy, dX, dW, dbias=None, flags=0, workspace=None, workspace_bytes=0,
+                     stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.linear_grad(M, K, N, dtype, W, ldw, X, ldx, Z, dY, ldy, dX, dW, dbias, flags, workspace, workspace_bytes,
+                                 stream)
+    if status:
+        raise HinmError(status, "hinm_linear_grad")
+
+
+def hinm_layer_norm_workspace(K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_layer_norm_workspace(_size(K), _size(N), C.byref(out)), "hinm_layer_norm_workspace")
+    return int(out.value)
+
+
+def hinm_layer_norm(K, N, dtype, eps, x, ldx, w, b, u, ldu, mean=None, rstd=None, workspace=None, workspace_bytes=0,
+                    stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.layer_norm(K, N, dtype, eps, x, ldx, w, b, u, ldu, mean, rstd, workspace, workspace_bytes, stream)
+    if status:
+        raise HinmError(status, "hinm_layer_norm")
+
+
+def hinm_layer_norm_grad_workspace(K, N) -> int:
+    out = C.c_size_t(0)
+    _check(load_library().hinm_layer_norm_grad_workspace(_size(K), _size(N), C.byref(out)), "hinm_layer_norm_grad_workspace")
+    return int(out.value)
+
+
+def hinm_layer_norm_grad(K, N, dtype, x, ldx, w, mean, rstd, du, ldu, dh, dx, dw=None, db=None, workspace=None, workspace_bytes=0,
+                         stream=None) -> None:
+    if _lib is None:
+        load_library()
+    status = _native.layer_norm_grad(K, N, dtype, x, ldx, w, mean, rstd, du, ldu, dh, dx, dw, db, workspace, workspace_bytes,
+                                     stream)
+    if status:
+        raise HinmError(status, "hinm_layer_norm_grad")
+
+
 # ---- measurement aids (include/hinm_calib.h) -------------------------------------------------------
 
 def hinm_calib_copy(src, dst, nbytes, nontemporal=False, stream=None) -> None:
@@ -552,6 +630,14 @@ def hinm_calib_mx4_plan(M, N, K, dtype, flags=0, quantize=False) -> str:
     buf = C.create_string_buffer(512)
     _check(load_library().hinm_calib_mx4_plan(_size(M), _size(N), _size(K), _dtype_code(dtype), int(flags), int(bool(quantize)), buf,
                                               len(buf)), "hinm_calib_mx4_plan")
+    return buf.value.decode()
+
+
+def hinm_calib_linear_plan(M, K, N, dtype, which=0, aligned=True) -> str:
+    """The launches of a dense layer's product (which = 0), or of the products of its gradients: of the input (1), the weights (2)."""
+    buf = C.create_string_buffer(512)
+    _check(load_library().hinm_calib_linear_plan(_size(M), _size(K), _size(N), _dtype_code(dtype), int(which), int(bool(aligned)), buf,
+                                                 len(buf)), "hinm_calib_linear_plan")
     return buf.value.decode()
 
 

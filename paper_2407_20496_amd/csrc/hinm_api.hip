@@ -2,6 +2,7 @@
 // Every check here runs before anything is launched, so the error paths need no GPU.
 #include "hinm_internal.h"
 
+#include "linear_tile.h"
 #include "mx4_form.h"
 #include "prepared_layout.h"
 #include "hinm_calib.h"
@@ -111,6 +112,31 @@ hinm_status check_norm(int32_t K, int32_t N, int32_t dtype) {
   if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
   if (K <= 0 || N <= 0) return HINM_ERR_SHAPE;
   return N > kMostTokens || K > kMostSize ? HINM_ERR_UNSUPPORTED : HINM_OK;
+}
+
+// ---- dense layers --------------------------------------------------------------------------------------
+// M x N results of sums over K: what a launch has workgroups for, 64 x 64 results each at the least
+hinm_status check_dense(int32_t M, int32_t K, int32_t N) {
+  if (M <= 0 || K <= 0 || N <= 0) return HINM_ERR_SHAPE;
+  if (M > kMostSize || K > kMostSize || N > kMostSize) return HINM_ERR_UNSUPPORTED;
+  return (int64_t)((M + 63) / 64) * ((N + 63) / 64) >= kMostGroups ? HINM_ERR_UNSUPPORTED : HINM_OK;
+}
+// ... of a layer's three products
+hinm_status check_dense_grad(int32_t M, int32_t K, int32_t N) {
+  const hinm_status st = check_dense(K, M, N);
+  return st != HINM_OK ? st : check_dense(M, N, K);
+}
+struct LinearGradPlan {
+  int64_t ldz;
+  size_t dz, product;  // bytes of dZ, rounded to 256, and of the products' partial sums
+};
+LinearGradPlan linear_grad_plan(int32_t M, int32_t K, int32_t N) {
+  LinearGradPlan p;
+  p.ldz = ((int64_t)N + 7) / 8 * 8;
+  p.dz = ((size_t)M * p.ldz * 2 + 255) & ~size_t{255};
+  const size_t x = dense_product_workspace_bytes(K, N, M), w = dense_product_workspace_bytes(M, K, N);
+  p.product = x > w ? x : w;
+  return p;
 }
 
 // ---- hinm_pack_static: the score workspace of the pack kernels in a file-scope device array -------------
@@ -839,6 +865,146 @@ hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float resi
   const BlockNormGradArgs a{K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh, du, dx,
                             ld_stream, dy, ld_block, dw_post, dgate, dtoken_gate, dw_pre, static_cast<float*>(workspace)};
   return launched(launch_block_norm_grad(a, static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  const hinm_status st = check_dense(M, K, N);
+  if (st != HINM_OK) return st;
+  *workspace_bytes = dense_product_workspace_bytes(M, N, K);
+  return HINM_OK;
+}
+
+hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw, const void* X, int64_t ldx,
+                        const float* bias, const void* residual, int64_t ldr, void* Z, void* Y, int64_t ldy, uint32_t flags,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  const hinm_status st = check_dense(M, K, N);
+  if (st != HINM_OK) return st;
+  if (!W || !X || !Y) return HINM_ERR_NULL;
+  const bool out_f32 = (flags & HINM_OUT_F32) != 0;
+  if (ldw < K || ldx < N || ldy < N || (residual && ldr < N)) return HINM_ERR_SHAPE;
+  if (!aligned(W, 2) || !aligned(X, 2) || !aligned(residual, 2) || !aligned(Z, 2) || !aligned(Y, out_f32 ? 4 : 2) || !aligned(bias, 4))
+    return HINM_ERR_SHAPE;
+  const int act = activation_of(flags);
+  if (act < 0 || (flags & ~(kActFlags | HINM_OUT_F32))) return HINM_ERR_UNSUPPORTED;
+  const size_t need = dense_product_workspace_bytes(M, N, K);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
+  const LinearEpilogue to{M, N, bias, static_cast<const uint16_t*>(residual), ldr, pieces_of_rows(residual, ldr, N),
+                          static_cast<uint16_t*>(Z), Y, ldy, act, out_f32};
+  return launched(launch_dense_product({M, N, K, dtype, kAlong, kAcross, W, ldw, X, ldx, to, workspace}, static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_linear_grad_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  const hinm_status st = check_dense_grad(M, K, N);
+  if (st != HINM_OK) return st;
+  const LinearGradPlan p = linear_grad_plan(M, K, N);
+  *workspace_bytes = p.dz + p.product;
+  return HINM_OK;
+}
+
+hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw, const void* X, int64_t ldx,
+                             const void* Z, const void* dY, int64_t ldy, void* dX, void* dW, float* dbias, uint32_t flags,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  hinm_status st = check_dense_grad(M, K, N);
+  if (st != HINM_OK) return st;
+  const int act = activation_of(flags);
+  if (!dY || (!dX && !dW && !dbias) || (dX && !W) || (dW && !X) || (act > kActNone && !Z)) return HINM_ERR_NULL;
+  const bool out_f32 = (flags & HINM_OUT_F32) != 0;
+  if (ldy < N || (dX && (ldw < K || ldx < N)) || (dW && (ldw < K || ldx < N))) return HINM_ERR_SHAPE;
+  if (!aligned(W, 2) || !aligned(X, 2) || !aligned(Z, 2) || !aligned(dY, 2) || !aligned(dX, 2) || !aligned(dW, out_f32 ? 4 : 2) ||
+      !aligned(dbias, 4))
+    return HINM_ERR_SHAPE;
+  if (act < 0 || (flags & ~(kActFlags | HINM_OUT_F32))) return HINM_ERR_UNSUPPORTED;
+  const LinearGradPlan p = linear_grad_plan(M, K, N);
+  if (!workspace || workspace_bytes < p.dz + p.product || !aligned(workspace, 256)) return HINM_ERR_WORKSPACE;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  uint16_t* const dz = act == kActNone || (!dX && !dW) ? nullptr : static_cast<uint16_t*>(workspace);
+  void* const partials = static_cast<uint8_t*>(workspace) + p.dz;
+  hipError_t e = hipSuccess;
+  if (dz || dbias) {
+    const void* z = act == kActNone ? nullptr : Z;
+    e = launch_linear_slope({M, N, static_cast<const uint16_t*>(z), static_cast<const uint16_t*>(dY), ldy,
+                             lesser(pieces_of_rows(z, ldy, N), pieces_of_rows(dY, ldy, N)), act, dz, p.ldz, dbias}, dtype, s);
+  }
+  const void* const g = dz ? dz : dY;
+  const int64_t ldg = dz ? p.ldz : ldy;
+  if (e == hipSuccess && dX)
+    e = launch_dense_product({K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
+                              {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials}, s);
+  if (e == hipSuccess && dW)
+    e = launch_dense_product({M, K, N, dtype, kAlong, kAlong, g, ldg, X, ldx,
+                              {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials}, s);
+  return launched(e);
+}
+
+hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtype, int32_t which, int32_t is_aligned, char* text,
+                                   size_t text_bytes) {
+  if (!text || text_bytes == 0) return HINM_ERR_NULL;
+  text[0] = 0;
+  if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
+  const hinm_status st = which == 0 ? check_dense(M, K, N) : check_dense_grad(M, K, N);
+  if (st != HINM_OK) return st;
+  if (which < 0 || which > 2) return HINM_ERR_UNSUPPORTED;
+  LaunchPlan plan{text, text_bytes};
+  const void* const at = reinterpret_cast<void*>((uintptr_t{1} << 20) + (is_aligned ? 0 : 2));  // never dereferenced
+  auto pitch = [](int32_t n) { return ((int64_t)n + 7) / 8 * 8; };
+  auto launch = [&](int32_t m, int32_t n, int32_t k, OperandForm a, OperandForm b) {
+    const LinearEpilogue to{m, n, nullptr, nullptr, 0, kAligned, nullptr, nullptr, pitch(n), kActNone, false};
+    return launch_dense_product({m, n, k, dtype, a, b, at, pitch(a == kAlong ? k : m), at, pitch(b == kAlong ? k : n), to, nullptr, &plan}, nullptr);
+  };
+  if (which == 0) return launched(launch(M, N, K, kAlong, kAcross));
+  return launched(which == 1 ? launch(K, N, M, kAcross, kAcross) : launch(M, K, N, kAlong, kAlong));
+}
+
+hinm_status hinm_layer_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  const hinm_status st = check_norm(K, N, HINM_F16);
+  if (st != HINM_OK) return st;
+  *workspace_bytes = layer_norm_workspace_bytes(K, N);
+  return HINM_OK;
+}
+
+hinm_status hinm_layer_norm(int32_t K, int32_t N, int32_t dtype, float eps, const void* x, int64_t ldx, const float* w, const float* b,
+                            void* u, int64_t ldu, float* mean, float* rstd, void* workspace, size_t workspace_bytes, void* stream) {
+  const hinm_status st = check_norm(K, N, dtype);
+  if (st != HINM_OK) return st;
+  if (!x || !u) return HINM_ERR_NULL;
+  if (ldx < N || ldu < N || !aligned(x, 2) || !aligned(u, 2)) return HINM_ERR_SHAPE;
+  if (!aligned(w, 4) || !aligned(b, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return HINM_ERR_SHAPE;
+  const size_t need = layer_norm_workspace_bytes(K, N);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
+  return launched(launch_layer_norm({K, N, dtype, eps, x, ldx, w, b, u, ldu, mean, rstd, static_cast<float*>(workspace)},
+                                    static_cast<hipStream_t>(stream)));
+}
+
+hinm_status hinm_layer_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {
+  if (!workspace_bytes) return HINM_ERR_NULL;
+  const hinm_status st = check_norm(K, N, HINM_F16);
+  if (st != HINM_OK) return st;
+  *workspace_bytes = layer_norm_grad_workspace_bytes(K, N);
+  return HINM_OK;
+}
+
+hinm_status hinm_layer_norm_grad(int32_t K, int32_t N, int32_t dtype, const void* x, int64_t ldx, const float* w, const float* mean,
+                                 const float* rstd, const void* du, int64_t ldu, const void* dh, void* dx, float* dw, float* db,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  const hinm_status st = check_norm(K, N, dtype);
+  if (st != HINM_OK) return st;
+  if (!x || !mean || !rstd || !du || (!dx && !dw && !db)) return HINM_ERR_NULL;
+  if (ldx < N || ldu < N) return HINM_ERR_SHAPE;
+  for (const void* p : {x, du, dh, const_cast<const void*>(dx)})
+    if (!aligned(p, 2)) return HINM_ERR_SHAPE;
+  for (const float* p : {w, mean, rstd, const_cast<const float*>(dw), const_cast<const float*>(db)})
+    if (!aligned(p, 4)) return HINM_ERR_SHAPE;
+  // channels' gradients of several strips of tokens are added by workgroups of 1024 threads, 32 channels each
+  if (K >= 32 * kMostGroups && N > 64 && (dw || db)) return HINM_ERR_UNSUPPORTED;
+  const size_t need = layer_norm_grad_workspace_bytes(K, N);
+  if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
+  return launched(launch_layer_norm_grad({K, N, dtype, x, ldx, w, mean, rstd, du, ldu, dh, dx, dw, db, static_cast<float*>(workspace)},
+                                         static_cast<hipStream_t>(stream)));
 }
 
 const char* hinm_status_str(hinm_status s) {

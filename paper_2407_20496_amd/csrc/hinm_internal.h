@@ -341,4 +341,33 @@ struct BlockNormGradArgs {
 size_t block_norm_grad_workspace_bytes(int K, int N);
 hipError_t launch_block_norm_grad(const BlockNormGradArgs& a, hipStream_t stream);
 
+// ---- layer norm (layer_norm.hip) -------------------------------------------------------------------------------
+struct LayerNormArgs {
+  int K, N, dtype;
+  float eps;
+  const void* x;
+  int64_t ldx;
+  const float *w, *b;
+  void* u;
+  int64_t ldu;
+  float *mean, *rstd;
+  float* workspace;
+};
+size_t layer_norm_workspace_bytes(int K, int N);
+hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream);
+struct LayerNormGradArgs {
+  int K, N, dtype;
+  const void* x;
+  int64_t ldx;
+  const float *w, *mean, *rstd;
+  const void* du;
+  int64_t ldu;
+  const void* dh;
+  void* dx;
+  float *dw, *db;
+  float* workspace;
+};
+size_t layer_norm_grad_workspace_bytes(int K, int N);
+hipError_t launch_layer_norm_grad(const LayerNormGradArgs& a, hipStream_t stream);
+
 }  // namespace hinm

@@ -1,0 +1,41 @@
+// Dense products of two 16-bit matrices: what the launchers of a layer's product and of its gradients share.
+#pragma once
+
+#include "hinm_internal.h"
+#include "linear_epilogue.h"
+
+namespace hinm {
+
+// How an operand lies: the values that are summed over follow one another, or the ones that become rows or columns of the result.
+enum OperandForm { kAlong, kAcross };
+
+// result [M][N] = sum over K of a(m, k) b(k, n).  Operands along: a at A[m][k], b at B[n][k]; across: a at A[k][m], b at B[k][n].
+struct DenseProduct {
+  int M, N, K, dtype;
+  OperandForm form_a, form_b;
+  const void* A;
+  int64_t lda;
+  const void* B;
+  int64_t ldb;
+  LinearEpilogue to;
+  void* workspace;
+  LaunchPlan* plan = nullptr;  // set: record what would be launched instead
+};
+size_t dense_product_workspace_bytes(int M, int N, int K);
+hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream);
+
+// dZ [M][ldz] = dY act'(Z), zero in columns from N on to the next multiple of 8 (ldz is one), and dbias [M] = its sums over N
+// columns; either may be NULL.  Z NULL: no activation.
+struct SlopeArgs {
+  int M, N;
+  const uint16_t *Z, *dY;
+  int64_t ldy;  // of both
+  Pieces rows;  // of both
+  int act;
+  uint16_t* dZ;
+  int64_t ldz;
+  float* dbias;
+};
+hipError_t launch_linear_slope(const SlopeArgs& a, int dtype, hipStream_t stream);
+
+}  // namespace hinm

@@ -1,6 +1,7 @@
 // Products of two matrices in microscaled 4-bit form, Y = A B^T, on the scaled matrix instructions (include/hinm.h).
 #include "direct_lds.h"
 #include "mx4_form.h"
+#include "workgroup_items.h"
 
 #include <type_traits>
 
@@ -55,15 +56,6 @@ __device__ __forceinline__ void store_four(void* Y, int64_t row_at, int n, f32x4
       if (n + e < p.N) to[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
   }
 }
-
-// Workgroups go to the eight XCDs in turn: each XCD takes a contiguous run of a list of `items`, so that neighbours in the
-// list share operands in its L2.  -1: nothing left for this workgroup.
-__device__ __forceinline__ int item_of_workgroup(int items) {
-  const int per = gridDim.x >> 3;
-  const int item = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  return item < items ? item : -1;
-}
-uint32_t grid_of_items(int64_t items) { return (uint32_t)((items + 7) / 8 * 8); }
 
 // ---- operands straight into registers, the summed axis split over the waves ------------------------------
 // A workgroup owns 32 WM rows of A times 32 WN rows of B; its waves take lines of 256 values in turn, each for the whole tile,

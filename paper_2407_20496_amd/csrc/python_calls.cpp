@@ -26,6 +26,10 @@ decltype(&hinm_mx4_product) f_mx4_product;
 decltype(&hinm_mx4_linear) f_mx4_linear;
 decltype(&hinm_block_norm) f_block_norm;
 decltype(&hinm_block_norm_grad) f_block_norm_grad;
+decltype(&hinm_linear) f_linear;
+decltype(&hinm_linear_grad) f_linear_grad;
+decltype(&hinm_layer_norm) f_layer_norm;
+decltype(&hinm_layer_norm_grad) f_layer_norm_grad;
 
 PyObject* g_dtype_code;      // any accepted dtype -> HINM_F16 / HINM_BF16
 PyObject* g_current_stream;  // () -> raw pointer of the current stream or None; used until a source is set
@@ -405,9 +409,72 @@ PyObject* block_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (M, K, N, dtype, W, ldw, X, ldx, bias, residual, ldr, Z, Y, ldy, flags, workspace, workspace_bytes, stream)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[3], dtype;
+  void *w, *x, *in[2], *out[2], *ws, *stream;
+  int64_t ldw, ldx, ldr, ldy, bytes;
+  uint32_t flags;
+  if (!takes(n, 18) || !to_sizes(a, 3, d) || !to_dtype(a[3], &dtype) || !to_ptr(a[4], &w) || !to_i64(a[5], &ldw) || !to_ptr(a[6], &x) ||
+      !to_i64(a[7], &ldx) || !to_ptrs(a + 8, 2, in) || !to_i64(a[10], &ldr) || !to_ptrs(a + 11, 2, out) || !to_i64(a[13], &ldy) ||
+      !to_flags(a[14], &flags) || !to_ptr(a[15], &ws) || !to_i64(a[16], &bytes) || !to_stream(a[17], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_linear(d[0], d[1], d[2], dtype, w, ldw, x, ldx, static_cast<float*>(in[0]), in[1], ldr, out[0], out[1], ldy, flags, ws,
+                    (size_t)bytes, stream);
+  });
+}
+
+// (M, K, N, dtype, W, ldw, X, ldx, Z, dY, ldy, dX, dW, dbias, flags, workspace, workspace_bytes, stream)
+PyObject* linear_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[3], dtype;
+  void *w, *x, *in[2], *out[3], *ws, *stream;
+  int64_t ldw, ldx, ldy, bytes;
+  uint32_t flags;
+  if (!takes(n, 18) || !to_sizes(a, 3, d) || !to_dtype(a[3], &dtype) || !to_ptr(a[4], &w) || !to_i64(a[5], &ldw) || !to_ptr(a[6], &x) ||
+      !to_i64(a[7], &ldx) || !to_ptrs(a + 8, 2, in) || !to_i64(a[10], &ldy) || !to_ptrs(a + 11, 3, out) || !to_flags(a[14], &flags) ||
+      !to_ptr(a[15], &ws) || !to_i64(a[16], &bytes) || !to_stream(a[17], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_linear_grad(d[0], d[1], d[2], dtype, w, ldw, x, ldx, in[0], in[1], ldy, out[0], out[1], static_cast<float*>(out[2]), flags, ws,
+                         (size_t)bytes, stream);
+  });
+}
+
+// (K, N, dtype, eps, x, ldx, w, b, u, ldu, mean, rstd, workspace, workspace_bytes, stream)
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[2], dtype;
+  float eps;
+  void *x, *in[2], *u, *out[2], *ws, *stream;
+  int64_t ldx, ldu, bytes;
+  if (!takes(n, 15) || !to_sizes(a, 2, d) || !to_dtype(a[2], &dtype) || !to_float(a[3], &eps) || !to_ptr(a[4], &x) || !to_i64(a[5], &ldx) ||
+      !to_ptrs(a + 6, 2, in) || !to_ptr(a[8], &u) || !to_i64(a[9], &ldu) || !to_ptrs(a + 10, 2, out) || !to_ptr(a[12], &ws) ||
+      !to_i64(a[13], &bytes) || !to_stream(a[14], &stream))
+    return nullptr;
+  return status_of([&] {
+    return f_layer_norm(d[0], d[1], dtype, eps, x, ldx, static_cast<float*>(in[0]), static_cast<float*>(in[1]), u, ldu,
+                        static_cast<float*>(out[0]), static_cast<float*>(out[1]), ws, (size_t)bytes, stream);
+  });
+}
+
+// (K, N, dtype, x, ldx, w, mean, rstd, du, ldu, dh, dx, dw, db, workspace, workspace_bytes, stream)
+PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  int32_t d[2], dtype;
+  void *x, *in[4], *out[4], *ws, *stream;
+  int64_t ldx, ldu, bytes;
+  if (!takes(n, 17) || !to_sizes(a, 2, d) || !to_dtype(a[2], &dtype) || !to_ptr(a[3], &x) || !to_i64(a[4], &ldx) || !to_ptrs(a + 5, 4, in) ||
+      !to_i64(a[9], &ldu) || !to_ptrs(a + 10, 4, out) || !to_ptr(a[14], &ws) || !to_i64(a[15], &bytes) || !to_stream(a[16], &stream))
+    return nullptr;
+  return status_of([&] {
+    auto f = [](void* p) { return static_cast<float*>(p); };
+    return f_layer_norm_grad(d[0], d[1], dtype, x, ldx, f(in[0]), f(in[1]), f(in[2]), in[3], ldu, out[0], out[1], f(out[2]), f(out[3]), ws,
+                             (size_t)bytes, stream);
+  });
+}
+
 // (addresses in the order below, dtype_code, current_stream)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  constexpr int kEntries = 12;
+  constexpr int kEntries = 16;
   void* f[kEntries];
   if (!takes(n, kEntries + 2) || !to_ptrs(a, kEntries, f)) return nullptr;
   f_pack = reinterpret_cast<decltype(f_pack)>(f[0]);
@@ -422,6 +489,10 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   f_mx4_linear = reinterpret_cast<decltype(f_mx4_linear)>(f[9]);
   f_block_norm = reinterpret_cast<decltype(f_block_norm)>(f[10]);
   f_block_norm_grad = reinterpret_cast<decltype(f_block_norm_grad)>(f[11]);
+  f_linear = reinterpret_cast<decltype(f_linear)>(f[12]);
+  f_linear_grad = reinterpret_cast<decltype(f_linear_grad)>(f[13]);
+  f_layer_norm = reinterpret_cast<decltype(f_layer_norm)>(f[14]);
+  f_layer_norm_grad = reinterpret_cast<decltype(f_layer_norm_grad)>(f[15]);
   Py_INCREF(a[kEntries]);
   Py_XSETREF(g_dtype_code, a[kEntries]);
   Py_INCREF(a[kEntries + 1]);
@@ -443,7 +514,8 @@ PyObject* set_stream_source(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {HINM_METHOD(pack),    HINM_METHOD(prepare), HINM_METHOD(spmm), HINM_METHOD(spmm_vectors),
                          HINM_METHOD(spmm_prepared), HINM_METHOD(chain), HINM_METHOD(mx4_quantize),
                          HINM_METHOD(mx4_unpack), HINM_METHOD(mx4_product), HINM_METHOD(mx4_linear), HINM_METHOD(block_norm),
-                         HINM_METHOD(block_norm_grad), HINM_METHOD(bind), HINM_METHOD(set_stream_source),
+                         HINM_METHOD(block_norm_grad), HINM_METHOD(linear), HINM_METHOD(linear_grad), HINM_METHOD(layer_norm),
+                         HINM_METHOD(layer_norm_grad), HINM_METHOD(bind), HINM_METHOD(set_stream_source),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -19,6 +19,7 @@
 #include "mfma_types.h"
 #include "prepared_layout.h"
 #include "direct_lds.h"
+#include "lds_in_flight.h"
 #include "tile_epilogue.h"
 
 #include <type_traits>
@@ -102,17 +103,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_buffer(const void* p, uin
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000);
 }
 
-// LDS reads as raw instructions, not waited for here: the compiler would hold every one until all copies in flight had
-// landed.  To it an output is written at once, so it has to stay in its register until `tie`: lds_reads.py looks at the built
-// code and the build fails where anything touches such a register before the wait.
-template <int OFFSET>
-__device__ __forceinline__ void lds_read_b128(uint32_t addr, u32x4& r) {
-  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=&v"(r) : "v"(addr), "n"(OFFSET));
-}
-template <int OFFSET>
-__device__ __forceinline__ void lds_read_tr16(uint32_t addr, uint64_t& r) {
-  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=&v"(r) : "v"(addr), "n"(OFFSET));
-}
 template <int OFFSET>
 __device__ __forceinline__ void lds_read_b32(uint32_t addr, int& r) {
   asm volatile("ds_read_b32 %0, %1 offset:%2" : "=&v"(r) : "v"(addr), "n"(OFFSET));
@@ -120,12 +110,6 @@ __device__ __forceinline__ void lds_read_b32(uint32_t addr, int& r) {
 
 __device__ __forceinline__ void lds_write_b32(uint32_t addr, int v) {
   asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v));
-}
-
-// No use of the register is moved before this point.
-template <class T>
-__device__ __forceinline__ void pin(T& r) {
-  asm volatile("" : "+v"(r));
 }
 
 typedef uint64_t u64x4 __attribute__((ext_vector_type(4)));
@@ -137,14 +121,6 @@ struct Fragments {
   u32x4 a[SPARSE ? RB : 2 * RB];  // before 2:4: both halves of 16 kept columns
   int idx[RB];
 };
-
-template <int I, int N, class F>
-__device__ __forceinline__ void unroll(F&& f) {
-  if constexpr (I < N) {
-    f(std::integral_constant<int, I>{});
-    unroll<I + 1, N>(f);
-  }
-}
 
 struct RingParams {
   const uint8_t* values;    // prepared blocks, or the stored values before 2:4
