@@ -48,29 +48,30 @@ __device__ __forceinline__ float sigmoid(float q) {
 constexpr float kTanhScale = 1.5957691216057308f;  // 2 sqrt(2 / pi): (1 + tanh q) / 2 = sigmoid(2 q)
 constexpr float kTanhCube = 0.044715f;
 
-// z sigmoid(scale z + cube z^3) serves two of them.
-__device__ __forceinline__ float sigmoid_scale(int act) { return act == kActSilu ? 1.0f : kTanhScale; }
-__device__ __forceinline__ float sigmoid_cube(int act) { return act == kActSilu ? 0.0f : kTanhScale * kTanhCube; }
+// What an epilogue's code holds of them, one of these: no function of the sum at all; nothing or relu; gelu; z sigmoid(scale z +
+// cube z^3), which serves two.
+enum Epilogue { kEpiBare, kEpiLinear, kEpiGelu, kEpiSigmoid };
+inline Epilogue epilogue_of(int act) { return act == kActGelu ? kEpiGelu : act >= kActGeluTanh ? kEpiSigmoid : kEpiLinear; }
 
-// Eight values at a time: the branch is the same for all lanes.
-__device__ __forceinline__ void activate(float (&v)[8], int act) {
-  if (act == kActNone) return;
-  if (act == kActRelu) {
+template <Epilogue E, int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act) {
+  if constexpr (E == kEpiLinear) {
+    if (act != kActRelu) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] < 0 ? 0.0f : v[j];  // keeps NaN
-  } else if (act == kActGelu) {
+    for (int j = 0; j < N; ++j) v[j] = v[j] < 0 ? 0.0f : v[j];  // keeps NaN
+  } else if constexpr (E == kEpiGelu) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < N; ++j) {
       float bell;
       v[j] *= normal_probability(v[j], bell);
     }
-  } else {
-    const float scale = sigmoid_scale(act), cube = sigmoid_cube(act);
+  } else if constexpr (E == kEpiSigmoid) {
+    const float scale = act == kActSilu ? 1.0f : kTanhScale, cube = act == kActSilu ? 0.0f : kTanhScale * kTanhCube;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float x = v[j];
-      // x^2 may leave float32 where x does not: beside a cube of zero it must not count
-      v[j] = x * sigmoid(x * (cube != 0 ? fmaf(cube, x * x, scale) : scale));
+    for (int j = 0; j < N; ++j) {
+      // where the square leaves float32, beside a cube of zero too, the sigmoid is at its end: a scale of its own for infinity
+      const float x = v[j], square = fminf(x * x, 3.0e38f);
+      v[j] = x * sigmoid(x * fmaf(cube, square, scale));
     }
   }
 }

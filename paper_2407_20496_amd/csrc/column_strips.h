@@ -2,6 +2,7 @@
 #pragma once
 
 #include "eight_values.h"
+#include "wave_reduce.h"
 
 namespace hinm {
 
@@ -94,15 +95,6 @@ __device__ __forceinline__ float add_lanes_by_8(float v) {
 // Eight values of every lane, added over the lanes with the same lane % 8 and left one to a lane: value j = lane / 8 with its
 // three bits turned round (lane / 32 the highest).  Each step adds what two halves of the lanes hold of half of the values:
 // swaps of register halves, no LDS.
-template <int LANES>  // 32: the upper lanes of a with the lower ones of b; 16: odd rows of 16 of a with even ones of b
-__device__ __forceinline__ void swap_lanes(uint32_t& a, uint32_t& b) {
-  typedef unsigned pair __attribute__((ext_vector_type(2)));
-  pair r;
-  if constexpr (LANES == 32) r = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(a, b, false, false));
-  else r = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(a, b, false, false));
-  a = r[0];
-  b = r[1];
-}
 template <int LANES>
 __device__ __forceinline__ float swapped_sum(float a, float b) {
   uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);

@@ -3,6 +3,7 @@
 
 #include "direct_lds.h"
 #include "lds_in_flight.h"
+#include "wave_reduce.h"
 #include "workgroup_items.h"
 
 namespace hinm {
@@ -14,7 +15,9 @@ struct TileArgs {
   int64_t lda;
   const uint16_t* B;
   int64_t ldb;
-  int K, splits, stages_of_split;
+  int K;
+  int whole_tiles;              // that one workgroup each has; the others are shared by `splits`, with so many stages each
+  int splits, stages_of_split;
   Pieces rows_a, rows_b;
   float* partials;  // of workgroups that share a tile
 };
@@ -86,11 +89,14 @@ struct OperandSource {
   __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t stage, int c, uint8_t* to) const {
     copy16_to_lds(stage, from[c], 0, to + 1024 * (first_copy + c));
   }
-  // ... of a stage that ends early: what lies beyond its end is beyond the buffer's, and zeros are written
-  __device__ __forceinline__ void copy_cut(__amdgpu_buffer_rsrc_t stage, int c, int lane, int left_k, uint8_t* to) const {
-    int row, value;
-    S::piece_of(first_copy + c, lane, row, value);
-    copy16_to_lds(stage, (F == kAlong ? value : row) < left_k ? from[c] : kNowhere, 0, to + 1024 * (first_copy + c));
+  // From here on a stage that ends early: what lies beyond its end is beyond the buffer's, and zeros are written.
+  __device__ __forceinline__ void cut(int lane, int left_k) {
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c) {
+      int row, value;
+      S::piece_of(first_copy + c, lane, row, value);
+      if ((F == kAlong ? value : row) >= left_k) from[c] = kNowhere;
+    }
   }
   // ... or through registers, where rows lie at any address: drawn, then trimmed
   __device__ __forceinline__ u32x4 draw(int stage, int c, int lane, int left_k, int tile0, int size, Pieces rows, int& valid) const {
@@ -106,6 +112,63 @@ struct OperandSource {
   }
 };
 
+// 32 rows of a wave's part of a tile to the result, from their registers.  acc[i]: columns 32 i .. of the wave; a lane holds row
+// lane % 32, columns 8 q + 4 (lane / 32) + 0 .. 3 in four registers of each q.  The halves of a wave exchange every second four: a
+// lower lane then holds columns 8 q .. 8 q + 7, its partner above those of q + 1, whole pieces of 16 bytes.  (By way of LDS, in
+// pieces of whole lines, a wave of four tiles each way took 29000 clocks for what takes some 6000 here.)
+// ACCUMULATION: the sums stand in accumulation registers, and leave them when their turn comes (the compiler would move all of
+// them at once, and spill).
+template <bool ACCUMULATION>
+__device__ __forceinline__ float taken(float sum) {
+  if constexpr (ACCUMULATION) {
+    float v;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(sum));
+    return v;
+  }
+  return sum;
+}
+template <int WN, bool ACCUMULATION>
+struct RowStore {
+  u32x4 residual[2 * WN];
+
+  // the residual's pieces, under way ahead of their sums
+  template <bool WHOLE>
+  __device__ __forceinline__ void draw(const LinearEpilogue& e, int m0, int n0) {
+    if (!e.residual) return;
+    const int lane = threadIdx.x & 63, m = m0 + (lane & 31);
+#pragma unroll
+    for (int t = 0; t < 2 * WN; ++t) {
+      const int n = n0 + 16 * t + 8 * (lane >> 5), left = e.N - n;
+      if (WHOLE) residual[t] = draw_residual(e, m, n, 8);
+      else residual[t] = m < e.M && left > 0 ? draw_residual(e, m, n, left) : u32x4{0, 0, 0, 0};
+    }
+  }
+  template <int DT, Epilogue E, bool WHOLE>
+  __device__ __forceinline__ void store(const f32x16 (&acc)[WN], float bias, int m0, int n0, const LinearEpilogue& e) {
+    const int lane = threadIdx.x & 63, m = m0 + (lane & 31);
+#pragma unroll
+    for (int t = 0; t < 2 * WN; ++t) {
+      float v[8];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t a = __builtin_bit_cast(uint32_t, taken<ACCUMULATION>(acc[t >> 1][8 * (t & 1) + c]) + bias);
+        uint32_t b = __builtin_bit_cast(uint32_t, taken<ACCUMULATION>(acc[t >> 1][8 * (t & 1) + 4 + c]) + bias);
+        swap_lanes<32>(a, b);
+        v[c] = __builtin_bit_cast(float, a);
+        v[4 + c] = __builtin_bit_cast(float, b);
+      }
+      const int n = n0 + 16 * t + 8 * (lane >> 5), left = e.N - n;
+      if (WHOLE || (m < e.M && left > 0)) finish_eight<DT, E, WHOLE>(e, m, n, left, residual[t], v);
+    }
+  }
+};
+// The bias of the row that a lane holds of 32.
+template <Epilogue E>
+__device__ __forceinline__ float bias_of_row(const LinearEpilogue& e, int m0) {
+  const int m = m0 + (threadIdx.x & 31);
+  return E != kEpiBare && e.bias && m < e.M ? e.bias[m] : 0.0f;
+}
+
 template <OperandForm FA, OperandForm FB, int WM, int WN, int GM, int GN, int BK, int RING>
 struct TileSizes {
   static constexpr int kWaves = GM * GN, kThreads = 64 * kWaves;
@@ -114,60 +177,10 @@ struct TileSizes {
   using StageB = OperandStage<TN, BK, FB>;
   static constexpr int kStageBytes = StageA::kBytes + StageB::kBytes;
   static constexpr int kCopiesA = StageA::kCopies / kWaves, kCopiesB = StageB::kCopies / kWaves, kCopies = kCopiesA + kCopiesB;
-  static constexpr int kSlabPitch = 32 * WN * 4 + 16, kSlabBytes = 32 * kSlabPitch;  // of a wave: 32 rows of sums
-  static constexpr int kLds = RING * kStageBytes > kWaves * kSlabBytes ? RING * kStageBytes : kWaves * kSlabBytes;
+  static constexpr int kLds = RING * kStageBytes;
   static_assert(StageA::kCopies % kWaves == 0 && StageB::kCopies % kWaves == 0, "whole copies for every wave");
-  static_assert(RING == 2 || RING == 4, "places by masks");
+  static_assert(RING >= 2 && (RING - 2) * kCopies + kCopies / 2 < 64 && kLds <= 160 * 1024, "copies in flight are counted; LDS of a unit");
 };
-
-// Rows 32 j .. of a wave's part of a tile: its sums to the wave's slab, and from there to the result in whole pieces.
-// acc[i]: columns 32 i .. of the wave; a lane holds row lane % 32, columns 8 (e / 4) + 4 (lane / 32) + e % 4.  Pieces are finished
-// two at a time, in a loop that stays one (a tile's code would outgrow the instruction cache), while the next two residuals
-// are on their way.
-template <int DT, int WN>
-__device__ __forceinline__ void store_rows(const f32x16 (&acc)[WN], uint8_t* slab, int m0, int n0, const LinearEpilogue& e) {
-  constexpr int kPitch = 32 * WN * 4 + 16, kPieces = 4 * WN, kRows = 64 / kPieces, kGroup = 2;
-  const int lane = threadIdx.x & 63, half = lane >> 5, r = lane & 31;
-  const int piece = lane % kPieces, n = n0 + 8 * piece, left = min(8, e.N - n);
-  const int most = left > 0 ? min(32, e.M - m0) : 0;  // rows of this lane's columns that exist
-  struct Group {
-    u32x4 residual[kGroup];
-    float bias[kGroup];
-  };
-  auto load = [&](int row0, Group& g) __attribute__((always_inline)) {
-#pragma unroll
-    for (int c = 0; c < kGroup; ++c) {
-      const int row = row0 + c * kRows;
-      g.residual[c] = row < most ? load_residual<DT>(e, m0 + row, n, left) : u32x4{0, 0, 0, 0};
-      g.bias[c] = row < most && e.bias ? e.bias[m0 + row] : 0.0f;
-    }
-  };
-  Group now;
-  load(lane / kPieces, now);
-#pragma unroll
-  for (int i = 0; i < WN; ++i)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<f32x4*>(slab + r * kPitch + (32 * i + 8 * q + 4 * half) * 4) =
-          f32x4{acc[i][4 * q], acc[i][4 * q + 1], acc[i][4 * q + 2], acc[i][4 * q + 3]};
-  asm volatile("" ::: "memory");  // LDS operations of a wave are done in order; the compiler is held to it
-#pragma unroll 1
-  for (int row0 = lane / kPieces; row0 < most; row0 += kGroup * kRows) {
-    Group next;
-    load(row0 + kGroup * kRows, next);
-#pragma unroll
-    for (int c = 0; c < kGroup; ++c) {
-      const int row = row0 + c * kRows;
-      if (row >= most) break;
-      const float* from = reinterpret_cast<const float*>(slab + row * kPitch + 32 * piece);
-      const f32x4 low = *reinterpret_cast<const f32x4*>(from), high = *reinterpret_cast<const f32x4*>(from + 4);
-      float v[8] = {low[0], low[1], low[2], low[3], high[0], high[1], high[2], high[3]};
-      finish_eight<DT>(e, m0 + row, n, left, now.bias[c], now.residual[c], v);
-    }
-    now = next;
-  }
-  asm volatile("" ::: "memory");
-}
 
 // Which tile an item of the list is: panels of eight tiles of rows times all columns, so that the tiles an XCD works on at a time
 // share operands.
@@ -190,19 +203,22 @@ struct TilePlace {
 // outstanding, all earlier ones are waited for, and so are the wave's LDS reads of stage p; past the barrier that holds for all
 // waves, so stage p + 1 is there and the place of stage p takes stage p + RING: half of its copies during the last step of p, the
 // others during the first of p + 1.
-template <int DT, OperandForm FA, OperandForm FB, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
+template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
 __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile_kernel(TileArgs a, LinearEpilogue e) {
   using T = TileSizes<FA, FB, WM, WN, GM, GN, BK, RING>;
   constexpr int kSteps = BK / 16;
   extern __shared__ __align__(1024) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tiles = ((e.M + T::TM - 1) / T::TM) * ((e.N + T::TN - 1) / T::TN);
-  const int item = item_of_workgroup(tiles * a.splits);
+  const int tiles = ((e.M + T::TM - 1) / T::TM) * ((e.N + T::TN - 1) / T::TN), shared = tiles - a.whole_tiles;
+  const int whole_groups = (a.whole_tiles + 7) & ~7;
+  const bool alone = (int)blockIdx.x < whole_groups;
+  const int item = alone ? item_of(blockIdx.x, whole_groups, a.whole_tiles)
+                         : item_of(blockIdx.x - whole_groups, gridDim.x - whole_groups, shared * a.splits);
   if (item < 0) return;
-  const int split = item / tiles, tile = item - split * tiles;
+  const int split = alone ? 0 : item / shared, tile = alone ? item : a.whole_tiles + item - split * shared;
   const TilePlace place(tile, T::TM, T::TN, e.M, e.N);
-  const int first = split * a.stages_of_split;
-  const int stages = min(a.stages_of_split, (a.K + BK - 1) / BK - first), k0 = first * BK;
+  const int all_stages = (a.K + BK - 1) / BK, first = split * a.stages_of_split;
+  const int stages = alone ? all_stages : min(a.stages_of_split, all_stages - first), k0 = first * BK;
   // stages that copies fill; the last one of all may be cut short
   const int whole = GUARDED ? 0 : min(stages, a.K / BK - first);
 
@@ -213,11 +229,16 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
   struct Buffers {
     __amdgpu_buffer_rsrc_t a, b;
   };
-  auto buffers_of = [&](int stage) __attribute__((always_inline)) { return Buffers{buffer_of(of_a.of_stage(stage), kWholeBuffer), buffer_of(of_b.of_stage(stage), kWholeBuffer)}; };
-  auto slot_of = [&](int stage) __attribute__((always_inline)) { return lds + (stage & (RING - 1)) * T::kStageBytes; };
-  auto copy_one = [&](const Buffers& from, int stage, int c) __attribute__((always_inline)) {
-    if (c < T::kCopiesA) of_a.copy(from.a, c, slot_of(stage));
-    else of_b.copy(from.b, c - T::kCopiesA, slot_of(stage) + T::StageA::kBytes);
+  auto buffers_of = [&](int stage) __attribute__((always_inline)) {
+    const uint32_t bytes = stage < stages ? kWholeBuffer : 0;  // a stage that does not exist: zeros, which nobody reads
+    return Buffers{buffer_of(of_a.of_stage(stage), bytes), buffer_of(of_b.of_stage(stage), bytes)};
+  };
+  // places of the ring, as bytes from its beginning
+  auto place_after = [](uint32_t place) { return place == (RING - 1) * T::kStageBytes ? 0u : place + T::kStageBytes; };
+  auto place_before = [](uint32_t place) { return place == 0 ? (RING - 1) * T::kStageBytes : place - T::kStageBytes; };
+  auto copy_one = [&](const Buffers& from, uint32_t place, int c) __attribute__((always_inline)) {
+    if (c < T::kCopiesA) of_a.copy(from.a, c, lds + place);
+    else of_b.copy(from.b, c - T::kCopiesA, lds + place + T::StageA::kBytes);
   };
   // stages through registers
   struct Held {
@@ -232,9 +253,9 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
                                : of_b.draw(stage, c - T::kCopiesA, lane, left_k, place.n0, e.N, a.rows_b, valid);
     }
   };
-  auto put_stage = [&](int stage, const Held& h) __attribute__((always_inline)) {
+  auto put_stage = [&](int stage, uint32_t place_of_it, const Held& h) __attribute__((always_inline)) {
     const int left_k = a.K - k0 - stage * BK;
-    uint8_t* const slot = slot_of(stage);
+    uint8_t* const slot = lds + place_of_it;
 #pragma unroll
     for (int c = 0; c < T::kCopies; ++c) {
       const bool is_a = c < T::kCopiesA;
@@ -253,28 +274,28 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
     }
   };
 
-  // the last stage where it is cut short: copied whole at a time, and cleared behind its end once it is there
+  // the last stage where it is cut short is cleared behind its end once it is there
   const int left_k = a.K - k0 - whole * BK;
-  auto copy_cut_stage = [&]() __attribute__((always_inline)) {
-    const Buffers from = buffers_of(whole);
-#pragma unroll
-    for (int c = 0; c < T::kCopies; ++c) {
-      if (c < T::kCopiesA) of_a.copy_cut(from.a, c, lane, left_k, slot_of(whole));
-      else of_b.copy_cut(from.b, c - T::kCopiesA, lane, left_k, slot_of(whole) + T::StageA::kBytes);
-    }
+  auto cut_offsets = [&]() __attribute__((always_inline)) {
+    of_a.cut(lane, left_k);
+    of_b.cut(lane, left_k);
   };
-  auto clear_cut_stage = [&]() __attribute__((always_inline)) {
-    if ((FA == kAcross && FB == kAcross) || !(left_k & 7)) return;
-    if constexpr (FA == kAlong) T::StageA::clear_behind(slot_of(whole), left_k, T::kThreads);
-    if constexpr (FB == kAlong) T::StageB::clear_behind(slot_of(whole) + T::StageA::kBytes, left_k, T::kThreads);
+  auto clear_cut_stage = [&](uint32_t at) __attribute__((always_inline)) {
+    if ((FA == kAcross && FB == kAcross) || whole == stages || !(left_k & 7)) return;
+    if constexpr (FA == kAlong) T::StageA::clear_behind(lds + at, left_k, T::kThreads);
+    if constexpr (FB == kAlong) T::StageB::clear_behind(lds + at + T::StageA::kBytes, left_k, T::kThreads);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
 
+  const int wave_m = (wave % GM) * 32 * WM, wave_n = (wave / GM) * 32 * WN;
+  float bias[WM];
+#pragma unroll
+  for (int j = 0; j < WM; ++j) bias[j] = bias_of_row<E>(e, place.m0 + wave_m + 32 * j);
+
   // LDS reads: by step along, by tile of 32 across
   const int half = lane >> 5, r = lane & 31, in16 = lane & 15;
-  const int wave_m = (wave % GM) * 32 * WM, wave_n = (wave / GM) * 32 * WN;
   const uint32_t lds_base = (uint32_t)(uintptr_t)(lds_void_t*)lds;
   constexpr int kAddressesA = FA == kAlong ? kSteps : WM, kAddressesB = FB == kAlong ? kSteps : WN;
   uint32_t at_a[kAddressesA], at_b[kAddressesB];
@@ -294,9 +315,8 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
     u32x4 a[WM], b[WN];
     uint64_t part_a[WM][2], part_b[WN][2];
   };
-  auto read_one = [&](auto step_tag, auto tile_tag, int stage, Operands& f) __attribute__((always_inline)) {
+  auto read_one = [&](auto step_tag, auto tile_tag, uint32_t slot, Operands& f) __attribute__((always_inline)) {
     constexpr int s = decltype(step_tag)::value, t = decltype(tile_tag)::value;
-    const uint32_t slot = (stage & (RING - 1)) * T::kStageBytes;
     if constexpr (t < WM) {
       if constexpr (FA == kAlong) {
         lds_read_b128<t * 32 * T::StageA::kRowBytes>(at_a[s] + slot, f.a[t]);
@@ -349,97 +369,78 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0;
 
-  // the first stages
+  // the first stages, of the last one half: the other half follows in the first step
   Held held;
-  const int ahead = min(RING, stages);
+  constexpr int kHalf = T::kCopies / 2;
   if constexpr (GUARDED) {
-    for (int q = 0; q < ahead; ++q) {
+    for (int q = 0; q < min(RING, stages); ++q) {
       draw_stage(q, held);
-      put_stage(q, held);
+      put_stage(q, q * T::kStageBytes, held);
     }
     if (RING < stages) draw_stage(RING, held);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   } else {
-    // beyond RING - 1 whole ones only half of the last: the other half follows in the first step
-    for (int q = 0; q < min(RING, whole); ++q) {
+#pragma unroll
+    for (int q = 0; q < RING; ++q) {
+      if (q == whole) cut_offsets();
       const Buffers from = buffers_of(q);
 #pragma unroll
-      for (int c = 0; c < T::kCopies; ++c)
-        if (q < RING - 1 || c < T::kCopies / 2 || whole < RING) copy_one(from, q, c);
+      for (int c = 0; c < (q < RING - 1 ? T::kCopies : kHalf); ++c) copy_one(from, q * T::kStageBytes, c);
     }
-    if (whole < ahead) copy_cut_stage();
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies + kHalf) : "memory");
   }
-  // stage 0 is waited for, and all of them where they are few
-  if (!GUARDED && whole >= RING) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies + T::kCopies / 2) : "memory");
-  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  if (!GUARDED && whole == 0) clear_cut_stage();
+  if (!GUARDED && whole == 0) clear_cut_stage(0);
 
   Operands sets[2];
   unroll<0, WM + WN>([&](auto t) { read_one(std::integral_constant<int, 0>{}, t, 0, sets[0]); });
 
-  // SECOND / FIRST: the second half of stage p + RING - 1 and the first of p + RING are copied; LAST: no stage follows
-  auto stage = [&](auto second_tag, auto first_tag, auto last_tag, int p) __attribute__((always_inline)) {
-    constexpr bool kSecond = decltype(second_tag)::value, kFirst = decltype(first_tag)::value, kLast = decltype(last_tag)::value;
+  uint32_t at = 0;  // the place of stage p, and of stage p + RING
+  for (int p = 0; p < stages; ++p) {
+    const uint32_t after = place_after(at), before = place_before(at);
     unroll<0, kSteps>([&](auto step_tag) __attribute__((always_inline)) {
       constexpr int s = decltype(step_tag)::value;
-      constexpr bool kEnds = s == kSteps - 1;
-      constexpr bool kCopying = (s == 0 && kSecond) || (kEnds && kFirst), kReading = !(kEnds && kLast);
-      constexpr int kTiles = WM * WN, kReads = WM + WN, kHalf = T::kCopies / 2, kOthers = T::kCopies - kHalf;
+      constexpr bool kEnds = s == kSteps - 1, kCopying = !GUARDED && (s == 0 || kEnds);
+      constexpr int kTiles = WM * WN, kReads = WM + WN, kCount = kEnds ? kHalf : T::kCopies - kHalf;
       Operands &now = sets[s & 1], &next = sets[(s + 1) & 1];
       wait_operands(now);
-      if constexpr (kEnds && !kLast) {
-        if constexpr (kSecond) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      if constexpr (kEnds) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(GUARDED ? 0 : (RING - 2) * T::kCopies) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if constexpr (GUARDED) {
-          if (p + RING < stages) put_stage(p + RING, held);
+          if (p + RING < stages) put_stage(p + RING, at, held);
           if (p + RING + 1 < stages) draw_stage(p + RING + 1, held);
-        } else if constexpr (!kFirst) {
-          if (whole < stages) {
-            if (p + RING == whole) copy_cut_stage();
-            if (!kSecond && p + 1 == whole) clear_cut_stage();
-          }
+        } else {
+          if (p + RING == whole) cut_offsets();
+          if (p + 1 == whole) clear_cut_stage(after);
         }
       }
-      const int copied = kEnds ? p + RING : p + RING - 1;
-      const Buffers from = buffers_of(kCopying ? copied : 0);
+      const Buffers from = buffers_of(kEnds ? p + RING : p + RING - 1);
       unroll<0, kTiles>([&](auto t_tag) __attribute__((always_inline)) {
         constexpr int t = decltype(t_tag)::value, i = t / WM, j = t % WM;
         acc[i][j] = mfma_32x32x16<DT>(now.b[i], now.a[j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kReading) {
-          constexpr int b = t * kReads * 2 / kTiles, to = (t + 1) * kReads * 2 / kTiles;
-          unroll<(b < kReads ? b : kReads), (to < kReads ? to : kReads)>([&](auto u) __attribute__((always_inline)) {
-            read_one(std::integral_constant<int, (s + 1) % kSteps>{}, u, kEnds ? p + 1 : p, next);
-          });
-        }
+        constexpr int b = t * kReads * 2 / kTiles, to = (t + 1) * kReads * 2 / kTiles;
+        unroll<(b < kReads ? b : kReads), (to < kReads ? to : kReads)>([&](auto u) __attribute__((always_inline)) {
+          read_one(std::integral_constant<int, (s + 1) % kSteps>{}, u, kEnds ? after : at, next);
+        });
         if constexpr (kCopying) {
-          constexpr int kCount = kEnds ? kHalf : kOthers;
 #pragma unroll
-          for (int c = t * kCount / kTiles; c < (t + 1) * kCount / kTiles; ++c) copy_one(from, copied, (kEnds ? 0 : kHalf) + c);
+          for (int c = t * kCount / kTiles; c < (t + 1) * kCount / kTiles; ++c) copy_one(from, kEnds ? at : before, (kEnds ? 0 : kHalf) + c);
         }
         __builtin_amdgcn_sched_barrier(0);
       });
     });
-  };
-  constexpr std::true_type yes{};
-  constexpr std::false_type no{};
-  int p = 0;
-  if constexpr (!GUARDED) {
-    for (; p + RING < whole; ++p) stage(yes, yes, no, p);
-    if (p + RING == whole && p + 1 < stages) stage(yes, no, no, p++);
+    at = after;
   }
-  for (; p + 1 < stages; ++p) stage(no, no, no, p);
-  stage(no, no, yes, p);
-  // every wave has read its operands: the ring becomes the waves' slabs
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
+  // what was read of the stage beyond the last one is not used, but has to be there before its registers are
+  wait_operands(sets[0]);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // copies of stages that do not exist: they write to this workgroup's LDS
 
-  if (a.splits > 1) {
-    float* const to = a.partials + ((int64_t)split * tiles + tile) * (T::TM * T::TN) + wave * (WM * WN * 1024) + 4 * lane;
+  if (!alone) {
+    float* const to = a.partials + (int64_t)item * (T::TM * T::TN) + wave * (WM * WN * 1024) + 4 * lane;
 #pragma unroll
     for (int j = 0; j < WM; ++j)
 #pragma unroll
@@ -450,37 +451,48 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
               f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     return;
   }
-  uint8_t* const slab = lds + wave * T::kSlabBytes;
-  unroll<0, WM>([&](auto j_tag) __attribute__((always_inline)) {
-    constexpr int j = decltype(j_tag)::value;
-    f32x16 rows[WN];
+  // the sums are read by instructions that the compiler does not look into: it sees no need to wait for the last products
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  auto store = [&](auto whole_tag) __attribute__((always_inline)) {
+    constexpr bool kWhole = decltype(whole_tag)::value;
+    RowStore<WN, (WM * WN > 8)> to[2];
+    if constexpr (E != kEpiBare) to[0].template draw<kWhole>(e, place.m0 + wave_m, place.n0 + wave_n);
+    unroll<0, WM>([&](auto j_tag) __attribute__((always_inline)) {
+      constexpr int j = decltype(j_tag)::value;
+      if constexpr (E != kEpiBare && j + 1 < WM) to[(j + 1) & 1].template draw<kWhole>(e, place.m0 + wave_m + 32 * (j + 1), place.n0 + wave_n);
+      f32x16 rows[WN];
 #pragma unroll
-    for (int i = 0; i < WN; ++i) rows[i] = acc[i][j];
-    store_rows<DT, WN>(rows, slab, place.m0 + wave_m + 32 * j, place.n0 + wave_n, e);
-  });
+      for (int i = 0; i < WN; ++i) rows[i] = acc[i][j];
+      to[j & 1].template store<DT, E, kWhole>(rows, bias[j], place.m0 + wave_m + 32 * j, place.n0 + wave_n, e);
+    });
+  };
+  if (!e.out_f32 && place.m0 + T::TM <= e.M && place.n0 + T::TN <= e.N) store(std::true_type{});
+  else store(std::false_type{});
 }
 
 // Tiles that several workgroups have summed parts of: the parts added in order, 32 rows of every wave a workgroup.
-template <int DT, int WM, int WN, int GM, int GN>
-__global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* partials, int splits, LinearEpilogue e) {
-  constexpr int TM = 32 * WM * GM, TN = 32 * WN * GN, kSlabBytes = 32 * (32 * WN * 4 + 16);
-  __shared__ __align__(16) uint8_t slabs[GM * GN * kSlabBytes];
+template <int DT, Epilogue E, int WM, int WN, int GM, int GN>
+__global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* partials, int whole_tiles, int splits, LinearEpilogue e) {
+  constexpr int TM = 32 * WM * GM, TN = 32 * WN * GN;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tiles = ((e.M + TM - 1) / TM) * ((e.N + TN - 1) / TN);
-  const int item = item_of_workgroup(tiles * WM);
+  const int shared = ((e.M + TM - 1) / TM) * ((e.N + TN - 1) / TN) - whole_tiles;
+  const int item = item_of_workgroup(shared * WM);
   if (item < 0) return;
   const int tile = item / WM, j = item - tile * WM;
-  const TilePlace place(tile, TM, TN, e.M, e.N);
+  const TilePlace place(whole_tiles + tile, TM, TN, e.M, e.N);
   const int m0 = place.m0 + (wave % GM) * 32 * WM + 32 * j, n0 = place.n0 + (wave / GM) * 32 * WN;
   if (m0 >= e.M || n0 >= e.N) return;
   const float* from = partials + (int64_t)tile * (TM * TN) + wave * (WM * WN * 1024) + j * (WN * 1024) + 4 * lane;
+  RowStore<WN, false> to;
+  if constexpr (E != kEpiBare) to.template draw<false>(e, m0, n0);
+  const float bias = bias_of_row<E>(e, m0);
   f32x16 acc[WN];
 #pragma unroll
   for (int i = 0; i < WN; ++i)
 #pragma unroll
     for (int q = 0; q < 16; ++q) acc[i][q] = 0;
 #pragma unroll 4
-  for (int s = 0; s < splits; ++s, from += (int64_t)tiles * (TM * TN)) {
+  for (int s = 0; s < splits; ++s, from += (int64_t)shared * (TM * TN)) {
 #pragma unroll
     for (int i = 0; i < WN; ++i)
 #pragma unroll
@@ -490,82 +502,79 @@ __global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* 
         for (int c = 0; c < 4; ++c) acc[i][4 * q + c] += v[c];
       }
   }
-  store_rows<DT, WN>(acc, slabs + wave * kSlabBytes, m0, n0, e);
+  to.template store<DT, E, false>(acc, bias, m0, n0, e);
 }
 
 // Which form serves a shape.
 struct TileForm {
   int rows, cols;
 };
-constexpr int kFormGuarded = 0, kFormSmall = 1, kFormLarge = 2;
-constexpr TileForm kTileForms[] = {{128, 128}, {128, 128}, {256, 256}};
+enum { kFormGuarded, kFormLarge, kFormWide, kFormMiddle, kFormSmall };
+constexpr TileForm kTileForms[] = {{128, 128}, {256, 256}, {256, 128}, {128, 128}, {64, 64}};
 constexpr int kStage = 64;  // summed values, of every form
 
 int64_t tiles_of(int form, int M, int N) {
   return (int64_t)((M + kTileForms[form].rows - 1) / kTileForms[form].rows) * ((N + kTileForms[form].cols - 1) / kTileForms[form].cols);
 }
 struct TilePlan {
-  int form, splits, stages_of_split;
+  int form, whole_tiles, splits, stages_of_split;
 };
 TilePlan plan_of(int M, int N, int K, bool guarded) {
-  TilePlan p{guarded ? kFormGuarded : kFormSmall, 1, 0};
   const int stages = (K + kStage - 1) / kStage;
+  TilePlan p{guarded ? kFormGuarded : kFormMiddle, 0, 1, stages};
   if (!guarded && tiles_of(kFormLarge, M, N) >= 224) p.form = kFormLarge;
-  const int64_t tiles = tiles_of(p.form, M, N);
-  if (p.form != kFormLarge && tiles < 256 && stages > 4) {
-    const int most = (int)(512 / tiles), least = stages / 4;
-    p.splits = most < least ? most : least;
-    if (p.splits < 1) p.splits = 1;
-  }
-  p.stages_of_split = (stages + p.splits - 1) / p.splits;
-  p.splits = (stages + p.stages_of_split - 1) / p.stages_of_split;
+  p.whole_tiles = (int)tiles_of(p.form, M, N);
   return p;
 }
 size_t partial_bytes(const TilePlan& p, int M, int N) {
-  return p.splits < 2 ? 0 : (size_t)p.splits * tiles_of(p.form, M, N) * kTileForms[p.form].rows * kTileForms[p.form].cols * sizeof(float);
+  return (size_t)p.splits * (tiles_of(p.form, M, N) - p.whole_tiles) * kTileForms[p.form].rows * kTileForms[p.form].cols * sizeof(float);
 }
 
-template <int DT, OperandForm FA, OperandForm FB, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
+template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
 hipError_t launch_tiles(const DenseProduct& d, const TileArgs& a, int64_t tiles, hipStream_t stream) {
   using T = TileSizes<FA, FB, WM, WN, GM, GN, BK, RING>;
-  const dim3 grid(grid_of_items(tiles * a.splits));
+  const int shared = (int)(tiles - a.whole_tiles);
+  const dim3 grid(grid_of_items(a.whole_tiles) + grid_of_items((int64_t)shared * a.splits)), join(grid_of_items((int64_t)shared * WM));
   if (d.plan) {
-    plan_record(d.plan, "linear_tile_kernel<DT=%d,FA=%d,FB=%d,WM=%d,WN=%d,GM=%d,GN=%d,BK=%d,RING=%d,GUARDED=%d> grid=%u block=%d lds=%d splits=%d", DT,
-                (int)FA, (int)FB, WM, WN, GM, GN, BK, RING, (int)GUARDED, grid.x, T::kThreads, T::kLds, a.splits);
-  } else {
-    const hipError_t e = raise_lds_limit<linear_tile_kernel<DT, FA, FB, WM, WN, GM, GN, BK, RING, GUARDED>>(T::kLds);
-    if (e != hipSuccess) return e;
-    linear_tile_kernel<DT, FA, FB, WM, WN, GM, GN, BK, RING, GUARDED><<<grid, T::kThreads, T::kLds, stream>>>(a, d.to);
+    plan_record(d.plan, "linear_tile_kernel<DT=%d,FA=%d,FB=%d,E=%d,WM=%d,WN=%d,GM=%d,GN=%d,BK=%d,RING=%d,GUARDED=%d> grid=%u block=%d lds=%d whole=%d splits=%d",
+                DT, (int)FA, (int)FB, (int)E, WM, WN, GM, GN, BK, RING, (int)GUARDED, grid.x, T::kThreads, T::kLds, a.whole_tiles, a.splits);
+    if (shared) plan_record(d.plan, "linear_join_kernel<DT=%d,E=%d,WM=%d,WN=%d,GM=%d,GN=%d> grid=%u block=%d", DT, (int)E, WM, WN, GM, GN, join.x, T::kThreads);
+    return hipSuccess;
   }
-  if (a.splits > 1) {
-    if constexpr (WN <= 2) {
-      const dim3 join(grid_of_items(tiles * WM));
-      if (d.plan) plan_record(d.plan, "linear_join_kernel<DT=%d,WM=%d,WN=%d,GM=%d,GN=%d> grid=%u block=%d", DT, WM, WN, GM, GN, join.x, T::kThreads);
-      else linear_join_kernel<DT, WM, WN, GM, GN><<<join, T::kThreads, 0, stream>>>(a.partials, a.splits, d.to);
-    }
-  }
-  return d.plan ? hipSuccess : hipGetLastError();
+  const hipError_t e = raise_lds_limit<linear_tile_kernel<DT, FA, FB, E, WM, WN, GM, GN, BK, RING, GUARDED>>(T::kLds);
+  if (e != hipSuccess) return e;
+  linear_tile_kernel<DT, FA, FB, E, WM, WN, GM, GN, BK, RING, GUARDED><<<grid, T::kThreads, T::kLds, stream>>>(a, d.to);
+  if (shared) linear_join_kernel<DT, E, WM, WN, GM, GN><<<join, T::kThreads, 0, stream>>>(a.partials, a.whole_tiles, a.splits, d.to);
+  return hipGetLastError();
 }
 
-template <int DT, OperandForm FA, OperandForm FB>
+template <int DT, OperandForm FA, OperandForm FB, Epilogue E>
 hipError_t launch_form(const DenseProduct& d, hipStream_t stream) {
   // copies take whole pieces at multiples of 16 bytes, from offsets of 31 bits within a stage
   const Pieces rows_a = pieces_of_rows(d.A, d.lda, FA == kAlong ? d.K : d.M), rows_b = pieces_of_rows(d.B, d.ldb, FB == kAlong ? d.K : d.N);
   const bool guarded = rows_a != kAligned || rows_b != kAligned || d.lda > (1 << 21) || d.ldb > (1 << 21);
   const TilePlan plan = plan_of(d.M, d.N, d.K, guarded);
-  const TileArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, plan.splits, plan.stages_of_split,
-                   rows_a, rows_b, static_cast<float*>(d.workspace)};
+  const TileArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, plan.whole_tiles, plan.splits,
+                   plan.stages_of_split, rows_a, rows_b, static_cast<float*>(d.workspace)};
   const int64_t tiles = tiles_of(plan.form, d.M, d.N);
   switch (plan.form) {
-    case kFormGuarded: return launch_tiles<DT, FA, FB, 2, 2, 2, 2, 64, 2, true>(d, a, tiles, stream);
-    case kFormSmall: return launch_tiles<DT, FA, FB, 2, 2, 2, 2, 64, 2, false>(d, a, tiles, stream);
-    default: return launch_tiles<DT, FA, FB, 4, 4, 2, 2, 64, 2, false>(d, a, tiles, stream);
+    case kFormGuarded: return launch_tiles<DT, FA, FB, E, 2, 2, 2, 2, 64, 2, true>(d, a, tiles, stream);
+    case kFormLarge: return launch_tiles<DT, FA, FB, E, 4, 4, 2, 2, 64, 2, false>(d, a, tiles, stream);
+    case kFormWide: return launch_tiles<DT, FA, FB, E, 4, 2, 2, 2, 64, 3, false>(d, a, tiles, stream);
+    case kFormMiddle: return launch_tiles<DT, FA, FB, E, 2, 2, 2, 2, 64, 4, false>(d, a, tiles, stream);
+    default: return launch_tiles<DT, FA, FB, E, 1, 1, 2, 2, 64, 4, false>(d, a, tiles, stream);
   }
 }
 template <int DT>
 hipError_t launch_dtype(const DenseProduct& d, hipStream_t stream) {
-  if (d.form_b == kAlong) return launch_form<DT, kAlong, kAlong>(d, stream);
-  return d.form_a == kAlong ? launch_form<DT, kAlong, kAcross>(d, stream) : launch_form<DT, kAcross, kAcross>(d, stream);
+  // the gradients' products have nothing behind them
+  if (d.form_b == kAlong) return launch_form<DT, kAlong, kAlong, kEpiBare>(d, stream);
+  if (d.form_a == kAcross) return launch_form<DT, kAcross, kAcross, kEpiBare>(d, stream);
+  switch (epilogue_of(d.to.act)) {
+    case kEpiGelu: return launch_form<DT, kAlong, kAcross, kEpiGelu>(d, stream);
+    case kEpiSigmoid: return launch_form<DT, kAlong, kAcross, kEpiSigmoid>(d, stream);
+    default: return launch_form<DT, kAlong, kAcross, kEpiLinear>(d, stream);
+  }
 }
 
 }  // namespace

@@ -40,4 +40,15 @@ __device__ __forceinline__ int wave_sum(int v) {
   return __builtin_amdgcn_readlane(v, 63);
 }
 
+// Exchanges register halves of two lanes' values, without LDS.
+template <int LANES>  // 32: the upper lanes of a with the lower ones of b; 16: odd rows of 16 of a with even ones of b
+__device__ __forceinline__ void swap_lanes(uint32_t& a, uint32_t& b) {
+  typedef unsigned pair __attribute__((ext_vector_type(2)));
+  pair r;
+  if constexpr (LANES == 32) r = __builtin_bit_cast(pair, __builtin_amdgcn_permlane32_swap(a, b, false, false));
+  else r = __builtin_bit_cast(pair, __builtin_amdgcn_permlane16_swap(a, b, false, false));
+  a = r[0];
+  b = r[1];
+}
+
 }  // namespace hinm
