@@ -134,7 +134,7 @@ LinearGradPlan linear_grad_plan(int32_t M, int32_t K, int32_t N) {
   LinearGradPlan p;
   p.ldz = ((int64_t)N + 7) / 8 * 8;
   p.dz = ((size_t)M * p.ldz * 2 + 255) & ~size_t{255};
-  const size_t x = dense_product_workspace_bytes(K, N, M), w = dense_product_workspace_bytes(M, K, N);
+  const size_t x = dense_product_workspace_bytes(K, N, M, false), w = dense_product_workspace_bytes(M, K, N, false);
   p.product = x > w ? x : w;
   return p;
 }
@@ -871,7 +871,7 @@ hinm_status hinm_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* works
   if (!workspace_bytes) return HINM_ERR_NULL;
   const hinm_status st = check_dense(M, K, N);
   if (st != HINM_OK) return st;
-  *workspace_bytes = dense_product_workspace_bytes(M, N, K);
+  *workspace_bytes = dense_product_workspace_bytes(M, N, K, true);
   return HINM_OK;
 }
 
@@ -888,7 +888,7 @@ hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const vo
     return HINM_ERR_SHAPE;
   const int act = activation_of(flags);
   if (act < 0 || (flags & ~(kActFlags | HINM_OUT_F32))) return HINM_ERR_UNSUPPORTED;
-  const size_t need = dense_product_workspace_bytes(M, N, K);
+  const size_t need = dense_product_workspace_bytes(M, N, K, true);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
   const LinearEpilogue to{M, N, bias, static_cast<const uint16_t*>(residual), ldr, pieces_of_rows(residual, ldr, N),
                           static_cast<uint16_t*>(Z), Y, ldy, act, out_f32};

@@ -1,0 +1,181 @@
+// A dense layer on few tokens (include/hinm.h, hinm_linear): the weights stream through registers once.
+//
+// A workgroup owns 16 rows of W and all tokens, at most 16; its waves take runs of 64 channels in turn, each
+// for the whole of that, with no barrier between them, and their sums meet in LDS in a fixed order.  The 16x16x32 instruction
+// takes W as it lies (a lane 16 bytes of a row, four lanes 64 consecutive bytes); X, whose channels lie apart, goes through a
+// place in LDS of the wave's own and comes back by transposing reads; a single token's vector needs no turning and comes
+// from memory as it is.  A run's loads are under way while the run before it multiplies.
+#include "linear_tile.h"
+
+#include "workgroup_items.h"
+
+namespace hinm {
+
+namespace {
+
+struct FewArgs {
+  const uint16_t* W;
+  int64_t ldw;
+  const uint16_t* X;
+  int64_t ldx;
+  int K;
+  Pieces rows_w, rows_x;
+};
+
+constexpr int kRun = 64;  // channels
+
+template <int DT>
+__device__ __forceinline__ f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (DT == HINM_F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// VECTOR: one token, its channels one after the other
+template <int DT, Epilogue E, bool VECTOR, int RB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(FewArgs a, LinearEpilogue e) {
+  constexpr int kSteps = kRun / 32, kFewRows = 16 * RB;
+  constexpr int kTokens = 16, kPitch = kTokens + 4;
+  constexpr int kTurned = VECTOR ? 0 : kRun * kTokens * 2, kSums = kFewRows * kPitch * 4;  // bytes
+  constexpr int kPlace = kTurned > kSums ? kTurned : kSums;  // of a wave: a run of X, and in the end its sums
+  __shared__ __align__(16) uint8_t places[WAVES][kPlace];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = item_of_workgroup((e.M + kFewRows - 1) / kFewRows);
+  if (item < 0) return;
+  const int m0 = item * kFewRows, r = lane & 15, g = lane >> 4;
+  const int runs = (a.K + kRun - 1) / kRun;
+  const uint16_t* w[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) w[b] = a.W + (int64_t)min(m0 + 16 * b + r, e.M - 1) * a.ldw + 8 * g;
+  const u32x4 none = {0, 0, 0, 0};
+  struct Run {
+    u32x4 w[RB][kSteps], x[2];
+  };
+  auto load = [&](int run, Run& f) __attribute__((always_inline)) {
+    const int k0 = run * kRun;
+    if (k0 + kRun <= a.K) {
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) f.w[b][s] = *reinterpret_cast<const u32x4_a2*>(w[b] + k0 + 32 * s);
+      if constexpr (VECTOR) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) f.x[s] = r == 0 ? u32x4(*reinterpret_cast<const u32x4_a2*>(a.X + k0 + 32 * s + 8 * g)) : none;
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int left = a.K - k0 - 32 * s - 8 * g;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) f.w[b][s] = left > 0 ? trim_eight(draw_eight(w[b] + k0 + 32 * s, left, a.rows_w), left, a.rows_w) : none;
+        if constexpr (VECTOR) f.x[s] = r == 0 && left > 0 ? trim_eight(draw_eight(a.X + k0 + 32 * s + 8 * g, left, a.rows_x), left, a.rows_x) : none;
+      }
+    }
+    if constexpr (!VECTOR) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int k = k0 + lane, left = e.N - 8 * t;
+        f.x[t] = k < a.K && left > 0 ? draw_eight(a.X + k * a.ldx + 8 * t, left, a.rows_x) : none;
+      }
+    }
+  };
+  f32x4 acc[RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) acc[b] = f32x4{0, 0, 0, 0};
+  uint8_t* const place = places[wave];
+  auto multiply = [&](Run& f) __attribute__((always_inline)) {
+    u32x4 x[kSteps];
+    if constexpr (VECTOR) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) x[s] = f.x[s];
+    } else {
+      asm volatile("" ::: "memory");  // LDS operations of a wave are done in order; the compiler is held to it
+#pragma unroll
+      for (int t = 0; t < 2; ++t) *reinterpret_cast<u32x4*>(place + lane * kTokens * 2 + 16 * t) = place_eight(f.x[t], e.N - 8 * t, a.rows_x);
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const uint8_t* from = place + (32 * s + 8 * g + (r >> 2)) * kTokens * 2 + 8 * (r & 3);
+        const u32x2 low = lds_read_tr16(from), high = lds_read_tr16(from + 4 * kTokens * 2);
+        x[s] = u32x4{low[0], low[1], high[0], high[1]};
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int b = 0; b < RB; ++b) acc[b] = mfma_16x16x32<DT>(x[s], f.w[b][s], acc[b]);
+  };
+  Run f;
+  if (wave < runs) {
+    load(wave, f);
+    int run = wave;
+    for (; run + WAVES < runs; run += WAVES) {
+      Run next;
+      load(run + WAVES, next);
+      multiply(f);
+      f = next;
+    }
+    multiply(f);
+  }
+  // a lane holds rows 16 b + lane % 16, tokens 4 (lane / 16) + 0 .. 3
+  auto sums = [&](int q) __attribute__((always_inline)) { return reinterpret_cast<float*>(places[q]); };
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int b = 0; b < RB; ++b) *reinterpret_cast<f32x4*>(sums(wave) + (16 * b + r) * kPitch + 4 * g) = acc[b];
+  __syncthreads();
+  const int count = min(WAVES, runs);
+  for (int i = threadIdx.x; i < kFewRows * kTokens; i += 64 * WAVES) {
+    const int at = i / kTokens * kPitch + i % kTokens;
+    float v = sums(0)[at];
+    for (int q = 1; q < count; ++q) v += sums(q)[at];
+    sums(0)[at] = v;
+  }
+  __syncthreads();
+  const int row = threadIdx.x >> 1, n = 8 * (threadIdx.x & 1), m = m0 + row, left = e.N - n;
+  if (row >= kFewRows || m >= e.M || left <= 0) return;
+  u32x4 residual = none;
+  if (e.residual) residual = draw_residual(e, m, n, min(left, 8));
+  const float b = e.bias ? e.bias[m] : 0.0f;
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = sums(0)[row * kPitch + n + j] + b;
+  finish_eight<DT, E, false>(e, m, n, min(left, 8), residual, v);
+}
+
+template <int DT, Epilogue E, bool VECTOR, int RB, int WAVES>
+hipError_t launch_few_as(const DenseProduct& d, const FewArgs& a, hipStream_t stream) {
+  const dim3 grid(grid_of_items(((int64_t)d.M + 16 * RB - 1) / (16 * RB)));
+  if (d.plan) {
+    plan_record(d.plan, "linear_few_kernel<DT=%d,E=%d,VECTOR=%d,RB=%d,WAVES=%d> grid=%u block=%d", DT, (int)E, (int)VECTOR, RB, WAVES, grid.x, 64 * WAVES);
+    return hipSuccess;
+  }
+  linear_few_kernel<DT, E, VECTOR, RB, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a, d.to);
+  return hipGetLastError();
+}
+template <int DT, Epilogue E>
+hipError_t launch_few_tokens(const DenseProduct& d, hipStream_t stream) {
+  const bool vector = d.N == 1 && d.ldb == 1;
+  const FewArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, pieces_of_rows(d.A, d.lda, d.K),
+                  vector ? pieces_of_rows(d.B, 8, d.K) : pieces_of_rows(d.B, d.ldb, d.N)};
+  if (vector) return launch_few_as<DT, E, true, 1, 16>(d, a, stream);
+  // More rows share what a workgroup draws of X, which every workgroup draws, where they are many enough to fill the chip all
+  // the same: 16384x16384 of 16 tokens 121 us with 16 rows and 98 with 64, 11008x4096 27.6 and 22.9, 4096x11008 25.4 and 50.7.
+  return (d.M + 63) / 64 >= 160 ? launch_few_as<DT, E, false, 4, 16>(d, a, stream) : launch_few_as<DT, E, false, 1, 16>(d, a, stream);
+}
+template <int DT>
+hipError_t launch_few_dtype(const DenseProduct& d, hipStream_t stream) {
+  switch (epilogue_of(d.to.act)) {
+    case kEpiGelu: return launch_few_tokens<DT, kEpiGelu>(d, stream);
+    case kEpiSigmoid: return launch_few_tokens<DT, kEpiSigmoid>(d, stream);
+    default: return launch_few_tokens<DT, kEpiLinear>(d, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_linear_few(const DenseProduct& d, hipStream_t stream) {
+  return d.dtype == HINM_F16 ? launch_few_dtype<HINM_F16>(d, stream) : launch_few_dtype<HINM_BF16>(d, stream);
+}
+
+}  // namespace hinm

@@ -20,9 +20,13 @@ struct DenseProduct {
   LinearEpilogue to;
   void* workspace;
   LaunchPlan* plan = nullptr;  // set: record what would be launched instead
+  bool is_layer() const { return form_a == kAlong && form_b == kAcross; }
 };
-size_t dense_product_workspace_bytes(int M, int N, int K);
+size_t dense_product_workspace_bytes(int M, int N, int K, bool layer);
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream);
+// a layer's product (A along, B across) on up to kFewTokens tokens
+constexpr int kFewTokens = 16;
+hipError_t launch_linear_few(const DenseProduct& p, hipStream_t stream);
 
 // dZ [M][ldz] = dY act'(Z), zero in columns from N on to the next multiple of 8 (ldz is one), and dbias [M] = its sums over N
 // columns; either may be NULL.  Z NULL: no activation.

@@ -505,29 +505,67 @@ __global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* 
   to.template store<DT, E, false>(acc, bias, m0, n0, e);
 }
 
-// Which form serves a shape.
+// Which form serves a shape, and by how many workgroups the tiles of its last round are shared: the least of estimates in
+// microseconds, fitted to launches at 69 shapes (M, N, K of 128 .. 16384, some from 4 on; operands from memory) with every form and up to
+// 12 workgroups a tile; what they choose is 2.3 % behind the best of these on the geometric mean, 27 % at most.  Both sides of
+// each line: 2048x2048 of 2048 columns 22.2 us in tiles of 128, 27.8 of 256x128, 33.4 of 64; 4096x4096 of 2048 67, 82 and 124,
+// in tiles of 256 100; of 4096 in those 113 (1208 TFLOP/s); 1024x1024 of 1024 8.0 in tiles of 64, 11.0 of 128; 11008x4096 of 1571
+// columns, 559 tiles of 256x128, 162 us with a third round of 47 workgroups and 152 where four share each of its tiles;
+// 4096x4096 of 200, 64 tiles of 128, 42 us alone, 23 in four parts.
 struct TileForm {
-  int rows, cols;
+  int rows, cols, at_once;    // of a tile; workgroups that the chip holds
+  double start;               // us of a launch and of what does not overlap
+  double alone, full, tile;   // us of a stage, with few workgroups and with all places taken; of a tile's beginning and end
+  double join, join_rate;     // sharing: us of the second launch, MB/us that the parts are written and read at
 };
-enum { kFormGuarded, kFormLarge, kFormWide, kFormMiddle, kFormSmall };
-constexpr TileForm kTileForms[] = {{128, 128}, {256, 256}, {256, 128}, {128, 128}, {64, 64}};
+enum { kFormGuarded, kFormLarge, kFormWide, kFormMiddle, kFormSmall, kTileFormCount };
+constexpr TileForm kTileForms[kTileFormCount] = {
+    {128, 128, 512, 2.6, 1.3, 2.3, 3.0, 3.0, 6.7},
+    {256, 256, 256, 2.67, 1.227, 1.693, 6.46, 3.05, 6.1},
+    {256, 128, 256, 2.26, 0.625, 0.935, 4.59, 2.37, 7.65},
+    {128, 128, 256, 2.62, 0.350, 0.583, 2.75, 3.01, 6.66},
+    {64, 64, 512, 1.97, 0.217, 0.466, 1.70, 2.70, 5.35},
+};
 constexpr int kStage = 64;  // summed values, of every form
+constexpr int kShares[] = {2, 3, 4, 6, 8, 12, 16};
 
-int64_t tiles_of(int form, int M, int N) {
-  return (int64_t)((M + kTileForms[form].rows - 1) / kTileForms[form].rows) * ((N + kTileForms[form].cols - 1) / kTileForms[form].cols);
+int64_t tiles_of(const TileForm& f, int M, int N) { return (int64_t)((M + f.rows - 1) / f.rows) * ((N + f.cols - 1) / f.cols); }
+double rounds_us(const TileForm& f, int64_t groups, int stages) {
+  const int64_t rounds = groups / f.at_once, left = groups - rounds * f.at_once;
+  const double last = left ? stages * (f.alone + (f.full - f.alone) * (double)left / f.at_once) + f.tile : 0;
+  return (double)rounds * (stages * f.full + f.tile) + last;
 }
 struct TilePlan {
   int form, whole_tiles, splits, stages_of_split;
 };
 TilePlan plan_of(int M, int N, int K, bool guarded) {
   const int stages = (K + kStage - 1) / kStage;
-  TilePlan p{guarded ? kFormGuarded : kFormMiddle, 0, 1, stages};
-  if (!guarded && tiles_of(kFormLarge, M, N) >= 224) p.form = kFormLarge;
-  p.whole_tiles = (int)tiles_of(p.form, M, N);
-  return p;
+  TilePlan best{};
+  double least = 1e300;
+  for (int i = guarded ? kFormGuarded : kFormGuarded + 1; i < (guarded ? kFormGuarded + 1 : (int)kTileFormCount); ++i) {
+    const TileForm& f = kTileForms[i];
+    const int64_t tiles = tiles_of(f, M, N);
+    auto take = [&](double us, int64_t whole, int splits, int each) {
+      if (us >= least) return;
+      least = us;
+      best = TilePlan{i, (int)whole, splits, each};
+    };
+    take(f.start + rounds_us(f, tiles, stages), tiles, 1, stages);
+    const int64_t whole = tiles / f.at_once * f.at_once, shared = tiles - whole;
+    if (shared == 0 || stages < 2) continue;
+    for (int splits : kShares) {
+      const int each = (stages + splits - 1) / splits, parts = (stages + each - 1) / each;
+      const int64_t groups = shared * parts;
+      if (parts < 2 || (splits > 2 && groups > 2 * f.at_once)) break;
+      const double moved = (double)groups * f.rows * f.cols * 8e-6;  // MB of parts written and read
+      take(f.start + rounds_us(f, whole, stages) + rounds_us(f, groups, each) + f.join + moved / f.join_rate, whole, parts, each);
+    }
+  }
+  return best;
 }
 size_t partial_bytes(const TilePlan& p, int M, int N) {
-  return (size_t)p.splits * (tiles_of(p.form, M, N) - p.whole_tiles) * kTileForms[p.form].rows * kTileForms[p.form].cols * sizeof(float);
+  const TileForm& f = kTileForms[p.form];
+  return (size_t)p.splits * (tiles_of(f, M, N) - p.whole_tiles) * f.rows * f.cols * sizeof(float);
 }
 
 template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
@@ -556,7 +594,7 @@ hipError_t launch_form(const DenseProduct& d, hipStream_t stream) {
   const TilePlan plan = plan_of(d.M, d.N, d.K, guarded);
   const TileArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, plan.whole_tiles, plan.splits,
                    plan.stages_of_split, rows_a, rows_b, static_cast<float*>(d.workspace)};
-  const int64_t tiles = tiles_of(plan.form, d.M, d.N);
+  const int64_t tiles = tiles_of(kTileForms[plan.form], d.M, d.N);
   switch (plan.form) {
     case kFormGuarded: return launch_tiles<DT, FA, FB, E, 2, 2, 2, 2, 64, 2, true>(d, a, tiles, stream);
     case kFormLarge: return launch_tiles<DT, FA, FB, E, 4, 4, 2, 2, 64, 2, false>(d, a, tiles, stream);
@@ -579,12 +617,14 @@ hipError_t launch_dtype(const DenseProduct& d, hipStream_t stream) {
 
 }  // namespace
 
-size_t dense_product_workspace_bytes(int M, int N, int K) {
+size_t dense_product_workspace_bytes(int M, int N, int K, bool layer) {
+  if (layer && N <= kFewTokens) return 0;
   const size_t a = partial_bytes(plan_of(M, N, K, false), M, N), b = partial_bytes(plan_of(M, N, K, true), M, N);
   return a > b ? a : b;
 }
 
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream) {
+  if (p.is_layer() && p.N <= kFewTokens) return launch_linear_few(p, stream);
   return p.dtype == HINM_F16 ? launch_dtype<HINM_F16>(p, stream) : launch_dtype<HINM_BF16>(p, stream);
 }
 
