@@ -134,7 +134,7 @@ LinearGradPlan linear_grad_plan(int32_t M, int32_t K, int32_t N) {
   LinearGradPlan p;
   p.ldz = ((int64_t)N + 7) / 8 * 8;
   p.dz = ((size_t)M * p.ldz * 2 + 255) & ~size_t{255};
-  const size_t x = dense_product_workspace_bytes(K, N, M, false), w = dense_product_workspace_bytes(M, K, N, false);
+  const size_t x = dense_product_workspace_bytes(K, N, M, kAcross, kAcross), w = dense_product_workspace_bytes(M, K, N, kAlong, kAlong);
   p.product = x > w ? x : w;
   return p;
 }
@@ -871,7 +871,7 @@ hinm_status hinm_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* works
   if (!workspace_bytes) return HINM_ERR_NULL;
   const hinm_status st = check_dense(M, K, N);
   if (st != HINM_OK) return st;
-  *workspace_bytes = dense_product_workspace_bytes(M, N, K, true);
+  *workspace_bytes = dense_product_workspace_bytes(M, N, K, kAlong, kAcross);
   return HINM_OK;
 }
 
@@ -888,7 +888,7 @@ hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const vo
     return HINM_ERR_SHAPE;
   const int act = activation_of(flags);
   if (act < 0 || (flags & ~(kActFlags | HINM_OUT_F32))) return HINM_ERR_UNSUPPORTED;
-  const size_t need = dense_product_workspace_bytes(M, N, K, true);
+  const size_t need = dense_product_workspace_bytes(M, N, K, kAlong, kAcross);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
   const LinearEpilogue to{M, N, bias, static_cast<const uint16_t*>(residual), ldr, pieces_of_rows(residual, ldr, N),
                           static_cast<uint16_t*>(Z), Y, ldy, act, out_f32};
@@ -953,7 +953,9 @@ hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtyp
   auto pitch = [](int32_t n) { return ((int64_t)n + 7) / 8 * 8; };
   auto launch = [&](int32_t m, int32_t n, int32_t k, OperandForm a, OperandForm b) {
     const LinearEpilogue to{m, n, nullptr, nullptr, 0, kAligned, nullptr, nullptr, pitch(n), kActNone, false};
-    return launch_dense_product({m, n, k, dtype, a, b, at, pitch(a == kAlong ? k : m), at, pitch(b == kAlong ? k : n), to, nullptr, &plan}, nullptr);
+    const void* const aligned_at = reinterpret_cast<const void*>(uintptr_t{1} << 20);
+    return launch_dense_product({m, n, k, dtype, a, b, at, pitch(a == kAlong ? k : m), which == 2 ? at : aligned_at, pitch(b == kAlong ? k : n), to,
+                                 const_cast<void*>(aligned_at), &plan}, nullptr);
   };
   if (which == 0) return launched(launch(M, N, K, kAlong, kAcross));
   return launched(which == 1 ? launch(K, N, M, kAcross, kAcross) : launch(M, K, N, kAlong, kAlong));

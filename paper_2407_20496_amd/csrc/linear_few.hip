@@ -22,7 +22,6 @@ struct FewArgs {
   Pieces rows_w, rows_x;
 };
 
-constexpr int kRun = 64;  // channels
 
 template <int DT>
 __device__ __forceinline__ f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c) {
@@ -32,25 +31,29 @@ __device__ __forceinline__ f32x4 mfma_16x16x32(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// VECTOR: one token, its channels one after the other
-template <int DT, Epilogue E, bool VECTOR, int RB, int WAVES>
+// VECTOR: one token, its channels one after the other.  PIECES: rows of W at multiples of 16 bytes.
+template <int DT, Epilogue E, bool VECTOR, bool PIECES, int RB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(FewArgs a, LinearEpilogue e) {
-  constexpr int kSteps = kRun / 32, kFewRows = 16 * RB;
+  constexpr int kRun = PIECES ? 64 : 128, kSteps = kRun / 32, kFewRows = 16 * RB;
+  static_assert(PIECES || RB == 1, "a place for 16 rows");
   constexpr int kTokens = 16, kPitch = kTokens + 4;
-  constexpr int kTurned = VECTOR ? 0 : kRun * kTokens * 2, kSums = kFewRows * kPitch * 4;  // bytes
-  constexpr int kPlace = kTurned > kSums ? kTurned : kSums;  // of a wave: a run of X, and in the end its sums
+  constexpr int kTurnedX = VECTOR ? 0 : kRun * kTokens * 2, kTurned = kTurnedX + (PIECES ? 0 : 16 * kRun * 2);  // bytes
+  constexpr int kSums = kFewRows * kPitch * 4;
+  constexpr int kPlace = kTurned > kSums ? kTurned : kSums;  // of a wave: a run of X and of W, and in the end its sums
   __shared__ __align__(16) uint8_t places[WAVES][kPlace];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int item = item_of_workgroup((e.M + kFewRows - 1) / kFewRows);
   if (item < 0) return;
   const int m0 = item * kFewRows, r = lane & 15, g = lane >> 4;
   const int runs = (a.K + kRun - 1) / kRun;
-  const uint16_t* w[RB];
+  constexpr int kPointers = PIECES ? RB : 4;
+  const uint16_t* w[kPointers];
 #pragma unroll
-  for (int b = 0; b < RB; ++b) w[b] = a.W + (int64_t)min(m0 + 16 * b + r, e.M - 1) * a.ldw + 8 * g;
+  for (int b = 0; b < kPointers; ++b)
+    w[b] = a.W + (int64_t)min(m0 + (PIECES ? 16 * b + r : 4 * b + g), e.M - 1) * a.ldw + (PIECES ? 8 * g : 8 * r);
   const u32x4 none = {0, 0, 0, 0};
   struct Run {
-    u32x4 w[RB][kSteps], x[2];
+    u32x4 w[RB][kSteps], x[kRun / 32];  // w: not of pieces, rows 4 i + lane / 16, eight channels each
   };
   auto load = [&](int run, Run& f) __attribute__((always_inline)) {
     const int k0 = run * kRun;
@@ -58,7 +61,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(FewArgs a, Linea
 #pragma unroll
       for (int b = 0; b < RB; ++b)
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) f.w[b][s] = *reinterpret_cast<const u32x4_a2*>(w[b] + k0 + 32 * s);
+        for (int s = 0; s < kSteps; ++s) f.w[b][s] = *reinterpret_cast<const u32x4_a2*>(PIECES ? w[b] + k0 + 32 * s : w[s] + k0);
       if constexpr (VECTOR) {
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) f.x[s] = r == 0 ? u32x4(*reinterpret_cast<const u32x4_a2*>(a.X + k0 + 32 * s + 8 * g)) : none;
@@ -68,15 +71,18 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(FewArgs a, Linea
       for (int s = 0; s < kSteps; ++s) {
         const int left = a.K - k0 - 32 * s - 8 * g;
 #pragma unroll
-        for (int b = 0; b < RB; ++b) f.w[b][s] = left > 0 ? trim_eight(draw_eight(w[b] + k0 + 32 * s, left, a.rows_w), left, a.rows_w) : none;
+        for (int b = 0; b < RB; ++b) {
+          const int of_w = PIECES ? left : a.K - k0 - 8 * r;
+          f.w[b][s] = of_w > 0 ? trim_eight(draw_eight(PIECES ? w[b] + k0 + 32 * s : w[s] + k0, of_w, a.rows_w), of_w, a.rows_w) : none;
+        }
         if constexpr (VECTOR) f.x[s] = r == 0 && left > 0 ? trim_eight(draw_eight(a.X + k0 + 32 * s + 8 * g, left, a.rows_x), left, a.rows_x) : none;
       }
     }
     if constexpr (!VECTOR) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int k = k0 + lane, left = e.N - 8 * t;
-        f.x[t] = k < a.K && left > 0 ? draw_eight(a.X + k * a.ldx + 8 * t, left, a.rows_x) : none;
+      for (int t = 0; t < kRun / 32; ++t) {
+        const int k = k0 + lane + 64 * (t >> 1), left = e.N - 8 * (t & 1);
+        f.x[t] = k < a.K && left > 0 ? draw_eight(a.X + k * a.ldx + 8 * (t & 1), left, a.rows_x) : none;
       }
     }
   };
@@ -86,14 +92,26 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(FewArgs a, Linea
   uint8_t* const place = places[wave];
   auto multiply = [&](Run& f) __attribute__((always_inline)) {
     u32x4 x[kSteps];
+    asm volatile("" ::: "memory");  // LDS operations of a wave are done in order; the compiler is held to it
+    if constexpr (!PIECES) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        *reinterpret_cast<u32x4*>(place + kTurnedX + (4 * s + g) * kRun * 2 + 16 * (r ^ (4 * s + g))) = f.w[0][s];
+    }
+    if constexpr (!VECTOR) {
+#pragma unroll
+      for (int t = 0; t < kRun / 32; ++t)
+        *reinterpret_cast<u32x4*>(place + (lane + 64 * (t >> 1)) * kTokens * 2 + 16 * (t & 1)) = place_eight(f.x[t], e.N - 8 * (t & 1), a.rows_x);
+    }
+    asm volatile("" ::: "memory");
+    if constexpr (!PIECES) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) f.w[0][s] = *reinterpret_cast<const u32x4*>(place + kTurnedX + r * kRun * 2 + 16 * ((4 * s + g) ^ r));
+    }
     if constexpr (VECTOR) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) x[s] = f.x[s];
     } else {
-      asm volatile("" ::: "memory");  // LDS operations of a wave are done in order; the compiler is held to it
-#pragma unroll
-      for (int t = 0; t < 2; ++t) *reinterpret_cast<u32x4*>(place + lane * kTokens * 2 + 16 * t) = place_eight(f.x[t], e.N - 8 * t, a.rows_x);
-      asm volatile("" ::: "memory");
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         const uint8_t* from = place + (32 * s + 8 * g + (r >> 2)) * kTokens * 2 + 8 * (r & 3);
@@ -143,14 +161,14 @@ __global__ __launch_bounds__(64 * WAVES) void linear_few_kernel(FewArgs a, Linea
   finish_eight<DT, E, false>(e, m, n, min(left, 8), residual, v);
 }
 
-template <int DT, Epilogue E, bool VECTOR, int RB, int WAVES>
+template <int DT, Epilogue E, bool VECTOR, bool PIECES, int RB, int WAVES>
 hipError_t launch_few_as(const DenseProduct& d, const FewArgs& a, hipStream_t stream) {
   const dim3 grid(grid_of_items(((int64_t)d.M + 16 * RB - 1) / (16 * RB)));
   if (d.plan) {
-    plan_record(d.plan, "linear_few_kernel<DT=%d,E=%d,VECTOR=%d,RB=%d,WAVES=%d> grid=%u block=%d", DT, (int)E, (int)VECTOR, RB, WAVES, grid.x, 64 * WAVES);
+    plan_record(d.plan, "linear_few_kernel<DT=%d,E=%d,VECTOR=%d,PIECES=%d,RB=%d,WAVES=%d> grid=%u block=%d", DT, (int)E, (int)VECTOR, (int)PIECES, RB, WAVES, grid.x, 64 * WAVES);
     return hipSuccess;
   }
-  linear_few_kernel<DT, E, VECTOR, RB, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a, d.to);
+  linear_few_kernel<DT, E, VECTOR, PIECES, RB, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a, d.to);
   return hipGetLastError();
 }
 template <int DT, Epilogue E>
@@ -158,10 +176,11 @@ hipError_t launch_few_tokens(const DenseProduct& d, hipStream_t stream) {
   const bool vector = d.N == 1 && d.ldb == 1;
   const FewArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, pieces_of_rows(d.A, d.lda, d.K),
                   vector ? pieces_of_rows(d.B, 8, d.K) : pieces_of_rows(d.B, d.ldb, d.N)};
-  if (vector) return launch_few_as<DT, E, true, 1, 16>(d, a, stream);
+  if (a.rows_w != kAligned) return vector ? launch_few_as<DT, E, true, false, 1, 8>(d, a, stream) : launch_few_as<DT, E, false, false, 1, 8>(d, a, stream);
+  if (vector) return launch_few_as<DT, E, true, true, 1, 16>(d, a, stream);
   // More rows share what a workgroup draws of X, which every workgroup draws, where they are many enough to fill the chip all
   // the same: 16384x16384 of 16 tokens 121 us with 16 rows and 98 with 64, 11008x4096 27.6 and 22.9, 4096x11008 25.4 and 50.7.
-  return (d.M + 63) / 64 >= 160 ? launch_few_as<DT, E, false, 4, 16>(d, a, stream) : launch_few_as<DT, E, false, 1, 16>(d, a, stream);
+  return (d.M + 63) / 64 >= 160 ? launch_few_as<DT, E, false, true, 4, 16>(d, a, stream) : launch_few_as<DT, E, false, true, 1, 16>(d, a, stream);
 }
 template <int DT>
 hipError_t launch_few_dtype(const DenseProduct& d, hipStream_t stream) {

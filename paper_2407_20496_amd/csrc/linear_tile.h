@@ -20,9 +20,9 @@ struct DenseProduct {
   LinearEpilogue to;
   void* workspace;
   LaunchPlan* plan = nullptr;  // set: record what would be launched instead
-  bool is_layer() const { return form_a == kAlong && form_b == kAcross; }
 };
-size_t dense_product_workspace_bytes(int M, int N, int K, bool layer);
+inline bool is_layer(OperandForm form_a, OperandForm form_b) { return form_a == kAlong && form_b == kAcross; }
+size_t dense_product_workspace_bytes(int M, int N, int K, OperandForm form_a, OperandForm form_b);  // a multiple of 256
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream);
 // a layer's product (A along, B across) on up to kFewTokens tokens
 constexpr int kFewTokens = 16;

@@ -537,6 +537,7 @@ double rounds_us(const TileForm& f, int64_t groups, int stages) {
 }
 struct TilePlan {
   int form, whole_tiles, splits, stages_of_split;
+  double us;
 };
 TilePlan plan_of(int M, int N, int K, bool guarded) {
   const int stages = (K + kStage - 1) / kStage;
@@ -548,7 +549,7 @@ TilePlan plan_of(int M, int N, int K, bool guarded) {
     auto take = [&](double us, int64_t whole, int splits, int each) {
       if (us >= least) return;
       least = us;
-      best = TilePlan{i, (int)whole, splits, each};
+      best = TilePlan{i, (int)whole, splits, each, us};
     };
     take(f.start + rounds_us(f, tiles, stages), tiles, 1, stages);
     const int64_t whole = tiles / f.at_once * f.at_once, shared = tiles - whole;
@@ -567,6 +568,44 @@ size_t partial_bytes(const TilePlan& p, int M, int N) {
   const TileForm& f = kTileForms[p.form];
   return (size_t)p.splits * (tiles_of(f, M, N) - p.whole_tiles) * f.rows * f.cols * sizeof(float);
 }
+
+// Rows of A that follow one another at any address (their length is not a multiple of 8) lie apart in the workspace first, in whole
+// pieces, where that and the product from there take less than the product through registers: 4095x4095 of 1000 columns 85 us as
+// they lie.
+struct CopyOfA {
+  int rows, row;  // how many, and their length
+  int64_t pitch() const { return ((int64_t)row + 7) / 8 * 8; }
+  size_t bytes() const { return ((size_t)rows * pitch() * 2 + 255) & ~size_t{255}; }
+  double us() const { return 2.5 + 4e-6 / 4.5 * rows * row; }
+};
+// Weights alone: the other operands have rows of whole pieces where a program uses this package's buffers.
+bool may_copy(int M, int K, OperandForm form_a, OperandForm form_b) { return form_b == kAcross && (form_a == kAlong ? K : M) % 8 != 0; }
+CopyOfA copy_of(int M, int K, OperandForm form_a) { return form_a == kAlong ? CopyOfA{M, K} : CopyOfA{K, M}; }
+__global__ __launch_bounds__(256) void linear_copy_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t pitch, int rows, int row, Pieces pieces) {
+  const int per_row = (int)(pitch / 8);
+  const int64_t all = (int64_t)rows * per_row, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
+    const int r = (int)(i / per_row), at = 8 * (int)(i - (int64_t)r * per_row), left = row - at;
+    *reinterpret_cast<u32x4*>(to + r * pitch + at) = trim_eight(draw_eight(from + r * ld + at, left, pieces), left, pieces);
+  }
+}
+
+// How the operands of a product lie.  Copies into LDS take whole pieces at multiples of 16 bytes, from offsets of 31 bits within a stage.
+struct Operands {
+  Pieces rows_a, rows_b;
+  bool far_a, far_b;
+  explicit Operands(const DenseProduct& d)
+      : rows_a(pieces_of_rows(d.A, d.lda, d.form_a == kAlong ? d.K : d.M)), rows_b(pieces_of_rows(d.B, d.ldb, d.form_b == kAlong ? d.K : d.N)),
+        far_a(d.lda > (1 << 21)), far_b(d.ldb > (1 << 21)) {}
+  bool guarded() const { return rows_a != kAligned || rows_b != kAligned || far_a || far_b; }
+  TilePlan plan(const DenseProduct& d) const { return plan_of(d.M, d.N, d.K, guarded()); }
+  // whether the product is sooner from a copy of A
+  bool copies(const DenseProduct& d) const {
+    if (rows_a == kAligned || rows_b != kAligned || far_b || !may_copy(d.M, d.K, d.form_a, d.form_b)) return false;
+    const CopyOfA c = copy_of(d.M, d.K, d.form_a);
+    return c.pitch() <= 1 << 21 && plan_of(d.M, d.N, d.K, false).us + c.us() < plan(d).us;
+  }
+};
 
 template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
 hipError_t launch_tiles(const DenseProduct& d, const TileArgs& a, int64_t tiles, hipStream_t stream) {
@@ -588,12 +627,10 @@ hipError_t launch_tiles(const DenseProduct& d, const TileArgs& a, int64_t tiles,
 
 template <int DT, OperandForm FA, OperandForm FB, Epilogue E>
 hipError_t launch_form(const DenseProduct& d, hipStream_t stream) {
-  // copies take whole pieces at multiples of 16 bytes, from offsets of 31 bits within a stage
-  const Pieces rows_a = pieces_of_rows(d.A, d.lda, FA == kAlong ? d.K : d.M), rows_b = pieces_of_rows(d.B, d.ldb, FB == kAlong ? d.K : d.N);
-  const bool guarded = rows_a != kAligned || rows_b != kAligned || d.lda > (1 << 21) || d.ldb > (1 << 21);
-  const TilePlan plan = plan_of(d.M, d.N, d.K, guarded);
+  const Operands o(d);
+  const TilePlan plan = o.plan(d);
   const TileArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, plan.whole_tiles, plan.splits,
-                   plan.stages_of_split, rows_a, rows_b, static_cast<float*>(d.workspace)};
+                   plan.stages_of_split, o.rows_a, o.rows_b, static_cast<float*>(d.workspace)};
   const int64_t tiles = tiles_of(kTileForms[plan.form], d.M, d.N);
   switch (plan.form) {
     case kFormGuarded: return launch_tiles<DT, FA, FB, E, 2, 2, 2, 2, 64, 2, true>(d, a, tiles, stream);
@@ -617,15 +654,34 @@ hipError_t launch_dtype(const DenseProduct& d, hipStream_t stream) {
 
 }  // namespace
 
-size_t dense_product_workspace_bytes(int M, int N, int K, bool layer) {
-  if (layer && N <= kFewTokens) return 0;
-  const size_t a = partial_bytes(plan_of(M, N, K, false), M, N), b = partial_bytes(plan_of(M, N, K, true), M, N);
-  return a > b ? a : b;
+size_t dense_product_workspace_bytes(int M, int N, int K, OperandForm form_a, OperandForm form_b) {
+  if (is_layer(form_a, form_b) && N <= kFewTokens) return 0;
+  const size_t guarded = partial_bytes(plan_of(M, N, K, true), M, N);
+  const size_t whole = partial_bytes(plan_of(M, N, K, false), M, N) + (may_copy(M, K, form_a, form_b) ? copy_of(M, K, form_a).bytes() : 0);
+  return whole > guarded ? whole : guarded;
 }
 
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream) {
-  if (p.is_layer() && p.N <= kFewTokens) return launch_linear_few(p, stream);
-  return p.dtype == HINM_F16 ? launch_dtype<HINM_F16>(p, stream) : launch_dtype<HINM_BF16>(p, stream);
+  if (is_layer(p.form_a, p.form_b) && p.N <= kFewTokens) return launch_linear_few(p, stream);
+  DenseProduct d = p;
+  const Operands o(p);
+  if (o.copies(p)) {
+    const CopyOfA c = copy_of(p.M, p.K, p.form_a);
+    const int64_t groups = (c.rows * (c.pitch() / 8) + 1023) / 1024;  // four pieces a thread
+    const dim3 grid((uint32_t)(groups < 1 << 20 ? groups : 1 << 20));
+    d.A = p.workspace;
+    d.lda = c.pitch();
+    d.workspace = static_cast<uint8_t*>(p.workspace) + c.bytes();
+    if (p.plan) {
+      plan_record(p.plan, "linear_copy_kernel grid=%u block=256", grid.x);
+    } else {
+      linear_copy_kernel<<<grid, 256, 0, stream>>>(static_cast<const uint16_t*>(p.A), p.lda, static_cast<uint16_t*>(p.workspace), c.pitch(), c.rows,
+                                                   c.row, o.rows_a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return d.dtype == HINM_F16 ? launch_dtype<HINM_F16>(d, stream) : launch_dtype<HINM_BF16>(d, stream);
 }
 
 }  // namespace hinm
