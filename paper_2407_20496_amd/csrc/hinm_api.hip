@@ -126,14 +126,18 @@ hinm_status check_dense_grad(int32_t M, int32_t K, int32_t N) {
   const hinm_status st = check_dense(K, M, N);
   return st != HINM_OK ? st : check_dense(M, N, K);
 }
+// The gradients' products take whole pieces of rows: dZ has them, and dY where it takes dZ's place, or it is written there as it is; X
+// of few tokens (a single token's vector has none) is copied.
+constexpr int32_t kMostCopiedTokens = 64;
 struct LinearGradPlan {
-  int64_t ldz;
-  size_t dz, product;  // bytes of dZ, rounded to 256, and of the products' partial sums
+  int64_t ldz;              // of dZ and of X's copy
+  size_t dz, x, product;  // bytes of dZ and of X's copy, rounded to 256, and of the products' partial sums
 };
 LinearGradPlan linear_grad_plan(int32_t M, int32_t K, int32_t N) {
   LinearGradPlan p;
   p.ldz = ((int64_t)N + 7) / 8 * 8;
   p.dz = ((size_t)M * p.ldz * 2 + 255) & ~size_t{255};
+  p.x = N <= kMostCopiedTokens ? ((size_t)K * p.ldz * 2 + 255) & ~size_t{255} : 0;
   const size_t x = dense_product_workspace_bytes(K, N, M, kAcross, kAcross), w = dense_product_workspace_bytes(M, K, N, kAlong, kAlong);
   p.product = x > w ? x : w;
   return p;
@@ -900,7 +904,7 @@ hinm_status hinm_linear_grad_workspace(int32_t M, int32_t K, int32_t N, size_t* 
   const hinm_status st = check_dense_grad(M, K, N);
   if (st != HINM_OK) return st;
   const LinearGradPlan p = linear_grad_plan(M, K, N);
-  *workspace_bytes = p.dz + p.product;
+  *workspace_bytes = p.dz + p.x + p.product;
   return HINM_OK;
 }
 
@@ -919,10 +923,12 @@ hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, con
     return HINM_ERR_SHAPE;
   if (act < 0 || (flags & ~(kActFlags | HINM_OUT_F32))) return HINM_ERR_UNSUPPORTED;
   const LinearGradPlan p = linear_grad_plan(M, K, N);
-  if (!workspace || workspace_bytes < p.dz + p.product || !aligned(workspace, 256)) return HINM_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < p.dz + p.x + p.product || !aligned(workspace, 256)) return HINM_ERR_WORKSPACE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  uint16_t* const dz = act == kActNone || (!dX && !dW) ? nullptr : static_cast<uint16_t*>(workspace);
-  void* const partials = static_cast<uint8_t*>(workspace) + p.dz;
+  const bool as_it_is = act == kActNone && pieces_of_rows(dY, ldy, N) == kAligned;
+  uint16_t* const dz = as_it_is || (!dX && !dW) ? nullptr : static_cast<uint16_t*>(workspace);
+  uint8_t* const x_copy = static_cast<uint8_t*>(workspace) + p.dz;
+  void* const partials = x_copy + p.x;
   hipError_t e = hipSuccess;
   if (dz || dbias) {
     const void* z = act == kActNone ? nullptr : Z;
@@ -934,6 +940,11 @@ hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, con
   if (e == hipSuccess && dX)
     e = launch_dense_product({K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
                               {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials}, s);
+  if (e == hipSuccess && dW && p.x && pieces_of_rows(X, ldx, N) != kAligned) {
+    e = launch_row_copy(X, ldx, x_copy, p.ldz, K, N, s);
+    X = x_copy;
+    ldx = p.ldz;
+  }
   if (e == hipSuccess && dW)
     e = launch_dense_product({M, K, N, dtype, kAlong, kAlong, g, ldg, X, ldx,
                               {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials}, s);

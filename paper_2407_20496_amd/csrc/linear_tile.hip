@@ -372,6 +372,9 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
   // the first stages, of the last one half: the other half follows in the first step
   Held held;
   constexpr int kHalf = T::kCopies / 2;
+  // Small tiles: a step's products do not cover the way through LDS, so a wave holds the operands of a whole stage and reads those
+  // of the next one meanwhile.
+  constexpr bool kWholeStages = !GUARDED && WM * WN <= 4;
   if constexpr (GUARDED) {
     for (int q = 0; q < min(RING, stages); ++q) {
       draw_stage(q, held);
@@ -385,18 +388,63 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
       if (q == whole) cut_offsets();
       const Buffers from = buffers_of(q);
 #pragma unroll
-      for (int c = 0; c < (q < RING - 1 ? T::kCopies : kHalf); ++c) copy_one(from, q * T::kStageBytes, c);
+      for (int c = 0; c < (kWholeStages || q < RING - 1 ? T::kCopies : kHalf); ++c) copy_one(from, q * T::kStageBytes, c);
     }
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies + kHalf) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kWholeStages ? (RING - 1) * T::kCopies : (RING - 2) * T::kCopies + kHalf) : "memory");
   }
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   if (!GUARDED && whole == 0) clear_cut_stage(0);
 
-  Operands sets[2];
+  uint32_t at = 0;  // the place of stage p, and of stage p + RING
+  Operands sets[kWholeStages ? 2 * kSteps : 2];
+  if constexpr (kWholeStages) {
+    // The barrier stands ahead of a stage's products: past it every wave has read the stage, whose place takes stage p + RING, and
+    // stage p + 1 is there.
+    unroll<0, kSteps>([&](auto s) __attribute__((always_inline)) {
+      unroll<0, WM + WN>([&](auto t) __attribute__((always_inline)) { read_one(s, t, 0, sets[decltype(s)::value]); });
+    });
+    auto stage = [&](auto odd_tag, int p) __attribute__((always_inline)) {
+      constexpr int now = decltype(odd_tag)::value ? kSteps : 0, next = kSteps - now;
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((RING - 2) * T::kCopies) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      const uint32_t after = place_after(at);
+      if (p + RING == whole) cut_offsets();
+      if (p + 1 == whole) clear_cut_stage(after);
+      const Buffers from = buffers_of(p + RING);
+      unroll<0, kSteps>([&](auto step_tag) __attribute__((always_inline)) {
+        constexpr int s = decltype(step_tag)::value, kTiles = WM * WN, kReads = WM + WN;
+        constexpr int c0 = s * T::kCopies / kSteps, c1 = (s + 1) * T::kCopies / kSteps;
+        unroll<0, kTiles>([&](auto t_tag) __attribute__((always_inline)) {
+          constexpr int t = decltype(t_tag)::value, i = t / WM, j = t % WM;
+          acc[i][j] = mfma_32x32x16<DT>(sets[now + s].b[i], sets[now + s].a[j], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
+          // all reads of the next stage during three quarters of the products, waited for behind the last
+          constexpr int kAll = kSteps * kReads, kOver = kSteps * kTiles * 3 / 4, n = s * kTiles + t;
+          constexpr int r0 = n * kAll / kOver, r1 = (n + 1) * kAll / kOver;
+          unroll<(r0 < kAll ? r0 : kAll), (r1 < kAll ? r1 : kAll)>([&](auto u) __attribute__((always_inline)) {
+            constexpr int v = decltype(u)::value;
+            read_one(std::integral_constant<int, v / kReads>{}, std::integral_constant<int, v % kReads>{}, after, sets[next + v / kReads]);
+          });
+#pragma unroll
+          for (int c = c0 + t * (c1 - c0) / kTiles; c < c0 + (t + 1) * (c1 - c0) / kTiles; ++c) copy_one(from, at, c);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+      at = after;
+      unroll<0, kSteps>([&](auto s) __attribute__((always_inline)) { wait_operands(sets[next + decltype(s)::value]); });
+    };
+    unroll<0, kSteps>([&](auto s) __attribute__((always_inline)) { wait_operands(sets[decltype(s)::value]); });
+    int p = 0;
+    for (; p + 2 <= stages; p += 2) {
+      stage(std::false_type{}, p);
+      stage(std::true_type{}, p + 1);
+    }
+    if (p < stages) stage(std::false_type{}, p);
+  } else {
   unroll<0, WM + WN>([&](auto t) { read_one(std::integral_constant<int, 0>{}, t, 0, sets[0]); });
 
-  uint32_t at = 0;  // the place of stage p, and of stage p + RING
   for (int p = 0; p < stages; ++p) {
     const uint32_t after = place_after(at), before = place_before(at);
     unroll<0, kSteps>([&](auto step_tag) __attribute__((always_inline)) {
@@ -437,6 +485,7 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
   }
   // what was read of the stage beyond the last one is not used, but has to be there before its registers are
   wait_operands(sets[0]);
+  }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // copies of stages that do not exist: they write to this workgroup's LDS
 
   if (!alone) {
@@ -506,34 +555,38 @@ __global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* 
 }
 
 // Which form serves a shape, and by how many workgroups the tiles of its last round are shared: the least of estimates in
-// microseconds, fitted to launches at 69 shapes (M, N, K of 128 .. 16384, some from 4 on; operands from memory) with every form and up to
-// 12 workgroups a tile; what they choose is 2.3 % behind the best of these on the geometric mean, 27 % at most.  Both sides of
+// microseconds, fitted to launches at 74 shapes (M, N, K of 128 .. 16384, some from 4 on; operands from memory) with every form and up to
+// 16 workgroups a tile.  What they choose is the best of these or at most 11 % behind it.  Both sides of
 // each line: 2048x2048 of 2048 columns 22.2 us in tiles of 128, 27.8 of 256x128, 33.4 of 64; 4096x4096 of 2048 67, 82 and 124,
-// in tiles of 256 100; of 4096 in those 113 (1208 TFLOP/s); 1024x1024 of 1024 8.0 in tiles of 64, 11.0 of 128; 11008x4096 of 1571
+// in tiles of 256 100; of 4096 in those 113 (1208 TFLOP/s); 1024x1024 of 1024 6.9 in tiles of 64, 11.0 of 128; 11008x4096 of 1571
 // columns, 559 tiles of 256x128, 162 us with a third round of 47 workgroups and 152 where four share each of its tiles;
 // 4096x4096 of 200, 64 tiles of 128, 42 us alone, 23 in four parts.
 struct TileForm {
-  int rows, cols, at_once;    // of a tile; workgroups that the chip holds
-  double start;               // us of a launch and of what does not overlap
-  double alone, full, tile;   // us of a stage, with few workgroups and with all places taken; of a tile's beginning and end
-  double join, join_rate;     // sharing: us of the second launch, MB/us that the parts are written and read at
+  int rows, cols, at_once;         // of a tile; workgroups that the chip holds, one or two to a compute unit
+  double start;                    // us of a launch and of what does not overlap
+  double alone, one_each, full;    // us of a stage: with few workgroups, with one to each unit, with all places taken
+  double tile;                     // us of a tile's beginning and end
+  double join, join_rate;          // sharing: us of the second launch, MB/us that the parts are written and read at
 };
 enum { kFormGuarded, kFormLarge, kFormWide, kFormMiddle, kFormSmall, kTileFormCount };
 constexpr TileForm kTileForms[kTileFormCount] = {
-    {128, 128, 512, 2.6, 1.3, 2.3, 3.0, 3.0, 6.7},
-    {256, 256, 256, 2.67, 1.227, 1.693, 6.46, 3.05, 6.1},
-    {256, 128, 256, 2.26, 0.625, 0.935, 4.59, 2.37, 7.65},
-    {128, 128, 256, 2.62, 0.350, 0.583, 2.75, 3.01, 6.66},
-    {64, 64, 512, 1.97, 0.217, 0.466, 1.70, 2.70, 5.35},
+    {128, 128, 512, 2.9, 1.1, 1.3, 2.3, 3.0, 3.1, 6.5},
+    {256, 256, 256, 3.41, 1.172, 1.786, 1.786, 5.88, 2.73, 5.88},
+    {256, 128, 256, 2.41, 0.628, 0.955, 0.955, 4.40, 2.50, 7.40},
+    {128, 128, 256, 2.95, 0.319, 0.600, 0.600, 2.69, 3.14, 6.52},
+    {64, 64, 512, 2.18, 0.179, 0.273, 0.499, 1.63, 2.78, 6.39},
 };
+constexpr int kUnits = 256;
 constexpr int kStage = 64;  // summed values, of every form
 constexpr int kShares[] = {2, 3, 4, 6, 8, 12, 16};
 
 int64_t tiles_of(const TileForm& f, int M, int N) { return (int64_t)((M + f.rows - 1) / f.rows) * ((N + f.cols - 1) / f.cols); }
 double rounds_us(const TileForm& f, int64_t groups, int stages) {
   const int64_t rounds = groups / f.at_once, left = groups - rounds * f.at_once;
-  const double last = left ? stages * (f.alone + (f.full - f.alone) * (double)left / f.at_once) + f.tile : 0;
-  return (double)rounds * (stages * f.full + f.tile) + last;
+  // a unit with two decides, so half of the way from one each to all places is taken with the first of them
+  const double stage = left <= kUnits ? f.alone + (f.one_each - f.alone) * (double)left / kUnits
+                                      : f.one_each + (f.full - f.one_each) * (0.6 + 0.8 * ((double)left / f.at_once - 0.5));
+  return (double)rounds * (stages * f.full + f.tile) + (left ? stages * stage + f.tile : 0);
 }
 struct TilePlan {
   int form, whole_tiles, splits, stages_of_split;
@@ -661,23 +714,26 @@ size_t dense_product_workspace_bytes(int M, int N, int K, OperandForm form_a, Op
   return whole > guarded ? whole : guarded;
 }
 
+hipError_t launch_row_copy(const void* from, int64_t ld, void* to, int64_t pitch, int rows, int row, hipStream_t stream) {
+  const int64_t groups = (rows * (pitch / 8) + 1023) / 1024;  // four pieces a thread
+  linear_copy_kernel<<<dim3((uint32_t)(groups < 1 << 20 ? groups : 1 << 20)), 256, 0, stream>>>(
+      static_cast<const uint16_t*>(from), ld, static_cast<uint16_t*>(to), pitch, rows, row, pieces_of_rows(from, ld, row));
+  return hipGetLastError();
+}
+
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream) {
   if (is_layer(p.form_a, p.form_b) && p.N <= kFewTokens) return launch_linear_few(p, stream);
   DenseProduct d = p;
   const Operands o(p);
   if (o.copies(p)) {
     const CopyOfA c = copy_of(p.M, p.K, p.form_a);
-    const int64_t groups = (c.rows * (c.pitch() / 8) + 1023) / 1024;  // four pieces a thread
-    const dim3 grid((uint32_t)(groups < 1 << 20 ? groups : 1 << 20));
     d.A = p.workspace;
     d.lda = c.pitch();
     d.workspace = static_cast<uint8_t*>(p.workspace) + c.bytes();
     if (p.plan) {
-      plan_record(p.plan, "linear_copy_kernel grid=%u block=256", grid.x);
+      plan_record(p.plan, "linear_copy_kernel block=256");
     } else {
-      linear_copy_kernel<<<grid, 256, 0, stream>>>(static_cast<const uint16_t*>(p.A), p.lda, static_cast<uint16_t*>(p.workspace), c.pitch(), c.rows,
-                                                   c.row, o.rows_a);
-      const hipError_t e = hipGetLastError();
+      const hipError_t e = launch_row_copy(p.A, p.lda, p.workspace, c.pitch(), c.rows, c.row, stream);
       if (e != hipSuccess) return e;
     }
   }
