@@ -2,14 +2,21 @@
 
     h = a x + gate . norm(layers(u)) w_post        u_next = norm(h) w_next
 
-Layers come in either compressed form: prepared HiNM layers (`Layer`, run by hinm_chain) or 4-bit ones (`Mx4Layer`, run by
-hinm_mx4_linear).  This module holds buffers and hands arrays from one call to the next; everything that is computed runs in
+Layers come in either compressed form, prepared HiNM layers (`Layer`, run by hinm_chain) or 4-bit ones (`Mx4Layer`, run by
+hinm_mx4_linear), or as they were before (`DenseLayer`, run by hinm_linear, with bias and activation).  This module holds buffers
+and hands arrays from one call to the next; everything that is computed runs in
 the library's kernels, on the current stream.  PyTorch is used for device memory only.
 
     up, down = mx4_layer(W_up, flags=hb.EPI_RELU), mx4_layer(W_down)
     block = FeedForward([up, down], tokens, w_post, w_next=w_next_block)
     u = block_input(x, w_pre, tokens)
     x, u = block(x, u)            # and on to the next block with these
+
+An encoder's block with a layer norm ahead of it, for inference and for a training step (dense layers):
+
+    ffn = LayerNormFeedForward([dense_layer(W_up, b_up, hb.EPI_GELU), dense_layer(W_down, b_down)], tokens, w, b)
+    h = ffn(x)                                  # x + down(gelu(up(layer_norm(x))))
+    dx, gradients = ffn.backward(x, dh)
 """
 from __future__ import annotations
 
@@ -29,6 +36,17 @@ class Mx4Layer:
     dtype: object
     codes: torch.Tensor
     scales: torch.Tensor
+    flags: int = 0
+
+
+@dataclass
+class DenseLayer:
+    """16-bit weights [M][K] in rows of any pitch, a float32 bias [M] or none; flags as for hinm_linear (an activation)."""
+    M: int
+    K: int
+    dtype: object
+    W: torch.Tensor
+    bias: Optional[torch.Tensor] = None
     flags: int = 0
 
 
@@ -83,6 +101,19 @@ def mx4_layer(W: torch.Tensor, flags: int = 0) -> Mx4Layer:
     return Mx4Layer(M, K, W.dtype, codes, scales, flags)
 
 
+_ACTIVATIONS = (0, hb.EPI_RELU, hb.EPI_GELU, hb.EPI_GELU_TANH, hb.EPI_SILU)
+
+
+def dense_layer(W: torch.Tensor, bias: Optional[torch.Tensor] = None, flags: int = 0) -> DenseLayer:
+    """A layer of the weights as they are (kept, not copied); flags: one activation or none."""
+    _row_pitch(W, "weights")
+    M, K = W.shape
+    _factors(bias, "bias", M, W.device)
+    if flags not in _ACTIVATIONS:
+        raise ValueError(f"flags: one activation or none wanted, not {flags:#x}")
+    return DenseLayer(M, K, W.dtype, W, bias, flags)
+
+
 def mx4_linear_grad(W: torch.Tensor, X: torch.Tensor, dY: torch.Tensor, tokens: Optional[int] = None,
                     want_input: bool = True, want_weights: bool = True):
     """Gradients of Y = W X where every product is taken on 4-bit operands, each quantised along the axis that is summed over
@@ -132,20 +163,29 @@ def block_input(x: torch.Tensor, w_pre: torch.Tensor, tokens: int, eps: float = 
     return u
 
 
+def _check_layers(layers: Sequence[DenseLayer], device) -> None:
+    """What the library cannot see of dense layers: their arrays' shapes, types and places."""
+    for l in layers:
+        _row_pitch(l.W, "weights")
+        if list(l.W.shape) != [l.M, l.K] or l.W.dtype != _TORCH_DTYPE[hb._dtype_code(l.dtype)] or l.W.device != device:
+            raise ValueError(f"weights: {l.dtype} [{l.M}][{l.K}] on {device} wanted, not {l.W.dtype} {list(l.W.shape)} on {l.W.device}")
+        _factors(l.bias, "bias", l.M, device)
+
+
 class FeedForward:
     """One block for a fixed number of tokens: its layers, norms and buffers.
 
     x is [K][>= tokens] in rows of any pitch, u [K][>= tokens] in rows of leading_dimension(tokens), which is the pitch of the
     block's own buffers too; both of the layers' type, on the block's device.  Other arrays raise ValueError."""
 
-    def __init__(self, layers: Sequence[Union[Mx4Layer, hb.Layer]], tokens: int, w_post: Optional[torch.Tensor],
+    def __init__(self, layers: Sequence[Union[Mx4Layer, DenseLayer, hb.Layer]], tokens: int, w_post: Optional[torch.Tensor],
                  gate: Optional[torch.Tensor] = None, w_next: Optional[torch.Tensor] = None, residual_scale: float = 1.0,
                  eps: float = 1e-6, device="cuda"):
         layers = list(layers)
         if not layers or any(a.M != b.K for a, b in zip(layers, layers[1:])) or layers[-1].M != layers[0].K:
             raise ValueError("layers must follow one another and lead back to the block's channels")
-        self.in_4_bits = all(isinstance(l, Mx4Layer) for l in layers)
-        if not self.in_4_bits and any(isinstance(l, Mx4Layer) for l in layers):
+        self.in_4_bits, self.dense = (all(isinstance(l, form) for l in layers) for form in (Mx4Layer, DenseLayer))
+        if not (self.in_4_bits or self.dense) and any(isinstance(l, (Mx4Layer, DenseLayer)) for l in layers):
             raise ValueError("one block's layers come in one form")
         if len({hb._dtype_code(l.dtype) for l in layers}) > 1:
             raise ValueError("one block's layers have one type")
@@ -161,9 +201,13 @@ class FeedForward:
             for t, n in zip((l.codes, l.scales), hb.hinm_mx4_sizes(l.M, l.K)):
                 if t.dtype != torch.uint8 or t.numel() < n or not t.is_contiguous() or t.device != self.y.device:
                     raise ValueError(f"weights: {n} bytes on {self.y.device} wanted, not {t.dtype} {list(t.shape)} on {t.device}")
-        if self.in_4_bits:
+        if self.dense:
+            _check_layers(layers, self.y.device)
+            self.ldw = [_row_pitch(l.W, "weights") for l in layers]
+        if self.in_4_bits or self.dense:
             self.between = [new(l.M) for l in layers[:-1]]
-            self.scratch_bytes = max(hb.hinm_mx4_linear_workspace(l.M, l.K, tokens) for l in layers)
+            bytes_of = hb.hinm_mx4_linear_workspace if self.in_4_bits else hb.hinm_linear_workspace
+            self.scratch_bytes = max(bytes_of(l.M, l.K, tokens) for l in layers)
         else:
             self.scratch_bytes = hb.hinm_chain_sizes(layers, tokens)
         self.scratch = _workspace(self.scratch_bytes, device)
@@ -175,6 +219,12 @@ class FeedForward:
         N, ld = self.tokens, self.ld
         if _pitch(u, "u", N, self.K, self.y.dtype, self.y.device) != ld:
             raise ValueError(f"u: rows of {ld} = leading_dimension({N}) values wanted, not strides {u.stride()}")
+        if self.dense:
+            for l, ldw, out in zip(self.layers, self.ldw, self.between + [self.y]):
+                hb.hinm_linear(l.M, l.K, N, l.dtype, l.W, ldw, u, ld, l.bias, None, 0, None, out, ld, l.flags, self.scratch,
+                               self.scratch_bytes)
+                u = out
+            return u
         if not self.in_4_bits:
             hb.hinm_chain(self.layers, N, u, ld, self.y, ld, self.scratch, self.scratch_bytes)
             return self.y
@@ -192,3 +242,95 @@ class FeedForward:
         hb.hinm_block_norm(self.K, self.tokens, self.dtype, self.residual_scale, self.eps, x, y, self.w_post, self.gate,
                            token_gate, self.w_next, x, ld_stream, u, self.ld, None, None, self.norm_workspace, self.norm_bytes)
         return x, u
+
+
+class LayerNormFeedForward:
+    """h = x + layers(layer_norm(x) w + b) for a fixed number of tokens, and its gradients: dense layers, buffers of one step.
+
+    x and dh are [K][>= tokens] in rows of one pitch, of the layers' type on the block's device; other arrays raise ValueError.  A
+    step of training is a call and then `backward` with the same x; h, dx and the gradients are the block's own buffers, which its
+    next call or backward pass overwrites."""
+
+    def __init__(self, layers: Sequence[DenseLayer], tokens: int, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
+                 eps: float = 1e-5, device="cuda"):
+        layers = list(layers)
+        if not layers or not all(isinstance(l, DenseLayer) for l in layers):
+            raise ValueError("dense layers wanted")
+        if any(a.M != b.K for a, b in zip(layers, layers[1:])) or layers[-1].M != layers[0].K:
+            raise ValueError("layers must follow one another and lead back to the block's channels")
+        if len({hb._dtype_code(l.dtype) for l in layers}) > 1:
+            raise ValueError("one block's layers have one type")
+        if layers[-1].flags:
+            raise ValueError("the last layer leads back to the stream: without an activation")
+        self.layers, self.tokens, self.ld, self.eps = layers, tokens, leading_dimension(tokens), eps
+        self.K, self.dtype = layers[0].K, layers[0].dtype
+        self.w, self.b = w, b
+        new = lambda rows: torch.empty((rows, self.ld), dtype=_TORCH_DTYPE[hb._dtype_code(self.dtype)], device=device)
+        f32 = lambda n: torch.empty(n, dtype=torch.float32, device=device)
+        self.u = new(self.K)
+        self.device = self.u.device
+        _check_layers(layers, self.device)
+        for what, t in (("w", w), ("b", b)):
+            _factors(t, what, self.K, self.device)
+        self.h, self.mean, self.rstd = new(self.K), f32(tokens), f32(tokens)
+        self.Z = [new(l.M) if l.flags else None for l in layers]
+        self.out = [new(l.M) for l in layers[:-1]]
+        sizes = [hb.hinm_linear_workspace(l.M, l.K, tokens) for l in layers] + [hb.hinm_layer_norm_workspace(self.K, tokens)]
+        self.scratch_bytes = max(sizes)
+        self.scratch = _workspace(self.scratch_bytes, device)
+        self.ldw = [_row_pitch(l.W, "weights") for l in layers]
+        self._backward = self._dx_buffer = None
+
+    def __call__(self, x: torch.Tensor, train: bool = True) -> torch.Tensor:
+        """h, in the block's own buffer; with `train` what `backward` needs is kept."""
+        N, ld, ws = self.tokens, self.ld, (self.scratch, self.scratch_bytes)
+        ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
+        hb.hinm_layer_norm(self.K, N, self.dtype, self.eps, x, ldx, self.w, self.b, self.u, ld, self.mean, self.rstd, *ws)
+        into = self.u
+        for l, ldw, z, out in zip(self.layers, self.ldw, self.Z, self.out + [self.h]):
+            last = out is self.h
+            hb.hinm_linear(l.M, l.K, N, l.dtype, l.W, ldw, into, ld, l.bias, x if last else None, ldx, z if train else None, out,
+                           ld, l.flags, *ws)
+            into = out
+        return self.h
+
+    def backward(self, x: torch.Tensor, dh: torch.Tensor):
+        """(dx, gradients): of x, in rows of its pitch; of every layer's W (its type, contiguous) and bias, and of the norm's
+        w and b, as a dict of tensors "W0", "bias0", ..., "w", "b" (no entry for what the block does not have)."""
+        N, ld = self.tokens, self.ld
+        ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
+        if _pitch(dh, "dh", N, self.K, self.u.dtype, self.device) != ldx:
+            raise ValueError(f"dh: rows of x's pitch {ldx} wanted, not strides {dh.stride()}")
+        if self._backward is None:
+            new = lambda rows, cols: torch.empty((rows, cols), dtype=self.u.dtype, device=self.device)
+            f32 = lambda n: torch.empty(n, dtype=torch.float32, device=self.device)
+            g = {}
+            for i, l in enumerate(self.layers):
+                g[f"W{i}"] = new(l.M, l.K)
+                if l.bias is not None:
+                    g[f"bias{i}"] = f32(l.M)
+            for what, t in (("w", self.w), ("b", self.b)):
+                if t is not None:
+                    g[what] = f32(self.K)
+            nbytes = max([hb.hinm_linear_grad_workspace(l.M, l.K, N) for l in self.layers] + [hb.hinm_layer_norm_grad_workspace(self.K, N)])
+            self._backward = g, [new(l.K, ld) for l in self.layers], (_workspace(nbytes, self.device), nbytes)
+        g, into, ws = self._backward
+        dy, ldy = dh, ldx
+        for i, l in reversed(list(enumerate(self.layers))):
+            X = self.out[i - 1] if i else self.u
+            ldw = self.ldw[i]
+            # dX and dW take the pitch of X and W
+            dW = g[f"W{i}"] if ldw == l.K else None
+            hb.hinm_linear_grad(l.M, l.K, N, l.dtype, l.W, ldw, X, ld, self.Z[i], dy, ldy, into[i], dW, g.get(f"bias{i}"), l.flags, *ws)
+            if dW is None:
+                hb.hinm_linear_grad(l.M, l.K, N, l.dtype, None, l.K, X, ld, self.Z[i], dy, ldy, None, g[f"W{i}"], None, l.flags, *ws)
+            dy, ldy = into[i], ld
+        dx = self._dx(ldx)
+        hb.hinm_layer_norm_grad(self.K, N, self.dtype, x, ldx, self.w, self.mean, self.rstd, into[0], ld, dh, dx, g.get("w"), g.get("b"), *ws)
+        return dx, g
+
+    def _dx(self, ldx: int) -> torch.Tensor:
+        """dx's buffer, in rows of x's pitch as the norm's gradients have it."""
+        if self._dx_buffer is None or self._dx_buffer.shape[1] != ldx:
+            self._dx_buffer = torch.empty((self.K, ldx), dtype=self.u.dtype, device=self.device)
+        return self._dx_buffer
