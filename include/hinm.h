@@ -480,8 +480,8 @@ hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float resi
  * NaN), _GELU, _GELU_TANH or _SILU.  bias, residual and Z may be NULL: none, none, not wanted.  Z and Y have
  * leading dimension ldy.  residual may be Y with ldr = ldy (the sum in place) unless HINM_OUT_F32; apart from
  * that outputs must not overlap inputs or each other.  Sums in a fixed order: the same call gives the same
- * bits.  Sizes above 2^30 and products of more than some 2^22 workgroups (64 x 64 results each) return
- * HINM_ERR_UNSUPPORTED.  workspace: hinm_linear_workspace bytes, 256-byte aligned; where that is 0 it may be NULL. */
+ * bits.  Sizes above 2^30, products of 2^22 workgroups (64 x 64 results each) or more, and more than some 2^26
+ * rows M of at most 16 tokens return HINM_ERR_UNSUPPORTED.  workspace: hinm_linear_workspace bytes, 256-byte aligned; where that is 0 it may be NULL. */
 hinm_status hinm_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw, const void* X,
                         int64_t ldx, const float* bias, const void* residual, int64_t ldr, void* Z, void* Y,
@@ -520,7 +520,8 @@ hinm_status hinm_layer_norm(int32_t K, int32_t N, int32_t dtype, float eps, cons
  * dh [K][N], the gradient that reaches x beside the norm (a residual stream's), may be NULL: none.  dx, dw and db
  * (float32 [K], overwritten) may be NULL where they are not wanted (one of them is).  dh and dx have leading
  * dimension ldx, du ldu.  dx may be dh, or du with ldu = ldx; apart from that outputs must not overlap inputs.  Sums in
- * fp32 in a fixed order.  workspace: hinm_layer_norm_grad_workspace bytes, 256-byte aligned; where few channels or
+ * fp32 in a fixed order.  dw and db of more than 64 tokens and some 2^27 channels return HINM_ERR_UNSUPPORTED.
+ * workspace: hinm_layer_norm_grad_workspace bytes, 256-byte aligned; where few channels or
  * tokens need 0, it may be NULL. */
 hinm_status hinm_layer_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_layer_norm_grad(int32_t K, int32_t N, int32_t dtype, const void* x, int64_t ldx, const float* w,

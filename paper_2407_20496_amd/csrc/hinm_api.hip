@@ -121,7 +121,11 @@ hinm_status check_dense(int32_t M, int32_t K, int32_t N) {
   if (M > kMostSize || K > kMostSize || N > kMostSize) return HINM_ERR_UNSUPPORTED;
   return (int64_t)((M + 63) / 64) * ((N + 63) / 64) >= kMostGroups ? HINM_ERR_UNSUPPORTED : HINM_OK;
 }
-// ... of a layer's three products
+// ... of a layer forward, whose few tokens have workgroups of 16 rows and up to 1024 threads; a launch has less than 2^32 threads
+hinm_status check_layer(int32_t M, int32_t K, int32_t N) {
+  return N <= kFewTokens && M / 16 >= kMostGroups - 8 ? HINM_ERR_UNSUPPORTED : check_dense(M, K, N);
+}
+// ... of a layer's gradients
 hinm_status check_dense_grad(int32_t M, int32_t K, int32_t N) {
   const hinm_status st = check_dense(K, M, N);
   return st != HINM_OK ? st : check_dense(M, N, K);
@@ -873,7 +877,7 @@ hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float resi
 
 hinm_status hinm_linear_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes) {
   if (!workspace_bytes) return HINM_ERR_NULL;
-  const hinm_status st = check_dense(M, K, N);
+  const hinm_status st = check_layer(M, K, N);
   if (st != HINM_OK) return st;
   *workspace_bytes = dense_product_workspace_bytes(M, N, K, kAlong, kAcross);
   return HINM_OK;
@@ -883,7 +887,7 @@ hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const vo
                         const float* bias, const void* residual, int64_t ldr, void* Z, void* Y, int64_t ldy, uint32_t flags,
                         void* workspace, size_t workspace_bytes, void* stream) {
   if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
-  const hinm_status st = check_dense(M, K, N);
+  const hinm_status st = check_layer(M, K, N);
   if (st != HINM_OK) return st;
   if (!W || !X || !Y) return HINM_ERR_NULL;
   const bool out_f32 = (flags & HINM_OUT_F32) != 0;
@@ -956,7 +960,7 @@ hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtyp
   if (!text || text_bytes == 0) return HINM_ERR_NULL;
   text[0] = 0;
   if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
-  const hinm_status st = which == 0 ? check_dense(M, K, N) : check_dense_grad(M, K, N);
+  const hinm_status st = which == 0 ? check_layer(M, K, N) : check_dense_grad(M, K, N);
   if (st != HINM_OK) return st;
   if (which < 0 || which > 2) return HINM_ERR_UNSUPPORTED;
   LaunchPlan plan{text, text_bytes};
@@ -1013,7 +1017,7 @@ hinm_status hinm_layer_norm_grad(int32_t K, int32_t N, int32_t dtype, const void
   for (const float* p : {w, mean, rstd, const_cast<const float*>(dw), const_cast<const float*>(db)})
     if (!aligned(p, 4)) return HINM_ERR_SHAPE;
   // channels' gradients of several strips of tokens are added by workgroups of 1024 threads, 32 channels each
-  if (K >= 32 * kMostGroups && N > 64 && (dw || db)) return HINM_ERR_UNSUPPORTED;
+  if (K > 32 * (kMostGroups - 1) && N > 64 && (dw || db)) return HINM_ERR_UNSUPPORTED;
   const size_t need = layer_norm_grad_workspace_bytes(K, N);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
   return launched(launch_layer_norm_grad({K, N, dtype, x, ldx, w, mean, rstd, du, ldu, dh, dx, dw, db, static_cast<float*>(workspace)},

@@ -104,3 +104,18 @@ def test_python_calls_raise_with_the_status():
     with pytest.raises(hinm.HinmError) as e:
         hinm.hinm_linear((1 << 32) + 16, 64, 8, "bf16", P, 64, P, 8, None, None, 0, None, P, 8, stream=1)
     assert e.value.status == UNSUPPORTED
+
+
+def test_a_launch_has_less_than_32_bits_of_threads():
+    """Few tokens have 16 rows a workgroup, of up to 1024 threads; channels' gradients 32 channels a workgroup of as many."""
+    lib, n = hinm.load_library(), C.c_size_t(0)
+    most = 16 * ((1 << 22) - 8) - 1
+    assert -(-most // 16) * 1024 < 1 << 32
+    for tokens in (1, 16):
+        assert lib.hinm_linear_workspace(most, 1, tokens, C.byref(n)) == OK
+        for M in (most + 1, 1 << 26, (1 << 28) - 64):
+            assert lib.hinm_linear_workspace(M, 1, tokens, C.byref(n)) == UNSUPPORTED
+            assert lib.hinm_linear(M, 1, tokens, 1, P, 8, P, 16, None, None, 0, None, P, 16, 0, P, BIG, None) == UNSUPPORTED
+    assert lib.hinm_linear_workspace(1 << 26, 1, 17, C.byref(n)) == OK
+    K = (1 << 27) - 31
+    assert lib.hinm_layer_norm_grad(K, 65, 0, P, 72, P, P, P, P, 72, P, P, P, P, P, 1 << 60, None) == UNSUPPORTED
