@@ -482,14 +482,20 @@ __global__ __launch_bounds__(32 * kAdders) void layer_norm_grad_weights_kernel(L
   if (a.db) a.db[k] = of_b;
 }
 
-// Rounds of the forward kernel that holds all rows, or 0.
+// Rounds of the forward kernel that holds all rows, or 0.  One launch that reads x once, but only a workgroup to eight columns: us held |
+// in strips, 512x64 4.4 | 5.8, 1024x256 4.8 | 5.9, 1024x2048 7.1 | 7.3, 768x4096 8.5 | 8.0, 512x8000 11.2 | 9.1; of four rounds 2048x128
+// 5.9 | 6.5, 2048x512 6.5 | 6.3; of eight 4096x17 7.1 | 7.8, 4096x64 11.3 | 7.5.
 int rounds_held(int K, int N) {
-  if (K <= 2 * kHeldThreads && (int64_t)K * N <= 3 << 20) return 2;
+  if (K <= 2 * kHeldThreads) return (int64_t)K * N <= 2 << 20 ? 2 : 0;
+  if (K <= 4 * kHeldThreads) return N <= 256 ? 4 : 0;
   return K <= 8 * kHeldThreads && N <= 16 ? 8 : 0;
 }
+// Backward, where a launch adds up the workgroups' shares of dw and db in either way: 512x64 6.4 | 7.4, 1024x256 7.3 | 9.4, 1024x2048
+// 11.6 | 12.6, 768x4096 14.1 | 14.9, 512x8000 19.5 | 16.1, 1024x8000 30.9 | 24.2; of four rounds 2048x32 8.4 | 7.5.  At most
+// eight columns have no shares.
 int grad_rounds_held(int K, int N) {
-  if (N <= 8) return K <= 2 * kHeldThreads ? 2 : K <= 4 * kHeldThreads ? 4 : 0;
-  return K <= 2 * kHeldThreads && N <= 4096 && (int64_t)K * N <= 3 << 18 ? 2 : 0;
+  if (K <= 2 * kHeldThreads) return (int64_t)K * N <= 3 << 20 ? 2 : 0;
+  return K <= 4 * kHeldThreads && N <= 8 ? 4 : 0;
 }
 
 template <int DT, Layout L>
@@ -519,6 +525,7 @@ hipError_t launch_forward(const LayerNorm& a, hipStream_t stream) {
   if (const int rounds = rounds_held(a.K, a.N)) {
     const dim3 held((uint32_t)(((a.N + 7) / 8 + 7) / 8 * 8));
     if (rounds == 2) layer_norm_held_kernel<DT, 2><<<held, kHeldThreads, 0, stream>>>(a);
+    else if (rounds == 4) layer_norm_held_kernel<DT, 4><<<held, kHeldThreads, 0, stream>>>(a);
     else layer_norm_held_kernel<DT, 8><<<held, kHeldThreads, 0, stream>>>(a);
     return hipGetLastError();
   }

@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 LAYOUTS = {"pieces": (0, 0), "lines": (None, 0), "odd": (3, 5), "close": (-1, 0)}
 # one channel, one token, vectors, columns held by one workgroup, strips; row ends of every kind
 SHAPES = [(1, 1), (1, 9), (9, 1), (4096, 1), (8000, 1), (16384, 1), (16390, 1), (20000, 1), (768, 7), (768, 130), (1024, 65), (4096, 16),
-          (4096, 17), (2048, 8), (2050, 8), (1100, 129), (5000, 63), (1025, 64), (3001, 200), (64, 5000)]
+          (4096, 17), (2048, 8), (2050, 8), (1100, 129), (5000, 63), (1025, 64), (3001, 200), (64, 5000),
+          (1500, 256), (2048, 41), (1024, 2048), (1024, 2049), (700, 4493), (4096, 5)]
 
 
 def _place(cols, layout):
