@@ -92,7 +92,7 @@ hinm_status hinm_calib_mid_plan(const hinm_shape* shape, int32_t N, int32_t form
 hinm_status hinm_calib_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t dtype, uint32_t flags, int32_t quantize, char* text,
                                 size_t text_bytes);
 
-/* The launches of a dense layer's product (which = 0), or of its gradients' products of the input (1) or the weights (2), as
+/* The launches of a dense layer's product (which = 0), or of its gradients' products of the input (1), the weights (2) or both (3), as
  * hinm_spmm_prepared_plan gives them, where the rows of the weights (2: of both operands) begin at multiples of 16 bytes or (aligned = 0) do not.
  * Launches nothing. */
 hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtype, int32_t which, int32_t aligned,

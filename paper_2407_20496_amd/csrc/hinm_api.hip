@@ -941,17 +941,20 @@ hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, con
   }
   const void* const g = dz ? dz : dY;
   const int64_t ldg = dz ? p.ldz : ldy;
-  if (e == hipSuccess && dX)
-    e = launch_dense_product({K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
-                              {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials}, s);
+  int64_t ldx_of_x = ldx;
   if (e == hipSuccess && dW && p.x && pieces_of_rows(X, ldx, N) != kAligned) {
     e = launch_row_copy(X, ldx, x_copy, p.ldz, K, N, s);
     X = x_copy;
-    ldx = p.ldz;
+    ldx_of_x = p.ldz;
   }
-  if (e == hipSuccess && dW)
-    e = launch_dense_product({M, K, N, dtype, kAlong, kAlong, g, ldg, X, ldx,
-                              {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials}, s);
+  if (e != hipSuccess) return launched(e);
+  const DenseProduct of_x{K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
+                          {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials};
+  const DenseProduct of_w{M, K, N, dtype, kAlong, kAlong, g, ldg, X, ldx_of_x,
+                          {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials};
+  if (dX && dW && launch_dense_pair(of_w, of_x, s, e)) return launched(e);
+  if (dX) e = launch_dense_product(of_x, s);
+  if (e == hipSuccess && dW) e = launch_dense_product(of_w, s);
   return launched(e);
 }
 
@@ -962,18 +965,23 @@ hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtyp
   if (!known_dtype(dtype)) return HINM_ERR_DTYPE;
   const hinm_status st = which == 0 ? check_layer(M, K, N) : check_dense_grad(M, K, N);
   if (st != HINM_OK) return st;
-  if (which < 0 || which > 2) return HINM_ERR_UNSUPPORTED;
+  if (which < 0 || which > 3) return HINM_ERR_UNSUPPORTED;
   LaunchPlan plan{text, text_bytes};
-  const void* const at = reinterpret_cast<void*>((uintptr_t{1} << 20) + (is_aligned ? 0 : 2));  // never dereferenced
+  const void* const aligned_at = reinterpret_cast<const void*>(uintptr_t{1} << 20);  // never dereferenced
+  const void* const at = reinterpret_cast<const void*>((uintptr_t{1} << 20) + (is_aligned ? 0 : 2));
   auto pitch = [](int32_t n) { return ((int64_t)n + 7) / 8 * 8; };
-  auto launch = [&](int32_t m, int32_t n, int32_t k, OperandForm a, OperandForm b) {
+  auto product = [&](int32_t m, int32_t n, int32_t k, OperandForm a, OperandForm b) {
     const LinearEpilogue to{m, n, nullptr, nullptr, 0, kAligned, nullptr, nullptr, pitch(n), kActNone, false};
-    const void* const aligned_at = reinterpret_cast<const void*>(uintptr_t{1} << 20);
-    return launch_dense_product({m, n, k, dtype, a, b, at, pitch(a == kAlong ? k : m), which == 2 ? at : aligned_at, pitch(b == kAlong ? k : n), to,
-                                 const_cast<void*>(aligned_at), &plan}, nullptr);
+    return DenseProduct{m, n, k, dtype, a, b, at, pitch(a == kAlong ? k : m), which == 2 ? at : aligned_at, pitch(b == kAlong ? k : n), to,
+                        const_cast<void*>(aligned_at), &plan};
   };
-  if (which == 0) return launched(launch(M, N, K, kAlong, kAcross));
-  return launched(which == 1 ? launch(K, N, M, kAcross, kAcross) : launch(M, K, N, kAlong, kAlong));
+  const DenseProduct of_x = product(K, N, M, kAcross, kAcross), of_w = product(M, K, N, kAlong, kAlong);
+  if (which == 0) return launched(launch_dense_product(product(M, N, K, kAlong, kAcross), nullptr));
+  hipError_t e = hipSuccess;
+  if (which == 3 && launch_dense_pair(of_w, of_x, nullptr, e)) return launched(e);
+  if (which != 2) e = launch_dense_product(of_x, nullptr);
+  if (which != 1 && e == hipSuccess) e = launch_dense_product(of_w, nullptr);
+  return launched(e);
 }
 
 hinm_status hinm_layer_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {

@@ -1,6 +1,9 @@
 // Dense products of two 16-bit matrices on the matrix cores, tiles through LDS (include/hinm.h, hinm_linear and its gradients).
 #include "linear_tile.h"
 
+#include <algorithm>
+#include <utility>
+
 #include "direct_lds.h"
 #include "lds_in_flight.h"
 #include "wave_reduce.h"
@@ -204,16 +207,15 @@ struct TilePlace {
 // waves, so stage p + 1 is there and the place of stage p takes stage p + RING: half of its copies during the last step of p, the
 // others during the first of p + 1.
 template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
-__global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile_kernel(TileArgs a, LinearEpilogue e) {
+__device__ __forceinline__ void multiply_tile(const TileArgs& a, const LinearEpilogue& e, int group, int groups) {
   using T = TileSizes<FA, FB, WM, WN, GM, GN, BK, RING>;
   constexpr int kSteps = BK / 16;
   extern __shared__ __align__(1024) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tiles = ((e.M + T::TM - 1) / T::TM) * ((e.N + T::TN - 1) / T::TN), shared = tiles - a.whole_tiles;
   const int whole_groups = (a.whole_tiles + 7) & ~7;
-  const bool alone = (int)blockIdx.x < whole_groups;
-  const int item = alone ? item_of(blockIdx.x, whole_groups, a.whole_tiles)
-                         : item_of(blockIdx.x - whole_groups, gridDim.x - whole_groups, shared * a.splits);
+  const bool alone = group < whole_groups;
+  const int item = alone ? item_of(group, whole_groups, a.whole_tiles) : item_of(group - whole_groups, groups - whole_groups, shared * a.splits);
   if (item < 0) return;
   const int split = alone ? 0 : item / shared, tile = alone ? item : a.whole_tiles + item - split * shared;
   const TilePlace place(tile, T::TM, T::TN, e.M, e.N);
@@ -519,6 +521,21 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
   else store(std::false_type{});
 }
 
+template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
+__global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile_kernel(TileArgs a, LinearEpilogue e) {
+  multiply_tile<DT, FA, FB, E, WM, WN, GM, GN, BK, RING, GUARDED>(a, e, blockIdx.x, gridDim.x);
+}
+
+// Both gradients of a layer in one launch: each fills a chip badly alone, and the beginning of one hides the other's end.  The product with
+// more stages has the first workgroups.
+template <int DT, int WM, int WN>
+__global__ __launch_bounds__(256, 2) void linear_pair_kernel(TileArgs w, LinearEpilogue to_w, TileArgs x, LinearEpilogue to_x, int first, bool w_first) {
+  const bool in_first = (int)blockIdx.x < first;
+  const int group = in_first ? blockIdx.x : blockIdx.x - first, groups = in_first ? first : gridDim.x - first;
+  if (in_first == w_first) multiply_tile<DT, kAlong, kAlong, kEpiBare, WM, WN, 2, 2, 64, 4, false>(w, to_w, group, groups);
+  else multiply_tile<DT, kAcross, kAcross, kEpiBare, WM, WN, 2, 2, 64, 4, false>(x, to_x, group, groups);
+}
+
 // Tiles that several workgroups have summed parts of: the parts added in order, 32 rows of every wave a workgroup.
 template <int DT, Epilogue E, int WM, int WN, int GM, int GN>
 __global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* partials, int whole_tiles, int splits, LinearEpilogue e) {
@@ -581,12 +598,15 @@ constexpr int kStage = 64;  // summed values, of every form
 constexpr int kShares[] = {2, 3, 4, 6, 8, 12, 16};
 
 int64_t tiles_of(const TileForm& f, int M, int N) { return (int64_t)((M + f.rows - 1) / f.rows) * ((N + f.cols - 1) / f.cols); }
+// of a stage with `groups` of at most f.at_once workgroups
+double stage_us(const TileForm& f, int64_t groups) {
+  // a unit with two decides, so half of the way from one each to all places is taken with the first of them
+  return groups <= kUnits ? f.alone + (f.one_each - f.alone) * (double)groups / kUnits
+                          : f.one_each + (f.full - f.one_each) * (0.6 + 0.8 * ((double)groups / f.at_once - 0.5));
+}
 double rounds_us(const TileForm& f, int64_t groups, int stages) {
   const int64_t rounds = groups / f.at_once, left = groups - rounds * f.at_once;
-  // a unit with two decides, so half of the way from one each to all places is taken with the first of them
-  const double stage = left <= kUnits ? f.alone + (f.one_each - f.alone) * (double)left / kUnits
-                                      : f.one_each + (f.full - f.one_each) * (0.6 + 0.8 * ((double)left / f.at_once - 0.5));
-  return (double)rounds * (stages * f.full + f.tile) + (left ? stages * stage + f.tile : 0);
+  return (double)rounds * (stages * f.full + f.tile) + (left ? stages * stage_us(f, left) + f.tile : 0);
 }
 struct TilePlan {
   int form, whole_tiles, splits, stages_of_split;
@@ -629,6 +649,39 @@ TilePlan plan_of(int M, int N, int K, bool guarded) {
   Kept& k = kept[((uint32_t)M * 2654435761u ^ (uint32_t)N * 2246822519u ^ (uint32_t)K * 3266489917u ^ (uint32_t)guarded) >> 26];
   if (k.M != M || k.N != N || k.K != K || k.guarded != guarded) k = Kept{M, N, K, guarded, find_plan(M, N, K, guarded)};
   return k.plan;
+}
+
+// Both gradients' products in one launch, no tiles shared: its form by estimates from the same table, or kFormGuarded where two launches
+// are sooner.  The longer workgroups begin, the shorter ones take the places beside them, and what is left of the longer ones goes on
+// with fewer on the chip.  us of two launches, of one in tiles of 128, in tiles of 64: 768x768 of 4096 columns 24.1, 24.8, 20.1, of 1000
+// 13.2, 13.4, 10.1; 256x256 of 64 6.9, 5.8, 3.8; 2304x768 of 512 13.9, 9.6, 10.5; 2048x2048 of 1024 29.8, 22.0, 29.9; 4096x4096 of 256
+// 43, 47, 49; 8192x128 of 512 16, 46, 29.  Of 33 such shapes the choice is the best or at most 7 % behind it.
+double pair_us(const TileForm& f, int M, int K, int N) {
+  int64_t longer = tiles_of(f, M, K), shorter = tiles_of(f, K, N);
+  int stages = (N + kStage - 1) / kStage, less = (M + kStage - 1) / kStage;
+  if (less > stages) {
+    std::swap(longer, shorter);
+    std::swap(stages, less);
+  }
+  const double stage = stage_us(f, std::min<int64_t>(longer + shorter, f.at_once));
+  const double long_us = stages * stage + f.tile, short_us = less * stage + f.tile;
+  if (longer < f.at_once) {
+    const double beside = short_us * std::max(1.0, (double)shorter / (double)(f.at_once - longer));
+    if (beside <= long_us) return f.start + beside + (long_us - beside) / stage * stage_us(f, longer);
+  }
+  return f.start + (longer * long_us + shorter * short_us) / f.at_once + 0.5 * short_us;
+}
+int pair_form(int M, int K, int N) {
+  int form = kFormGuarded;
+  double least = plan_of(M, K, N, false).us + plan_of(K, N, M, false).us;
+  for (int i : {kFormMiddle, kFormSmall}) {
+    const double us = pair_us(kTileForms[i], M, K, N);
+    if (us < least) {
+      least = us;
+      form = i;
+    }
+  }
+  return form;
 }
 size_t partial_bytes(const TilePlan& p, int M, int N) {
   const TileForm& f = kTileForms[p.form];
@@ -718,6 +771,32 @@ hipError_t launch_dtype(const DenseProduct& d, hipStream_t stream) {
   }
 }
 
+template <int DT, int WM, int WN>
+hipError_t launch_pair(const TileForm& f, const DenseProduct& w, const DenseProduct& x, hipStream_t stream) {
+  constexpr int kLds = TileSizes<kAlong, kAlong, WM, WN, 2, 2, 64, 4>::kLds;
+  static_assert(kLds == TileSizes<kAcross, kAcross, WM, WN, 2, 2, 64, 4>::kLds, "of either product");
+  auto args = [&](const DenseProduct& d) {
+    const int stages = (d.K + kStage - 1) / kStage;
+    return TileArgs{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, (int)tiles_of(f, d.M, d.N), 1, stages,
+                    kAligned, kAligned, nullptr};
+  };
+  const TileArgs of_w = args(w), of_x = args(x);
+  const bool w_first = w.K >= x.K;
+  const uint32_t groups_w = grid_of_items(of_w.whole_tiles), groups_x = grid_of_items(of_x.whole_tiles);
+  if (w.plan) {
+    plan_record(w.plan, "linear_pair_kernel<DT=%d,WM=%d,WN=%d> grid=%u block=256 lds=%d", DT, WM, WN, groups_w + groups_x, kLds);
+    return hipSuccess;
+  }
+  const hipError_t e = raise_lds_limit<linear_pair_kernel<DT, WM, WN>>(kLds);
+  if (e != hipSuccess) return e;
+  linear_pair_kernel<DT, WM, WN><<<groups_w + groups_x, 256, kLds, stream>>>(of_w, w.to, of_x, x.to, (int)(w_first ? groups_w : groups_x), w_first);
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_pair_of(int form, const DenseProduct& w, const DenseProduct& x, hipStream_t stream) {
+  return form == kFormMiddle ? launch_pair<DT, 2, 2>(kTileForms[form], w, x, stream) : launch_pair<DT, 1, 1>(kTileForms[form], w, x, stream);
+}
+
 }  // namespace
 
 size_t dense_product_workspace_bytes(int M, int N, int K, OperandForm form_a, OperandForm form_b) {
@@ -751,6 +830,15 @@ hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream) {
     }
   }
   return d.dtype == HINM_F16 ? launch_dtype<HINM_F16>(d, stream) : launch_dtype<HINM_BF16>(d, stream);
+}
+
+// dW [M][K] and dX [K][N] of one layer
+bool launch_dense_pair(const DenseProduct& w, const DenseProduct& x, hipStream_t stream, hipError_t& e) {
+  if (Operands(w).guarded() || Operands(x).guarded()) return false;
+  const int form = pair_form(w.M, w.N, w.K);
+  if (form == kFormGuarded) return false;
+  e = w.dtype == HINM_F16 ? launch_pair_of<HINM_F16>(form, w, x, stream) : launch_pair_of<HINM_BF16>(form, w, x, stream);
+  return true;
 }
 
 }  // namespace hinm

@@ -28,6 +28,10 @@ TILES = [
     (2, 271, 6551, 152, MIDDLE, False, True), (2, 334, 9756, 256, MIDDLE, False, True), (2, 11561, 134, 299, MIDDLE, False, True),
     (0, 4097, 4097, 600, MIDDLE, False, False), (1, 4097, 4097, 600, MIDDLE, False, False), (0, 700, 30, 1030, SMALL, False, False),
     (0, 31, 2500, 250, SMALL, True, False), (1, 5, 33, 300, SMALL, False, False)]
+# both gradients in one launch, of fewer and more workgroups than a chip holds; M, K, N; tiles of a wave
+PAIRS = [(21, 16, 64, SMALL), (64, 2697, 101, SMALL), (128, 687, 144, SMALL), (166, 178, 205, SMALL), (188, 3263, 3596, SMALL), (384, 573, 4603, SMALL),
+         (371, 4802, 64, SMALL), (106, 201, 9, SMALL), (2487, 2992, 9, SMALL), (282, 3880, 98, SMALL), (3615, 1628, 239, SMALL), (2752, 520, 840, SMALL),
+         (1, 1, 1, SMALL), (170, 4632, 1855, MIDDLE), (320, 3138, 3369, MIDDLE), (231, 5318, 167, MIDDLE), (4104, 5315, 195, MIDDLE), (2050, 2048, 1024, MIDDLE)]
 FEW = [(10300, 100, 9, 4), (10300, 200, 16, 4), (300, 1030, 16, 1), (257, 64, 2, 1)]
 
 
@@ -45,6 +49,15 @@ def test_few_tokens_reach_their_form(M, K, N, blocks):
     import paper_2407_20496_amd as hinm
     assert "linear_few_kernel" in hinm.hinm_calib_linear_plan(M, K, N, "f16") and "RB=%d," % blocks in hinm.hinm_calib_linear_plan(M, K, N, "f16")
     assert "PIECES=0" in hinm.hinm_calib_linear_plan(M, K, N, "f16", 0, False)
+
+
+@pytest.mark.parametrize("M,K,N,tiles", PAIRS)
+def test_both_gradients_reach_one_launch(M, K, N, tiles):
+    import paper_2407_20496_amd as hinm
+    text = hinm.hinm_calib_linear_plan(M, K, N, "bf16", 3)
+    assert text.startswith("linear_pair_kernel<") and "WM=%d,WN=%d>" % tiles in text and ";" not in text.strip("; \n"), text
+    apart = hinm.hinm_calib_linear_plan(4096, 4096, 2048, "bf16", 3)
+    assert "pair" not in apart and apart.count("linear_tile_kernel") == 2
 
 
 def _integers(rows, cols, gen, most=2):
@@ -80,3 +93,30 @@ def test_products_of_integers(which, M, K, N, aligned):
     torch.cuda.synchronize()
     assert torch.equal(out.view.double(), want)
     assert torch.equal(out.surroundings(), around)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", [False, True])
+@pytest.mark.parametrize("M,K,N", [p[:3] for p in PAIRS])
+def test_both_gradients_of_integers(M, K, N, act):
+    """With relu as the activation, whose slopes are 0 and 1; rows have numbers behind their ends that are no part of a sum."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    from tests.dense_util import Matrix, result, workspace
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(M + K + N)
+    dtype = ("f16", "bf16")[M % 2]
+    W, X, G, Z = _integers(M, K, gen), _integers(K, N, gen), _integers(M, N, gen), _integers(M, N, gen)
+    w, x, g, z = (Matrix(*v.shape, dtype, values=v) for v in (W, X, G, Z))
+    dx, dw, db = result(K, N, dtype), result(M, K, dtype), torch.full((M + 1,), 77.0, device="cuda:0")
+    around = dx.surroundings(), dw.surroundings()
+    hinm.hinm_linear_grad(M, K, N, dtype, w.data, w.ld, x.data, x.ld, z.data if act else None, g.data, g.ld, dx.data, dw.data, db,
+                          hinm.EPI_RELU if act else 0, *workspace(hinm.hinm_linear_grad_workspace(M, K, N)))
+    torch.cuda.synchronize()
+    if act:
+        G = torch.where(Z > 0, G, 0.0)
+    real = lambda v: v.to(w.kind).double()
+    assert torch.equal(torch.as_tensor(dx.f64(), device="cuda:0"), real(W.t().contiguous() @ G))
+    assert torch.equal(torch.as_tensor(dw.f64(), device="cuda:0"), real(G @ X.t().contiguous()))
+    assert torch.equal(db[:M].double(), G.sum(1)) and db[M].item() == 77.0
+    assert torch.equal(dx.surroundings(), around[0]) and torch.equal(dw.surroundings(), around[1])
