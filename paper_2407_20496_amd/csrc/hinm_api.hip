@@ -933,26 +933,23 @@ hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, con
   uint16_t* const dz = as_it_is || (!dX && !dW) ? nullptr : static_cast<uint16_t*>(workspace);
   uint8_t* const x_copy = static_cast<uint8_t*>(workspace) + p.dz;
   void* const partials = x_copy + p.x;
+  const void* const g = dz ? dz : dY;
+  const int64_t ldg = dz ? p.ldz : ldy;
+  const bool copied = dW && p.x && pieces_of_rows(X, ldx, N) != kAligned;
+  const DenseProduct of_x{K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
+                          {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials};
+  const DenseProduct of_w{M, K, N, dtype, kAlong, kAlong, g, ldg, copied ? x_copy : X, copied ? p.ldz : ldx,
+                          {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials};
+  const bool pair = dX && dW && dense_pair_serves(of_w, of_x), sums_in_pair = pair && dbias && !dz && M <= kMostGroups;
   hipError_t e = hipSuccess;
-  if (dz || dbias) {
+  if (dz || (dbias && !sums_in_pair)) {
     const void* z = act == kActNone ? nullptr : Z;
     e = launch_linear_slope({M, N, static_cast<const uint16_t*>(z), static_cast<const uint16_t*>(dY), ldy,
                              lesser(pieces_of_rows(z, ldy, N), pieces_of_rows(dY, ldy, N)), act, dz, p.ldz, dbias}, dtype, s);
   }
-  const void* const g = dz ? dz : dY;
-  const int64_t ldg = dz ? p.ldz : ldy;
-  int64_t ldx_of_x = ldx;
-  if (e == hipSuccess && dW && p.x && pieces_of_rows(X, ldx, N) != kAligned) {
-    e = launch_row_copy(X, ldx, x_copy, p.ldz, K, N, s);
-    X = x_copy;
-    ldx_of_x = p.ldz;
-  }
+  if (e == hipSuccess && copied) e = launch_row_copy(X, ldx, x_copy, p.ldz, K, N, s);
   if (e != hipSuccess) return launched(e);
-  const DenseProduct of_x{K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
-                          {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials};
-  const DenseProduct of_w{M, K, N, dtype, kAlong, kAlong, g, ldg, X, ldx_of_x,
-                          {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials};
-  if (dX && dW && launch_dense_pair(of_w, of_x, s, e)) return launched(e);
+  if (pair) return launched(launch_dense_pair(of_w, of_x, sums_in_pair ? dbias : nullptr, s));
   if (dX) e = launch_dense_product(of_x, s);
   if (e == hipSuccess && dW) e = launch_dense_product(of_w, s);
   return launched(e);
@@ -978,7 +975,7 @@ hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtyp
   const DenseProduct of_x = product(K, N, M, kAcross, kAcross), of_w = product(M, K, N, kAlong, kAlong);
   if (which == 0) return launched(launch_dense_product(product(M, N, K, kAlong, kAcross), nullptr));
   hipError_t e = hipSuccess;
-  if (which == 3 && launch_dense_pair(of_w, of_x, nullptr, e)) return launched(e);
+  if (which == 3 && dense_pair_serves(of_w, of_x)) return launched(launch_dense_pair(of_w, of_x, nullptr, nullptr));
   if (which != 2) e = launch_dense_product(of_x, nullptr);
   if (which != 1 && e == hipSuccess) e = launch_dense_product(of_w, nullptr);
   return launched(e);

@@ -491,10 +491,10 @@ int rounds_held(int K, int N) {
   return K <= 8 * kHeldThreads && N <= 16 ? 8 : 0;
 }
 // Backward, where a launch adds up the workgroups' shares of dw and db in either way: 512x64 6.4 | 7.4, 1024x256 7.3 | 9.4, 1024x2048
-// 11.6 | 12.6, 768x4096 14.1 | 14.9, 512x8000 19.5 | 16.1, 1024x8000 30.9 | 24.2; of four rounds 2048x32 8.4 | 7.5.  At most
-// eight columns have no shares.
+// 11.6 | 12.6, and with dh 12.8 | 13.1; 768x4096 14.4 | 15.0, but with dh 17.2 | 15.6; 1024x8000 30.9 | 24.2; of four rounds 2048x32
+// 8.4 | 7.5.  At most eight columns have no shares.
 int grad_rounds_held(int K, int N) {
-  if (K <= 2 * kHeldThreads) return (int64_t)K * N <= 3 << 20 ? 2 : 0;
+  if (K <= 2 * kHeldThreads) return (int64_t)K * N <= 2 << 20 ? 2 : 0;
   return K <= 4 * kHeldThreads && N <= 8 ? 4 : 0;
 }
 

@@ -24,8 +24,10 @@ struct DenseProduct {
 inline bool is_layer(OperandForm form_a, OperandForm form_b) { return form_a == kAlong && form_b == kAcross; }
 size_t dense_product_workspace_bytes(int M, int N, int K, OperandForm form_a, OperandForm form_b);  // a multiple of 256
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream);
-// w: dW = A B of a layer's gradients, x: its dX, in one launch; false where two are sooner, and nothing is launched
-bool launch_dense_pair(const DenseProduct& w, const DenseProduct& x, hipStream_t stream, hipError_t& e);
+// Of one layer's gradients w is the product dW [M][K], x dX [K][N]: whether one launch of both is sooner than two.  That launch also sums
+// the rows of w's A, as they are, to sums [M] unless it is NULL.
+bool dense_pair_serves(const DenseProduct& w, const DenseProduct& x);
+hipError_t launch_dense_pair(const DenseProduct& w, const DenseProduct& x, float* sums, hipStream_t stream);
 // rows of any pitch and address to rows of `pitch` (a multiple of 8) from an aligned address on, zeros behind them
 hipError_t launch_row_copy(const void* from, int64_t ld, void* to, int64_t pitch, int rows, int row, hipStream_t stream);
 // a layer's product (A along, B across) on up to kFewTokens tokens

@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <utility>
 
+#include "column_strips.h"
 #include "direct_lds.h"
 #include "lds_in_flight.h"
 #include "wave_reduce.h"
@@ -526,12 +527,46 @@ __global__ __launch_bounds__(64 * GM * GN, WM * WN > 8 ? 1 : 2) void linear_tile
   multiply_tile<DT, FA, FB, E, WM, WN, GM, GN, BK, RING, GUARDED>(a, e, blockIdx.x, gridDim.x);
 }
 
+// Sums of A's rows (whole pieces), a wave each.
+struct RowSums {
+  float* to;
+  int first;  // workgroup of the launch
+};
+template <int DT>
+__device__ __forceinline__ void add_rows(const TileArgs& a, int M, float* to, int group) {
+  const int lane = threadIdx.x & 63, m = 4 * group + (threadIdx.x >> 6);
+  if (m >= M) return;
+  constexpr int kAtOnce = 4;
+  const uint16_t* const row = a.A + m * a.lda;
+  float sum = 0;
+  for (int k0 = 8 * lane; k0 < a.K; k0 += 512 * kAtOnce) {
+    u32x4 v[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = k0 + 512 * i;
+      v[i] = k < a.K ? trim_eight(*reinterpret_cast<const u32x4*>(row + k), a.K - k, kAligned) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      float x[8];
+      widen<DT>(v[i], x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += x[j];
+    }
+  }
+  sum = add_lanes_by_8(add_eight_lanes(sum));
+  if (lane == 0) to[m] = sum;
+}
+
 // Both gradients of a layer in one launch: each fills a chip badly alone, and the beginning of one hides the other's end.  The product with
-// more stages has the first workgroups.
+// more stages has the first workgroups; the bias's gradient, where dZ is dY, the last ones (768x768 of 4096 columns: instead of a launch
+// of 3 to 4 us ahead).
 template <int DT, int WM, int WN>
-__global__ __launch_bounds__(256, 2) void linear_pair_kernel(TileArgs w, LinearEpilogue to_w, TileArgs x, LinearEpilogue to_x, int first, bool w_first) {
-  const bool in_first = (int)blockIdx.x < first;
-  const int group = in_first ? blockIdx.x : blockIdx.x - first, groups = in_first ? first : gridDim.x - first;
+__global__ __launch_bounds__(256, 2) void linear_pair_kernel(TileArgs w, LinearEpilogue to_w, TileArgs x, LinearEpilogue to_x, int first, bool w_first, RowSums sums) {
+  const int block = blockIdx.x;
+  if (block >= sums.first) return add_rows<DT>(w, to_w.M, sums.to, block - sums.first);
+  const bool in_first = block < first;
+  const int group = in_first ? block : block - first, groups = in_first ? first : sums.first - first;
   if (in_first == w_first) multiply_tile<DT, kAlong, kAlong, kEpiBare, WM, WN, 2, 2, 64, 4, false>(w, to_w, group, groups);
   else multiply_tile<DT, kAcross, kAcross, kEpiBare, WM, WN, 2, 2, 64, 4, false>(x, to_x, group, groups);
 }
@@ -772,7 +807,7 @@ hipError_t launch_dtype(const DenseProduct& d, hipStream_t stream) {
 }
 
 template <int DT, int WM, int WN>
-hipError_t launch_pair(const TileForm& f, const DenseProduct& w, const DenseProduct& x, hipStream_t stream) {
+hipError_t launch_pair(const TileForm& f, const DenseProduct& w, const DenseProduct& x, float* sums, hipStream_t stream) {
   constexpr int kLds = TileSizes<kAlong, kAlong, WM, WN, 2, 2, 64, 4>::kLds;
   static_assert(kLds == TileSizes<kAcross, kAcross, WM, WN, 2, 2, 64, 4>::kLds, "of either product");
   auto args = [&](const DenseProduct& d) {
@@ -783,18 +818,21 @@ hipError_t launch_pair(const TileForm& f, const DenseProduct& w, const DenseProd
   const TileArgs of_w = args(w), of_x = args(x);
   const bool w_first = w.K >= x.K;
   const uint32_t groups_w = grid_of_items(of_w.whole_tiles), groups_x = grid_of_items(of_x.whole_tiles);
+  const uint32_t tiles = groups_w + groups_x, rows = sums ? (uint32_t)((w.M + 3) / 4) : 0;
   if (w.plan) {
-    plan_record(w.plan, "linear_pair_kernel<DT=%d,WM=%d,WN=%d> grid=%u block=256 lds=%d", DT, WM, WN, groups_w + groups_x, kLds);
+    plan_record(w.plan, "linear_pair_kernel<DT=%d,WM=%d,WN=%d> grid=%u block=256 lds=%d", DT, WM, WN, tiles + rows, kLds);
     return hipSuccess;
   }
   const hipError_t e = raise_lds_limit<linear_pair_kernel<DT, WM, WN>>(kLds);
   if (e != hipSuccess) return e;
-  linear_pair_kernel<DT, WM, WN><<<groups_w + groups_x, 256, kLds, stream>>>(of_w, w.to, of_x, x.to, (int)(w_first ? groups_w : groups_x), w_first);
+  linear_pair_kernel<DT, WM, WN><<<tiles + rows, 256, kLds, stream>>>(of_w, w.to, of_x, x.to, (int)(w_first ? groups_w : groups_x), w_first, {sums, (int)tiles});
   return hipGetLastError();
 }
 template <int DT>
-hipError_t launch_pair_of(int form, const DenseProduct& w, const DenseProduct& x, hipStream_t stream) {
-  return form == kFormMiddle ? launch_pair<DT, 2, 2>(kTileForms[form], w, x, stream) : launch_pair<DT, 1, 1>(kTileForms[form], w, x, stream);
+hipError_t launch_pair_of(const DenseProduct& w, const DenseProduct& x, float* sums, hipStream_t stream) {
+  const int form = pair_form(w.M, w.N, w.K);
+  const TileForm& f = kTileForms[form];
+  return form == kFormMiddle ? launch_pair<DT, 2, 2>(f, w, x, sums, stream) : launch_pair<DT, 1, 1>(f, w, x, sums, stream);
 }
 
 }  // namespace
@@ -832,13 +870,11 @@ hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream) {
   return d.dtype == HINM_F16 ? launch_dtype<HINM_F16>(d, stream) : launch_dtype<HINM_BF16>(d, stream);
 }
 
-// dW [M][K] and dX [K][N] of one layer
-bool launch_dense_pair(const DenseProduct& w, const DenseProduct& x, hipStream_t stream, hipError_t& e) {
-  if (Operands(w).guarded() || Operands(x).guarded()) return false;
-  const int form = pair_form(w.M, w.N, w.K);
-  if (form == kFormGuarded) return false;
-  e = w.dtype == HINM_F16 ? launch_pair_of<HINM_F16>(form, w, x, stream) : launch_pair_of<HINM_BF16>(form, w, x, stream);
-  return true;
+bool dense_pair_serves(const DenseProduct& w, const DenseProduct& x) {
+  return !Operands(w).guarded() && !Operands(x).guarded() && pair_form(w.M, w.N, w.K) != kFormGuarded;
+}
+hipError_t launch_dense_pair(const DenseProduct& w, const DenseProduct& x, float* sums, hipStream_t stream) {
+  return w.dtype == HINM_F16 ? launch_pair_of<HINM_F16>(w, x, sums, stream) : launch_pair_of<HINM_BF16>(w, x, sums, stream);
 }
 
 }  // namespace hinm
