@@ -280,11 +280,13 @@ class LayerNormFeedForward:
         self.scratch = _workspace(self.scratch_bytes, device)
         self.ldw = [_row_pitch(l.W, "weights") for l in layers]
         self._backward = self._dx_buffer = None
+        self._kept = True
 
     def __call__(self, x: torch.Tensor, train: bool = True) -> torch.Tensor:
-        """h, in the block's own buffer; with `train` what `backward` needs is kept."""
+        """h, in the block's own buffer; with `train` what `backward` needs is kept, without it `backward` raises ValueError."""
         N, ld, ws = self.tokens, self.ld, (self.scratch, self.scratch_bytes)
         ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
+        self._kept = train
         hb.hinm_layer_norm(self.K, N, self.dtype, self.eps, x, ldx, self.w, self.b, self.u, ld, self.mean, self.rstd, *ws)
         into = self.u
         for l, ldw, z, out in zip(self.layers, self.ldw, self.Z, self.out + [self.h]):
@@ -301,6 +303,8 @@ class LayerNormFeedForward:
         ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
         if _pitch(dh, "dh", N, self.K, self.u.dtype, self.device) != ldx:
             raise ValueError(f"dh: rows of x's pitch {ldx} wanted, not strides {dh.stride()}")
+        if not self._kept:
+            raise ValueError("the last call kept nothing for a backward pass")
         if self._backward is None:
             new = lambda rows, cols: torch.empty((rows, cols), dtype=self.u.dtype, device=self.device)
             f32 = lambda n: torch.empty(n, dtype=torch.float32, device=self.device)

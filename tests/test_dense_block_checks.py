@@ -103,3 +103,16 @@ def test_dense_layers_are_not_mixed():
     other = blk.Mx4Layer(K, F, torch.float16, *blk.mx4_form(K, F, "cpu"))
     with pytest.raises(ValueError):
         blk.FeedForward([_layers()[0], other], N, torch.ones(K), device="cpu")
+
+
+def test_no_backward_pass_behind_a_call_that_kept_nothing(calls):
+    """Z would be an earlier step's."""
+    block = _block()
+    block(_new())
+    block(_new(), train=False)
+    made = len(calls)
+    with pytest.raises(ValueError):
+        block.backward(_new(), _new())
+    assert len(calls) == made
+    block(_new())
+    block.backward(_new(), _new())
