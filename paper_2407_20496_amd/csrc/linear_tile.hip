@@ -651,7 +651,7 @@ struct TilePlan {
   int form, whole_tiles, splits, stages_of_split;
   double us;
 };
-TilePlan find_plan(int M, int N, int K, bool guarded) {
+TilePlan plan_of(int M, int N, int K, bool guarded) {
   const int stages = (K + kStage - 1) / kStage;
   TilePlan best{};
   double least = 1e300;
@@ -676,20 +676,6 @@ TilePlan find_plan(int M, int N, int K, bool guarded) {
   }
   return best;
 }
-// A call asks for its plan more than once, and a program for the same ones again: each thread keeps the last of a few dozen shapes
-// (finding one takes some 0.7 us of the caller).
-TilePlan plan_of(int M, int N, int K, bool guarded) {
-  struct Kept {
-    int M, N, K;
-    bool guarded;
-    TilePlan plan;
-  };
-  static thread_local Kept kept[64];
-  Kept& k = kept[((uint32_t)M * 2654435761u ^ (uint32_t)N * 2246822519u ^ (uint32_t)K * 3266489917u ^ (uint32_t)guarded) >> 26];
-  if (k.M != M || k.N != N || k.K != K || k.guarded != guarded) k = Kept{M, N, K, guarded, find_plan(M, N, K, guarded)};
-  return k.plan;
-}
-
 // Both gradients' products in one launch, no tiles shared: its form by estimates from the same table, or kFormGuarded where two launches
 // are sooner.  The longer workgroups begin, the shorter ones take the places beside them, and what is left of the longer ones goes on
 // with fewer on the chip.  us of two launches, of one in tiles of 128, in tiles of 64: 768x768 of 4096 columns 24.1, 24.8, 20.1, of 1000
