@@ -131,7 +131,7 @@ hinm_status check_dense_grad(int32_t M, int32_t K, int32_t N) {
   return st != HINM_OK ? st : check_dense(M, N, K);
 }
 // The gradients' products take whole pieces of rows: dZ has them, and dY where it takes dZ's place, or it is written there as it is; X
-// of few tokens (a single token's vector has none) is copied.
+// of few tokens is copied, but not of so few that dW has a kernel which takes rows of any kind.
 constexpr int32_t kMostCopiedTokens = 64;
 struct LinearGradPlan {
   int64_t ldz;              // of dZ and of X's copy
@@ -141,7 +141,7 @@ LinearGradPlan linear_grad_plan(int32_t M, int32_t K, int32_t N) {
   LinearGradPlan p;
   p.ldz = ((int64_t)N + 7) / 8 * 8;
   p.dz = ((size_t)M * p.ldz * 2 + 255) & ~size_t{255};
-  p.x = N <= kMostCopiedTokens ? ((size_t)K * p.ldz * 2 + 255) & ~size_t{255} : 0;
+  p.x = N > kOuterTokens && N <= kMostCopiedTokens ? ((size_t)K * p.ldz * 2 + 255) & ~size_t{255} : 0;
   const size_t x = dense_product_workspace_bytes(K, N, M, kAcross, kAcross), w = dense_product_workspace_bytes(M, K, N, kAlong, kAlong);
   p.product = x > w ? x : w;
   return p;

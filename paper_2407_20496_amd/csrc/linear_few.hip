@@ -10,6 +10,8 @@
 // odd rows are turned in LDS, from whole runs of 256 bytes a row: 11008x4095 of one token 26 us, 43.5 where a lane draws 16 bytes of each row.
 #include "linear_tile.h"
 
+#include <type_traits>
+
 #include "workgroup_items.h"
 
 namespace hinm {
@@ -193,8 +195,74 @@ hipError_t launch_few_dtype(const DenseProduct& d, hipStream_t stream) {
   }
 }
 
+// The weights' gradient of up to 32 tokens: dW = dZ X^T in one step of the instruction, bound by dW's bytes, which leave straight from
+// registers.  A wave owns 64 rows and 128 columns, a workgroup 512 columns; there is nothing in LDS and nothing to wait for but
+// the first loads.  X is the row operand, its rows in such an order that a lane ends with eight consecutive columns: row
+// i of instruction t is column 8 (i / 4) + 4 t + i % 4 of 32.  11008x4096 of 16 tokens 18.8 us (4.8 TB/s; in tiles of 256 through LDS 32.0),
+// 4096x4096 of 16 9.8 (13.8), 5482x5960 of 3 15.9 (28.3).
+constexpr int kOuterRows = 64, kOuterColumns = 128;
+template <int DT>
+__global__ __launch_bounds__(256) void linear_outer_kernel(FewArgs a, LinearEpilogue e) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int across = (e.N + 4 * kOuterColumns - 1) / (4 * kOuterColumns);
+  const int item = item_of_workgroup((e.M + kOuterRows - 1) / kOuterRows * across);
+  if (item < 0) return;
+  const int m0 = item / across * kOuterRows, k0 = (item % across * 4 + wave) * kOuterColumns, left = a.K - 8 * g;
+  if (k0 >= e.N) return;
+  constexpr int kBlocks = kOuterRows / 16, kParts = kOuterColumns / 32;
+  const u32x4 none = {0, 0, 0, 0};
+  u32x4 z[kBlocks], x[kParts][2];
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b) z[b] = left > 0 ? draw_eight(a.W + min(m0 + 16 * b + r, e.M - 1) * a.ldw + 8 * g, left, a.rows_w) : none;
+#pragma unroll
+  for (int s = 0; s < kParts; ++s)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int k = k0 + 32 * s + 8 * (r >> 2) + 4 * t + (r & 3);
+      x[s][t] = left > 0 && k < e.N ? draw_eight(a.X + k * a.ldx + 8 * g, left, a.rows_x) : none;
+    }
+  if (left > 0) {
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) z[b] = trim_eight(z[b], left, a.rows_w);
+#pragma unroll
+    for (int s = 0; s < kParts; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) x[s][t] = trim_eight(x[s][t], left, a.rows_x);
+  }
+  auto store = [&](auto whole_tag) __attribute__((always_inline)) {
+    constexpr bool kWhole = decltype(whole_tag)::value;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) {
+        const f32x4 zero = {0, 0, 0, 0}, low = mfma_16x16x32<DT>(x[s][0], z[b], zero), high = mfma_16x16x32<DT>(x[s][1], z[b], zero);
+        float v[8] = {low[0], low[1], low[2], low[3], high[0], high[1], high[2], high[3]};
+        const int m = m0 + 16 * b + r, n = k0 + 32 * s + 8 * g;
+        if (kWhole || (m < e.M && n < e.N)) finish_eight<DT, kEpiBare, kWhole>(e, m, n, min(e.N - n, 8), none, v);
+      }
+  };
+  if (!e.out_f32 && m0 + kOuterRows <= e.M && k0 + kOuterColumns <= e.N) store(std::true_type{});
+  else store(std::false_type{});
+}
+
+template <int DT>
+hipError_t launch_outer(const DenseProduct& d, hipStream_t stream) {
+  const FewArgs a{static_cast<const uint16_t*>(d.A), d.lda, static_cast<const uint16_t*>(d.B), d.ldb, d.K, pieces_of_rows(d.A, d.lda, d.K),
+                  pieces_of_rows(d.B, d.ldb, d.K)};
+  const dim3 grid(grid_of_items(((int64_t)d.M + kOuterRows - 1) / kOuterRows * ((d.N + 4 * kOuterColumns - 1) / (4 * kOuterColumns))));
+  if (d.plan) {
+    plan_record(d.plan, "linear_outer_kernel<DT=%d> grid=%u block=256", DT, grid.x);
+    return hipSuccess;
+  }
+  linear_outer_kernel<DT><<<grid, 256, 0, stream>>>(a, d.to);
+  return hipGetLastError();
+}
+
 }  // namespace
 
+hipError_t launch_linear_outer(const DenseProduct& d, hipStream_t stream) {
+  return d.dtype == HINM_F16 ? launch_outer<HINM_F16>(d, stream) : launch_outer<HINM_BF16>(d, stream);
+}
 hipError_t launch_linear_few(const DenseProduct& d, hipStream_t stream) {
   return d.dtype == HINM_F16 ? launch_few_dtype<HINM_F16>(d, stream) : launch_few_dtype<HINM_BF16>(d, stream);
 }

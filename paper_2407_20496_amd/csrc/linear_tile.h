@@ -33,6 +33,10 @@ hipError_t launch_row_copy(const void* from, int64_t ld, void* to, int64_t pitch
 // a layer's product (A along, B across) on up to kFewTokens tokens
 constexpr int kFewTokens = 16;
 hipError_t launch_linear_few(const DenseProduct& p, hipStream_t stream);
+// the weights' gradient (both along) of up to kOuterTokens
+constexpr int kOuterTokens = 32;
+inline bool is_outer(OperandForm form_a, OperandForm form_b, int K) { return form_a == kAlong && form_b == kAlong && K <= kOuterTokens; }
+hipError_t launch_linear_outer(const DenseProduct& p, hipStream_t stream);
 
 // dZ [M][ldz] = dY act'(Z), zero in columns from N on to the next multiple of 8 (ldz is one), and dbias [M] = its sums over N
 // columns; either may be NULL.  Z NULL: no activation.

@@ -696,9 +696,11 @@ double pair_us(const TileForm& f, int M, int K, int N) {
   }
   return f.start + (longer * long_us + shorter * short_us) / f.at_once + 0.5 * short_us;
 }
+// the weights' gradient of few tokens by itself
+double outer_us(int M, int K) { return 2.5 + 2e-6 / 4.5 * M * K; }
 int pair_form(int M, int K, int N) {
   int form = kFormGuarded;
-  double least = plan_of(M, K, N, false).us + plan_of(K, N, M, false).us;
+  double least = (N <= kOuterTokens ? outer_us(M, K) : plan_of(M, K, N, false).us) + plan_of(K, N, M, false).us;
   for (int i : {kFormMiddle, kFormSmall}) {
     const double us = pair_us(kTileForms[i], M, K, N);
     if (us < least) {
@@ -828,7 +830,7 @@ hipError_t launch_pair_of(const DenseProduct& w, const DenseProduct& x, float* s
 }  // namespace
 
 size_t dense_product_workspace_bytes(int M, int N, int K, OperandForm form_a, OperandForm form_b) {
-  if (is_layer(form_a, form_b) && N <= kFewTokens) return 0;
+  if ((is_layer(form_a, form_b) && N <= kFewTokens) || is_outer(form_a, form_b, K)) return 0;
   const size_t guarded = partial_bytes(plan_of(M, N, K, true), M, N);
   const size_t whole = partial_bytes(plan_of(M, N, K, false), M, N) + (may_copy(M, K, form_a, form_b) ? copy_of(M, K, form_a).bytes() : 0);
   return whole > guarded ? whole : guarded;
@@ -843,6 +845,7 @@ hipError_t launch_row_copy(const void* from, int64_t ld, void* to, int64_t pitch
 
 hipError_t launch_dense_product(const DenseProduct& p, hipStream_t stream) {
   if (is_layer(p.form_a, p.form_b) && p.N <= kFewTokens) return launch_linear_few(p, stream);
+  if (is_outer(p.form_a, p.form_b, p.K)) return launch_linear_outer(p, stream);
   DenseProduct d = p;
   const Operands o(p);
   if (o.copies(p)) {

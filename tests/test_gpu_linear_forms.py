@@ -23,7 +23,7 @@ TILES = [
     (1, 5676, 2908, 65, MIDDLE, True, True), (1, 1, 223, 9225, MIDDLE, False, True), (1, 88, 2546, 856, MIDDLE, False, True),
     (1, 130, 328, 5829, MIDDLE, False, True), (1, 224, 7196, 372, MIDDLE, False, True), (1, 704, 152, 11330, MIDDLE, False, True),
     (2, 9309, 3471, 367, LARGE, True, True), (2, 4098, 968, 64, WIDE, False, True), (2, 7097, 602, 72, WIDE, False, True),
-    (2, 6152, 136, 5611, WIDE, True, True), (2, 1688, 2650, 132, WIDE, False, True), (2, 872, 4775, 1, WIDE, False, True),
+    (2, 6152, 136, 5611, WIDE, True, True), (2, 1688, 2650, 132, WIDE, False, True), (2, 1707, 2799, 58, WIDE, False, True),
     (2, 96, 1355, 10882, MIDDLE, True, True), (2, 1054, 2013, 64, MIDDLE, False, True), (2, 9977, 193, 68, MIDDLE, False, True),
     (2, 271, 6551, 152, MIDDLE, False, True), (2, 334, 9756, 256, MIDDLE, False, True), (2, 11561, 134, 299, MIDDLE, False, True),
     (0, 4097, 4097, 600, MIDDLE, False, False), (1, 4097, 4097, 600, MIDDLE, False, False), (0, 700, 30, 1030, SMALL, False, False),
@@ -32,6 +32,9 @@ TILES = [
 PAIRS = [(21, 16, 64, SMALL), (64, 2697, 101, SMALL), (128, 687, 144, SMALL), (166, 178, 205, SMALL), (188, 3263, 3596, SMALL), (384, 573, 4603, SMALL),
          (371, 4802, 64, SMALL), (106, 201, 9, SMALL), (2487, 2992, 9, SMALL), (282, 3880, 98, SMALL), (3615, 1628, 239, SMALL), (2752, 520, 840, SMALL),
          (1, 1, 1, SMALL), (170, 4632, 1855, MIDDLE), (320, 3138, 3369, MIDDLE), (231, 5318, 167, MIDDLE), (4104, 5315, 195, MIDDLE), (2050, 2048, 1024, MIDDLE)]
+# weights' gradients of few tokens; M, K, N
+OUTER = [(872, 4775, 1), (1, 1, 1), (64, 512, 32), (128, 1024, 8), (65, 513, 7), (63, 511, 9), (200, 129, 16), (17, 8, 31), (1, 700, 17), (513, 1, 5), (1000, 1000, 3),
+         (96, 2056, 24)]
 FEW = [(10300, 100, 9, 4), (10300, 200, 16, 4), (300, 1030, 16, 1), (257, 64, 2, 1)]
 
 
@@ -120,3 +123,35 @@ def test_both_gradients_of_integers(M, K, N, act):
     assert torch.equal(torch.as_tensor(dw.f64(), device="cuda:0"), real(G @ X.t().contiguous()))
     assert torch.equal(db[:M].double(), G.sum(1)) and db[M].item() == 77.0
     assert torch.equal(dx.surroundings(), around[0]) and torch.equal(dw.surroundings(), around[1])
+
+
+@pytest.mark.parametrize("M,K,N", OUTER)
+def test_few_tokens_reach_their_gradient(M, K, N):
+    import paper_2407_20496_amd as hinm
+    for aligned in (True, False):
+        assert hinm.hinm_calib_linear_plan(M, K, N, "f16", 2, aligned).startswith("linear_outer_kernel")
+    assert "outer" not in hinm.hinm_calib_linear_plan(M, K, 33, "f16", 2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["pieces", "odd", "close"])
+@pytest.mark.parametrize("out", ["same", "f32"])
+@pytest.mark.parametrize("M,K,N", OUTER)
+def test_weights_gradient_of_few_tokens(M, K, N, out, layout):
+    """Integers, whose sums are exact; rows have NaN behind and around them."""
+    import torch
+    import paper_2407_20496_amd as hinm
+    from tests.dense_util import Matrix, pitch8, result, workspace
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(M + K + N)
+    dtype = ("f16", "bf16")[K % 2]
+    X, G = _integers(K, N, gen, 7), _integers(M, N, gen, 7)
+    place = {"pieces": lambda n: (pitch8(n), 0), "odd": lambda n: (n + 3, 5), "close": lambda n: (n, 1)}[layout]
+    x, g = Matrix(K, N, dtype, *place(N), X), Matrix(M, N, dtype, *place(N), G)
+    dw = result(M, K, torch.float32 if out == "f32" else dtype, *place(K))
+    around = dw.surroundings()
+    hinm.hinm_linear_grad(M, K, N, dtype, None, dw.ld, x.data, x.ld, None, g.data, g.ld, None, dw.data, None,
+                          hinm.OUT_F32 if out == "f32" else 0, *workspace(hinm.hinm_linear_grad_workspace(M, K, N)))
+    torch.cuda.synchronize()
+    assert torch.equal(dw.view.double(), (G @ X.t().contiguous()).to(dw.kind).double())
+    assert torch.equal(dw.surroundings(), around)
