@@ -30,7 +30,8 @@ from . import binding as hb
 
 @dataclass
 class Mx4Layer:
-    """Weights [M][K] in microscaled 4-bit form; flags as for hinm_mx4_linear (EPI_RELU between layers)."""
+    """Weights [M][K] in microscaled 4-bit form; flags as for hinm_mx4_linear (EPI_RELU between layers;
+    OUT_F32 is not for layers of a block)."""
     M: int
     K: int
     dtype: object
@@ -41,7 +42,7 @@ class Mx4Layer:
 
 @dataclass
 class DenseLayer:
-    """16-bit weights [M][K] in rows of any pitch, a float32 bias [M] or none; flags as for hinm_linear (an activation)."""
+    """16-bit weights [M][K] in rows of any pitch, a float32 bias [M] or none; flags: an activation of hinm_linear's."""
     M: int
     K: int
     dtype: object
@@ -104,13 +105,17 @@ def mx4_layer(W: torch.Tensor, flags: int = 0) -> Mx4Layer:
 _ACTIVATIONS = (0, hb.EPI_RELU, hb.EPI_GELU, hb.EPI_GELU_TANH, hb.EPI_SILU)
 
 
+def _check_activation(flags: int) -> None:
+    if flags not in _ACTIVATIONS:
+        raise ValueError(f"flags: one activation or none wanted, not {flags:#x}")
+
+
 def dense_layer(W: torch.Tensor, bias: Optional[torch.Tensor] = None, flags: int = 0) -> DenseLayer:
     """A layer of the weights as they are (kept, not copied); flags: one activation or none."""
     _row_pitch(W, "weights")
     M, K = W.shape
     _factors(bias, "bias", M, W.device)
-    if flags not in _ACTIVATIONS:
-        raise ValueError(f"flags: one activation or none wanted, not {flags:#x}")
+    _check_activation(flags)
     return DenseLayer(M, K, W.dtype, W, bias, flags)
 
 
@@ -164,8 +169,10 @@ def block_input(x: torch.Tensor, w_pre: torch.Tensor, tokens: int, eps: float = 
 
 
 def _check_layers(layers: Sequence[DenseLayer], device) -> None:
-    """What the library cannot see of dense layers: their arrays' shapes, types and places."""
+    """What the library cannot see of dense layers: their arrays' shapes, types and places, and that their results go to 16-bit
+    buffers."""
     for l in layers:
+        _check_activation(l.flags)
         _row_pitch(l.W, "weights")
         if list(l.W.shape) != [l.M, l.K] or l.W.dtype != _TORCH_DTYPE[hb._dtype_code(l.dtype)] or l.W.device != device:
             raise ValueError(f"weights: {l.dtype} [{l.M}][{l.K}] on {device} wanted, not {l.W.dtype} {list(l.W.shape)} on {l.W.device}")
@@ -189,6 +196,8 @@ class FeedForward:
             raise ValueError("one block's layers come in one form")
         if len({hb._dtype_code(l.dtype) for l in layers}) > 1:
             raise ValueError("one block's layers have one type")
+        if any(l.flags & hb.OUT_F32 for l in layers):
+            raise ValueError("flags: OUT_F32 is not for a block, whose buffers are 16-bit")
         self.layers, self.tokens, self.ld = layers, tokens, leading_dimension(tokens)
         self.w_post, self.gate, self.w_next = w_post, gate, w_next
         self.residual_scale, self.eps = residual_scale, eps
