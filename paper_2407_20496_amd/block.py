@@ -289,13 +289,13 @@ class LayerNormFeedForward:
         self.scratch = _workspace(self.scratch_bytes, device)
         self.ldw = [_row_pitch(l.W, "weights") for l in layers]
         self._backward = self._dx_buffer = None
-        self._kept = True
+        self._kept = None  # no call yet; then whether the last one left what a backward pass needs
 
     def __call__(self, x: torch.Tensor, train: bool = True) -> torch.Tensor:
-        """h, in the block's own buffer; with `train` what `backward` needs is kept, without it `backward` raises ValueError."""
+        """h, in the block's own buffer; with `train` what `backward` needs is kept."""
         N, ld, ws = self.tokens, self.ld, (self.scratch, self.scratch_bytes)
         ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
-        self._kept = train
+        self._kept = False
         hb.hinm_layer_norm(self.K, N, self.dtype, self.eps, x, ldx, self.w, self.b, self.u, ld, self.mean, self.rstd, *ws)
         into = self.u
         for l, ldw, z, out in zip(self.layers, self.ldw, self.Z, self.out + [self.h]):
@@ -303,15 +303,19 @@ class LayerNormFeedForward:
             hb.hinm_linear(l.M, l.K, N, l.dtype, l.W, ldw, into, ld, l.bias, x if last else None, ldx, z if train else None, out,
                            ld, l.flags, *ws)
             into = out
+        self._kept = train
         return self.h
 
     def backward(self, x: torch.Tensor, dh: torch.Tensor):
         """(dx, gradients): of x, in rows of its pitch; of every layer's W (its type, contiguous) and bias, and of the norm's
-        w and b, as a dict of tensors "W0", "bias0", ..., "w", "b" (no entry for what the block does not have)."""
+        w and b, as a dict of tensors "W0", "bias0", ..., "w", "b" (no entry for what the block does not have).  Ahead of any call it
+        makes the call itself; behind one without `train`, or one that failed, it raises ValueError."""
         N, ld = self.tokens, self.ld
         ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
         if _pitch(dh, "dh", N, self.K, self.u.dtype, self.device) != ldx:
             raise ValueError(f"dh: rows of x's pitch {ldx} wanted, not strides {dh.stride()}")
+        if self._kept is None:
+            self(x)
         if not self._kept:
             raise ValueError("the last call kept nothing for a backward pass")
         if self._backward is None:
