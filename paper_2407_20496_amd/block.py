@@ -81,6 +81,23 @@ def _pitch(t: torch.Tensor, what: str, tokens: int, K: Optional[int] = None, dty
     return ld
 
 
+def _place(t: torch.Tensor) -> Tuple[int, int, int, int]:
+    """Where a block's buffer lies: address, bytes, rows, leading dimension."""
+    return t.data_ptr(), t.nbytes, t.shape[0], t.stride(0)
+
+
+def _is_own(t: torch.Tensor, ld: int, what: str, tokens: int, own: Tuple[int, int, int, int]) -> bool:
+    """Whether an array that _pitch took is a block's buffer itself, which lies at `own`; ValueError where it shares memory with it
+    in another way, so that one would be written while the other is still read.  0.3 us of a call."""
+    at, nbytes, rows, pitch = own
+    distance = t.data_ptr() - at
+    if distance >= nbytes or distance <= -2 * ((rows - 1) * ld + tokens):
+        return False
+    if distance or (rows > 1 and ld != pitch):
+        raise ValueError(f"{what}: overlaps the block's own buffer")
+    return True
+
+
 def _factors(t: Optional[torch.Tensor], what: str, n: int, device) -> None:
     """n float32 values or more, one after the other, or none at all."""
     if t is not None and (t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous() or t.device != device):
@@ -204,6 +221,7 @@ class FeedForward:
         self.K, self.dtype = layers[0].K, layers[0].dtype
         new = lambda rows: torch.empty((rows, self.ld), dtype=_TORCH_DTYPE[hb._dtype_code(self.dtype)], device=device)
         self.y = new(self.K)
+        self._y_place = _place(self.y)
         for what, t in (("w_post", w_post), ("gate", gate), ("w_next", w_next)):
             _factors(t, what, self.K, self.y.device)
         for l in layers if self.in_4_bits else ():
@@ -228,6 +246,8 @@ class FeedForward:
         N, ld = self.tokens, self.ld
         if _pitch(u, "u", N, self.K, self.y.dtype, self.y.device) != ld:
             raise ValueError(f"u: rows of {ld} = leading_dimension({N}) values wanted, not strides {u.stride()}")
+        if _is_own(u, ld, "u", N, self._y_place) and len(self.layers) == 1:
+            raise ValueError("u: one layer cannot write over its input")
         if self.dense:
             for l, ldw, out in zip(self.layers, self.ldw, self.between + [self.y]):
                 hb.hinm_linear(l.M, l.K, N, l.dtype, l.W, ldw, u, ld, l.bias, None, 0, None, out, ld, l.flags, self.scratch,
@@ -282,6 +302,7 @@ class LayerNormFeedForward:
         for what, t in (("w", w), ("b", b)):
             _factors(t, what, self.K, self.device)
         self.h, self.mean, self.rstd = new(self.K), f32(tokens), f32(tokens)
+        self._h_place = _place(self.h)
         self.Z = [new(l.M) if l.flags else None for l in layers]
         self.out = [new(l.M) for l in layers[:-1]]
         sizes = [hb.hinm_linear_workspace(l.M, l.K, tokens) for l in layers] + [hb.hinm_layer_norm_workspace(self.K, tokens)]
@@ -292,9 +313,11 @@ class LayerNormFeedForward:
         self._kept = None  # no call yet; then whether the last one left what a backward pass needs
 
     def __call__(self, x: torch.Tensor, train: bool = True) -> torch.Tensor:
-        """h, in the block's own buffer; with `train` what `backward` needs is kept."""
+        """h, in the block's own buffer; with `train` what `backward` needs is kept.  x may be h (a block
+        applied again), but then it is overwritten, and nothing is kept."""
         N, ld, ws = self.tokens, self.ld, (self.scratch, self.scratch_bytes)
         ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
+        in_place = _is_own(x, ldx, "x", N, self._h_place)
         self._kept = False
         hb.hinm_layer_norm(self.K, N, self.dtype, self.eps, x, ldx, self.w, self.b, self.u, ld, self.mean, self.rstd, *ws)
         into = self.u
@@ -303,17 +326,22 @@ class LayerNormFeedForward:
             hb.hinm_linear(l.M, l.K, N, l.dtype, l.W, ldw, into, ld, l.bias, x if last else None, ldx, z if train else None, out,
                            ld, l.flags, *ws)
             into = out
-        self._kept = train
+        self._kept = train and not in_place
         return self.h
 
     def backward(self, x: torch.Tensor, dh: torch.Tensor):
         """(dx, gradients): of x, in rows of its pitch; of every layer's W (its type, contiguous) and bias, and of the norm's
         w and b, as a dict of tensors "W0", "bias0", ..., "w", "b" (no entry for what the block does not have).  Ahead of any call it
-        makes the call itself; behind one without `train`, or one that failed, it raises ValueError."""
+        makes the call itself; behind one that kept nothing, or one that failed, it raises ValueError.  dh may be dx."""
         N, ld = self.tokens, self.ld
         ldx = _pitch(x, "x", N, self.K, self.u.dtype, self.device)
         if _pitch(dh, "dh", N, self.K, self.u.dtype, self.device) != ldx:
             raise ValueError(f"dh: rows of x's pitch {ldx} wanted, not strides {dh.stride()}")
+        dx = self._dx(ldx)
+        dx_place = _place(dx)
+        if _is_own(x, ldx, "x", N, self._h_place) or _is_own(x, ldx, "x", N, dx_place):
+            raise ValueError("x: overwritten by the block")
+        _is_own(dh, ldx, "dh", N, dx_place)
         if self._kept is None:
             self(x)
         if not self._kept:
@@ -342,7 +370,6 @@ class LayerNormFeedForward:
             if dW is None:
                 hb.hinm_linear_grad(l.M, l.K, N, l.dtype, None, l.K, X, ld, self.Z[i], dy, ldy, None, g[f"W{i}"], None, l.flags, *ws)
             dy, ldy = into[i], ld
-        dx = self._dx(ldx)
         hb.hinm_layer_norm_grad(self.K, N, self.dtype, x, ldx, self.w, self.mean, self.rstd, into[0], ld, dh, dx, g.get("w"), g.get("b"), *ws)
         return dx, g
 
