@@ -76,22 +76,23 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
   }
 }
 
+// An infinite v has the limit, 0 or 1 (a sum beyond 16 bits is kept as one): far out the factor beside v is zero, and their product
+// would be no number.
 __device__ __forceinline__ float activation_slope(float v, int act) {
   switch (act) {
     case kActRelu: return v > 0 ? 1.0f : v <= 0 ? 0.0f : v;
     case kActGelu: {
       float bell;
       const float p = normal_probability(v, bell);
-      return fmaf(v, bell * 0.3989422804014327f, p);
+      return bell == 0 ? p : fmaf(v, bell * 0.3989422804014327f, p);
     }
     case kActGeluTanh: {
       const float s = sigmoid(kTanhScale * fmaf(kTanhCube * v * v, v, v)), both = s * (1.0f - s);
-      // far out both is zero where the factor beside it may have no bound
       return both > 0 ? fmaf(v * both, kTanhScale * fmaf(3.0f * kTanhCube, v * v, 1.0f), s) : s;
     }
     case kActSilu: {
-      const float s = sigmoid(v);
-      return s * fmaf(v, 1.0f - s, 1.0f);
+      const float s = sigmoid(v), rest = 1.0f - s;
+      return s * rest == 0 ? s : s * fmaf(v, rest, 1.0f);
     }
   }
   return 1.0f;
