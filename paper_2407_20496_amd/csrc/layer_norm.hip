@@ -212,12 +212,15 @@ __global__ __launch_bounds__(kHeldThreads) void layer_norm_held_kernel(LayerNorm
 }
 
 // One token without a stride: a vector, held by one workgroup, eight channels a thread and round.  WHOLE: whole pieces at
-// multiples of 16 bytes (channels and factors).
+// multiples of 16 bytes (channels and factors).  Sums of more than 2^13 values of 11 bits may need more than float32's 24, and a
+// mean off by one of its steps counts where the deviations are no larger (equal channels of 65504: 0.004 beside a root of eps of
+// 0.003): there what the deviations' own mean is beside zero is taken off them.
 constexpr int kVectorMost = 2 * 8 * 1024;  // channels
 
 template <int DT, int THREADS, int ROUNDS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void layer_norm_vector_kernel(LayerNorm a) {
-  __shared__ __align__(16) float by_wave[2][THREADS / 64];
+  constexpr bool kLong = 8 * THREADS * ROUNDS > 1 << 13;
+  __shared__ __align__(16) float by_wave[3][THREADS / 64];
   float x[ROUNDS][8], w[ROUNDS][8], b[ROUNDS][8];
   u32x4 of_x[ROUNDS];
   const u32x4 none = {0, 0, 0, 0};
@@ -238,6 +241,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_vector_kernel(LayerNorm a)
     for (int j = 0; j < 8; ++j) sum += x[i][j];
   }
   const float mean = add_workgroup<THREADS>(sum, by_wave[0]) / (float)a.K;
+  float rest = 0;
   sum = 0;
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
@@ -246,11 +250,18 @@ __global__ __launch_bounds__(THREADS) void layer_norm_vector_kernel(LayerNorm a)
     for (int j = 0; j < 8; ++j) {
       x[i][j] = j < left ? x[i][j] - mean : 0.0f;
       sum += x[i][j] * x[i][j];
+      if constexpr (kLong) rest += x[i][j];
     }
   }
-  const float r = 1.0f / sqrtf(add_workgroup<THREADS>(sum, by_wave[1]) / (float)a.K + a.eps);
+  float variance = add_workgroup<THREADS>(sum, by_wave[1]) / (float)a.K;
+  if constexpr (kLong) {
+    rest = add_workgroup<THREADS>(rest, by_wave[2]) / (float)a.K;
+    variance -= rest * rest;
+    if (variance < 0) variance = 0;  // all of it cancelled; keeps NaN
+  }
+  const float r = 1.0f / sqrtf(variance + a.eps);
   if (threadIdx.x == 0) {
-    if (a.mean) a.mean[0] = mean;
+    if (a.mean) a.mean[0] = mean + rest;
     if (a.rstd) a.rstd[0] = r;
   }
 #pragma unroll
@@ -258,7 +269,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_vector_kernel(LayerNorm a)
     const int k = 8 * (threadIdx.x + i * THREADS), left = a.K - k;
     if (left <= 0) break;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[i][j] = x[i][j] * (r * w[i][j]) + (a.b ? b[i][j] : 0.0f);
+    for (int j = 0; j < 8; ++j) x[i][j] = (x[i][j] - rest) * (r * w[i][j]) + (a.b ? b[i][j] : 0.0f);
     store_eight(a.u + k, narrow<DT>(x[i]), left);
   }
 }
