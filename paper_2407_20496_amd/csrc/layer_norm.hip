@@ -33,6 +33,10 @@ struct LayerNorm {
 
 __device__ __forceinline__ float root_of(double variance, float eps) { return 1.0f / sqrtf((float)variance + eps); }
 
+// Sums in float32 are of 2^-14 of the values, of which there are at most 2^14: as many bf16 values of any size do not leave its range.
+constexpr float kSumScale = 0x1p-14f;
+__device__ __forceinline__ float mean_of_sum(float sum, int K) { return sum / ((float)K * kSumScale); }
+
 // kRounds rows of a lane's columns, from row k on in steps of a round
 template <Layout L>
 __device__ __forceinline__ void load_rows(const uint16_t* x, int64_t ld, const Place& p, int k, int end, Pieces rows, u32x4 (&v)[kRounds]) {
@@ -175,12 +179,12 @@ __global__ __launch_bounds__(kHeldThreads) void layer_norm_held_kernel(LayerNorm
     float x[8];
     widen<DT>(v[i], x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[0][j] += x[j];
+    for (int j = 0; j < 8; ++j) sum[0][j] = fmaf(x[j], kSumScale, sum[0][j]);
   }
   add_held<1>(sum, by_wave, total[0]);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    m[j] = total[0][0][j] / (float)a.K;
+    m[j] = mean_of_sum(total[0][0][j], a.K);
     sum[0][j] = 0;
   }
 #pragma unroll
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(kHeldThreads) void layer_norm_held_kernel(LayerNorm
 #pragma unroll
   for (int j = 0; j < 8; ++j) r[j] = 1.0f / sqrtf(total[1][0][j] / (float)a.K + a.eps);
   if (threadIdx.x < left) {
-    const float mean = total[0][0][threadIdx.x] / (float)a.K;
+    const float mean = mean_of_sum(total[0][0][threadIdx.x], a.K);
     if (a.mean) a.mean[n + threadIdx.x] = mean;
     if (a.rstd) a.rstd[n + threadIdx.x] = 1.0f / sqrtf(total[1][0][threadIdx.x] / (float)a.K + a.eps);
   }
@@ -238,9 +242,9 @@ __global__ __launch_bounds__(THREADS) void layer_norm_vector_kernel(LayerNorm a)
     const int left = a.K - 8 * (int)(threadIdx.x + i * THREADS);
     widen<DT>(WHOLE ? (left > 0 ? of_x[i] : none) : left > 0 ? trim_eight(of_x[i], left, a.rows) : none, x[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += x[i][j];
+    for (int j = 0; j < 8; ++j) sum = fmaf(x[i][j], kSumScale, sum);
   }
-  const float mean = add_workgroup<THREADS>(sum, by_wave[0]) / (float)a.K;
+  const float mean = mean_of_sum(add_workgroup<THREADS>(sum, by_wave[0]), a.K);
   float rest = 0;
   sum = 0;
 #pragma unroll

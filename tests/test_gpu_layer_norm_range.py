@@ -34,6 +34,14 @@ def test_equal_channels(K, N, dtype, value):
     assert np.allclose(rstd, 1 / np.sqrt(1e-5), rtol=2.0 ** -21, atol=0)
 
 
+@pytest.mark.parametrize("K,N", SHAPES)
+@pytest.mark.parametrize("value", [255.0 * 2 ** 120, -(2.0 ** 127), 2.0 ** 112])
+def test_equal_channels_whose_sum_leaves_float32(K, N, value):
+    u, mean, rstd = _constant(K, N, "bf16", value)
+    assert (mean == value).all() and (u == 0.5).all()
+    assert np.allclose(rstd, 1 / np.sqrt(1e-5), rtol=2.0 ** -21, atol=0)
+
+
 @pytest.mark.parametrize("K", [k for k, _ in VECTORS])
 def test_one_channel_of_a_token_apart(K):
     """One value a step beside the rest, far from zero: the smallest spread that 16 bits have."""
