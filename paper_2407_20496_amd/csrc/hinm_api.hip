@@ -114,6 +114,10 @@ hinm_status check_norm(int32_t K, int32_t N, int32_t dtype) {
   return N > kMostTokens || K > kMostSize ? HINM_ERR_UNSUPPORTED : HINM_OK;
 }
 
+// Channels' gradients of several strips of tokens are added by workgroups of 1024 threads, 32 channels each; a launch has less than
+// 2^32 threads.
+bool too_many_to_add(int32_t K, int32_t N) { return K > 32 * (kMostGroups - 1) && N > 64; }
+
 // ---- dense layers --------------------------------------------------------------------------------------
 // M x N results of sums over K: what a launch has workgroups for, 64 x 64 results each at the least
 hinm_status check_dense(int32_t M, int32_t K, int32_t N) {
@@ -866,8 +870,7 @@ hinm_status hinm_block_norm_grad(int32_t K, int32_t N, int32_t dtype, float resi
   for (const float* p : {w_post, gate, token_gate, w_pre, rstd_y, rstd_h, const_cast<const float*>(dw_post),
                          const_cast<const float*>(dgate), const_cast<const float*>(dtoken_gate), const_cast<const float*>(dw_pre)})
     if (!aligned(p, 4)) return HINM_ERR_SHAPE;
-  // channels' gradients of several strips of tokens are added by workgroups of 1024 threads, 32 channels each
-  if (K >= 32 * kMostGroups && N > 64 && (dw_post || dgate || dw_pre)) return HINM_ERR_UNSUPPORTED;
+  if (too_many_to_add(K, N) && (dw_post || dgate || dw_pre)) return HINM_ERR_UNSUPPORTED;
   const size_t need = block_norm_grad_workspace_bytes(K, N);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
   const BlockNormGradArgs a{K, N, dtype, residual_scale, h, y, w_post, gate, token_gate, w_pre, rstd_y, rstd_h, dh, du, dx,
@@ -1021,8 +1024,7 @@ hinm_status hinm_layer_norm_grad(int32_t K, int32_t N, int32_t dtype, const void
     if (!aligned(p, 2)) return HINM_ERR_SHAPE;
   for (const float* p : {w, mean, rstd, const_cast<const float*>(dw), const_cast<const float*>(db)})
     if (!aligned(p, 4)) return HINM_ERR_SHAPE;
-  // channels' gradients of several strips of tokens are added by workgroups of 1024 threads, 32 channels each
-  if (K > 32 * (kMostGroups - 1) && N > 64 && (dw || db)) return HINM_ERR_UNSUPPORTED;
+  if (too_many_to_add(K, N) && (dw || db)) return HINM_ERR_UNSUPPORTED;
   const size_t need = layer_norm_grad_workspace_bytes(K, N);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 256))) return HINM_ERR_WORKSPACE;
   return launched(launch_layer_norm_grad({K, N, dtype, x, ldx, w, mean, rstd, du, ldu, dh, dx, dw, db, static_cast<float*>(workspace)},
