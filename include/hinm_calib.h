@@ -93,8 +93,8 @@ hinm_status hinm_calib_mx4_plan(int32_t M, int32_t N, int32_t K, int32_t dtype, 
                                 size_t text_bytes);
 
 /* The launches of a dense layer's product (which = 0), or of its gradients' products of the input (1), the weights (2) or both (3), as
- * hinm_spmm_prepared_plan gives them, where the rows of the weights (2: of both operands) begin at multiples of 16 bytes or (aligned = 0) do not.
- * Launches nothing. */
+ * hinm_spmm_prepared_plan gives them, where the rows of the weights (2: of the input X) begin at multiples of 16 bytes or (aligned = 0) do not.
+ * dZ always lies in whole pieces; the launch that computes it ahead of the gradients' products is not among them.  Launches nothing. */
 hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtype, int32_t which, int32_t aligned,
                                    char* text, size_t text_bytes);
 

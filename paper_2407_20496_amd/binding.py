@@ -635,7 +635,7 @@ def hinm_calib_mx4_plan(M, N, K, dtype, flags=0, quantize=False) -> str:
 
 def hinm_calib_linear_plan(M, K, N, dtype, which=0, aligned=True) -> str:
     """The launches of a dense layer's product (which = 0), or of the products of its gradients: of the input (1), the weights (2), both (3)."""
-    buf = C.create_string_buffer(1024)
+    buf = C.create_string_buffer(2048)
     _check(load_library().hinm_calib_linear_plan(_size(M), _size(K), _size(N), _dtype_code(dtype), int(which), int(bool(aligned)), buf,
                                                  len(buf)), "hinm_calib_linear_plan")
     return buf.value.decode()

@@ -150,6 +150,39 @@ LinearGradPlan linear_grad_plan(int32_t M, int32_t K, int32_t N) {
   p.product = x > w ? x : w;
   return p;
 }
+// ... from dZ (dY where that takes its place) on, which lies in whole pieces.
+struct LinearGradProducts {
+  DenseProduct of_x, of_w;
+  bool wants_x, wants_w, copied, pair;  // X to whole pieces first; both products in one launch
+  const void* X;                        // as the call has it
+  int64_t ldx;
+  void* x_copy;
+};
+LinearGradProducts linear_grad_products(const LinearGradPlan& p, int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw,
+                                        const void* X, int64_t ldx, const void* dz, int64_t ldz, void* dX, void* dW, bool out_f32,
+                                        void* workspace, LaunchPlan* record) {
+  uint8_t* const x_copy = static_cast<uint8_t*>(workspace) + p.dz;
+  void* const partials = x_copy + p.x;
+  const bool copied = dW && p.x && pieces_of_rows(X, ldx, N) != kAligned;
+  LinearGradProducts g{{K, N, M, dtype, kAcross, kAcross, W, ldw, dz, ldz,
+                        {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials, record},
+                       {M, K, N, dtype, kAlong, kAlong, dz, ldz, copied ? x_copy : X, copied ? p.ldz : ldx,
+                        {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials, record},
+                       dX != nullptr, dW != nullptr, copied, false, X, ldx, x_copy};
+  g.pair = dX && dW && dense_pair_serves(g.of_w, g.of_x);
+  return g;
+}
+// ... with the sums of dZ's rows to `sums`, unless it is NULL, where both products are one launch
+hipError_t launch_grad_products(const LinearGradProducts& g, float* sums, hipStream_t stream) {
+  LaunchPlan* const record = g.of_w.plan;
+  hipError_t e = hipSuccess;
+  if (g.copied && record) plan_record(record, "linear_copy_kernel block=256");
+  else if (g.copied) e = launch_row_copy(g.X, g.ldx, g.x_copy, g.of_w.ldb, g.of_w.N, g.of_w.K, stream);
+  if (e != hipSuccess) return e;
+  if (g.pair) return launch_dense_pair(g.of_w, g.of_x, sums, stream);
+  if (g.wants_x) e = launch_dense_product(g.of_x, stream);
+  return e == hipSuccess && g.wants_w ? launch_dense_product(g.of_w, stream) : e;
+}
 
 // ---- hinm_pack_static: the score workspace of the pack kernels in a file-scope device array -------------
 // One binary64 score per tile and column, at most kStaticScoreCount of them (4 MiB).  Every GPU the library runs
@@ -934,28 +967,16 @@ hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, con
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool as_it_is = act == kActNone && pieces_of_rows(dY, ldy, N) == kAligned;
   uint16_t* const dz = as_it_is || (!dX && !dW) ? nullptr : static_cast<uint16_t*>(workspace);
-  uint8_t* const x_copy = static_cast<uint8_t*>(workspace) + p.dz;
-  void* const partials = x_copy + p.x;
-  const void* const g = dz ? dz : dY;
-  const int64_t ldg = dz ? p.ldz : ldy;
-  const bool copied = dW && p.x && pieces_of_rows(X, ldx, N) != kAligned;
-  const DenseProduct of_x{K, N, M, dtype, kAcross, kAcross, W, ldw, g, ldg,
-                          {K, N, nullptr, nullptr, 0, kAligned, nullptr, dX, ldx, kActNone, false}, partials};
-  const DenseProduct of_w{M, K, N, dtype, kAlong, kAlong, g, ldg, copied ? x_copy : X, copied ? p.ldz : ldx,
-                          {M, K, nullptr, nullptr, 0, kAligned, nullptr, dW, ldw, kActNone, out_f32}, partials};
-  const bool pair = dX && dW && dense_pair_serves(of_w, of_x), sums_in_pair = pair && dbias && !dz && M <= kMostGroups;
+  const LinearGradProducts g = linear_grad_products(p, M, K, N, dtype, W, ldw, X, ldx, dz ? dz : dY, dz ? p.ldz : ldy, dX, dW, out_f32,
+                                                    workspace, nullptr);
+  const bool sums_in_pair = g.pair && dbias && !dz && M <= kMostGroups;
   hipError_t e = hipSuccess;
   if (dz || (dbias && !sums_in_pair)) {
     const void* z = act == kActNone ? nullptr : Z;
     e = launch_linear_slope({M, N, static_cast<const uint16_t*>(z), static_cast<const uint16_t*>(dY), ldy,
                              lesser(pieces_of_rows(z, ldy, N), pieces_of_rows(dY, ldy, N)), act, dz, p.ldz, dbias}, dtype, s);
   }
-  if (e == hipSuccess && copied) e = launch_row_copy(X, ldx, x_copy, p.ldz, K, N, s);
-  if (e != hipSuccess) return launched(e);
-  if (pair) return launched(launch_dense_pair(of_w, of_x, sums_in_pair ? dbias : nullptr, s));
-  if (dX) e = launch_dense_product(of_x, s);
-  if (e == hipSuccess && dW) e = launch_dense_product(of_w, s);
-  return launched(e);
+  return launched(e == hipSuccess ? launch_grad_products(g, sums_in_pair ? dbias : nullptr, s) : e);
 }
 
 hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtype, int32_t which, int32_t is_aligned, char* text,
@@ -970,18 +991,15 @@ hinm_status hinm_calib_linear_plan(int32_t M, int32_t K, int32_t N, int32_t dtyp
   const void* const aligned_at = reinterpret_cast<const void*>(uintptr_t{1} << 20);  // never dereferenced
   const void* const at = reinterpret_cast<const void*>((uintptr_t{1} << 20) + (is_aligned ? 0 : 2));
   auto pitch = [](int32_t n) { return ((int64_t)n + 7) / 8 * 8; };
-  auto product = [&](int32_t m, int32_t n, int32_t k, OperandForm a, OperandForm b) {
-    const LinearEpilogue to{m, n, nullptr, nullptr, 0, kAligned, nullptr, nullptr, pitch(n), kActNone, false};
-    return DenseProduct{m, n, k, dtype, a, b, at, pitch(a == kAlong ? k : m), which == 2 ? at : aligned_at, pitch(b == kAlong ? k : n), to,
-                        const_cast<void*>(aligned_at), &plan};
-  };
-  const DenseProduct of_x = product(K, N, M, kAcross, kAcross), of_w = product(M, K, N, kAlong, kAlong);
-  if (which == 0) return launched(launch_dense_product(product(M, N, K, kAlong, kAcross), nullptr));
-  hipError_t e = hipSuccess;
-  if (which == 3 && dense_pair_serves(of_w, of_x)) return launched(launch_dense_pair(of_w, of_x, nullptr, nullptr));
-  if (which != 2) e = launch_dense_product(of_x, nullptr);
-  if (which != 1 && e == hipSuccess) e = launch_dense_product(of_w, nullptr);
-  return launched(e);
+  void* const written = const_cast<void*>(aligned_at);
+  if (which == 0) {
+    const LinearEpilogue to{M, N, nullptr, nullptr, 0, kAligned, nullptr, nullptr, pitch(N), kActNone, false};
+    return launched(launch_dense_product({M, N, K, dtype, kAlong, kAcross, at, pitch(K), aligned_at, pitch(N), to, written, &plan}, nullptr));
+  }
+  return launched(launch_grad_products(linear_grad_products(linear_grad_plan(M, K, N), M, K, N, dtype, which == 2 ? aligned_at : at, pitch(K),
+                                                            which == 2 ? at : aligned_at, pitch(N), aligned_at, pitch(N),
+                                                            which == 2 ? nullptr : written, which == 1 ? nullptr : written, false, written,
+                                                            &plan), nullptr, nullptr));
 }
 
 hinm_status hinm_layer_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes) {
