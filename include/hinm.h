@@ -370,7 +370,7 @@ hinm_status hinm_chain(int32_t L, const hinm_layer* layers, int32_t N,
  * bytes (aligned base, leading dimension a multiple of 8) a piece that holds at least one element of a
  * row is read whole (what lies beyond never reaches a result); otherwise nothing beyond a row is read.
  * Nothing beyond the row length is written.  Sizes above 2^30, more than 2^22 tokens of a norm, calls of more than some
- * 2^22 workgroups (32 x 256 values or 128 x 128 outputs each), and a norm's gradients of channels from 2^27 on over more than 64
+ * 2^22 workgroups (32 x 256 values or 128 x 128 outputs each), and a norm's gradients of channels from 2^27 - 31 on over more than 64
  * tokens return HINM_ERR_UNSUPPORTED.
  *
  * Microscaled 4-bit form of `rows` x `length` values ("MXFP4" of the OCP microscaling formats,
@@ -490,12 +490,12 @@ hinm_status hinm_linear(int32_t M, int32_t K, int32_t N, int32_t dtype, const vo
 /* Gradients of hinm_linear from dY [M][N] (of Y; it is the residual's gradient as it stands):
  *   dZ = dY act'(Z),   dX = W^T dZ,   dW = dZ X^T,   dbias = sum_n dZ.
  * act by flags, Z as hinm_linear left it; without an activation Z is not read and dZ is dY.  relu' is 1 above
- * zero and 0 elsewhere.  dZ is rounded to dtype ahead of the products, whose operands the matrix cores take in 16
+ * zero and 0 elsewhere; at an infinite Z, as a sum beyond dtype is kept, act' is its limit, 0 or 1.  dZ is rounded to dtype ahead of the products, whose operands the matrix cores take in 16
  * bits; dbias (float32 [M]) is summed from the values before that.  dX [K][N] has leading dimension ldx, as X;
  * dW [M][K] ldw, as W, in dtype, float32 with HINM_OUT_F32; Z and dY have ldy.  dX, dW and dbias may be NULL
  * where they are not wanted (one of them is): W is needed for dX, X for dW.  Outputs must not overlap inputs
- * or each other.  Sums in a fixed order.  workspace: hinm_linear_grad_workspace bytes, 256-byte aligned; where
- * that is 0 it may be NULL. */
+ * or each other.  Sums in a fixed order.  workspace: hinm_linear_grad_workspace bytes (never 0: dZ's are among them,
+ * in every call of these sizes), 256-byte aligned. */
 hinm_status hinm_linear_grad_workspace(int32_t M, int32_t K, int32_t N, size_t* workspace_bytes);
 hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, const void* W, int64_t ldw, const void* X,
                              int64_t ldx, const void* Z, const void* dY, int64_t ldy, void* dX, void* dW, float* dbias,
@@ -506,7 +506,8 @@ hinm_status hinm_linear_grad(int32_t M, int32_t K, int32_t N, int32_t dtype, con
  *   u[k][n] = w[k] rstd[n] (x[k][n] - mean[n]) + b[k].
  * x, u 16-bit; w, b float32 [K], NULL = one and zero; mean, rstd float32 [N] outputs, NULL where not wanted.
  * u may be x with ldu = ldx; apart from that outputs must not overlap inputs.  Sums in a fixed order, in binary64
- * or of a column that one workgroup holds, whose deviations are squared in fp32: a token's deviations may be at most 10^17.
+ * or of a column that one workgroup holds, whose deviations are squared in fp32: a token's deviations may be at most 10^17, around a mean
+ * of any size (rounded to fp32 ahead of them: by up to 2^-25 of it).
  * A token that holds an infinity or a NaN has NaN results, the others theirs.  Sizes as for hinm_block_norm.  workspace:
  * hinm_layer_norm_workspace bytes, 256-byte aligned; where few channels or tokens need 0, it may be NULL. */
 hinm_status hinm_layer_norm_workspace(int32_t K, int32_t N, size_t* workspace_bytes);
@@ -520,7 +521,7 @@ hinm_status hinm_layer_norm(int32_t K, int32_t N, int32_t dtype, float eps, cons
  * dh [K][N], the gradient that reaches x beside the norm (a residual stream's), may be NULL: none.  dx, dw and db
  * (float32 [K], overwritten) may be NULL where they are not wanted (one of them is).  dh and dx have leading
  * dimension ldx, du ldu.  dx may be dh, or du with ldu = ldx; apart from that outputs must not overlap inputs.  Sums in
- * fp32 in a fixed order.  dw and db of more than 64 tokens and some 2^27 channels return HINM_ERR_UNSUPPORTED.
+ * fp32 in a fixed order.  dw and db of more than 64 tokens and 2^27 - 31 channels or more return HINM_ERR_UNSUPPORTED.
  * workspace: hinm_layer_norm_grad_workspace bytes, 256-byte aligned; where few channels or
  * tokens need 0, it may be NULL. */
 hinm_status hinm_layer_norm_grad_workspace(int32_t K, int32_t N, size_t* workspace_bytes);

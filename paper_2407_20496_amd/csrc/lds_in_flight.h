@@ -11,7 +11,7 @@
 namespace hinm {
 
 // LDS reads as raw instructions, not waited for here: the compiler would hold every one until all copies in flight had
-// landed.  To it an output is written at once, so it has to stay in its register until `tie`: lds_reads.py looks at the built
+// landed.  To it an output is written at once, so it has to stay in its register until `pin`: lds_reads.py looks at the built
 // code and the build fails where anything touches such a register before the wait.
 template <int OFFSET>
 __device__ __forceinline__ void lds_read_b128(uint32_t addr, u32x4& r) {

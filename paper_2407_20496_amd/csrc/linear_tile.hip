@@ -208,9 +208,11 @@ struct TilePlace {
 // waves, so stage p + 1 is there and the place of stage p takes stage p + RING: half of its copies during the last step of p, the
 // others during the first of p + 1.
 //   What bounds it, at rates of bf16: tiles of 256 the power (16384x16384 of 8192 columns 3.47 ms, 1270 TFLOP/s: matrix units busy 74 % of the
-// clocks at 1.6 GHz; 8192x8192 of 8192 0.81 to 0.86 ms, 1280 to 1360), 2300 clocks a stage of which 2048 are products; tiles of 256x128 and 128
-// the LDS, whose reads take 110 of its 128 bytes a clock: 1340 and 900 clocks a stage for 1024 and 512 of products (11008x4096 of 1571 columns
-// 164 us, 863 TFLOP/s; 4096x4096 of 2048 columns 67 us, 1025); small products a start of 2.5 to 3 us, the first stage's way from memory.
+// clocks at 1.6 GHz, some 2700 a stage for 2048 of products; 8192x8192 of 8192 0.81 to 0.86 ms, 1280 to 1360).  Tiles of 256x128 and 128 with few
+// workgroups the LDS: 0.63 and 0.32 us a stage, whose reads (98 and 66 KB) and copies (49 and 33 KB) take 0.48 and 0.32 at 128 bytes a clock of
+// 2.4 GHz.  On a full chip such a stage takes 0.95 and 0.60 us (11008x4096 of 1571 columns 164 us, 863 TFLOP/s; 4096x4096 of 2048 columns 67 us,
+// 1025, matrix units busy 46 %): the LDS moves some 75 of its 128 bytes a clock then, the copies draw 13 TB/s from the L2s, and what holds them
+// (these, or the waits between waves) was not taken apart.  Small products: a start of 2.5 to 3 us, the first stage's way from memory.
 template <int DT, OperandForm FA, OperandForm FB, Epilogue E, int WM, int WN, int GM, int GN, int BK, int RING, bool GUARDED>
 __device__ __forceinline__ void multiply_tile(const TileArgs& a, const LinearEpilogue& e, int group, int groups) {
   using T = TileSizes<FA, FB, WM, WN, GM, GN, BK, RING>;
@@ -616,7 +618,7 @@ __global__ __launch_bounds__(64 * GM * GN) void linear_join_kernel(const float* 
 // each line: 2048x2048 of 2048 columns 22.2 us in tiles of 128, 27.8 of 256x128, 33.4 of 64; 4096x4096 of 2048 67, 82 and 124,
 // in tiles of 256 100; of 4096 in those 113 (1208 TFLOP/s); 1024x1024 of 1024 6.9 in tiles of 64, 11.0 of 128; 11008x4096 of 1571
 // columns, 559 tiles of 256x128, 162 us with a third round of 47 workgroups and 152 where four share each of its tiles;
-// 4096x4096 of 200, 64 tiles of 128, 42 us alone, 23 in four parts.
+// 4096x4096 of 200, 256 tiles of 64 unshared, 21 us; 64 tiles of 128 take 42 alone and 23 in four parts.
 struct TileForm {
   int rows, cols, at_once;         // of a tile; workgroups that the chip holds, one or two to a compute unit
   double start;                    // us of a launch and of what does not overlap
